@@ -391,6 +391,171 @@ int dlm_kv_refresh(const dlm_kv_seg *src, int32_t B, int32_t Hkv, int32_t d,
                    int64_t c_stride_b, int64_t c_stride_h, int64_t c_stride_t,
                    int32_t cache_pos0, void *stream);
 
+/* ------------------------------------------------------------------------- *
+ * Paged cache, head norms and rotation: what stands between a layer's projections and its attention.
+ *
+ * dlm_paged_kv -- a cache of n_pages pages of page_size token rows each: row r of page p, KV head h is the d entries at
+ *   base + p*stride_page + h*stride_h + r*stride_t   (strides in elements; both orders of head and row are fine).
+ * A sequence's pages are the entries of its row of a block table, in order; token t sits in row t % page_size of entry
+ * t / page_size.  page_size is a power of two, 16 .. 65536.
+ *   type   DLM_KV_BF16; DLM_KV_E4M3 (8-bit OCP e4m3, 4 exponent and 3 mantissa bits, no infinities, largest 448): an
+ *          entry x stands for x * k_scale[h] (v_scale[h] for values)
+ *   k_scale, v_scale  optional fp32 [Hkv], DLM_KV_E4M3 only; NULL: 1.  Positive.
+ * Alignment: bases 16 bytes, strides multiples of 16 bytes; n_pages * page_size < 2^31.
+ * ------------------------------------------------------------------------- */
+#define DLM_KV_BF16            0
+#define DLM_KV_E4M3            1
+
+typedef struct dlm_paged_kv {
+    void *k, *v;
+    int32_t n_pages, page_size;
+    int64_t stride_page, stride_h, stride_t;
+    int32_t type;
+    const float *k_scale, *v_scale;
+} dlm_paged_kv;
+
+/* Which entries of a head a rotation turns together (rot = dlm_head_map.rot_dim) */
+#define DLM_ROPE_HALVES        0    /* entry c with entry c + rot/2, by angle c   (c < rot/2) */
+#define DLM_ROPE_PAIRS         1    /* entry 2c with entry 2c + 1,   by angle c   (c < rot/2) */
+
+/* dlm_head_map -- what happens to each query and key head x (d entries) of a token:
+ *   z = x * w / sqrt(mean(x^2) + eps)     with w = q_weight or k_weight (bf16 [d]); NULL: z = x
+ *   y = z, its first rot_dim entries rotated by the token's angles: (a, b) -> (a cos - b sin, b cos + a sin)
+ *   rope       fp32 [rope_len, rot_dim] contiguous, 16-byte aligned: row p holds the rot_dim/2 cosines, then the sines, of position p.  NULL: no
+ *              rotation.  (A table from angles in 64 bits: 32 bits lose the angles of far positions.)
+ *   positions  int32 [T], needed with rope: row of the table for each token.  The rotated entries of a token whose position
+ *              is outside [0, rope_len) come out as NaN.
+ *   rot_dim    a multiple of 16, at most d
+ * All in fp32, rounded once at the end. */
+typedef struct dlm_head_map {
+    const void *q_weight, *k_weight;
+    float eps;
+    const float *rope;
+    int32_t rope_len, rot_dim, rope_style;
+    const int32_t *positions;
+} dlm_head_map;
+
+/* dlm_qk_norm_rope -- dlm_head_map for the T tokens of a batch: training, and prompts whose keys go to a dense cache.
+ *   q [T, Hq, d], k [T, Hkv, d] bf16, token and head strides of their own (views of one projection are fine); Hq or Hkv may be
+ *   0 (that tensor absent).  q_out, k_out likewise; an output may be its input itself (same pointer and strides).
+ * Supported: d in {64, 128}; bases 16-byte aligned, strides multiples of 8; T * max(Hq, Hkv) < 2^31. */
+typedef struct dlm_qk_args {
+    uint32_t struct_size;
+    int32_t T, Hq, Hkv, d;
+    const void *q;
+    int64_t q_stride_t, q_stride_h;
+    const void *k;
+    int64_t k_stride_t, k_stride_h;
+    void *q_out;
+    int64_t qo_stride_t, qo_stride_h;
+    void *k_out;
+    int64_t ko_stride_t, ko_stride_h;
+    dlm_head_map map;
+} dlm_qk_args;
+
+int dlm_qk_norm_rope(const dlm_qk_args *args, void *stream);
+
+/* dlm_qk_norm_rope_bwd -- gradients of dlm_qk_norm_rope.  With dz = dy rotated back, r = 1 / sqrt(mean(x^2) + eps), n = x r:
+ *   dw = sum over tokens and heads of dz n;   dx = r (dz w - n mean(dz w n));   without a weight dx = dz
+ *   d_q_out, d_k_out  upstream gradients, bf16 [T, Hq, d], [T, Hkv, d] with their own strides
+ *   q, k              the forward inputs; read for a tensor with a weight only
+ *   d_q, d_k          written (may be d_q_out / d_k_out themselves, or q / k themselves)
+ *   d_q_weight, d_k_weight  optional fp32 [d], written (not added to); only with that weight
+ * fp32 sums in a fixed order, no atomics: deterministic.
+ * workspace: dlm_qk_norm_rope_bwd_workspace_bytes(args) bytes, 16-byte aligned; needed for the weights' gradients only. */
+typedef struct dlm_qk_bwd_args {
+    uint32_t struct_size;
+    int32_t T, Hq, Hkv, d;
+    const void *d_q_out;
+    int64_t dqo_stride_t, dqo_stride_h;
+    const void *d_k_out;
+    int64_t dko_stride_t, dko_stride_h;
+    const void *q;
+    int64_t q_stride_t, q_stride_h;
+    const void *k;
+    int64_t k_stride_t, k_stride_h;
+    void *d_q;
+    int64_t dq_stride_t, dq_stride_h;
+    void *d_k;
+    int64_t dk_stride_t, dk_stride_h;
+    float *d_q_weight, *d_k_weight;
+    dlm_head_map map;
+    void *workspace;
+    size_t workspace_bytes;
+} dlm_qk_bwd_args;
+
+int dlm_qk_norm_rope_bwd(const dlm_qk_bwd_args *args, void *stream);
+size_t dlm_qk_norm_rope_bwd_workspace_bytes(const dlm_qk_bwd_args *args);
+
+/* dlm_paged_append -- the keys (through dlm_head_map) and values of T tokens into the pages, and their queries beside them.
+ *   q [T, Hq, d], k, v [T, Hkv, d] bf16 with token and head strides of their own; q and q_out may be absent (Hq = 0); q_out may
+ *   be q itself
+ *   slots   int32 [T]: page * page_size + row for each token.  A negative slot, or one behind the last page: the token has none (the padding of
+ *           a batch) and nothing of it is stored; its query is still written.  Slots that are used are distinct: which of two
+ *           tokens a slot named twice ends up with, in whole or in part, is not defined.
+ *   DLM_KV_E4M3: an entry y is stored as the nearest e4m3 of y * (1 / scale[h]) (ties to even), +-448 where it is larger; NaN stays NaN.
+ * Rows that no slot names are left as they are.  k, v, q must not overlap the cache. */
+typedef struct dlm_append_args {
+    uint32_t struct_size;
+    int32_t T, Hq, Hkv, d;
+    const void *q;
+    int64_t q_stride_t, q_stride_h;
+    const void *k;
+    int64_t k_stride_t, k_stride_h;
+    const void *v;
+    int64_t v_stride_t, v_stride_h;
+    void *q_out;
+    int64_t qo_stride_t, qo_stride_h;
+    const int32_t *slots;
+    dlm_paged_kv cache;
+    dlm_head_map map;
+} dlm_append_args;
+
+int dlm_paged_append(const dlm_append_args *args, void *stream);
+
+/* dlm_paged_attn -- dlm_block_attn against a paged cache: O = softmax(scale * Q K^T) V for the last Lq tokens of each sequence, whose
+ * keys and values are in the pages already (dlm_paged_append): a block being denoised (its rows are stored again at every
+ * step), or Lq = 1, a single new token.
+ *   q, out       bf16 [B, Lq, Hq, d] with strides; lse optional fp32 [B, Hq, Lq] contiguous (natural log)
+ *   block_table  int32 [B, table_stride] (row b: the pages of sequence b).  A page outside [0, n_pages) is absent: no row sees its
+ *                keys, nothing of it is read.
+ *   kv_len       int32 [B]: tokens of sequence b in the cache, the new ones among them; values outside [0, max_kv_len] are taken as
+ *                the nearer end
+ *   max_kv_len   an upper bound of kv_len, at most table_stride * page_size; it sizes the launch
+ *   q_len        optional int32 [B]: sequence b has only q_len[b] <= Lq query rows; rows behind them are left as they are in out and
+ *                lse.  NULL: Lq each
+ *   mask_mode    DLM_MASK_FULL: every row sees all kv_len keys.  DLM_MASK_BLOCK_CAUSAL: row i stands at position
+ *                kv_len - q_len + i and sees the keys whose position / block_size is at most its own (block_size 1: causal)
+ *   scale        <= 0 selects 1/sqrt(d)
+ * A row that sees no key, or only scores of -inf, gets out = 0 and lse = -inf.  Arithmetic as dlm_block_attn; e4m3 entries are exact in bf16, their scales
+ * are applied in fp32.
+ * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it several workgroups share the keys
+ * of a sequence (fp32 partial results, joined in a fixed order by a second launch: deterministic); calls that may overlap need one each.
+ * Without one, or with a smaller one, a call runs unsplit; results then differ by the rounding of another summation order only.
+ * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8. */
+typedef struct dlm_paged_attn_args {
+    uint32_t struct_size;
+    int32_t B, Lq, Hq, Hkv, d;
+    const void *q;
+    int64_t q_stride_b, q_stride_t, q_stride_h;
+    void *out;
+    int64_t o_stride_b, o_stride_t, o_stride_h;
+    float *lse;
+    dlm_paged_kv cache;
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *kv_len;
+    int32_t max_kv_len;
+    const int32_t *q_len;
+    int32_t mask_mode, block_size;
+    float scale;
+    void *workspace;
+    size_t workspace_bytes;
+} dlm_paged_attn_args;
+
+int dlm_paged_attn(const dlm_paged_attn_args *args, void *stream);
+size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
+
 /* dlm_set_option -- process-wide tuning / test knobs (not thread-safe against running calls).  These integers are the
  * ONLY mutable state the library keeps between calls (besides the per-device address of the built-in scratch of
  * dlm_lmhead_confidence_static); every default is the planner's choice, and every setting computes the same function.
