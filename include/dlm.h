@@ -532,7 +532,8 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it several workgroups share the keys
  * of a sequence (fp32 partial results, joined in a fixed order by a second launch: deterministic); calls that may overlap need one each.
  * Without one, or with a smaller one, a call runs unsplit; results then differ by the rounding of another summation order only.
- * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8. */
+ * Values that a row does not see have to be finite where another of the 32 rows of its tile sees them (they are multiplied by zero).
+ * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8; stride_t of the cache below 2^26. */
 typedef struct dlm_paged_attn_args {
     uint32_t struct_size;
     int32_t B, Lq, Hq, Hkv, d;
@@ -598,6 +599,8 @@ size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
  *                   grid; forward and the dQ pass), 2 = under a block-causal mask the row tile with the longest
  *                   key range is dispatched first, 4 = the same grouping for the dK / dV passes; 0 = plain
  *                   (tile, KV head, sequence) grids.
+ *   "paged_chunk"   0 = the library decides how many keys of a sequence a workgroup of dlm_paged_attn takes (default); n >= 1 = 32 n
+ *                   (the workspace's size depends on it).
  * The knobs exist for tests and tuning sweeps. */
 int dlm_set_option(const char *name, int value);
 

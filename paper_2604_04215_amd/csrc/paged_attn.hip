@@ -14,6 +14,7 @@ namespace dlm {
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 
 struct PagedAttnParams {
     int B, Lq, Hq, Hkv, g;
@@ -48,7 +49,6 @@ __device__ __forceinline__ int clamped(int v, int hi) { return min(max(v, 0), hi
 
 // eight e4m3 entries as bf16 (exact: bf16 has more of both exponent and mantissa)
 __device__ __forceinline__ u32x4 widen_e4m3(uint32_t lo, uint32_t hi) {
-    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
     const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
     return u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), pack_bf16x2(c[0], c[1]), pack_bf16x2(d[0], d[1])};
@@ -62,7 +62,8 @@ __device__ __forceinline__ int visible_keys(const PagedAttnParams& p, int len, i
     return pos < 0 ? 0 : min((int64_t)len, ((int64_t)(pos / p.bs) + 1) * p.bs);
 }
 
-template <int D, bool F8, bool BC>
+// NT: non-temporal loads, where one workgroup is the only reader of its keys.
+template <int D, bool F8, bool BC, bool NT>
 __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
     constexpr int NW = 4;
     constexpr int KP = D * 2 + 16;          // pitch of a K row in LDS: 16-byte reads of 16 rows hit distinct banks
@@ -76,17 +77,26 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
     constexpr int MERGE = NW * 32 * MP * 4;
     __shared__ __attribute__((aligned(16))) unsigned char smem[NW * TILE > MERGE ? NW * TILE : MERGE];
 
+    fetch_args<sizeof(PagedAttnParams)>();
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hi = lane >> 5;
     int grp, rt;
     if (!remap_decode(p.remap, p.B * p.Hkv * p.nsplit, grp, rt)) return;
     const int split = grp % p.nsplit, bh = grp / p.nsplit, kvh = bh % p.Hkv, b = bh / p.Hkv;
+    // Pages of the wavefront's next 32 tiles: lane 2j + h holds the one of half h (16 keys, a page is no smaller) of its j-th tile.  One load for 32
+    // tiles, requested 32 tiles ahead: a look-up a tile was a trip to memory in front of every fetch.  The first one travels with the
+    // sequence's lengths, so it may look at entries behind the sequence's end (but inside the table's row): whatever they hold, a page
+    // outside the cache is not read and a key behind the end not seen.
+    const int t0 = split * p.chunk, last_entry = (max(p.max_kv_len, 1) - 1) >> p.page_shift;
+    const int32_t* table = p.table + b * p.table_stride;
+    auto pages_from = [&](int j) { return table[min((int)(((int64_t)(t0 + w + NW * (j + (lane >> 1))) * 32 + 16 * (lane & 1)) >> p.page_shift), last_entry)]; };
+    int pages = p.max_kv_len > 0 ? pages_from(0) : 0;
     const int len = clamped(p.kv_len[b], p.max_kv_len), ql = p.q_len ? clamped(p.q_len[b], p.Lq) : p.Lq;
     const int R = ql * p.g, r0 = rt * 32;
     if (r0 >= R) return;
     const int seen = visible_keys<BC>(p, len, ql, min(r0 + 32, R));
     const int T = (seen + 31) >> 5;
-    const int t0 = split * p.chunk, Tn = min(T - t0, p.chunk);
+    const int Tn = min(T - t0, p.chunk);
     if (split > 0 && Tn <= 0) return;
     const bool alone = T <= p.chunk;        // no other stretch: this workgroup writes the output
 
@@ -100,7 +110,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
         if (r < R) v = *reinterpret_cast<const u32x4*>(qp + 16 * c + 8 * hi);
         qf[c] = as_bf16x8(v);
     }
-    const int limit = visible_keys<BC>(p, len, ql, r < R ? (r / p.g + 1) * p.g : 1);     // keys this lane's row sees
+    const int limit = visible_keys<BC>(p, len, ql, r < R ? (r / p.g + 1) * p.g : min(r0 + 32, R));     // keys this lane's row sees
+    const int limit_min = visible_keys<BC>(p, len, ql, r0 + 1);                                         // fewest of any row (the first one's)
     const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[kvh] : p.scale_log2;
 
     f32x16 O[D / 32];
@@ -113,41 +124,50 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
     unsigned char* Kl = smem + w * TILE;
     unsigned char* Vl = Kl + 32 * KP;
     const int lrow = lane / C, lc = lane % C;
-    const int32_t* table = p.table + b * p.table_stride;
     const unsigned char* kb = (const unsigned char*)p.k + (int64_t)kvh * p.sh * ES;
     const unsigned char* vb = (const unsigned char*)p.v + (int64_t)kvh * p.sh * ES;
-    const int last_entry = (max(len, 1) - 1) >> p.page_shift;
+    uint32_t off[NLD];                      // of this lane's piece of load q, from the first row of its half tile
+#pragma unroll
+    for (int q = 0; q < NLD; ++q) off[q] = (uint32_t)(((q * RPL + lrow) & 15) * (int)p.st * ES + lc * 16);
 
+    int pages_next = 0;
     u32x4 kr[NLD], vr[NLD];
-    bool there[2];                          // whether the pages of the tile's two halves of 16 keys exist (a page is no smaller)
-    auto fetch = [&](int t) {
-        int64_t base[2];
+    bool there[2];                          // whether the pages of the two halves exist
+    auto fetch = [&](int j) {               // requests the wavefront's j-th tile
+        const int key = (t0 + w + NW * j) * 32;
+        const unsigned char *ks[2], *vs[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int key = (t0 + t) * 32 + 16 * h;
-            const int page = table[min(key >> p.page_shift, last_entry)];
+            const int page = __builtin_amdgcn_readlane(pages, 2 * (j & 31) + h);
             there[h] = (unsigned)page < (unsigned)p.n_pages;
-            base[h] = ((int64_t)(there[h] ? page : 0) * p.sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.st) * ES;
+            const int64_t base = ((int64_t)(there[h] ? page : 0) * p.sp + (int64_t)((key + 16 * h) & ((1 << p.page_shift) - 1)) * p.st) * ES;
+            ks[h] = kb + base;
+            vs[h] = vb + base;
         }
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
-            const int row = q * RPL + lrow;
-            const int64_t off = (row < 16 ? base[0] : base[1]) + (int64_t)(row & 15) * p.st * ES + lc * 16;
-            kr[q] = *reinterpret_cast<const u32x4*>(kb + off);
-            vr[q] = *reinterpret_cast<const u32x4*>(vb + off);
+            const int h = q * RPL / 16;
+            kr[q] = NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ks[h] + off[q])) : *reinterpret_cast<const u32x4*>(ks[h] + off[q]);
+            vr[q] = NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vs[h] + off[q])) : *reinterpret_cast<const u32x4*>(vs[h] + off[q]);
         }
     };
-    if (w < Tn) fetch(w);
-    for (int t = w; t < Tn; t += NW) {
-        const int key0 = (t0 + t) * 32;
+    const int J = (Tn - w + NW - 1) / NW;   // tiles of this wavefront
+    if (J > 0) {
+        if (J > 32) pages_next = pages_from(32);
+        fetch(0);
+    }
+    for (int j = 0; j < J; ++j) {
+        const int key0 = (t0 + w + NW * j) * 32;
         const bool here0 = there[0], here1 = there[1];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile before has been read (one wavefront's LDS operations keep their order)
+        const bool whole = key0 + 32 <= seen && here0 && here1;
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
             const int row = q * RPL + lrow;
+            const u32x4 z = {0, 0, 0, 0}, kv = kr[q];
+            u32x4 vv = vr[q];
             // rows behind the end hold anything, NaN too: as values they have to be zeros (as keys their scores are replaced)
-            const bool live = key0 + row < seen && (row < 16 ? here0 : here1);
-            const u32x4 z = {0, 0, 0, 0}, kv = kr[q], vv = live ? vr[q] : z;
+            if (!whole && !(key0 + row < seen && (q * RPL < 16 ? here0 : here1))) vv = z;
             if constexpr (F8) {
                 u32x4* kd = reinterpret_cast<u32x4*>(Kl + row * KP + lc * 32);
                 u32x4* vd = reinterpret_cast<u32x4*>(Vl + row * VP + lc * 32);
@@ -161,7 +181,13 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (t + NW < Tn) fetch(t + NW);
+        if (j + 1 < J) {
+            if (((j + 1) & 31) == 0) {
+                pages = pages_next;
+                if (j + 33 < J) pages_next = pages_from(j + 33);
+            }
+            fetch(j + 1);
+        }
         f32x16 S;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = 0.f;
@@ -169,19 +195,21 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
         for (int c = 0; c < D / 16; ++c)
             S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Kl + n * KP + (16 * c + 8 * hi) * 2), qf[c], S, 0, 0, 0);
         // entry i is key key0 + 8 (i / 4) + 4 hi + i % 4
-        if (key0 + 32 > (BC ? 0 : len) || !here0 || !here1) {
+        if (key0 + 32 > limit_min || !here0 || !here1) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (key0 + 8 * (i >> 2) + 4 * hi + (i & 3) >= limit || !(i < 8 ? here0 : here1)) S[i] = -INFINITY;
         }
         float mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = __builtin_fmaxf(mx, S[i]);
+        for (int i = 0; i < 16; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = __builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
-        const float m_new = __builtin_fmaxf(m_run, mx);
+        // The maximum that the exponentials are relative to follows the running one only when that has grown by 2^8 (p stays in range of bf16 and
+        // of the sums): the 64 accumulators are rescaled a few times a row instead of at every tile.
+        const bool grow = mx > m_run + 8.0f;
+        const float m_new = grow ? mx : m_run;
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = fast_exp2(m_run - m_use);
         float rs = 0.f;
         uint32_t pk[8];
 #pragma unroll
@@ -190,12 +218,16 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
             rs += p0 + p1;
             pk[i >> 1] = pack_bf16x2(p0, p1);
         }
-        l_run = l_run * alpha + rs;
+        if (__any(grow)) {
+            const float alpha = grow ? fast_exp2(m_run - m_use) : 1.0f;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
+        }
+        l_run += rs;
         m_run = m_new;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
         const u32x4 plo = {pk[0], pk[1], pk[2], pk[3]}, phi = {pk[4], pk[5], pk[6], pk[7]};
         const bf16x8 pf[2] = {as_bf16x8(plo), as_bf16x8(phi)};
         const int s16 = lane & 15, blk = (lane >> 4) & 1;
@@ -267,30 +299,62 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
     }
 }
 
-// Joins the stretches of each (sequence, head, row) that has more than one, in their order: M = max m_s, w_s = 2^(m_s - M), out = sum w_s o_s /
-// sum w_s l_s, lse = (M + log2 sum w_s l_s) ln 2.  D / 4 threads a row.
-template <int D, bool F8, bool BC>
+// Joins the stretches of each (sequence, head, row) that has more than one: M = max m_s, w_s = 2^(m_s - M), out = sum w_s o_s / sum w_s l_s,
+// lse = (M + log2 sum w_s l_s) ln 2.  D / 4 threads a row and group of stretches, G groups: group k takes stretches k, k + G, .. in their
+// order, four requested at a time, and the groups are added up in theirs.
+template <int D, bool F8, bool BC, int G>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
-    constexpr int TPR = D / 4;
-    const int64_t rows = (int64_t)p.B * p.Hq * p.Lq, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    if (row >= rows) return;
-    const int c4 = threadIdx.x % TPR, i = (int)(row % p.Lq), bh = (int)(row / p.Lq), h = bh % p.Hq, b = bh / p.Hq;
+    constexpr int TPR = D / 4, RPW = 256 / TPR / G;
+    __shared__ float part[G > 1 ? 256 / TPR : 1][D + 2];
+    const int64_t rows = (int64_t)p.B * p.Hq * p.Lq, row = min((int64_t)blockIdx.x * RPW + threadIdx.x / (TPR * G), rows - 1);
+    const int c4 = threadIdx.x % TPR, gi = threadIdx.x / TPR, k = gi % G;
+    const int i = (int)(row % p.Lq), bh = (int)(row / p.Lq), h = bh % p.Hq, b = bh / p.Hq;
     const int len = clamped(p.kv_len[b], p.max_kv_len), ql = p.q_len ? clamped(p.q_len[b], p.Lq) : p.Lq;
-    if (i >= ql) return;
-    const int r = i * p.g + h % p.g, r0 = r & ~31;
-    const int T = (visible_keys<BC>(p, len, ql, min(r0 + 32, ql * p.g)) + 31) >> 5;
-    if (T <= p.chunk) return;
-    const int n = (T + p.chunk - 1) / p.chunk;
+    const int r0 = (i * p.g + h % p.g) & ~31;
+    const int T = i < ql ? (visible_keys<BC>(p, len, ql, min(r0 + 32, ql * p.g)) + 31) >> 5 : 0;
+    const int n = T <= p.chunk ? 0 : (T + p.chunk - 1) / p.chunk;          // 0: nothing to join here
     float M = -INFINITY, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < n; ++s) M = __builtin_fmaxf(M, p.part_ml[(s * rows + row) * 2]);
-    for (int s = 0; s < n; ++s) {
-        const float m = p.part_ml[(s * rows + row) * 2], l = p.part_ml[(s * rows + row) * 2 + 1];
-        const float wgt = m == -INFINITY ? 0.f : fast_exp2(m - M);
-        const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + 4 * c4);
-        den += wgt * l;
+    for (int s0 = k; s0 < n; s0 += 4 * G) {
+        float m[4], l[4];
+        f32x4 v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += wgt * v[e];
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = min(s0 + u * G, n - 1) * rows + row;        // (past the last one it is loaded again and not used)
+            m[u] = p.part_ml[at * 2];
+            l[u] = p.part_ml[at * 2 + 1];
+            v[u] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + 4 * c4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (s0 + u * G >= n) continue;
+            const float m_new = __builtin_fmaxf(M, m[u]), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float a = fast_exp2(M - m_use), w = fast_exp2(m[u] - m_use);
+            M = m_new;
+            den = den * a + l[u] * w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * a + v[u][e] * w;
+        }
     }
+    if constexpr (G > 1) {
+        *reinterpret_cast<f32x2*>(&part[gi][4 * c4]) = f32x2{o[0], o[1]};
+        *reinterpret_cast<f32x2*>(&part[gi][4 * c4 + 2]) = f32x2{o[2], o[3]};
+        if (c4 == 0) {
+            part[gi][D] = M;
+            part[gi][D + 1] = den;
+        }
+        __syncthreads();
+        if (k > 0) return;
+#pragma unroll
+        for (int u = 1; u < G; ++u) {
+            const float m = part[gi + u][D], m_new = __builtin_fmaxf(M, m), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float a = fast_exp2(M - m_use), w = fast_exp2(m - m_use);
+            M = m_new;
+            den = den * a + part[gi + u][D + 1] * w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * a + part[gi + u][4 * c4 + e] * w;
+        }
+    }
+    if (n == 0) return;
     const float inv = (den == 0.f ? 0.f : 1.f / den) * (F8 && p.v_scale ? p.v_scale[h / p.g] : 1.f);
     const u32x2 v = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
     *reinterpret_cast<u32x2*>(p.out + b * p.o_sb + i * p.o_st + (int64_t)h * p.o_sh + 4 * c4) = v;
@@ -298,8 +362,11 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
+static int g_paged_chunk = 0;      // "paged_chunk"
+
 // Tiles of a stretch: as many workgroups as give the chip two each, no stretch under 8 tiles (two a wavefront).
 static int plan_chunk(const dlm_paged_attn_args* a) {
+    if (g_paged_chunk > 0) return g_paged_chunk;
     const int64_t tiles = ((int64_t)a->max_kv_len + 31) / 32, groups = (int64_t)a->B * a->Hkv * (((int64_t)a->Lq * (a->Hq / a->Hkv) + 31) / 32);
     int64_t n = groups >= 512 ? 1 : 512 / groups;
     const int64_t most = tiles / 8;
@@ -331,6 +398,7 @@ static int validate_paged_attn(const dlm_paged_attn_args* a) {
     if (a->max_kv_len < 0 || a->max_kv_len > (1 << 30)) return fail(DLM_ERR_INVALID_ARG, "%s: max_kv_len outside [0, 2^30]", who);
     int rc = validate_cache(a->cache, a->Hkv, a->d, who, false);
     if (rc != DLM_OK) return rc;
+    if (a->cache.stride_t >= 1 << 26) return fail(DLM_ERR_UNSUPPORTED, "%s: stride_t of the cache is 2^26 or more", who);     // 15 of them in 32 bits
     if (a->table_stride < 0) return fail(DLM_ERR_INVALID_ARG, "%s: table_stride < 0", who);
     // (in pages: no product that could overflow)
     if (((int64_t)a->max_kv_len + a->cache.page_size - 1) / a->cache.page_size > a->table_stride)
@@ -348,12 +416,21 @@ static int validate_paged_attn(const dlm_paged_attn_args* a) {
 
 template <int D, bool F8, bool BC>
 static int launch_paged(const PagedAttnParams& p, unsigned grid, hipStream_t st) {
-    hipLaunchKernelGGL((paged_attn_kernel<D, F8, BC>), dim3(grid), dim3(256), 0, st, p);
+    if (p.remap.nx == 1) hipLaunchKernelGGL((paged_attn_kernel<D, F8, BC, true>), dim3(grid), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((paged_attn_kernel<D, F8, BC, false>), dim3(grid), dim3(256), 0, st, p);
     int rc = check_hip(hipGetLastError(), "paged_attn_kernel launch");
     if (rc != DLM_OK || p.nsplit <= 1) return rc;
+    constexpr int GROUPS = 1024 / D;
     const int64_t rows = (int64_t)p.B * p.Hq * p.Lq;
-    hipLaunchKernelGGL((paged_merge_kernel<D, F8, BC>), dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, p);
+    if (p.nsplit > 4) hipLaunchKernelGGL((paged_merge_kernel<D, F8, BC, GROUPS>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((paged_merge_kernel<D, F8, BC, 1>), dim3((unsigned)((rows + GROUPS - 1) / GROUPS)), dim3(256), 0, st, p);
     return check_hip(hipGetLastError(), "paged_merge_kernel launch");
+}
+
+int paged_set_chunk(int v) {
+    if (v < 0) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_chunk must be >= 0");
+    g_paged_chunk = v;
+    return DLM_OK;
 }
 
 }  // namespace dlm
@@ -401,7 +478,7 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
     if (groups > 0x7fffffff || row_tiles > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
     const int64_t grid = set_remap(p.remap, groups, (int)row_tiles, false);
     if (grid == 0) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
-    if (p.nsplit > 1 && ((int64_t)a->B * a->Hq * a->Lq + 1024 / a->d - 1) / (1024 / a->d) > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many rows");
+    if (p.nsplit > 1 && (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many rows");
     hipStream_t st = (hipStream_t)stream;
     const bool f8 = c.type == DLM_KV_E4M3, bc = a->mask_mode == DLM_MASK_BLOCK_CAUSAL;
 #define PAGED_LAUNCH(D)                                                                                                    \
