@@ -92,47 +92,6 @@ class CommitArgs(C.Structure):
                 ("host_remaining_total", C.c_void_p), ("active_in", C.c_void_p), ("host_remaining_max", C.c_void_p)]
 
 
-class PagedKv(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32),
-                ("stride_page", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64), ("type", C.c_int32),
-                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
-
-
-class HeadMap(C.Structure):
-    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rope", C.c_void_p),
-                ("rope_len", C.c_int32), ("rot_dim", C.c_int32), ("rope_style", C.c_int32), ("positions", C.c_void_p)]
-
-
-def _heads(name, stride):
-    return [(name, C.c_void_p), (stride + "_stride_t", C.c_int64), (stride + "_stride_h", C.c_int64)]
-
-
-class QkArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_uint32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
-                *_heads("q", "q"), *_heads("k", "k"), *_heads("q_out", "qo"), *_heads("k_out", "ko"), ("map", HeadMap)]
-
-
-class QkBwdArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_uint32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
-                *_heads("d_q_out", "dqo"), *_heads("d_k_out", "dko"), *_heads("q", "q"), *_heads("k", "k"), *_heads("d_q", "dq"), *_heads("d_k", "dk"),
-                ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p), ("map", HeadMap), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
-
-
-class AppendArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_uint32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
-                *_heads("q", "q"), *_heads("k", "k"), *_heads("v", "v"), *_heads("q_out", "qo"), ("slots", C.c_void_p), ("cache", PagedKv),
-                ("map", HeadMap)]
-
-
-class PagedAttnArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_uint32), ("B", C.c_int32), ("Lq", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
-                ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_t", C.c_int64), ("q_stride_h", C.c_int64),
-                ("out", C.c_void_p), ("o_stride_b", C.c_int64), ("o_stride_t", C.c_int64), ("o_stride_h", C.c_int64),
-                ("lse", C.c_void_p), ("cache", PagedKv), ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("kv_len", C.c_void_p),
-                ("max_kv_len", C.c_int32), ("q_len", C.c_void_p), ("mask_mode", C.c_int32), ("block_size", C.c_int32), ("scale", C.c_float),
-                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
-
-
 class DlmError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"libdlm error {code}: {msg}")
@@ -179,12 +138,6 @@ def lib():
         L.dlm_seq_logprob.restype = C.c_int
         L.dlm_seq_logprob.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32,
                                       C.c_void_p, C.c_void_p, C.c_void_p]
-        for name in ("dlm_qk_norm_rope", "dlm_qk_norm_rope_bwd", "dlm_paged_append", "dlm_paged_attn"):
-            fn = getattr(L, name)
-            fn.restype, fn.argtypes = C.c_int, [C.c_void_p, C.c_void_p]
-        for name in ("dlm_qk_norm_rope_bwd_workspace_bytes", "dlm_paged_attn_workspace_bytes"):
-            fn = getattr(L, name)
-            fn.restype, fn.argtypes = C.c_size_t, [C.c_void_p]
         L.dlm_set_option.restype = C.c_int
         L.dlm_set_option.argtypes = [C.c_char_p, C.c_int]
         L.dlm_last_error.restype = C.c_char_p
@@ -539,74 +492,36 @@ def seq_logprob(ztarget, lse, mask, out, *, weight=None, n_terms=None, stream=No
 
 
 # ---- paged cache, head norms and rotation ---------------------------------------------------------------------------
-# These calls stand in every layer of a step, so their host side is kept short: one look at each tensor, structs filled by
-# position.  They run on the device of their tensors, on the stream that is torch's current one there.
+# These calls stand in every layer of a step, so their structs are filled in C++ (csrc/marshal.cpp); here they get their names, the
+# device of their tensors and the stream.
 
-def _launch(fn, args, device, stream) -> None:
+_native = None
+
+
+def _load_native():
+    global _native, _raw_stream, _current_device
+    lib()
     import torch
-    if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(device.index)
+    from . import _marshal
+    _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _native = _marshal
+    return _marshal
+
+
+def _enqueue(fn, t, stream, *args) -> None:
+    """One call on the device of tensor t and torch's current stream there, or on `stream`."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError("tensors must live on the GPU (no CPU path exists)")
+    s = _raw_stream(device) if stream is None else stream.cuda_stream
+    if _current_device() == device:
+        rc = fn(s, *args)
     else:
-        stream = stream.cuda_stream
-    if torch._C._cuda_getDevice() == device.index:
-        rc = fn(C.byref(args), stream)
-    else:
+        import torch
         with torch.cuda.device(device):
-            rc = fn(C.byref(args), stream)
-    if rc != DLM_OK:
+            rc = fn(s, *args)
+    if rc:
         raise DlmError(rc, last_error())
-
-
-def _on(t, dtype, shape, device, name):
-    """Pointer of a tensor of this type, shape (None: any length) and device whose rows are contiguous; None for None."""
-    if t is None:
-        return None
-    if t.device != device or device.type != "cuda":
-        raise ValueError(f"{name} must live on the GPU of the other tensors (no CPU path exists)")
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{name}: innermost axis must be contiguous")
-    return t.data_ptr()
-
-
-def _flat(t, dtype, shape, device, name):
-    """_on for a tensor that has to be contiguous as a whole."""
-    if t is not None and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return _on(t, dtype, shape, device, name)
-
-
-def _rows(t, shape, device, name):
-    """(pointer, token stride, head stride) of a bf16 [T, H, d] tensor."""
-    import torch
-    if t is None:
-        return None, 0, 0
-    return _on(t, torch.bfloat16, shape, device, name), t.stride(0), t.stride(1)
-
-
-def _head_map(T, d, device, q_weight, k_weight, eps, rope, positions, rope_style) -> HeadMap:
-    import torch
-    if rope is not None:
-        if rope.dim() != 2:
-            raise ValueError("rope must be [positions, rot_dim]")
-        if positions is None:
-            raise ValueError("a rotation needs positions")
-    return HeadMap(_flat(q_weight, torch.bfloat16, (d,), device, "q_weight"), _flat(k_weight, torch.bfloat16, (d,), device, "k_weight"), eps,
-                   _flat(rope, torch.float32, None, device, "rope"), 0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1],
-                   rope_style, _flat(positions, torch.int32, (T,), device, "positions"))
-
-
-def _head_sizes(q, k):
-    """(T, Hq, Hkv, d, device) of queries and keys, either of which may be None."""
-    t = q if q is not None else k
-    if t is None:
-        raise ValueError("queries or keys are needed")
-    if t.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != t.shape[0] or k.shape[2] != t.shape[2])):
-        raise ValueError("queries [T, Hq, d] and keys [T, Hkv, d] expected")
-    return t.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], t.shape[2], t.device
 
 
 def qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: float = 1e-6, rope=None, positions=None,
@@ -614,17 +529,13 @@ def qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: float
     """Norm (with a weight, bf16 [d]) and rotation (with a table, fp32 [positions, rot_dim]: cosines, then sines) of query and key heads.
     q, q_out bf16 [T, Hq, d]; k, k_out bf16 [T, Hkv, d] (views, and an output that is its input, are fine; q or k may be None);
     positions int32 [T]."""
-    T, Hq, Hkv, d, dev = _head_sizes(q, k)
-    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
-        raise ValueError("an output goes with its input")
-    a = QkArgs(C.sizeof(QkArgs), T, Hq, Hkv, d, *_rows(q, (T, Hq, d), dev, "q"), *_rows(k, (T, Hkv, d), dev, "k"),
-               *_rows(q_out, (T, Hq, d), dev, "q_out"), *_rows(k_out, (T, Hkv, d), dev, "k_out"),
-               _head_map(T, d, dev, q_weight, k_weight, eps, rope, positions, rope_style))
-    _launch(lib().dlm_qk_norm_rope, a, dev, stream)
+    if q is None and k is None:
+        raise ValueError("queries or keys are needed")
+    _enqueue((_native or _load_native()).qk_norm_rope, k if q is None else q, stream, q, k, q_out, k_out, q_weight, k_weight, eps, rope, positions, rope_style)
 
 
 def qk_norm_rope_bwd_workspace_bytes(T: int, Hq: int, Hkv: int, d: int) -> int:
-    return int(lib().dlm_qk_norm_rope_bwd_workspace_bytes(C.byref(QkBwdArgs(C.sizeof(QkBwdArgs), T, Hq, Hkv, d))))
+    return (_native or _load_native()).qk_norm_rope_bwd_workspace(T, Hq, Hkv, d)
 
 
 def qk_norm_rope_bwd(d_q_out, d_k_out, d_q, d_k, *, q=None, k=None, q_weight=None, k_weight=None, d_q_weight=None, d_k_weight=None,
@@ -632,38 +543,10 @@ def qk_norm_rope_bwd(d_q_out, d_k_out, d_q, d_k, *, q=None, k=None, q_weight=Non
     """Gradients of qk_norm_rope: upstream d_q_out [T, Hq, d], d_k_out [T, Hkv, d] bf16 (either may be None) into d_q, d_k; with a weight also
     its gradient (optional fp32 [d], overwritten), which needs the forward's q / k and a workspace of
     qk_norm_rope_bwd_workspace_bytes(...) bytes."""
-    import torch
-    T, Hq, Hkv, d, dev = _head_sizes(d_q_out, d_k_out)
-    if (d_q_out is None) != (d_q is None) or (d_k_out is None) != (d_k is None):
-        raise ValueError("a gradient goes with its upstream gradient")
-    sq, sk = (T, Hq, d), (T, Hkv, d)
-    a = QkBwdArgs(C.sizeof(QkBwdArgs), T, Hq, Hkv, d, *_rows(d_q_out, sq, dev, "d_q_out"), *_rows(d_k_out, sk, dev, "d_k_out"),
-                  *_rows(q, sq, dev, "q"), *_rows(k, sk, dev, "k"), *_rows(d_q, sq, dev, "d_q"), *_rows(d_k, sk, dev, "d_k"),
-                  _flat(d_q_weight, torch.float32, (d,), dev, "d_q_weight"), _flat(d_k_weight, torch.float32, (d,), dev, "d_k_weight"),
-                  _head_map(T, d, dev, q_weight, k_weight, eps, rope, positions, rope_style), *_buffer(workspace, dev))
-    _launch(lib().dlm_qk_norm_rope_bwd, a, dev, stream)
-
-
-def _buffer(workspace, device):
-    if workspace is None:
-        return None, 0
-    if workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous and live on the GPU of the other tensors")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def _paged_kv(cache_k, cache_v, k_scale, v_scale, Hkv, d, device) -> PagedKv:
-    import torch
-    if cache_k.dim() != 4 or cache_k.shape != cache_v.shape or cache_k.stride() != cache_v.stride():
-        raise ValueError("cache_k and cache_v must be [pages, Hkv, page_size, d] and share strides")
-    n_pages, heads, page_size, dc = cache_k.shape
-    if (Hkv is not None and heads != Hkv) or dc != d:
-        raise ValueError(f"cache of {heads} heads of {dc} entries, {Hkv} of {d} expected")
-    kind = KV_E4M3 if cache_k.dtype == torch.float8_e4m3fn else KV_BF16
-    dtype = cache_k.dtype if kind == KV_E4M3 else torch.bfloat16
-    sp, sh, st, _ = cache_k.stride()
-    return PagedKv(_on(cache_k, dtype, None, device, "cache_k"), _on(cache_v, dtype, None, device, "cache_v"), n_pages, page_size, sp, sh, st, kind,
-                   _flat(k_scale, torch.float32, (heads,), device, "k_scale"), _flat(v_scale, torch.float32, (heads,), device, "v_scale"))
+    if d_q_out is None and d_k_out is None:
+        raise ValueError("gradients of queries or keys are needed")
+    _enqueue((_native or _load_native()).qk_norm_rope_bwd, d_k_out if d_q_out is None else d_q_out, stream, d_q_out, d_k_out, d_q, d_k, q, k, d_q_weight,
+             d_k_weight, q_weight, k_weight, eps, rope, positions, rope_style, workspace)
 
 
 def paged_append(k, v, cache_k, cache_v, slots, *, q=None, q_out=None, q_weight=None, k_weight=None, eps: float = 1e-6, rope=None,
@@ -671,53 +554,24 @@ def paged_append(k, v, cache_k, cache_v, slots, *, q=None, q_out=None, q_weight=
     """Keys (normed and rotated as by qk_norm_rope) and values of T tokens into a paged cache, their queries into q_out in the same launch.
     k, v bf16 [T, Hkv, d]; q, q_out bf16 [T, Hq, d] or None; cache_k, cache_v [pages, Hkv, page_size, d], bf16 or float8_e4m3fn (then with optional
     k_scale / v_scale fp32 [Hkv]); slots int32 [T]: page * page_size + row, negative: none."""
-    import torch
-    if k is None or v is None:
+    if k is None:
         raise ValueError("keys and values are needed")
-    _head_sizes(q, k)
-    T, Hkv, d = k.shape
-    Hq, dev = 0 if q is None else q.shape[1], k.device
-    if (q is None) != (q_out is None):
-        raise ValueError("q_out goes with q")
-    a = AppendArgs(C.sizeof(AppendArgs), T, Hq, Hkv, d, *_rows(q, (T, Hq, d), dev, "q"), *_rows(k, (T, Hkv, d), dev, "k"),
-                   *_rows(v, (T, Hkv, d), dev, "v"), *_rows(q_out, (T, Hq, d), dev, "q_out"), _flat(slots, torch.int32, (T,), dev, "slots"),
-                   _paged_kv(cache_k, cache_v, k_scale, v_scale, Hkv, d, dev),
-                   _head_map(T, d, dev, q_weight, k_weight, eps, rope, positions, rope_style))
-    _launch(lib().dlm_paged_append, a, dev, stream)
+    _enqueue((_native or _load_native()).paged_append, k, stream, k, v, cache_k, cache_v, slots, q, q_out, k_scale, v_scale, q_weight, k_weight, eps, rope,
+             positions, rope_style)
 
 
-def _paged_attn_args(q, out, cache_k, cache_v, block_table, kv_len, *, max_kv_len: Optional[int] = None, q_len=None, mask_mode: int = MASK_FULL,
-                     block_size: int = 0, scale: float = 0.0, lse=None, k_scale=None, v_scale=None, workspace=None) -> PagedAttnArgs:
-    import torch
-    if q.dim() != 4 or block_table.dim() != 2:
-        raise ValueError("q [B, Lq, Hq, d] and block_table [B, pages of a sequence] expected")
-    B, Lq, Hq, d = q.shape
-    dev = q.device
-    kv = _paged_kv(cache_k, cache_v, k_scale, v_scale, None, d, dev)
-    width = block_table.shape[1] * kv.page_size
-    if max_kv_len is None:
-        max_kv_len = width
-    elif max_kv_len > width:
-        raise ValueError(f"max_kv_len {max_kv_len} exceeds the {width} tokens of a row of block_table")
-    qb, qt, qh, _ = q.stride()
-    ob, ot, oh, _ = out.stride()
-    return PagedAttnArgs(C.sizeof(PagedAttnArgs), B, Lq, Hq, cache_k.shape[1], d, _on(q, torch.bfloat16, None, dev, "q"), qb, qt, qh,
-                         _on(out, torch.bfloat16, q.shape, dev, "out"), ob, ot, oh, _flat(lse, torch.float32, (B, Hq, Lq), dev, "lse"), kv,
-                         _on(block_table, torch.int32, (B, block_table.shape[1]), dev, "block_table"), block_table.stride(0) if B > 1 else block_table.shape[1],
-                         _flat(kv_len, torch.int32, (B,), dev, "kv_len"), max_kv_len, _flat(q_len, torch.int32, (B,), dev, "q_len"), mask_mode, block_size,
-                         scale, *_buffer(workspace, dev))
+def paged_attn_workspace_bytes(q, out, cache_k, cache_v, block_table, kv_len, *, max_kv_len: Optional[int] = None, q_len=None, mask_mode: int = MASK_FULL,
+                               block_size: int = 0, scale: float = 0.0, lse=None, k_scale=None, v_scale=None) -> int:
+    """Bytes of workspace paged_attn wants for this call (0: none)."""
+    return (_native or _load_native()).paged_attn_workspace(0, q, out, cache_k, cache_v, block_table, kv_len, max_kv_len, q_len, mask_mode, block_size, scale,
+                                                            lse, k_scale, v_scale, None)
 
 
-def paged_attn_workspace_bytes(q, out, cache_k, cache_v, block_table, kv_len, **kw) -> int:
-    """Bytes of workspace paged_attn wants for this call (0: none).  Arguments as paged_attn's."""
-    kw.pop("stream", None)
-    return int(lib().dlm_paged_attn_workspace_bytes(C.byref(_paged_attn_args(q, out, cache_k, cache_v, block_table, kv_len, **kw))))
-
-
-def paged_attn(q, out, cache_k, cache_v, block_table, kv_len, *, stream=None, **kw) -> None:
+def paged_attn(q, out, cache_k, cache_v, block_table, kv_len, *, max_kv_len: Optional[int] = None, q_len=None, mask_mode: int = MASK_FULL,
+               block_size: int = 0, scale: float = 0.0, lse=None, k_scale=None, v_scale=None, workspace=None, stream=None) -> None:
     """Attention of the last Lq tokens of each sequence over a paged cache that holds them already.  q, out bf16 [B, Lq, Hq, d]; cache_k,
     cache_v as paged_append's; block_table int32 [B, pages]; kv_len int32 [B].  Keywords: max_kv_len (an upper bound of kv_len; default: what a
     row of block_table can hold), q_len (int32 [B]), mask_mode, block_size, scale, lse (fp32 [B, Hq, Lq]), k_scale, v_scale, workspace (a uint8
     tensor of paged_attn_workspace_bytes(...) bytes when that is not 0)."""
-    a = _paged_attn_args(q, out, cache_k, cache_v, block_table, kv_len, **kw)
-    _launch(lib().dlm_paged_attn, a, q.device, stream)
+    _enqueue((_native or _load_native()).paged_attn, q, stream, q, out, cache_k, cache_v, block_table, kv_len, max_kv_len, q_len, mask_mode, block_size, scale,
+             lse, k_scale, v_scale, workspace)

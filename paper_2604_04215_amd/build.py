@@ -25,6 +25,23 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE,
 SOURCE_FLAGS = {"attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]}
 
 
+MARSHAL = os.path.join(HERE, "_marshal.so")           # host side of the calls in every layer (csrc/marshal.cpp), a CPython module
+
+
+def build_marshal() -> None:
+    """Compile the marshalling module against torch's headers; it calls libdlm.so beside it."""
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + INCLUDE, "-I" + sysconfig.get_paths()["include"],
+                           *("-I" + p for p in include_paths()), f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L" + HERE, "-ldlm", "-L" + torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10",
+                           "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, MARSHAL)
+
+
 def build_lib(verbose: bool = False, save_temps: str | None = None) -> str:
     """Compile every source and link libdlm.so; always recompiles."""
     objdir = os.path.join(HERE, "_build")
@@ -50,6 +67,7 @@ def build_lib(verbose: bool = False, save_temps: str | None = None) -> str:
         tmp = lib + f".tmp{os.getpid()}"
         subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *lib_objs])
         os.replace(tmp, lib)
+    build_marshal()
     return LIB
 
 

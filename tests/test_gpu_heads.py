@@ -269,3 +269,38 @@ def test_rows_past_32_bits_of_offset():
     dlm.paged_append(x, x, ck, cv, torch.tensor([3, 21], dtype=I32, device=DEV))
     assert (ck[0, 0, 3] == 1).all() and (ck[1, 0, 5] == 2).all() and (cv[1, 0, 5] == 2).all() and (cv[0, 0, 3] == 1).all()
     assert int((flat != 0).sum()) == 6 * d
+
+
+def refused(match, fn, *args, **kw):
+    with pytest.raises(ValueError, match=match):
+        fn(*args, **kw)
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    x, w = torch.zeros((4, 2, 64), dtype=BF16, device=DEV), torch.zeros(64, dtype=BF16, device=DEV)
+    i4, table = torch.zeros(4, dtype=I32, device=DEV), torch.zeros((8, 64), device=DEV)
+    refused("goes with", dlm.qk_norm_rope, x, x, x, None)
+    refused("axis 0, expected 4", dlm.qk_norm_rope, x, x[:3], x, x[:3])
+    refused("dtype Float", dlm.qk_norm_rope, x.float(), None, x, None)
+    refused("innermost", dlm.qk_norm_rope, x.transpose(1, 2), None, x.transpose(1, 2), None)
+    refused("q_weight: size 64", dlm.qk_norm_rope, x[..., :32], None, x[..., :32], None, q_weight=w)
+    refused("needs positions", dlm.qk_norm_rope, x, None, x, None, rope=table)
+    refused("positions: size 4", dlm.qk_norm_rope, x[:3], None, x[:3], None, rope=table, positions=i4)
+    refused("rope: must be contiguous", dlm.qk_norm_rope, x, None, x, None, rope=table[:, :32], positions=i4)
+    refused("GPU", dlm.qk_norm_rope, x, None, x, None, q_weight=w.cpu())
+    refused("a tensor", dlm.qk_norm_rope, x, None, [1], None)
+    refused("goes with", dlm.qk_norm_rope_bwd, x, None, None, None)
+    pages = torch.zeros((2, 2, 16, 64), dtype=BF16, device=DEV)
+    refused("expected 2", dlm.paged_append, x, x, pages[:, :1], pages[:, :1], i4)
+    refused("strides", dlm.paged_append, x, x, pages, pages.transpose(1, 2).contiguous().transpose(1, 2), i4)
+    refused("slots", dlm.paged_append, x, x, pages, pages, None)
+    refused("v: is needed", dlm.paged_append, x, None, pages, pages, i4)
+    refused("dtype", dlm.paged_append, x, x, pages.half(), pages.half(), i4)
+    q, tab, two = torch.zeros((2, 1, 4, 64), dtype=BF16, device=DEV), torch.zeros((2, 3), dtype=I32, device=DEV), torch.zeros(2, dtype=I32, device=DEV)
+    refused("exceeds the 48", dlm.paged_attn, q, q.clone(), pages, pages, tab, two, max_kv_len=49)
+    refused("block_table", dlm.paged_attn, q, q.clone(), pages, pages, tab[:1], two)
+    refused("kv_len", dlm.paged_attn, q, q.clone(), pages, pages, tab, two.long())
+    refused("lse", dlm.paged_attn, q, q.clone(), pages, pages, tab, two, lse=torch.zeros((2, 1, 4), device=DEV))
+    with pytest.raises(dlm.DlmError, match="power of two") as e:
+        dlm.paged_attn(q, q.clone(), pages[:, :, :15], pages[:, :, :15], tab, two)
+    assert e.value.code == dlm.DLM_ERR_INVALID_ARG

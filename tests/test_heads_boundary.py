@@ -6,11 +6,12 @@ import subprocess
 import pytest
 import torch
 
+import heads_structs as S
 from paper_2604_04215_amd import binding as dlm
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-STRUCTS = [("dlm_paged_kv", dlm.PagedKv), ("dlm_head_map", dlm.HeadMap), ("dlm_qk_args", dlm.QkArgs), ("dlm_qk_bwd_args", dlm.QkBwdArgs),
-           ("dlm_append_args", dlm.AppendArgs), ("dlm_paged_attn_args", dlm.PagedAttnArgs)]
+STRUCTS = [("dlm_paged_kv", S.PagedKv), ("dlm_head_map", S.HeadMap), ("dlm_qk_args", S.QkArgs), ("dlm_qk_bwd_args", S.QkBwdArgs),
+           ("dlm_append_args", S.AppendArgs), ("dlm_paged_attn_args", S.PagedAttnArgs)]
 BAD, UNSUPPORTED, WORKSPACE = dlm.DLM_ERR_INVALID_ARG, dlm.DLM_ERR_UNSUPPORTED, dlm.DLM_ERR_WORKSPACE
 
 
@@ -41,18 +42,18 @@ def _fill(struct, fields):
 
 
 def _qk(**kw):
-    f = dict(struct_size=C.sizeof(dlm.QkArgs), T=4, Hq=4, Hkv=2, d=128, q=P, k=P, q_out=P, k_out=P, map=_map())
+    f = dict(struct_size=C.sizeof(S.QkArgs), T=4, Hq=4, Hkv=2, d=128, q=P, k=P, q_out=P, k_out=P, map=_map())
     for x, h in (("q", 4), ("k", 2), ("qo", 4), ("ko", 2)):
         f[x + "_stride_t"], f[x + "_stride_h"] = h * 128, 128
-    return _fill(dlm.QkArgs(), dict(f, **kw))
+    return _fill(S.QkArgs(), dict(f, **kw))
 
 
 def _bwd(**kw):
-    f = dict(struct_size=C.sizeof(dlm.QkBwdArgs), T=4, Hq=4, Hkv=2, d=128, d_q_out=P, d_k_out=P, q=P, k=P, d_q=P, d_k=P, d_q_weight=P, d_k_weight=P,
+    f = dict(struct_size=C.sizeof(S.QkBwdArgs), T=4, Hq=4, Hkv=2, d=128, d_q_out=P, d_k_out=P, q=P, k=P, d_q=P, d_k=P, d_q_weight=P, d_k_weight=P,
              map=_map(), workspace=P, workspace_bytes=1 << 20)
     for x, h in (("dqo", 4), ("dko", 2), ("q", 4), ("k", 2), ("dq", 4), ("dk", 2)):
         f[x + "_stride_t"], f[x + "_stride_h"] = h * 128, 128
-    return _fill(dlm.QkBwdArgs(), dict(f, **kw))
+    return _fill(S.QkBwdArgs(), dict(f, **kw))
 
 
 def _cache(**kw):
@@ -60,18 +61,18 @@ def _cache(**kw):
 
 
 def _append(**kw):
-    f = dict(struct_size=C.sizeof(dlm.AppendArgs), T=4, Hq=4, Hkv=2, d=128, q=P, k=P, v=P, q_out=P, slots=P, cache=_cache(), map=_map())
+    f = dict(struct_size=C.sizeof(S.AppendArgs), T=4, Hq=4, Hkv=2, d=128, q=P, k=P, v=P, q_out=P, slots=P, cache=_cache(), map=_map())
     for x, h in (("q", 4), ("k", 2), ("v", 2), ("qo", 4)):
         f[x + "_stride_t"], f[x + "_stride_h"] = h * 128, 128
-    return _fill(dlm.AppendArgs(), dict(f, **kw))
+    return _fill(S.AppendArgs(), dict(f, **kw))
 
 
 def _attn(**kw):
-    f = dict(struct_size=C.sizeof(dlm.PagedAttnArgs), B=2, Lq=1, Hq=4, Hkv=2, d=128, q=P, out=P, cache=_cache(), block_table=P, table_stride=4, kv_len=P,
+    f = dict(struct_size=C.sizeof(S.PagedAttnArgs), B=2, Lq=1, Hq=4, Hkv=2, d=128, q=P, out=P, cache=_cache(), block_table=P, table_stride=4, kv_len=P,
              max_kv_len=64)
     for x in "qo":
         f[x + "_stride_b"], f[x + "_stride_t"], f[x + "_stride_h"] = 4 * 128, 4 * 128, 128
-    return _fill(dlm.PagedAttnArgs(), dict(f, **kw))
+    return _fill(S.PagedAttnArgs(), dict(f, **kw))
 
 
 # rotation and norm: the same for all three calls that have them
@@ -125,23 +126,19 @@ def test_workspace_sizes():
     assert dlm.qk_norm_rope_bwd_workspace_bytes(1, 4, 2, 128) == 2 * 128 * 4                    # one workgroup a tensor
     assert dlm.qk_norm_rope_bwd_workspace_bytes(1 << 20, 32, 8, 64) == 2 * 1024 * 64 * 4        # at most 1024 a tensor
     L = dlm.lib()
+    L.dlm_paged_attn_workspace_bytes.restype = C.c_size_t
     assert L.dlm_paged_attn_workspace_bytes(C.byref(_attn())) == 0                              # four tiles: nothing to share out
     one = L.dlm_paged_attn_workspace_bytes(C.byref(_attn(table_stride=1 << 20, max_kv_len=65536)))
     assert one > 0 and one % (2 * 4 * (128 + 2) * 4) == 0
     assert L.dlm_paged_attn_workspace_bytes(None) == 0
 
 
-def test_binding_refuses_tensors_that_do_not_fit():
+def test_binding_refuses_what_is_not_on_the_gpu():
     x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
-    with pytest.raises(ValueError, match="GPU"):
-        dlm.qk_norm_rope(x, None, x, None)
-    with pytest.raises(ValueError, match="needed"):
-        dlm.qk_norm_rope(None, None, None, None)
-    with pytest.raises(ValueError, match="goes with"):
-        dlm.qk_norm_rope(x, x, x, None)
-    with pytest.raises(ValueError, match="expected"):
-        dlm.qk_norm_rope(x, x[:3], x, x[:3])
-    with pytest.raises(ValueError, match="goes with"):
-        dlm.qk_norm_rope_bwd(x, None, None, None)
-    with pytest.raises(ValueError, match="needed"):
-        dlm.paged_append(None, x, x, x, None)
+    for call in (lambda: dlm.qk_norm_rope(x, None, x, None), lambda: dlm.qk_norm_rope_bwd(x, None, x, None), lambda: dlm.paged_append(x, x, x, x, x),
+                 lambda: dlm.paged_attn(x, x, x, x, x, x), lambda: dlm.paged_attn_workspace_bytes(x[None], x[None], x[None], x[None], x, x)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    for call in (lambda: dlm.qk_norm_rope(None, None, None, None), lambda: dlm.qk_norm_rope_bwd(None, None, None, None), lambda: dlm.paged_append(None, x, x, x, x)):
+        with pytest.raises(ValueError, match="needed"):
+            call()
