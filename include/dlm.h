@@ -419,7 +419,7 @@ typedef struct dlm_paged_kv {
 #define DLM_ROPE_PAIRS         1    /* entry 2c with entry 2c + 1,   by angle c   (c < rot/2) */
 
 /* dlm_head_map -- what happens to each query and key head x (d entries) of a token:
- *   z = x * w / sqrt(mean(x^2) + eps)     with w = q_weight or k_weight (bf16 [d]); NULL: z = x
+ *   z = x * w / sqrt(mean(x^2) + eps)     with w = q_weight or k_weight (bf16 [d]) and eps >= 2^-126; NULL: z = x
  *   y = z, its first rot_dim entries rotated by the token's angles: (a, b) -> (a cos - b sin, b cos + a sin)
  *   rope       fp32 [rope_len, rot_dim] contiguous, 16-byte aligned: row p holds the rot_dim/2 cosines, then the sines, of position p.  NULL: no
  *              rotation.  (A table from angles in 64 bits: 32 bits lose the angles of far positions.)

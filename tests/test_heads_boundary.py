@@ -76,7 +76,7 @@ def _attn(**kw):
 
 
 # rotation and norm: the same for all three calls that have them
-MAP = [(dict(eps=-1.0), BAD), (dict(eps=float("nan")), BAD), (dict(rope_style=2), BAD), (dict(rot_dim=8), UNSUPPORTED), (dict(rot_dim=24), UNSUPPORTED),
+MAP = [(dict(eps=-1.0), BAD), (dict(eps=0.0), BAD), (dict(eps=float("nan")), BAD), (dict(rope_style=2), BAD), (dict(rot_dim=8), UNSUPPORTED), (dict(rot_dim=24), UNSUPPORTED),
        (dict(rot_dim=144), UNSUPPORTED), (dict(rope_len=0), BAD), (dict(positions=None), BAD), (dict(rope=P + 4), UNSUPPORTED), (dict(q_weight=P + 2), UNSUPPORTED)]
 CACHE = [(dict(type=2), BAD), (dict(n_pages=-1), BAD), (dict(page_size=24), BAD), (dict(page_size=0), BAD), (dict(page_size=8), UNSUPPORTED),
          (dict(page_size=1 << 17), UNSUPPORTED), (dict(n_pages=1 << 27), UNSUPPORTED), (dict(k=None), BAD), (dict(v=P + 8), UNSUPPORTED),
@@ -124,7 +124,7 @@ def test_null_args_and_empty_problems():
 def test_workspace_sizes():
     assert dlm.qk_norm_rope_bwd_workspace_bytes(0, 4, 2, 128) == 0
     assert dlm.qk_norm_rope_bwd_workspace_bytes(1, 4, 2, 128) == 2 * 128 * 4                    # one workgroup a tensor
-    assert dlm.qk_norm_rope_bwd_workspace_bytes(1 << 20, 32, 8, 64) == 2 * 1024 * 64 * 4        # at most 1024 a tensor
+    assert 0 < dlm.qk_norm_rope_bwd_workspace_bytes(1 << 20, 32, 8, 64) <= 16386 * 64 * 4        # however many tokens
     L = dlm.lib()
     L.dlm_paged_attn_workspace_bytes.restype = C.c_size_t
     assert L.dlm_paged_attn_workspace_bytes(C.byref(_attn())) == 0                              # four tiles: nothing to share out
