@@ -529,9 +529,10 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  *   scale        <= 0 selects 1/sqrt(d)
  * A row that sees no key, or only scores of -inf, gets out = 0 and lse = -inf.  Arithmetic as dlm_block_attn; e4m3 entries are exact in bf16, their scales
  * are applied in fp32.
- * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it several workgroups share the keys
- * of a sequence (fp32 partial results, joined in a fixed order by a second launch: deterministic); calls that may overlap need one each.
- * Without one, or with a smaller one, a call runs unsplit; results then differ by the rounding of another summation order only.
+ * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it the keys of all sequences are dealt out evenly to the
+ * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
+ * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,
+ * a call runs one workgroup for each sequence and KV head; results then differ by the rounding of another summation order only.
  * Values that a row does not see have to be finite where another of the 32 rows of its tile sees them (they are multiplied by zero).
  * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8; stride_t of the cache below 2^26. */
 typedef struct dlm_paged_attn_args {
@@ -599,7 +600,10 @@ size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
  *                   grid; forward and the dQ pass), 2 = under a block-causal mask the row tile with the longest
  *                   key range is dispatched first, 4 = the same grouping for the dK / dV passes; 0 = plain
  *                   (tile, KV head, sequence) grids.
- *   "paged_chunk"   0 = the library decides how many keys of a sequence a workgroup of dlm_paged_attn takes (default); n >= 1 = 32 n
+ *   "paged_shares"  0 = the library decides whether the keys of a dlm_paged_attn with a workspace are dealt out evenly to a number of workgroups
+ *                   whatever the sequences' lengths (default); -1 = one workgroup for each sequence, KV head and group of rows; n >= 1 = n
+ *                   workgroups share them (the workspace's size depends on it).
+ *   "paged_shape"   0 = the library picks dlm_paged_attn's workgroups from the rows a KV head has (default); 1, 2, 3 = 16, 32, 128 rows
  *                   (the workspace's size depends on it).
  * The knobs exist for tests and tuning sweeps. */
 int dlm_set_option(const char *name, int value);

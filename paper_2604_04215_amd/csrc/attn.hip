@@ -1232,7 +1232,8 @@ extern "C" int dlm_set_option(const char* name, int value) {
     if (!strcmp(name, "lmhead_nt")) return lm_set_nt(value);
     if (!strcmp(name, "lmhead_cus")) return lm_set_cus(value);
     if (!strcmp(name, "kv_copy_unroll")) return copy_set_unroll(value);
-    if (!strcmp(name, "paged_chunk")) return paged_set_chunk(value);
+    if (!strcmp(name, "paged_shares")) return paged_set_shares(value);
+    if (!strcmp(name, "paged_shape")) return paged_set_shape(value);
     if (!strcmp(name, "attn_remap")) {
         if (value < 0 || value > 7) return fail(DLM_ERR_INVALID_ARG, "set_option: attn_remap must be 0..7");
         g_attn_remap = value;

@@ -27,7 +27,8 @@ int lm_set_block(int v);     // lmhead.hip
 int lm_set_nt(int v);        // lmhead.hip
 int lm_set_cus(int v);       // lmhead.hip
 int copy_set_unroll(int v);  // commit.hip
-int paged_set_chunk(int v);  // paged_attn.hip
+int paged_set_shares(int v);  // paged_attn.hip
+int paged_set_shape(int v);  // paged_attn.hip
 extern int g_attn_remap;     // attn.hip: bit 0 forward + dQ, bit 1 longest key range first, bit 2 dK / dV passes
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

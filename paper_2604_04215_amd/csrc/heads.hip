@@ -13,19 +13,6 @@
 
 namespace dlm {
 
-// quotient of n < 2^31 by a divisor fixed on the host
-struct FastDiv {
-    uint32_t mul, shift;
-};
-inline FastDiv fast_div(uint32_t d) {
-    FastDiv f;
-    f.shift = 0;
-    while ((1ull << f.shift) < d) ++f.shift;
-    f.mul = (uint32_t)((((1ull << f.shift) - d) << 32) / d + 1);
-    return f;
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t n, FastDiv f) { return (__umulhi(n, f.mul) + n) >> f.shift; }
-
 // How the wavefronts of a part go over its T * H heads, 1024 / D at a time: with H of at least as many, `per` wavefronts share a token, else a
 // wavefront takes `tokens` whole ones.  Either way the addresses of a step are a lane's own constant plus something uniform.
 struct Walk {

@@ -1,8 +1,21 @@
-// What dlm_paged_append and dlm_paged_attn share: checks of a paged cache, the addresses of its rows.
+// What the paged-cache and head kernels share: division by what the host knows, checks of a paged cache.
 #pragma once
 #include "common.hpp"
 
 namespace dlm {
+
+// quotient of n < 2^31 by a divisor fixed on the host
+struct FastDiv {
+    uint32_t mul, shift;
+};
+inline FastDiv fast_div(uint32_t d) {
+    FastDiv f;
+    f.shift = 0;
+    while ((1ull << f.shift) < d) ++f.shift;
+    f.mul = (uint32_t)((((1ull << f.shift) - d) << 32) / d + 1);
+    return f;
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, FastDiv f) { return (__umulhi(n, f.mul) + n) >> f.shift; }
 
 // true if a tensor of n[i] steps of stride[i] over rows of `row` entries has no two entries at one place
 template <int N>

@@ -1,13 +1,15 @@
 // dlm_paged_attn: a block of new tokens, or one, against the pages of its sequence.
 //
-// The g = Hq/Hkv query heads of a KV head and the sequence's query rows are packed into R = g * q_len rows (row = i*g + head), so
-// a KV head's keys are read once for 32 of them.  A workgroup owns 32 rows of one (sequence, KV head) and a stretch of its keys; its
-// four wavefronts take every fourth 32-key tile, each with LDS of its own, and join through LDS at the end; with a workspace the
-// stretches of one sequence go to several workgroups and paged_merge_kernel joins those.
-//
-// Per tile and wavefront: S^T = K Q^T (a lane then has 16 keys of one row: maximum and sum are in-lane plus one swap of lane
-// halves), p rounded to bf16 for the second product (its relative error 2^-9 an entry averages out; the sum uses the unrounded p),
-// O^T += V^T P^T with V^T from the transposing LDS read.  Everything else is fp32.
+// The g = Hq/Hkv query heads of a KV head and the sequence's query rows are packed into R = g * q_len rows (row = i*g + head), and a workgroup
+// takes some of them, a "row group" of one (sequence, KV head).  With a workspace the 32-key tiles of all row groups are dealt
+// out evenly whatever the lengths (see Shares), and paged_merge_kernel joins what belongs together.  Three shapes, by R (see plan_rows):
+//   paged_thin_kernel   16 rows, keys split over the wavefronts (a few short sequences): bound by latency
+//   paged_wide_kernel   32 rows, keys split over the wavefronts (single tokens, small blocks): bound by HBM
+//   paged_tall_kernel   128 rows, 32 a wavefront, which share the tiles of keys in LDS (blocks with many heads a KV head): bound by the products
+//                       and what stands between them
+// Per 32-key tile: S^T = K Q^T (a lane then has 8 or 16 keys of one row: maximum and sum are in-lane but for one or two swaps), p rounded to bf16
+// for the second product (its relative error 2^-9 an entry averages out; the sum uses the unrounded p), O^T += V^T P^T with V^T from the
+// transposing LDS read.  Everything else is fp32.
 #include "paged.hpp"
 
 namespace dlm {
@@ -33,11 +35,15 @@ struct PagedAttnParams {
     int max_kv_len;
     const int32_t* q_len;
     int bs;                        // block size of the block-causal mask
+    FastDiv by_g, by_bs;
     float scale_log2;              // scale * log2(e): the softmax is evaluated with exp2
-    // Stretches of `chunk` 32-key tiles: a sequence of T tiles has max(1, ceil(T / chunk)) of them, one workgroup each.
-    int chunk, nsplit, row_tiles;
-    GridRemap remap;
-    float *part_o, *part_ml;       // [nsplit][B * Hq * Lq][d] and [..][2]: sums and (maximum in log2 units, sum) of a stretch
+    int rows_wg, row_groups;       // rows of a workgroup; row groups that Lq rows make
+    GridRemap remap;               // one workgroup a row group
+    // even shares: workgroups, and what they leave to be joined: sums [2 * shares][rows_wg][d] with (maximum in log2 units, sum) [..][2], and for each
+    // row group its first workgroup and their number
+    int shares;
+    float *part_o, *part_ml;
+    int32_t* meta;
 };
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) {
@@ -49,73 +55,559 @@ __device__ __forceinline__ int clamped(int v, int hi) { return min(max(v, 0), hi
 
 // eight e4m3 entries as bf16 (exact: bf16 has more of both exponent and mantissa)
 __device__ __forceinline__ u32x4 widen_e4m3(uint32_t lo, uint32_t hi) {
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
-    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    return u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), pack_bf16x2(c[0], c[1]), pack_bf16x2(d[0], d[1])};
+    auto pair = [](uint32_t w, bool upper) {
+        union { __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 b; uint32_t u; } x;
+        if (upper) x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        else x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+        return x.u;
+    };
+    return u32x4{pair(lo, false), pair(lo, true), pair(hi, false), pair(hi, true)};
 }
 
-// How many keys of the sequence any of the rows before `rows_end` sees
+// Keys that query i of a sequence sees
 template <bool BC>
-__device__ __forceinline__ int visible_keys(const PagedAttnParams& p, int len, int ql, int rows_end) {
+__device__ __forceinline__ int visible_keys(const PagedAttnParams& p, int len, int ql, int i) {
     if (!BC) return len;
-    const int pos = len - ql + (rows_end - 1) / p.g;
-    return pos < 0 ? 0 : min((int64_t)len, ((int64_t)(pos / p.bs) + 1) * p.bs);
+    const int pos = len - ql + i;
+    return pos < 0 ? 0 : (int)min((int64_t)len, ((int64_t)quotient(pos, p.by_bs) + 1) * p.bs);
 }
 
-// NT: non-temporal loads, where one workgroup is the only reader of its keys.
+__device__ __forceinline__ int query_of(const PagedAttnParams& p, int r) { return (int)quotient(r, p.by_g); }
+
+// What a workgroup works on: RT rows of one (sequence, KV head) from r0 on, tiles t0 .. t0 + Tn - 1 of 32 keys.
+template <int RT, bool BC>
+struct Work {
+    int b, kvh, r0, len, ql, R, seen, t0, Tn;
+    int slot;                               // where its sums go; -1: nobody else has keys of these rows, it writes the output
+    // one workgroup a row group
+    __device__ __forceinline__ bool place(const PagedAttnParams& p) {
+        int grp, rg;
+        if (!remap_decode(p.remap, p.B * p.Hkv, grp, rg)) return false;
+        kvh = grp % p.Hkv;
+        b = grp / p.Hkv;
+        r0 = rg * RT;
+        t0 = 0;
+        slot = -1;
+        return true;
+    }
+    __device__ __forceinline__ void lengths(const PagedAttnParams& p, int len_, int ql_) {
+        len = clamped(len_, p.max_kv_len);
+        ql = p.q_len ? clamped(ql_, p.Lq) : p.Lq;
+        R = ql * p.g;
+    }
+    // (once r0 is known)
+    __device__ __forceinline__ void see(const PagedAttnParams& p) {
+        seen = visible_keys<BC>(p, len, ql, query_of(p, min(r0 + RT, R) - 1));
+        Tn = (seen + 31) >> 5;
+    }
+    // keys that row r sees
+    __device__ __forceinline__ int limit(const PagedAttnParams& p, int r) const { return visible_keys<BC>(p, len, ql, query_of(p, r)); }
+    __device__ __forceinline__ const uint16_t* query(const PagedAttnParams& p, int r) const {
+        const int i = query_of(p, r);
+        return p.q + b * p.q_sb + i * p.q_st + (int64_t)(kvh * p.g + r - i * p.g) * p.q_sh;
+    }
+};
+
+constexpr int SMALLEST_SHARE = 8;           // tiles: two a wavefront
+
+// Even shares.  The tiles of all row groups, sequence by sequence, KV head by KV head, make one line of N (a row group has at least one, so that somebody
+// writes its zeros; under a block-causal mask each has as many as its sequence's last); workgroup w of W takes [w N / W, (w + 1) N / W).  So one long
+// sequence among short ones, or too few sequences for the chip, cost nothing but the joins, and the host need not know the lengths.  A share is the end of one
+// row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began elsewhere) and 2w + 1.
+template <int RT, bool BC>
+struct Shares {
+    int w, W, N, at, end;                   // its tiles: at .. end - 1
+    int b, base, len, ql;                   // the sequence of `at`, its first tile, its lengths as given
+    // tiles of each row group of a sequence, and the row groups
+    static __device__ __forceinline__ int tiles_of(const PagedAttnParams& p, int len_, int ql_, int& groups) {
+        const int len = clamped(len_, p.max_kv_len), ql = p.q_len ? clamped(ql_, p.Lq) : p.Lq;
+        groups = p.Hkv * ((ql * p.g + RT - 1) / RT);
+        return ql > 0 ? max((visible_keys<BC>(p, len, ql, ql - 1) + 31) >> 5, 1) : 0;
+    }
+    // (v, W <= 65536, so the remainders' product fits 32 bits; a quotient of whole numbers below 2^47 by N < 2^31 that is under 2^17 is at least 2^-31 from
+    // the next whole one unless it is one, which 53 bits tell apart)
+    __device__ __forceinline__ int start_of(uint32_t v) const {
+        const uint32_t q = (uint32_t)N / (uint32_t)W, r = (uint32_t)N - q * W;
+        return __builtin_amdgcn_readfirstlane(v * q + v * r / (uint32_t)W);
+    }
+    __device__ __forceinline__ int owner_of(int tile) const { return (int)((((double)tile + 1.0) * W - 1.0) / N); }
+    // false: no share for this workgroup.  smem: 8 ints
+    __device__ bool find(const PagedAttnParams& p, int* smem) {
+        const int tid = threadIdx.x & 255, lane = lane_id(), wave = tid >> 6;        // (a second 256 threads do the same)
+        const int each = (p.B + 255) / 256, from = min(tid * each, p.B), to = min(from + each, p.B);
+        int own = 0, groups;
+        for (int i = from; i < to; ++i) {
+            const int u = tiles_of(p, p.kv_len[i], p.q_len ? p.q_len[i] : 0, groups);
+            own += u * groups;
+        }
+        int sum = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += v;
+        }
+        if (lane == 63) smem[wave] = sum;
+        __syncthreads();
+        const int s0 = smem[0], s1 = smem[1], s2 = smem[2], s3 = smem[3];
+        N = __builtin_amdgcn_readfirstlane(s0 + s1 + s2 + s3);
+        W = __builtin_amdgcn_readfirstlane(min(p.shares, max(N / SMALLEST_SHARE, 1)));
+        w = blockIdx.x;
+        if (w >= W || N == 0) return false;
+        at = start_of(w);
+        end = start_of(w + 1);
+        int first = sum - own + (wave > 0 ? s0 : 0) + (wave > 1 ? s1 : 0) + (wave > 2 ? s2 : 0);
+        if (at >= first && at < first + own) {
+            for (int i = from; i < to; ++i) {
+                const int l = p.kv_len[i], q = p.q_len ? p.q_len[i] : 0, u = tiles_of(p, l, q, groups);
+                if (at < first + u * groups) {
+                    smem[4] = i;
+                    smem[5] = first;
+                    smem[6] = l;
+                    smem[7] = q;
+                    break;
+                }
+                first += u * groups;
+            }
+        }
+        __syncthreads();
+        b = __builtin_amdgcn_readfirstlane(smem[4]);
+        base = __builtin_amdgcn_readfirstlane(smem[5]);
+        len = __builtin_amdgcn_readfirstlane(smem[6]);
+        ql = __builtin_amdgcn_readfirstlane(smem[7]);
+        __syncthreads();                    // smem is the tiles' place
+        return true;
+    }
+    // the next piece of the share; false: done
+    __device__ __forceinline__ bool next(const PagedAttnParams& p, Work<RT, BC>& wk) {
+        if (at >= end) return false;
+        int groups, units = tiles_of(p, len, ql, groups);
+        while (at >= base + units * groups) {        // (on to the next sequence that has rows; there is one, end being at most N)
+            base += units * groups;
+            ++b;
+            len = p.kv_len[b];
+            ql = p.q_len ? p.q_len[b] : 0;
+            units = tiles_of(p, len, ql, groups);
+        }
+        const int grp = __builtin_amdgcn_readfirstlane((at - base) / units), first = base + grp * units;
+        wk.b = b;
+        wk.lengths(p, len, ql);
+        const int rgs = (wk.R + RT - 1) / RT;
+        wk.kvh = rgs > 1 ? __builtin_amdgcn_readfirstlane(grp / rgs) : grp;
+        wk.r0 = (grp - wk.kvh * rgs) * RT;
+        wk.see(p);
+        wk.t0 = at - first;
+        const int stop = min(end, first + units);
+        wk.Tn = max(min(stop - first, wk.Tn) - wk.t0, 0);       // (tiles behind the last one that any of these rows sees are left out)
+        const bool whole = wk.t0 == 0 && stop == first + units;
+        wk.slot = whole ? -1 : 2 * w + (wk.t0 == 0);
+        if (wk.t0 == 0 && threadIdx.x == 0) {
+            int32_t* m = p.meta + 2 * (((int64_t)b * p.Hkv + wk.kvh) * p.row_groups + wk.r0 / RT);
+            m[0] = w;
+            m[1] = owner_of(first + units - 1) - w + 1;
+        }
+        at = stop;
+        return true;
+    }
+};
+
+// Pages of a wavefront's next 32 tiles, `step` apart: lane 2j + h holds the one of half h (16 keys, a page is no smaller) of its j-th tile.  One
+// load for 32 tiles, requested 32 tiles ahead: a look-up a tile was a trip to memory in front of every fetch.  The first one travels with the
+// sequence's lengths, so it may look at entries behind the sequence's end (but inside the table's row): whatever they hold, a page outside the
+// cache is not read and a key behind the end not seen.
+template <int ES>
+struct Pages {
+    const int32_t* table;
+    int first, step, last, now, next;
+    __device__ __forceinline__ int look(const PagedAttnParams& p, int j) const {
+        const int lane = lane_id();
+        return table[min((int)(((int64_t)(first + step * (j + (lane >> 1))) * 32 + 16 * (lane & 1)) >> p.page_shift), last)];
+    }
+    __device__ __forceinline__ Pages(const PagedAttnParams& p, int b, int first_tile, int step_) {
+        table = p.table + b * p.table_stride;
+        first = first_tile;
+        step = step_;
+        last = (max(p.max_kv_len, 1) - 1) >> p.page_shift;
+        now = p.max_kv_len > 0 ? look(p, 0) : 0;
+        next = 0;
+    }
+    // before tile 0: `n` tiles in all
+    __device__ __forceinline__ void begin(const PagedAttnParams& p, int n) {
+        if (n > 32) next = look(p, 32);
+    }
+    // before tile j > 0 of n
+    __device__ __forceinline__ void advance(const PagedAttnParams& p, int j, int n) {
+        if ((j & 31) == 0) {
+            now = next;
+            if (j + 32 < n) next = look(p, j + 32);
+        }
+    }
+    // byte offset of half h of tile j in the cache; false: there is no such page
+    __device__ __forceinline__ bool half(const PagedAttnParams& p, int j, int h, int64_t& base) const {
+        const int page = __builtin_amdgcn_readlane(now, 2 * (j & 31) + h), key = (first + step * j) * 32 + 16 * h;
+        const bool there = (unsigned)page < (unsigned)p.n_pages;
+        base = ((int64_t)(there ? page : 0) * p.sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.st) * ES;
+        return there;
+    }
+};
+
+// Runs `rows(work, pages)` for what this workgroup has to do; the pages are those of every STEP-th tile from the wavefront's (STEP 2: its half of the
+// workgroup's) first on.
+template <int RT, bool BC, bool EVEN, int ES, int STEP, typename F>
+__device__ __forceinline__ void run_rows(const PagedAttnParams& p, unsigned char* smem, const F& rows) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> (STEP == 2 ? 8 : 6));
+    Work<RT, BC> wk;
+    if constexpr (EVEN) {
+        Shares<RT, BC> sh;
+        if (!sh.find(p, reinterpret_cast<int*>(smem))) return;
+        while (sh.next(p, wk)) {
+            Pages<ES> pages(p, wk.b, wk.t0 + w, STEP);
+            rows(wk, pages);
+            __syncthreads();                // the LDS is the next piece's
+        }
+    } else {
+        if (!wk.place(p)) return;
+        Pages<ES> pages(p, wk.b, w, STEP);  // (in flight together with the lengths)
+        wk.lengths(p, p.kv_len[wk.b], p.q_len ? p.q_len[wk.b] : 0);
+        if (wk.r0 >= wk.R) return;
+        wk.see(p);
+        rows(wk, pages);
+    }
+}
+
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const unsigned char* a) {
+    return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a)) : *reinterpret_cast<const u32x4*>(a);
+}
+
+// 16 bytes of cache into LDS as bf16
+template <bool F8>
+__device__ __forceinline__ void stage16(unsigned char* dst, u32x4 v) {
+    u32x4* d = reinterpret_cast<u32x4*>(dst);
+    if constexpr (F8) {
+        d[0] = widen_e4m3(v[0], v[1]);
+        d[1] = widen_e4m3(v[2], v[3]);
+    } else d[0] = v;
+}
+
+// The maximum that exponentials are relative to follows the running one only when that has grown by 2^8 (p stays in range of bf16 and of the
+// sums): the accumulators are rescaled a few times a row instead of at every tile.
+struct Running {
+    float m, l;
+    // mx: largest score of the tile in log2 units.  Returns the factor for what has been summed up; m_use: what to subtract.
+    __device__ __forceinline__ float follow(float mx, float& m_use) {
+        const bool grow = mx > m + 8.0f;
+        const float m_new = grow ? mx : m;
+        m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = grow ? fast_exp2(m - m_use) : 1.0f;
+        m = m_new;
+        return alpha;
+    }
+};
+
+// scores of keys that the lane's row does not see; entry i of S is key at + STEP * (i / 4) + i % 4, entries from N/2 on lie in the second half
+template <int N, int STEP, typename V>
+__device__ __forceinline__ void hide(V& S, int at, int limit, bool here0, bool here1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (at + STEP * (i >> 2) + (i & 3) >= limit || !(i < N / 2 ? here0 : here1)) S[i] = -INFINITY;
+}
+
+// One 32-key tile in LDS (K rows KP bytes apart, V rows VP) for the 32 rows of a wavefront: scores, softmax, P V.
+template <int D, int KP, int VP>
+__device__ __forceinline__ void tile32(const unsigned char* Kl, const unsigned char* Vl, const bf16x8 (&qf)[D / 16], int key0, int limit, int limit_min,
+                                       bool here0, bool here1, float scale_log2, Running& run, f32x16 (&O)[D / 32], int lane) {
+    const int n = lane & 31, hi = lane >> 5;
+    f32x16 S;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Kl + n * KP + (16 * c + 8 * hi) * 2), qf[c], S, 0, 0, 0);
+    if (key0 + 32 > limit_min || !here0 || !here1) hide<16, 8>(S, key0 + 4 * hi, limit, here0, here1);
+    float mx = -INFINITY, m_use, rs = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2, m_use);
+    uint32_t pk[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
+        rs += p0 + p1;
+        pk[i >> 1] = pack_bf16x2(p0, p1);
+    }
+    if (__any(alpha != 1.0f)) {
+        run.l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
+    }
+    run.l += rs;
+    const u32x4 plo = {pk[0], pk[1], pk[2], pk[3]}, phi = {pk[4], pk[5], pk[6], pk[7]};
+    const bf16x8 pf[2] = {as_bf16x8(plo), as_bf16x8(phi)};
+    const int s16 = lane & 15, blk = (lane >> 4) & 1;
+    const unsigned char* vbase = Vl + (4 * hi + (s16 >> 2)) * VP + (16 * blk + 4 * (s16 & 3)) * 2;
+#pragma unroll
+    for (int e = 0; e < 2 * (D / 32); ++e) {
+        union { s16x4 h[2]; bf16x8 v; } f;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            f.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vbase + (16 * (e & 1) + 8 * q) * VP + 32 * (e >> 1) * 2));
+        O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[e & 1], O[e >> 1], 0, 0, 0);
+    }
+}
+
+// What becomes of row r0 + rr: sums to be joined, or the output.  o: 8 entries from c8 * 8 on, relative to M.
+template <int D, bool F8, int RT, bool BC>
+__device__ __forceinline__ void put_row(const PagedAttnParams& p, const Work<RT, BC>& wk, int rr, int c8, const float (&o)[8], float M, float den) {
+    if (wk.slot >= 0) {
+        const int64_t at = (int64_t)wk.slot * RT + rr;
+        *reinterpret_cast<f32x4*>(p.part_o + at * D + 8 * c8) = f32x4{o[0], o[1], o[2], o[3]};
+        *reinterpret_cast<f32x4*>(p.part_o + at * D + 8 * c8 + 4) = f32x4{o[4], o[5], o[6], o[7]};
+        if (c8 == 0) {
+            p.part_ml[at * 2] = M;
+            p.part_ml[at * 2 + 1] = den;
+        }
+        return;
+    }
+    const int r = wk.r0 + rr, i = query_of(p, r), h = wk.kvh * p.g + r - i * p.g;
+    const float inv = (den == 0.f ? 0.f : 1.f / den) * (F8 && p.v_scale ? p.v_scale[wk.kvh] : 1.f);
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+    *reinterpret_cast<u32x4*>(p.out + wk.b * p.o_sb + i * p.o_st + (int64_t)h * p.o_sh + 8 * c8) = v;
+    if (p.lse && c8 == 0) p.lse[((int64_t)wk.b * p.Hq + h) * p.Lq + i] = den == 0.f ? -INFINITY : (M + log2f(den)) * 0.6931471805599453f;
+}
+
+// Joins NW wavefronts' sums of the same RT rows from LDS: row k * RT + r of `mb` has MP floats, the D entries, the maximum, the sum.
+template <int D, bool F8, int RT, int NW, int MP, bool BC>
+__device__ __forceinline__ void join_rows(const PagedAttnParams& p, const Work<RT, BC>& wk, const float* mb, int tid) {
+    constexpr int C8 = D / 8;
+    for (int task = tid; task < RT * C8; task += 64 * NW) {
+        const int rr = task / C8, c8 = task - rr * C8;
+        if (wk.r0 + rr >= wk.R) continue;
+        float M = -INFINITY, den = 0.f, wgt[NW], o[8];
+#pragma unroll
+        for (int k = 0; k < NW; ++k) M = __builtin_fmaxf(M, mb[(k * RT + rr) * MP + D]);
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            const float mk = mb[(k * RT + rr) * MP + D];
+            wgt[k] = mk == -INFINITY ? 0.f : fast_exp2(mk - M);
+            den += wgt[k] * mb[(k * RT + rr) * MP + D + 1];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            const float* src = mb + (k * RT + rr) * MP + 8 * c8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += wgt[k] * src[e];
+        }
+        put_row<D, F8>(p, wk, rr, c8, o, M, den);
+    }
+}
+
+// The thread's index, made anew: what the shapes derive from it is not kept in registers from one row group of a workgroup to the next (the compiler
+// hoisted a hundred values out of that loop and spilled them).
+__device__ __forceinline__ int fresh_thread() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
+// LDS of the three shapes: values (or keys and values) of a tile a wavefront, which the join's sums replace; two tiles a workgroup
+constexpr int larger(int a, int b) { return a > b ? a : b; }
+constexpr int THIN_WAVES = 8;
+constexpr int thin_smem(int d) { return larger(THIN_WAVES * 32 * (2 * d + 64), THIN_WAVES * 16 * (d + 4) * 4); }
+constexpr int wide_smem(int d) { return larger(4 * 32 * (4 * d + 80), 4 * 32 * (d + 4) * 4); }
+constexpr int tall_smem(int d) { return 4 * 32 * (4 * d + 80); }
+
+// ---- 16 rows ------------------------------------------------------------------------------------------------
+// For short sequences, where latency counts: eight wavefronts split the keys, 16 x 16 x 32 products, and K goes from memory straight into operand
+// registers (lane: key l % 16, 16 bytes of its row); V through LDS for the transposing read.  (3 sequences of up to 400 tokens, 14/2 heads
+// of 64: four wavefronts of the 32-row shape 6.3 us, of this one 5.8.)
+template <int D, bool F8, bool BC>
+__device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const Work<16, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
+    constexpr int NW = THIN_WAVES, RT = 16;
+    constexpr int VP = D * 2 + 64;
+    constexpr int ES = F8 ? 1 : 2;
+    constexpr int C = D * ES / 16, RPL = 64 / C, NLD = 32 / RPL;      // V: 16-byte pieces a row, rows a load, loads
+    constexpr int NK = D * ES / 64;                                   // K: loads a half tile; 4 lanes have 64 bytes of a row each time
+    constexpr int MP = D + 4;
+
+    const int tid = fresh_thread(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
+
+    // Query row n (B operand).  Which 8 entries of a row the 4 lane groups multiply in step c only has to be the same for K: with an 8-bit cache 16 bytes
+    // of K are two steps' entries.
+    bf16x8 qf[D / 32];
+    const int r = wk.r0 + n;
+    const uint16_t* qp = wk.query(p, r < wk.R ? r : wk.r0);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(qp + (F8 ? 64 * (c >> 1) + 16 * q4 + 8 * (c & 1) : 32 * c + 8 * q4));
+        if (r >= wk.R) v = u32x4{0, 0, 0, 0};
+        qf[c] = as_bf16x8(v);
+    }
+    const int limit = wk.limit(p, r < wk.R ? r : wk.R - 1), limit_min = wk.limit(p, wk.r0);
+    const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
+
+    f32x4 O[D / 16];
+    Running run = {-INFINITY, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    unsigned char* Vl = smem + w * 32 * VP;
+    const int lrow = lane / C, lc = lane % C;
+    const unsigned char* kb = (const unsigned char*)p.k + (int64_t)wk.kvh * p.sh * ES;
+    const unsigned char* vb = (const unsigned char*)p.v + (int64_t)wk.kvh * p.sh * ES;
+    uint32_t voff[NLD];
+#pragma unroll
+    for (int q = 0; q < NLD; ++q) voff[q] = (uint32_t)(((q * RPL + lrow) & 15) * (int)p.st * ES + lc * 16);
+    const uint32_t koff = (uint32_t)(n * (int)p.st * ES + q4 * 16);
+
+    u32x4 kr[2][NK], vr[NLD];
+    bool there[2];
+    auto fetch = [&](int j) {
+        const unsigned char *ks[2], *vs[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int64_t base;
+            there[h] = pages.half(p, j, h, base);
+            ks[h] = kb + base;
+            vs[h] = vb + base;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < NK; ++c) kr[h][c] = load16<false>(ks[h] + koff + 64 * c);
+#pragma unroll
+        for (int q = 0; q < NLD; ++q) vr[q] = load16<false>(vs[q * RPL / 16] + voff[q]);
+    };
+    const int J = (wk.Tn - w + NW - 1) / NW;        // tiles of this wavefront
+    if (J > 0) {
+        pages.begin(p, J);
+        fetch(0);
+    }
+    for (int j = 0; j < J; ++j) {
+        const int key0 = (wk.t0 + w + NW * j) * 32;
+        const bool here0 = there[0], here1 = there[1], whole = key0 + 32 <= wk.seen && here0 && here1;
+        f32x4 S0 = {0.f, 0.f, 0.f, 0.f}, S1 = S0;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            bf16x8 k0, k1;
+            if constexpr (F8) {
+                k0 = as_bf16x8(widen_e4m3(kr[0][c >> 1][2 * (c & 1)], kr[0][c >> 1][2 * (c & 1) + 1]));
+                k1 = as_bf16x8(widen_e4m3(kr[1][c >> 1][2 * (c & 1)], kr[1][c >> 1][2 * (c & 1) + 1]));
+            } else {
+                k0 = as_bf16x8(kr[0][c]);
+                k1 = as_bf16x8(kr[1][c]);
+            }
+            S0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[c], S0, 0, 0, 0);
+            S1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[c], S1, 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the values before have been read (one wavefront's LDS operations keep their order)
+#pragma unroll
+        for (int q = 0; q < NLD; ++q) {
+            const int row = q * RPL + lrow;
+            u32x4 v = vr[q];
+            // rows behind the end hold anything, NaN too: as values they have to be zeros (as keys their scores are replaced)
+            if (!whole && !(key0 + row < wk.seen && (q * RPL < 16 ? here0 : here1))) v = u32x4{0, 0, 0, 0};
+            stage16<F8>(Vl + row * VP + lc * 16 * (2 / ES), v);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (j + 1 < J) {
+            pages.advance(p, j + 1, J);
+            fetch(j + 1);
+        }
+        // entry i of S0 / S1 is key key0 + 4 q4 + i (+ 16)
+        float S[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            S[i] = S0[i];
+            S[4 + i] = S1[i];
+        }
+        if (key0 + 32 > limit_min || !here0 || !here1) hide<8, 16>(S, key0 + 4 * q4, limit, here0, here1);
+        float mx = -INFINITY, m_use, rs = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
+        auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = __builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2, m_use);
+        u32x4 pk;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
+            rs += p0 + p1;
+            pk[i >> 1] = pack_bf16x2(p0, p1);
+        }
+        if (__any(alpha != 1.0f)) {
+            run.l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) O[dt][i] *= alpha;
+        }
+        run.l += rs;
+        const unsigned char* vbase = Vl + (4 * q4 + (n >> 2)) * VP + 8 * (n & 3);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            union { s16x4 h[2]; bf16x8 v; } f;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) f.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vbase + 16 * q * VP + 32 * dt));
+            O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, as_bf16x8(pk), O[dt], 0, 0, 0);
+        }
+    }
+    float* mb = reinterpret_cast<float*>(smem);
+    __syncthreads();
+    run.l += shfl_xor(run.l, 16);
+    run.l += shfl_xor(run.l, 32);
+    float* row = mb + (w * RT + n) * MP;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(row + 16 * dt + 4 * q4) = O[dt];
+    if (q4 == 0) {
+        row[D] = run.m;
+        row[D + 1] = run.l;
+    }
+    __syncthreads();
+    join_rows<D, F8, RT, NW, MP>(p, wk, mb, tid);
+}
+
+template <int D, bool F8, bool BC>
+__global__ __launch_bounds__(64 * THIN_WAVES, 1) void paged_thin_kernel(PagedAttnParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char smem[thin_smem(D)];
+    fetch_args<sizeof(PagedAttnParams)>();
+    run_rows<16, BC, false, F8 ? 1 : 2, THIN_WAVES>(p, smem, [&](const Work<16, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_thin_rows<D, F8, BC>(p, wk, pages, smem); });
+}
+
+// ---- 32 rows ------------------------------------------------------------------------------------------------
 template <int D, bool F8, bool BC, bool NT>
-__global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
-    constexpr int NW = 4;
+__device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
+    constexpr int NW = 4, RT = 32;
     constexpr int KP = D * 2 + 16;          // pitch of a K row in LDS: 16-byte reads of 16 rows hit distinct banks
     constexpr int VP = D * 2 + 64;          // of a V row: the 4 rows x 64 bytes of a transposing read tile the banks
     constexpr int TILE = 32 * KP + 32 * VP;
     constexpr int ES = F8 ? 1 : 2;          // bytes an entry of the cache
-    constexpr int C = D * ES / 16;          // 16-byte pieces a row
-    constexpr int RPL = 64 / C;             // rows a load of the wavefront covers
-    constexpr int NLD = 32 / RPL;
-    constexpr int MP = D + 4;               // pitch of a row of partial sums (floats)
-    constexpr int MERGE = NW * 32 * MP * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[NW * TILE > MERGE ? NW * TILE : MERGE];
+    constexpr int C = D * ES / 16, RPL = 64 / C, NLD = 32 / RPL;      // 16-byte pieces a row, rows a load, loads
+    constexpr int MP = D + 4;               // pitch of a row of sums (floats)
 
-    fetch_args<sizeof(PagedAttnParams)>();
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 31, hi = lane >> 5;
-    int grp, rt;
-    if (!remap_decode(p.remap, p.B * p.Hkv * p.nsplit, grp, rt)) return;
-    const int split = grp % p.nsplit, bh = grp / p.nsplit, kvh = bh % p.Hkv, b = bh / p.Hkv;
-    // Pages of the wavefront's next 32 tiles: lane 2j + h holds the one of half h (16 keys, a page is no smaller) of its j-th tile.  One load for 32
-    // tiles, requested 32 tiles ahead: a look-up a tile was a trip to memory in front of every fetch.  The first one travels with the
-    // sequence's lengths, so it may look at entries behind the sequence's end (but inside the table's row): whatever they hold, a page
-    // outside the cache is not read and a key behind the end not seen.
-    const int t0 = split * p.chunk, last_entry = (max(p.max_kv_len, 1) - 1) >> p.page_shift;
-    const int32_t* table = p.table + b * p.table_stride;
-    auto pages_from = [&](int j) { return table[min((int)(((int64_t)(t0 + w + NW * (j + (lane >> 1))) * 32 + 16 * (lane & 1)) >> p.page_shift), last_entry)]; };
-    int pages = p.max_kv_len > 0 ? pages_from(0) : 0;
-    const int len = clamped(p.kv_len[b], p.max_kv_len), ql = p.q_len ? clamped(p.q_len[b], p.Lq) : p.Lq;
-    const int R = ql * p.g, r0 = rt * 32;
-    if (r0 >= R) return;
-    const int seen = visible_keys<BC>(p, len, ql, min(r0 + 32, R));
-    const int T = (seen + 31) >> 5;
-    const int Tn = min(T - t0, p.chunk);
-    if (split > 0 && Tn <= 0) return;
-    const bool alone = T <= p.chunk;        // no other stretch: this workgroup writes the output
+    const int tid = fresh_thread(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
 
-    // ---- this lane's query row (B operand: row, 8 consecutive entries) ----
-    bf16x8 qf[D / 16];
-    const int r = r0 + n, qi = r < R ? r / p.g : 0, qh = r < R ? r - qi * p.g : 0;
-    const uint16_t* qp = p.q + b * p.q_sb + qi * p.q_st + (int64_t)(kvh * p.g + qh) * p.q_sh;
+    bf16x8 qf[D / 16];                      // this lane's query row (B operand: row n, 8 consecutive entries)
+    const int r = wk.r0 + n;
+    const uint16_t* qp = wk.query(p, r < wk.R ? r : wk.r0);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
-        u32x4 v = {0, 0, 0, 0};
-        if (r < R) v = *reinterpret_cast<const u32x4*>(qp + 16 * c + 8 * hi);
+        u32x4 v = *reinterpret_cast<const u32x4*>(qp + 16 * c + 8 * hi);
+        if (r >= wk.R) v = u32x4{0, 0, 0, 0};
         qf[c] = as_bf16x8(v);
     }
-    const int limit = visible_keys<BC>(p, len, ql, r < R ? (r / p.g + 1) * p.g : min(r0 + 32, R));     // keys this lane's row sees
-    const int limit_min = visible_keys<BC>(p, len, ql, r0 + 1);                                         // fewest of any row (the first one's)
-    const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[kvh] : p.scale_log2;
+    const int limit = wk.limit(p, r < wk.R ? r : wk.R - 1), limit_min = wk.limit(p, wk.r0);
+    const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
 
     f32x16 O[D / 32];
-    float m_run = -INFINITY, l_run = 0.f;
+    Running run = {-INFINITY, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -124,202 +616,274 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnParams p) {
     unsigned char* Kl = smem + w * TILE;
     unsigned char* Vl = Kl + 32 * KP;
     const int lrow = lane / C, lc = lane % C;
-    const unsigned char* kb = (const unsigned char*)p.k + (int64_t)kvh * p.sh * ES;
-    const unsigned char* vb = (const unsigned char*)p.v + (int64_t)kvh * p.sh * ES;
+    const unsigned char* kb = (const unsigned char*)p.k + (int64_t)wk.kvh * p.sh * ES;
+    const unsigned char* vb = (const unsigned char*)p.v + (int64_t)wk.kvh * p.sh * ES;
     uint32_t off[NLD];                      // of this lane's piece of load q, from the first row of its half tile
 #pragma unroll
     for (int q = 0; q < NLD; ++q) off[q] = (uint32_t)(((q * RPL + lrow) & 15) * (int)p.st * ES + lc * 16);
 
-    int pages_next = 0;
     u32x4 kr[NLD], vr[NLD];
     bool there[2];                          // whether the pages of the two halves exist
     auto fetch = [&](int j) {               // requests the wavefront's j-th tile
-        const int key = (t0 + w + NW * j) * 32;
         const unsigned char *ks[2], *vs[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int page = __builtin_amdgcn_readlane(pages, 2 * (j & 31) + h);
-            there[h] = (unsigned)page < (unsigned)p.n_pages;
-            const int64_t base = ((int64_t)(there[h] ? page : 0) * p.sp + (int64_t)((key + 16 * h) & ((1 << p.page_shift) - 1)) * p.st) * ES;
+            int64_t base;
+            there[h] = pages.half(p, j, h, base);
             ks[h] = kb + base;
             vs[h] = vb + base;
         }
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
-            const int h = q * RPL / 16;
-            kr[q] = NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ks[h] + off[q])) : *reinterpret_cast<const u32x4*>(ks[h] + off[q]);
-            vr[q] = NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vs[h] + off[q])) : *reinterpret_cast<const u32x4*>(vs[h] + off[q]);
+            kr[q] = load16<NT>(ks[q * RPL / 16] + off[q]);
+            vr[q] = load16<NT>(vs[q * RPL / 16] + off[q]);
         }
     };
-    const int J = (Tn - w + NW - 1) / NW;   // tiles of this wavefront
+    const int J = (wk.Tn - w + NW - 1) / NW;        // tiles of this wavefront
     if (J > 0) {
-        if (J > 32) pages_next = pages_from(32);
+        pages.begin(p, J);
         fetch(0);
     }
     for (int j = 0; j < J; ++j) {
-        const int key0 = (t0 + w + NW * j) * 32;
-        const bool here0 = there[0], here1 = there[1];
+        const int key0 = (wk.t0 + w + NW * j) * 32;
+        const bool here0 = there[0], here1 = there[1], whole = key0 + 32 <= wk.seen && here0 && here1;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile before has been read (one wavefront's LDS operations keep their order)
-        const bool whole = key0 + 32 <= seen && here0 && here1;
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
             const int row = q * RPL + lrow;
-            const u32x4 z = {0, 0, 0, 0}, kv = kr[q];
-            u32x4 vv = vr[q];
+            u32x4 v = vr[q];
             // rows behind the end hold anything, NaN too: as values they have to be zeros (as keys their scores are replaced)
-            if (!whole && !(key0 + row < seen && (q * RPL < 16 ? here0 : here1))) vv = z;
-            if constexpr (F8) {
-                u32x4* kd = reinterpret_cast<u32x4*>(Kl + row * KP + lc * 32);
-                u32x4* vd = reinterpret_cast<u32x4*>(Vl + row * VP + lc * 32);
-                kd[0] = widen_e4m3(kv[0], kv[1]);
-                kd[1] = widen_e4m3(kv[2], kv[3]);
-                vd[0] = widen_e4m3(vv[0], vv[1]);
-                vd[1] = widen_e4m3(vv[2], vv[3]);
-            } else {
-                *reinterpret_cast<u32x4*>(Kl + row * KP + lc * 16) = kv;
-                *reinterpret_cast<u32x4*>(Vl + row * VP + lc * 16) = vv;
-            }
+            if (!whole && !(key0 + row < wk.seen && (q * RPL < 16 ? here0 : here1))) v = u32x4{0, 0, 0, 0};
+            stage16<F8>(Kl + row * KP + lc * 16 * (2 / ES), kr[q]);
+            stage16<F8>(Vl + row * VP + lc * 16 * (2 / ES), v);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (j + 1 < J) {
-            if (((j + 1) & 31) == 0) {
-                pages = pages_next;
-                if (j + 33 < J) pages_next = pages_from(j + 33);
-            }
+            pages.advance(p, j + 1, J);
             fetch(j + 1);
         }
-        f32x16 S;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = 0.f;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-            S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Kl + n * KP + (16 * c + 8 * hi) * 2), qf[c], S, 0, 0, 0);
-        // entry i is key key0 + 8 (i / 4) + 4 hi + i % 4
-        if (key0 + 32 > limit_min || !here0 || !here1) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (key0 + 8 * (i >> 2) + 4 * hi + (i & 3) >= limit || !(i < 8 ? here0 : here1)) S[i] = -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = __builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
-        // The maximum that the exponentials are relative to follows the running one only when that has grown by 2^8 (p stays in range of bf16 and
-        // of the sums): the 64 accumulators are rescaled a few times a row instead of at every tile.
-        const bool grow = mx > m_run + 8.0f;
-        const float m_new = grow ? mx : m_run;
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        float rs = 0.f;
-        uint32_t pk[8];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
-            rs += p0 + p1;
-            pk[i >> 1] = pack_bf16x2(p0, p1);
-        }
-        if (__any(grow)) {
-            const float alpha = grow ? fast_exp2(m_run - m_use) : 1.0f;
-            l_run *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
-        }
-        l_run += rs;
-        m_run = m_new;
-        const u32x4 plo = {pk[0], pk[1], pk[2], pk[3]}, phi = {pk[4], pk[5], pk[6], pk[7]};
-        const bf16x8 pf[2] = {as_bf16x8(plo), as_bf16x8(phi)};
-        const int s16 = lane & 15, blk = (lane >> 4) & 1;
-        const unsigned char* vbase = Vl + (4 * hi + (s16 >> 2)) * VP + (16 * blk + 4 * (s16 & 3)) * 2;
-#pragma unroll
-        for (int e = 0; e < 2 * (D / 32); ++e) {
-            union { s16x4 h[2]; bf16x8 v; } f;
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                f.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vbase + (16 * (e & 1) + 8 * q) * VP + 32 * (e >> 1) * 2));
-            O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[e & 1], O[e >> 1], 0, 0, 0);
-        }
+        tile32<D, KP, VP>(Kl, Vl, qf, key0, limit, limit_min, here0, here1, scale_log2, run, O, lane);
     }
-
-    // ---- join the wavefronts ----
-    constexpr float LN2 = 0.6931471805599453f;
-    constexpr int C8 = D / 8;
     float* mb = reinterpret_cast<float*>(smem);
     __syncthreads();
-    l_run += shfl_xor(l_run, 32);
-    float* row = mb + (w * 32 + n) * MP;
+    run.l += shfl_xor(run.l, 32);
+    float* row = mb + (w * RT + n) * MP;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<f32x4*>(row + 32 * dt + 8 * q4 + 4 * hi) = f32x4{O[dt][4 * q4], O[dt][4 * q4 + 1], O[dt][4 * q4 + 2], O[dt][4 * q4 + 3]};
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(row + 32 * dt + 8 * q + 4 * hi) = f32x4{O[dt][4 * q], O[dt][4 * q + 1], O[dt][4 * q + 2], O[dt][4 * q + 3]};
     if (hi == 0) {
-        row[D] = m_run;
-        row[D + 1] = l_run;
+        row[D] = run.m;
+        row[D + 1] = run.l;
     }
     __syncthreads();
-    for (int task = tid; task < 32 * C8; task += 256) {
-        const int rr = task / C8, c8 = task - rr * C8;
-        if (r0 + rr >= R) continue;
-        const int i = (r0 + rr) / p.g, h = kvh * p.g + (r0 + rr) - i * p.g;
-        float M = -INFINITY, den = 0.f, wgt[NW], o[8];
+    join_rows<D, F8, RT, NW, MP>(p, wk, mb, tid);
+}
+
+template <int D, bool F8, bool BC, bool NT, bool EVEN>
+__global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedAttnParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char smem[wide_smem(D)];
+    fetch_args<sizeof(PagedAttnParams)>();
+    run_rows<32, BC, EVEN, F8 ? 1 : 2, 4>(p, smem, [&](const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_wide_rows<D, F8, BC, NT>(p, wk, pages, smem); });
+}
+
+// ---- 128 rows -----------------------------------------------------------------------------------------------
+// Two key groups of four wavefronts take every second tile; wavefront w of a group has rows 32 w .. 32 w + 31.  A group's t-th tile sits in its LDS
+// buffer t % 2: while it is multiplied, tile t + 1 is stored into the other one and tile t + 3 requested, one barrier a tile.
+template <int D, bool F8, bool BC>
+__device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
+    constexpr int RT = 128, PF = 2, MP = D + 4;
+    constexpr int KP = D * 2 + 16, VP = D * 2 + 64, TILE = 32 * KP + 32 * VP;
+    constexpr int ES = F8 ? 1 : 2;
+    constexpr int C = D * ES / 16, RPL = 256 / C, NLD = RPL > 32 ? 1 : 32 / RPL;      // rows that one load of the workgroup covers (64 at d = 64, e4m3: half the threads)
+    constexpr int OPB = D * 2 + 16;
+    static_assert(4 * 32 * OPB <= 4 * TILE && RT * MP * 4 <= 4 * TILE, "sums and results pass through the tiles' place");
+
+    const int thread = fresh_thread(), tid = thread & 255, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
+    const int wg = __builtin_amdgcn_readfirstlane(thread >> 8);              // key group
+    smem += wg * 2 * TILE;
+
+    const int w0 = wk.r0 + 32 * w;          // this wavefront's first row; without one it only helps with the tiles
+    const bool mine = w0 < wk.R;
+    bf16x8 qf[D / 16];
+    const int r = w0 + n;
+    const uint16_t* qp = wk.query(p, r < wk.R ? r : wk.r0);
 #pragma unroll
-        for (int k = 0; k < NW; ++k) M = __builtin_fmaxf(M, mb[(k * 32 + rr) * MP + D]);
+    for (int c = 0; c < D / 16; ++c) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(qp + 16 * c + 8 * hi);
+        if (r >= wk.R) v = u32x4{0, 0, 0, 0};
+        qf[c] = as_bf16x8(v);
+    }
+    const int limit = wk.limit(p, r < wk.R ? r : wk.R - 1), limit_min = wk.limit(p, mine ? w0 : wk.r0);
+    const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
+
+    f32x16 O[D / 32];
+    Running run = {-INFINITY, 0.f};
 #pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            const float mk = mb[(k * 32 + rr) * MP + D];
-            wgt[k] = mk == -INFINITY ? 0.f : fast_exp2(mk - M);
-            den += wgt[k] * mb[(k * 32 + rr) * MP + D + 1];
-        }
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = 0.f;
+        for (int i = 0; i < 16; ++i) O[dt][i] = 0.f;
+
+    const int lrow = tid / C, lc = tid % C;
+    const bool loads = lrow < 32;
+    const unsigned char* kb = (const unsigned char*)p.k + (int64_t)wk.kvh * p.sh * ES;
+    const unsigned char* vb = (const unsigned char*)p.v + (int64_t)wk.kvh * p.sh * ES;
+    const uint32_t off = (uint32_t)((lrow & 15) * (int)p.st * ES + lc * 16);      // (a load covers 16 rows or 32)
+    u32x4 kr[PF][NLD], vr[PF][NLD];
+    bool there[4][2];                       // of the tiles in flight and the one at work: tile t's are there[t % 4]
+    auto fetch = [&](int slot, int flag, int t) {
+        int64_t base[2];
 #pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            const float* src = mb + (k * 32 + rr) * MP + 8 * c8;
+        for (int h = 0; h < 2; ++h) there[flag][h] = pages.half(p, t, h, base[h]);
+        if (loads) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] += wgt[k] * src[e];
-        }
-        if (!alone) {
-            const int64_t at = ((int64_t)split * p.B + b) * p.Hq * p.Lq + (int64_t)h * p.Lq + i;
-            *reinterpret_cast<f32x4*>(p.part_o + at * D + 8 * c8) = f32x4{o[0], o[1], o[2], o[3]};
-            *reinterpret_cast<f32x4*>(p.part_o + at * D + 8 * c8 + 4) = f32x4{o[4], o[5], o[6], o[7]};
-            if (c8 == 0) {
-                p.part_ml[at * 2] = M;
-                p.part_ml[at * 2 + 1] = den;
+            for (int q = 0; q < NLD; ++q) {
+                const int64_t where = (NLD == 1 ? (lrow < 16 ? base[0] : base[1]) : base[q]) + off;
+                kr[slot][q] = load16<false>(kb + where);
+                vr[slot][q] = load16<false>(vb + where);
             }
-            continue;
         }
-        const float inv = (den == 0.f ? 0.f : 1.f / den) * (F8 && p.v_scale ? p.v_scale[kvh] : 1.f);
-        u32x4 v;
+    };
+    auto store = [&](int slot, int flag, int t) {
+        if (!loads) return;
+        unsigned char* Kl = smem + (t & 1) * TILE;
+        unsigned char* Vl = Kl + 32 * KP;
+        const int key0 = (wk.t0 + 2 * t + wg) * 32;
+        const bool whole = key0 + 32 <= wk.seen && there[flag][0] && there[flag][1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
-        *reinterpret_cast<u32x4*>(p.out + b * p.o_sb + i * p.o_st + (int64_t)h * p.o_sh + 8 * c8) = v;
-        if (p.lse && c8 == 0) p.lse[((int64_t)b * p.Hq + h) * p.Lq + i] = den == 0.f ? -INFINITY : (M + log2f(den)) * LN2;
+        for (int q = 0; q < NLD; ++q) {
+            const int row = q * RPL + lrow;
+            u32x4 v = vr[slot][q];
+            if (!whole && !(key0 + row < wk.seen && (row < 16 ? there[flag][0] : there[flag][1]))) v = u32x4{0, 0, 0, 0};
+            stage16<F8>(Kl + row * KP + lc * 16 * (2 / ES), kr[slot][q]);
+            stage16<F8>(Vl + row * VP + lc * 16 * (2 / ES), v);
+        }
+    };
+    const int Tn = (wk.Tn - wg + 1) / 2, steps = (wk.Tn + 1) / 2;     // tiles of this key group, and of the other one if it has more
+    if (Tn > 0) {
+        pages.begin(p, Tn);
+        fetch(0, 0, 0);
+        if (Tn > 1) fetch(1, 1, 1);
+        store(0, 0, 0);
+        if (Tn > 2) fetch(0, 2, 2);
+    }
+    __syncthreads();
+    for (int t4 = 0; t4 < steps; t4 += 4) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int t = t4 + u;
+            if (t >= steps) break;          // (uniform)
+            if (t + 1 < Tn) {
+                store((u + 1) % PF, (u + 1) % 4, t + 1);
+                if (t + 3 < Tn) {
+                    pages.advance(p, t + 3, Tn);
+                    fetch((u + 1) % PF, (u + 3) % 4, t + 3);
+                }
+            }
+            const unsigned char* Kl = smem + (t & 1) * TILE;
+            if (mine && t < Tn) tile32<D, KP, VP>(Kl, Kl + 32 * KP, qf, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, there[u][0], there[u][1], scale_log2, run, O, lane);
+            __syncthreads();
+        }
+    }
+    // the second key group hands its sums to the first, lane for lane
+    smem -= wg * 2 * TILE;
+    float* row = reinterpret_cast<float*>(smem) + (32 * w + n) * MP;
+    if (wg == 1) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4*>(row + 32 * dt + 8 * q + 4 * hi) = f32x4{O[dt][4 * q], O[dt][4 * q + 1], O[dt][4 * q + 2], O[dt][4 * q + 3]};
+        if (hi == 0) row[D] = run.m;
+        row[D + 1 + hi] = run.l;
+    }
+    __syncthreads();
+    if (wg == 0) {
+        const float m1 = row[D], l1 = row[D + 1 + hi], M = __builtin_fmaxf(run.m, m1);
+        const float a0 = run.m == -INFINITY ? 0.f : fast_exp2(run.m - M), a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(row + 32 * dt + 8 * q + 4 * hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[dt][4 * q + e] = a0 * O[dt][4 * q + e] + a1 * v[e];
+            }
+        run.l = a0 * run.l + a1 * l1;
+        run.m = M;
+    }
+    __syncthreads();                        // (the results pass through the same place)
+    if (wg == 1 || !mine) return;
+    run.l += shfl_xor(run.l, 32);
+    if (wk.slot >= 0) {
+        if (r < wk.R) {
+            const int64_t at = (int64_t)wk.slot * RT + 32 * w + n;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4*>(p.part_o + at * D + 32 * dt + 8 * q + 4 * hi) = f32x4{O[dt][4 * q], O[dt][4 * q + 1], O[dt][4 * q + 2], O[dt][4 * q + 3]};
+            if (hi == 0) {
+                p.part_ml[at * 2] = run.m;
+                p.part_ml[at * 2 + 1] = run.l;
+            }
+        }
+        return;
+    }
+    // the accumulators have a row a lane: through LDS (a part of its own a wavefront; the tiles are done with) whole rows are written
+    const float inv = (run.l == 0.f ? 0.f : 1.f / run.l) * (F8 && p.v_scale ? p.v_scale[wk.kvh] : 1.f);
+    unsigned char* ob = smem + w * (32 * OPB);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<u32x2*>(ob + n * OPB + (32 * dt + 8 * q + 4 * hi) * 2) =
+                u32x2{pack_bf16x2(O[dt][4 * q] * inv, O[dt][4 * q + 1] * inv), pack_bf16x2(O[dt][4 * q + 2] * inv, O[dt][4 * q + 3] * inv)};
+    if (p.lse && hi == 0 && r < wk.R) {
+        const int i = query_of(p, r), h = wk.kvh * p.g + r - i * p.g;
+        p.lse[((int64_t)wk.b * p.Hq + h) * p.Lq + i] = run.l == 0.f ? -INFINITY : (run.m + log2f(run.l)) * 0.6931471805599453f;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int C8 = D / 8;
+#pragma unroll
+    for (int q = 0; q < 32 * C8 / 64; ++q) {
+        const int id = q * 64 + lane, row = id / C8, c8 = id - row * C8;
+        if (w0 + row >= wk.R) continue;
+        const int i = query_of(p, w0 + row), h = wk.kvh * p.g + (w0 + row) - i * p.g;
+        *reinterpret_cast<u32x4*>(p.out + wk.b * p.o_sb + i * p.o_st + (int64_t)h * p.o_sh + 8 * c8) = *reinterpret_cast<const u32x4*>(ob + row * OPB + c8 * 16);
     }
 }
 
-// Joins the stretches of each (sequence, head, row) that has more than one: M = max m_s, w_s = 2^(m_s - M), out = sum w_s o_s / sum w_s l_s,
-// lse = (M + log2 sum w_s l_s) ln 2.  D / 4 threads a row and group of stretches, G groups: group k takes stretches k, k + G, .. in their
-// order, four requested at a time, and the groups are added up in theirs.
-template <int D, bool F8, bool BC, int G>
+template <int D, bool F8, bool BC, bool EVEN>
+__global__ __launch_bounds__(512, 1) void paged_tall_kernel(PagedAttnParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char smem[tall_smem(D)];
+    fetch_args<sizeof(PagedAttnParams)>();
+    run_rows<128, BC, EVEN, F8 ? 1 : 2, 2>(p, smem, [&](const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_tall_rows<D, F8, BC>(p, wk, pages, smem); });
+}
+
+// Joins the sums of each (sequence, head, row) whose keys were shared out: M = max m_s, w_s = 2^(m_s - M), out = sum w_s o_s / sum w_s l_s,
+// lse = (M + log2 sum w_s l_s) ln 2.  D / 4 threads a row and group of shares, G groups: group k takes shares k, k + G, .. in their order, four
+// requested at a time, and the groups are added up in theirs.
+template <int D, bool F8, int G>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
     constexpr int TPR = D / 4, RPW = 256 / TPR / G;
     __shared__ float part[G > 1 ? 256 / TPR : 1][D + 2];
     const int64_t rows = (int64_t)p.B * p.Hq * p.Lq, row = min((int64_t)blockIdx.x * RPW + threadIdx.x / (TPR * G), rows - 1);
     const int c4 = threadIdx.x % TPR, gi = threadIdx.x / TPR, k = gi % G;
     const int i = (int)(row % p.Lq), bh = (int)(row / p.Lq), h = bh % p.Hq, b = bh / p.Hq;
-    const int len = clamped(p.kv_len[b], p.max_kv_len), ql = p.q_len ? clamped(p.q_len[b], p.Lq) : p.Lq;
-    const int r0 = (i * p.g + h % p.g) & ~31;
-    const int T = i < ql ? (visible_keys<BC>(p, len, ql, min(r0 + 32, ql * p.g)) + 31) >> 5 : 0;
-    const int n = T <= p.chunk ? 0 : (T + p.chunk - 1) / p.chunk;          // 0: nothing to join here
+    const int ql = p.q_len ? clamped(p.q_len[b], p.Lq) : p.Lq;
+    const int r = i * p.g + h % p.g, rr = r % p.rows_wg;
+    const int32_t* m = p.meta + 2 * (((int64_t)b * p.Hkv + h / p.g) * p.row_groups + r / p.rows_wg);
+    const int w0 = m[0], n = i < ql && m[1] > 1 ? m[1] : 0;                // 0: nothing to join here (rows behind q_len: nobody has written m)
     float M = -INFINITY, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = k; s0 < n; s0 += 4 * G) {
         float m[4], l[4];
         f32x4 v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t at = min(s0 + u * G, n - 1) * rows + row;        // (past the last one it is loaded again and not used)
+            const int s = min(s0 + u * G, n - 1);                          // (past the last one it is loaded again and not used)
+            const int64_t at = (int64_t)(2 * (w0 + s) + (s == 0)) * p.rows_wg + rr;
             m[u] = p.part_ml[at * 2];
             l[u] = p.part_ml[at * 2 + 1];
             v[u] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + 4 * c4);
@@ -362,25 +926,43 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
-static int g_paged_chunk = 0;      // "paged_chunk"
+static int g_paged_shape = 0;      // "paged_shape"
+static int g_paged_shares = 0;     // "paged_shares"
 
-// Tiles of a stretch: as many workgroups as give the chip two each, no stretch under 8 tiles (two a wavefront).
-static int plan_chunk(const dlm_paged_attn_args* a) {
-    if (g_paged_chunk > 0) return g_paged_chunk;
-    const int64_t tiles = ((int64_t)a->max_kv_len + 31) / 32, groups = (int64_t)a->B * a->Hkv * (((int64_t)a->Lq * (a->Hq / a->Hkv) + 31) / 32);
-    int64_t n = groups >= 512 ? 1 : 512 / groups;
-    const int64_t most = tiles / 8;
-    if (n > most) n = most;
-    if (n < 1) n = 1;
-    const int64_t chunk = (tiles + n - 1) / n;
-    return (int)(chunk > 1 ? chunk : 1);
-}
-static int splits_of(const dlm_paged_attn_args* a, int chunk) {
-    const int64_t tiles = ((int64_t)a->max_kv_len + 31) / 32;
-    return (int)(tiles > 0 ? (tiles + chunk - 1) / chunk : 1);
-}
-static size_t paged_workspace_bytes(const dlm_paged_attn_args* a, int nsplit) {
-    return nsplit <= 1 ? 0 : (size_t)nsplit * (size_t)a->B * (size_t)a->Hq * (size_t)a->Lq * (size_t)(a->d + 2) * sizeof(float);
+// How a call is laid out.
+struct PagedPlan {
+    int rows, row_groups;   // rows of a workgroup, row groups of Lq rows
+    int shares;             // workgroups that share the tiles evenly; 0: one workgroup a row group
+    size_t sums, meta;      // of the workspace: floats of sums and (maximum, sum) pairs, ints behind them
+    size_t bytes() const { return shares ? sums * sizeof(float) + meta * sizeof(int32_t) : 0; }
+};
+// One workgroup a row group costs least where the row groups fill the chip; it leaves CUs idle where they are few, and one that is much longer than the
+// others runs on alone.  Even shares cost a second launch, a scan of the lengths and what is left half done at each border.  Estimates, in
+// microseconds, T = the longest sequence's tiles (the lengths are not known here):
+//   32 rows:  a CU streams 49 GB/s, the chip 6.6 TB/s, shares cost 9.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168 with shares, of 2048 - 4096 134 /
+//             142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.  From 256 tiles on always shares.
+//   128 rows: a tile takes a CU 0.7, shares cost 20.  32 x 32 rows of 28/4 heads, 1024 tokens: 29 / 38.
+static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
+    static const int shape_rows[4] = {0, 16, 32, 128};
+    PagedPlan pl = {};
+    const int64_t R = (int64_t)a->Lq * (a->Hq / a->Hkv), T = ((int64_t)a->max_kv_len + 31) / 32, heads = (int64_t)a->B * a->Hkv;
+    // few short sequences: latency counts (16 sequences of 700 tokens, 14/2 heads of 64: 16 rows and eight wavefronts 7.0 us, 32 and four 8.1)
+    pl.rows = g_paged_shape > 0 ? shape_rows[g_paged_shape] : R <= 16 && T <= 24 && heads <= 256 ? 16 : R <= 64 ? 32 : 128;
+    pl.row_groups = (int)((R + pl.rows - 1) / pl.rows);
+    const int64_t groups = heads * pl.row_groups, rounds = (groups + 255) / 256;
+    if (pl.rows == 16 || groups > 0x7fffffff / (T + 1)) return pl;          // (the line of tiles is counted in 32 bits)
+    const int most = pl.rows == 128 ? 256 : 512;
+    if (g_paged_shares) pl.shares = g_paged_shares > 0 ? g_paged_shares : 0;
+    else if (T > 256) pl.shares = most;
+    else if (pl.rows == 128) pl.shares = 0.7 * T * rounds > 0.7 * T * groups / 256 + 20 ? most : 0;
+    else {
+        const double tile = 64.0 * a->d * (a->cache.type == DLM_KV_E4M3 ? 1 : 2), all = (double)groups * T * tile / 6.6e6, alone = (double)T * rounds * tile / 49e3;
+        pl.shares = (alone > all ? alone : all) > all + 9 ? most : 0;
+    }
+    if (pl.shares > groups * T / SMALLEST_SHARE) pl.shares = (int)(groups * T / SMALLEST_SHARE);
+    pl.sums = (size_t)2 * pl.shares * pl.rows * (a->d + 2);
+    pl.meta = (size_t)2 * groups;
+    return pl;
 }
 
 static int validate_paged_attn(const dlm_paged_attn_args* a) {
@@ -414,22 +996,37 @@ static int validate_paged_attn(const dlm_paged_attn_args* a) {
     return DLM_OK;
 }
 
-template <int D, bool F8, bool BC>
-static int launch_paged(const PagedAttnParams& p, unsigned grid, hipStream_t st) {
-    if (p.remap.nx == 1) hipLaunchKernelGGL((paged_attn_kernel<D, F8, BC, true>), dim3(grid), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((paged_attn_kernel<D, F8, BC, false>), dim3(grid), dim3(256), 0, st, p);
-    int rc = check_hip(hipGetLastError(), "paged_attn_kernel launch");
-    if (rc != DLM_OK || p.nsplit <= 1) return rc;
+template <int D, bool F8, bool BC, bool EVEN>
+static int launch_rows(const PagedAttnParams& p, unsigned grid, hipStream_t st) {
+    if (p.rows_wg == 128) hipLaunchKernelGGL((paged_tall_kernel<D, F8, BC, EVEN>), dim3(grid), dim3(512), 0, st, p);
+    else if (p.rows_wg == 16) {
+        if constexpr (!EVEN) hipLaunchKernelGGL((paged_thin_kernel<D, F8, BC>), dim3(grid), dim3(64 * THIN_WAVES), 0, st, p);
+    } else if (p.row_groups == 1) hipLaunchKernelGGL((paged_wide_kernel<D, F8, BC, true, EVEN>), dim3(grid), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((paged_wide_kernel<D, F8, BC, false, EVEN>), dim3(grid), dim3(256), 0, st, p);
+    return check_hip(hipGetLastError(), "paged attention launch");
+}
+
+template <int D, bool F8>
+static int launch_paged(const PagedAttnParams& p, bool bc, unsigned grid, hipStream_t st) {
+    if (!p.shares) return bc ? launch_rows<D, F8, true, false>(p, grid, st) : launch_rows<D, F8, false, false>(p, grid, st);
+    int rc = bc ? launch_rows<D, F8, true, true>(p, p.shares, st) : launch_rows<D, F8, false, true>(p, p.shares, st);
+    if (rc != DLM_OK) return rc;
+    // few row groups: many shares each
     constexpr int GROUPS = 1024 / D;
     const int64_t rows = (int64_t)p.B * p.Hq * p.Lq;
-    if (p.nsplit > 4) hipLaunchKernelGGL((paged_merge_kernel<D, F8, BC, GROUPS>), dim3((unsigned)rows), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((paged_merge_kernel<D, F8, BC, 1>), dim3((unsigned)((rows + GROUPS - 1) / GROUPS)), dim3(256), 0, st, p);
+    if ((int64_t)p.B * p.Hkv * p.row_groups * 4 < p.shares) hipLaunchKernelGGL((paged_merge_kernel<D, F8, GROUPS>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((paged_merge_kernel<D, F8, 1>), dim3((unsigned)((rows + GROUPS - 1) / GROUPS)), dim3(256), 0, st, p);
     return check_hip(hipGetLastError(), "paged_merge_kernel launch");
 }
 
-int paged_set_chunk(int v) {
-    if (v < 0) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_chunk must be >= 0");
-    g_paged_chunk = v;
+int paged_set_shape(int v) {
+    if (v < 0 || v > 3) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_shape must be 0..3");
+    g_paged_shape = v;
+    return DLM_OK;
+}
+int paged_set_shares(int v) {
+    if (v < -1 || v > 65536) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_shares must be -1..65536");
+    g_paged_shares = v;
     return DLM_OK;
 }
 
@@ -441,7 +1038,7 @@ extern "C" size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args* a) {
     if (!a || a->struct_size != sizeof(dlm_paged_attn_args) || a->B <= 0 || a->Lq <= 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv || a->d <= 0 ||
         a->max_kv_len <= 0)
         return 0;
-    return paged_workspace_bytes(a, splits_of(a, plan_chunk(a)));
+    return plan_paged(a).bytes();
 }
 
 extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
@@ -461,29 +1058,22 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
     p.kv_len = a->kv_len; p.max_kv_len = c.n_pages > 0 ? a->max_kv_len : 0;     // without pages there are no keys
     p.q_len = a->q_len;
     p.bs = a->block_size;
+    p.by_g = fast_div(p.g);
+    p.by_bs = fast_div(a->block_size > 0 ? a->block_size : 1);
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)a->d)) * 1.4426950408889634f;
-    const int64_t tiles = ((int64_t)a->max_kv_len + 31) / 32;
-    p.chunk = plan_chunk(a);
-    p.nsplit = splits_of(a, p.chunk);
-    if (p.nsplit > 1) {
-        if (a->workspace && a->workspace_bytes >= paged_workspace_bytes(a, p.nsplit) && aligned16(a->workspace)) {
-            p.part_o = (float*)a->workspace;
-            p.part_ml = p.part_o + (size_t)p.nsplit * a->B * a->Hq * a->Lq * a->d;
-        } else {
-            p.nsplit = 1;
-            p.chunk = (int)(tiles > 1 ? tiles : 1);
-        }
+    const PagedPlan pl = plan_paged(a);
+    p.rows_wg = pl.rows;
+    p.row_groups = pl.row_groups;
+    if (pl.shares && p.max_kv_len > 0 && a->workspace && a->workspace_bytes >= pl.bytes() && aligned16(a->workspace)) {
+        p.shares = pl.shares;
+        p.part_o = (float*)a->workspace;
+        p.part_ml = p.part_o + (size_t)2 * pl.shares * pl.rows * a->d;
+        p.meta = (int32_t*)(p.part_o + pl.sums);
     }
-    const int64_t row_tiles = ((int64_t)a->Lq * p.g + 31) / 32, groups = (int64_t)a->B * a->Hkv * p.nsplit;
-    if (groups > 0x7fffffff || row_tiles > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
-    const int64_t grid = set_remap(p.remap, groups, (int)row_tiles, false);
-    if (grid == 0) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
-    if (p.nsplit > 1 && (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many rows");
+    const int64_t grid = set_remap(p.remap, (int64_t)a->B * a->Hkv, pl.row_groups, false);
+    if (grid == 0 || (int64_t)a->B * a->Hkv > 0x7fffffff || (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
     hipStream_t st = (hipStream_t)stream;
     const bool f8 = c.type == DLM_KV_E4M3, bc = a->mask_mode == DLM_MASK_BLOCK_CAUSAL;
-#define PAGED_LAUNCH(D)                                                                                                    \
-    (f8 ? (bc ? launch_paged<D, true, true>(p, (unsigned)grid, st) : launch_paged<D, true, false>(p, (unsigned)grid, st))  \
-        : (bc ? launch_paged<D, false, true>(p, (unsigned)grid, st) : launch_paged<D, false, false>(p, (unsigned)grid, st)))
-    return a->d == 128 ? PAGED_LAUNCH(128) : PAGED_LAUNCH(64);
-#undef PAGED_LAUNCH
+    if (a->d == 128) return f8 ? launch_paged<128, true>(p, bc, (unsigned)grid, st) : launch_paged<128, false>(p, bc, (unsigned)grid, st);
+    return f8 ? launch_paged<64, true>(p, bc, (unsigned)grid, st) : launch_paged<64, false>(p, bc, (unsigned)grid, st);
 }

@@ -113,6 +113,57 @@ def test_fewer_rows_than_the_batch_has(mask):
     c.check(**mask)
 
 
+@pytest.fixture
+def options():
+    yield dlm.set_option
+    dlm.set_option("paged_shape", 0)
+    dlm.set_option("paged_shares", 0)
+
+
+@pytest.mark.parametrize("shares", [0, -1, 1, 2, 7, 64, 1000])
+@pytest.mark.parametrize("shape", [1, 2, 3])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_shape_of_workgroup(options, shape, shares, d):
+    """16, 32 and 128 rows a workgroup, keys dealt out to few workgroups and to more than there are, for few rows and many, every mask and type."""
+    options("paged_shape", shape)
+    options("paged_shares", shares)
+    for i, (lens, Lq, Hq, Hkv, page) in enumerate([([1, 40, 333], 1, 4, 2, 16), ([700, 95], 5, 14, 2, 64), ([200, 513], 33, 8, 2, 32), ([1500], 3, 5, 1, 128)]):
+        for e4m3 in (False, True):
+            for mask in ({}, dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=(1, 4, 32, 7)[i])):
+                c = Case(lens, Lq, Hq, Hkv, d, page, e4m3, q_len=[max(Lq - 2 * k, 0) for k in range(len(lens))] if i % 2 else None, seed=i)
+                c.run(**mask)
+                c.check(**mask)
+
+
+@pytest.mark.parametrize("shape", [1, 2, 3])
+def test_more_than_32_tiles_a_wavefront(options, shape):
+    """The look-ups of pages go on past the first 32 tiles."""
+    options("paged_shape", shape)
+    options("paged_shares", -1)
+    c = Case([9001, 4097, 31], 1, 2, 1, 64, 16)
+    assert c.run() == 0
+    c.check()
+
+
+@pytest.mark.parametrize("B", [1, 255, 300, 700])
+def test_many_sequences_share_the_workgroups(options, B):
+    """Lengths from nothing to long, sequences without rows among them, more sequences than a workgroup has threads."""
+    options("paged_shape", 2)
+    options("paged_shares", 64)
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(0, 60, B)]
+    lens[-1], lens[B // 2] = 0, 700
+    q_len = [int(x) for x in rng.integers(0, 3, B)]
+    for mask in ({}, dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=1)):
+        c = Case(lens, 2, 2, 1, 64, 16, q_len=q_len)
+        assert c.run(**mask) > 0
+        c.check(**mask)
+    c.q_len.zero_()                                   # nobody asks
+    c.out.fill_(7.0), c.lse.fill_(7.0)
+    c.run()
+    assert (c.out == 7).all() and (c.lse == 7).all()
+
+
 def test_long_sequence_split_and_not():
     """Enough keys for many stretches; both sides of a stretch's border; lengths outside [0, max_kv_len] are clamped."""
     for lens in ([9000], [8191, 12, 0, 6000], [70000]):
@@ -165,6 +216,27 @@ def test_what_is_not_finite():
     assert c.out[3].isfinite().all()
 
 
+@pytest.mark.parametrize("shape", [1, 2, 3])
+def test_every_8_bit_value(options, shape):
+    """One key: the output is its value, every e4m3 there is, exactly (powers of two as scales); NaN stays NaN."""
+    options("paged_shape", shape)
+    c = Case([1], 1, 2, 2, 128, 16, e4m3=True)
+    page = int(c.table[0, 0])
+    c.pages[1].view(torch.uint8)[page, :, 0] = torch.arange(256, dtype=torch.uint8, device=DEV).view(2, 128)
+    c.scales[1].copy_(torch.tensor([0.25, 8.0], device=DEV))
+    c.run()
+    want = heads.e4m3_values().reshape(2, 128) * np.array([[0.25], [8.0]])
+    assert np.array_equal(wide(c.out)[0, 0], want, equal_nan=True)
+    # and as a key: the score of a query of ones at one entry
+    c.pages[0].view(torch.uint8)[page, 0, 0] = torch.arange(128, dtype=torch.uint8, device=DEV)
+    c.pages[0].view(torch.uint8)[page, 0, 0, 127] = 0
+    c.q.zero_()
+    c.q[0, 0, 0] = 1.0
+    c.scales[0].fill_(0.5)
+    c.run(scale=1.0)
+    assert abs(float(c.lse[0, 0, 0]) - heads.e4m3_values()[:127].sum() * 0.5) <= 1e-5 * heads.e4m3_values()[:127].sum()
+
+
 def test_scores_far_apart():
     """One key that outweighs all others in a late tile, and scores in the hundreds."""
     c = Case([900], 1, 4, 2, 128, 64)
@@ -182,7 +254,7 @@ def test_views_another_stream_and_repeats():
     wide_q, wide_out = torch.zeros((2, 6, 12, 160), dtype=BF16, device=DEV), torch.full((2, 8, 5, 128), 7.0, dtype=BF16, device=DEV)
     q, out = wide_q[:, 1:5, 2:10, 16:144], wide_out.permute(0, 2, 1, 3)[:, 1:]          # [B, Lq, Hq, d], heads outside
     q.copy_(c.q)
-    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(dlm.paged_attn_workspace_bytes(q, out, *c.pages, c.table, c.lens), dtype=torch.uint8, device=DEV)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):

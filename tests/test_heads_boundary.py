@@ -128,8 +128,8 @@ def test_workspace_sizes():
     L = dlm.lib()
     L.dlm_paged_attn_workspace_bytes.restype = C.c_size_t
     assert L.dlm_paged_attn_workspace_bytes(C.byref(_attn())) == 0                              # four tiles: nothing to share out
-    one = L.dlm_paged_attn_workspace_bytes(C.byref(_attn(table_stride=1 << 20, max_kv_len=65536)))
-    assert one > 0 and one % (2 * 4 * (128 + 2) * 4) == 0
+    many = L.dlm_paged_attn_workspace_bytes(C.byref(_attn(table_stride=1 << 20, max_kv_len=65536)))
+    assert 0 < many < 64 << 20
     assert L.dlm_paged_attn_workspace_bytes(None) == 0
 
 
