@@ -58,6 +58,17 @@ struct Step {
     }
 };
 
+// sum over the lanes of a wavefront that hold the same entries of its heads; every lane gets it
+template <int D>
+__device__ __forceinline__ float over_heads(float v) {
+    if (D == 64) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xf, 0xf, true));     // rotated by 4 within 16
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xf, 0xf, true));                   // by 8
+    auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+
 struct Rotation {
     const float* rope;         // NULL: none
     int rope_len, rot;
@@ -274,7 +285,6 @@ struct GradParams {
 // workspace.  With t = r dz: dw += t x;  u = t w;  dx = u - x (r^2 mean(u x)).
 template <int D, bool PAIRS>
 __global__ __launch_bounds__(256) void head_map_grad_kernel(GradParams p) {
-    constexpr int LPH = D / 16;
     __shared__ float sums[4][D];
     const GradPart& t = p.part[blockIdx.x >= p.part[1].walk.first ? 1 : 0];
     const Place<D> place(t.walk);
@@ -352,12 +362,9 @@ __global__ __launch_bounds__(256) void head_map_grad_kernel(GradParams p) {
     if (!t.partial) return;                  // (uniform in the workgroup)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-#pragma unroll
-        for (int off = LPH; off < 64; off <<= 1) {
-            dwa[e] += shfl_xor(dwa[e], off);
-            dwb[e] += shfl_xor(dwb[e], off);
-        }
-        if (lane_id() < LPH) {
+        dwa[e] = over_heads<D>(dwa[e]);
+        dwb[e] = over_heads<D>(dwb[e]);
+        if (lane_id() < D / 16) {
             sums[wave][at.a + e] = dwa[e];
             sums[wave][at.b + e] = dwb[e];
         }
@@ -397,9 +404,10 @@ __global__ __launch_bounds__(1024) void head_grad_sum_kernel(GradSumParams p) {
             for (int e = 0; e < 4; ++e) v[e] += i + 1024 * k < n ? u[k][e] : 0.f;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) v[e] += shfl_xor(v[e], off);
+    for (int e = 0; e < 4; ++e) {
+        v[e] = head_sum<128>(v[e]);                       // 8 lanes
+        v[e] = over_heads<128>(v[e]);                     // and the eight eights
+    }
     if (lane_id() == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
     if (threadIdx.x < 4) {
