@@ -603,8 +603,8 @@ size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
  *   "paged_shares"  0 = the library decides whether the keys of a dlm_paged_attn with a workspace are dealt out evenly to a number of workgroups
  *                   whatever the sequences' lengths (default); -1 = one workgroup for each sequence, KV head and group of rows; n >= 1 = n
  *                   workgroups share them (the workspace's size depends on it).
- *   "paged_shape"   0 = the library picks dlm_paged_attn's workgroups from the rows a KV head has (default); 1, 2, 3 = 16, 32, 128 rows
- *                   (the workspace's size depends on it).
+ *   "paged_shape"   0 = the library picks dlm_paged_attn's workgroups from the rows a KV head has (default); 1, 2, 3, 4 = 16, 32, 128, 16
+ *                   rows (of 8, 4, 8, 2 wavefronts; the workspace's size depends on it).
  * The knobs exist for tests and tuning sweeps. */
 int dlm_set_option(const char *name, int value);
 

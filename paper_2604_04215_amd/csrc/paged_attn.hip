@@ -38,6 +38,7 @@ struct PagedAttnParams {
     FastDiv by_g, by_bs;
     float scale_log2;              // scale * log2(e): the softmax is evaluated with exp2
     int rows_wg, row_groups;       // rows of a workgroup; row groups that Lq rows make
+    int thin_waves;                // wavefronts of a workgroup of 16 rows
     GridRemap remap;               // one workgroup a row group
     // even shares: workgroups, and what they leave to be joined: sums [2 * shares][rows_wg][d] with (maximum in log2 units, sum) [..][2], and for each
     // row group its first workgroup and their number
@@ -250,11 +251,11 @@ struct Pages {
     }
 };
 
-// Runs `rows(work, pages)` for what this workgroup has to do; the pages are those of every STEP-th tile from the wavefront's (STEP 2: its half of the
+// Runs `rows(work, pages)` for what this workgroup has to do; the pages are those of every STEP-th tile from the wavefront's (128 rows: its half of the
 // workgroup's) first on.
 template <int RT, bool BC, bool EVEN, int ES, int STEP, typename F>
 __device__ __forceinline__ void run_rows(const PagedAttnParams& p, unsigned char* smem, const F& rows) {
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> (STEP == 2 ? 8 : 6));
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> (RT == 128 ? 8 : 6));
     Work<RT, BC> wk;
     if constexpr (EVEN) {
         Shares<RT, BC> sh;
@@ -418,8 +419,7 @@ __device__ __forceinline__ int fresh_thread() {
 
 // LDS of the three shapes: values (or keys and values) of a tile a wavefront, which the join's sums replace; two tiles a workgroup
 constexpr int larger(int a, int b) { return a > b ? a : b; }
-constexpr int THIN_WAVES = 8;
-constexpr int thin_smem(int d) { return larger(THIN_WAVES * 32 * (2 * d + 64), THIN_WAVES * 16 * (d + 4) * 4); }
+constexpr int thin_smem(int d, int waves) { return waves * larger(32 * (2 * d + 64), 16 * (d + 4) * 4); }
 constexpr int wide_smem(int d) { return larger(4 * 32 * (4 * d + 80), 4 * 32 * (d + 4) * 4); }
 constexpr int tall_smem(int d) { return 4 * 32 * (4 * d + 80); }
 
@@ -427,9 +427,9 @@ constexpr int tall_smem(int d) { return 4 * 32 * (4 * d + 80); }
 // For short sequences, where latency counts: eight wavefronts split the keys, 16 x 16 x 32 products, and K goes from memory straight into operand
 // registers (lane: key l % 16, 16 bytes of its row); V through LDS for the transposing read.  (3 sequences of up to 400 tokens, 14/2 heads
 // of 64: four wavefronts of the 32-row shape 6.3 us, of this one 5.8.)
-template <int D, bool F8, bool BC>
+template <int D, bool F8, bool BC, int NW>
 __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const Work<16, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
-    constexpr int NW = THIN_WAVES, RT = 16;
+    constexpr int RT = 16;
     constexpr int VP = D * 2 + 64;
     constexpr int ES = F8 ? 1 : 2;
     constexpr int C = D * ES / 16, RPL = 64 / C, NLD = 32 / RPL;      // V: 16-byte pieces a row, rows a load, loads
@@ -574,11 +574,11 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
     join_rows<D, F8, RT, NW, MP>(p, wk, mb, tid);
 }
 
-template <int D, bool F8, bool BC>
-__global__ __launch_bounds__(64 * THIN_WAVES, 1) void paged_thin_kernel(PagedAttnParams p) {
-    __shared__ __attribute__((aligned(16))) unsigned char smem[thin_smem(D)];
+template <int D, bool F8, bool BC, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void paged_thin_kernel(PagedAttnParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char smem[thin_smem(D, NW)];
     fetch_args<sizeof(PagedAttnParams)>();
-    run_rows<16, BC, false, F8 ? 1 : 2, THIN_WAVES>(p, smem, [&](const Work<16, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_thin_rows<D, F8, BC>(p, wk, pages, smem); });
+    run_rows<16, BC, false, F8 ? 1 : 2, NW>(p, smem, [&](const Work<16, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_thin_rows<D, F8, BC, NW>(p, wk, pages, smem); });
 }
 
 // ---- 32 rows ------------------------------------------------------------------------------------------------
@@ -932,22 +932,33 @@ static int g_paged_shares = 0;     // "paged_shares"
 // How a call is laid out.
 struct PagedPlan {
     int rows, row_groups;   // rows of a workgroup, row groups of Lq rows
+    int thin_waves;         // with 16 rows: wavefronts
     int shares;             // workgroups that share the tiles evenly; 0: one workgroup a row group
     size_t sums, meta;      // of the workspace: floats of sums and (maximum, sum) pairs, ints behind them
     size_t bytes() const { return shares ? sums * sizeof(float) + meta * sizeof(int32_t) : 0; }
 };
+// T = the longest sequence's tiles; the lengths themselves are not known here.
+// Up to 16 rows: two wavefronts for sequences of a few tiles (T <= 4; 64 sequences of up to 120 tokens, 32/32 heads: 23 us, four wavefronts and 32 rows
+// 27), eight for few row groups whose keys a CU streams quickly (16 sequences of 1100 tokens, 32/8 heads: 15.3 / 16.3, in 8 bits 10 / 16), else
+// 32 rows; 128 for blocks of many heads.
 // One workgroup a row group costs least where the row groups fill the chip; it leaves CUs idle where they are few, and one that is much longer than the
 // others runs on alone.  Even shares cost a second launch, a scan of the lengths and what is left half done at each border.  Estimates, in
-// microseconds, T = the longest sequence's tiles (the lengths are not known here):
-//   32 rows:  a CU streams 49 GB/s, the chip 6.6 TB/s, shares cost 9.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168 with shares, of 2048 - 4096 134 /
-//             142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.  From 256 tiles on always shares.
+// microseconds:
+//   32 rows:  a CU streams 49 GB/s, the chip 6.6 TB/s; 4.5 for the launch, with shares 11 and at least 17.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168
+//             with shares, of 2048 - 4096 134 / 142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.
+//             From 256 tiles on always shares.
 //   128 rows: a tile takes a CU 0.7, shares cost 20.  32 x 32 rows of 28/4 heads, 1024 tokens: 29 / 38.
 static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
-    static const int shape_rows[4] = {0, 16, 32, 128};
+    static const int shape_rows[5] = {0, 16, 32, 128, 16};
     PagedPlan pl = {};
     const int64_t R = (int64_t)a->Lq * (a->Hq / a->Hkv), T = ((int64_t)a->max_kv_len + 31) / 32, heads = (int64_t)a->B * a->Hkv;
-    // few short sequences: latency counts (16 sequences of 700 tokens, 14/2 heads of 64: 16 rows and eight wavefronts 7.0 us, 32 and four 8.1)
-    pl.rows = g_paged_shape > 0 ? shape_rows[g_paged_shape] : R <= 16 && T <= 24 && heads <= 256 ? 16 : R <= 64 ? 32 : 128;
+    const int64_t tile = (int64_t)64 * a->d * (a->cache.type == DLM_KV_E4M3 ? 1 : 2);      // bytes
+    pl.thin_waves = T <= 4 ? 2 : 8;
+    pl.rows = R <= 16 && (T <= 4 || (heads <= 128 && T * tile <= 560 << 10)) ? 16 : R <= 64 ? 32 : 128;
+    if (g_paged_shape > 0) {
+        pl.rows = shape_rows[g_paged_shape];
+        pl.thin_waves = g_paged_shape == 4 ? 2 : 8;
+    }
     pl.row_groups = (int)((R + pl.rows - 1) / pl.rows);
     const int64_t groups = heads * pl.row_groups, rounds = (groups + 255) / 256;
     if (pl.rows == 16 || groups > 0x7fffffff / (T + 1)) return pl;          // (the line of tiles is counted in 32 bits)
@@ -956,8 +967,8 @@ static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
     else if (T > 256) pl.shares = most;
     else if (pl.rows == 128) pl.shares = 0.7 * T * rounds > 0.7 * T * groups / 256 + 20 ? most : 0;
     else {
-        const double tile = 64.0 * a->d * (a->cache.type == DLM_KV_E4M3 ? 1 : 2), all = (double)groups * T * tile / 6.6e6, alone = (double)T * rounds * tile / 49e3;
-        pl.shares = (alone > all ? alone : all) > all + 9 ? most : 0;
+        const double all = (double)groups * T * tile / 6.6e6, alone = (double)T * rounds * tile / 49e3;
+        pl.shares = (alone > all ? alone : all) + 4.5 > (all + 11 > 17 ? all + 11 : 17) ? most : 0;
     }
     if (pl.shares > groups * T / SMALLEST_SHARE) pl.shares = (int)(groups * T / SMALLEST_SHARE);
     pl.sums = (size_t)2 * pl.shares * pl.rows * (a->d + 2);
@@ -1000,7 +1011,10 @@ template <int D, bool F8, bool BC, bool EVEN>
 static int launch_rows(const PagedAttnParams& p, unsigned grid, hipStream_t st) {
     if (p.rows_wg == 128) hipLaunchKernelGGL((paged_tall_kernel<D, F8, BC, EVEN>), dim3(grid), dim3(512), 0, st, p);
     else if (p.rows_wg == 16) {
-        if constexpr (!EVEN) hipLaunchKernelGGL((paged_thin_kernel<D, F8, BC>), dim3(grid), dim3(64 * THIN_WAVES), 0, st, p);
+        if constexpr (!EVEN) {
+            if (p.thin_waves == 2) hipLaunchKernelGGL((paged_thin_kernel<D, F8, BC, 2>), dim3(grid), dim3(128), 0, st, p);
+            else hipLaunchKernelGGL((paged_thin_kernel<D, F8, BC, 8>), dim3(grid), dim3(512), 0, st, p);
+        }
     } else if (p.row_groups == 1) hipLaunchKernelGGL((paged_wide_kernel<D, F8, BC, true, EVEN>), dim3(grid), dim3(256), 0, st, p);
     else hipLaunchKernelGGL((paged_wide_kernel<D, F8, BC, false, EVEN>), dim3(grid), dim3(256), 0, st, p);
     return check_hip(hipGetLastError(), "paged attention launch");
@@ -1020,7 +1034,7 @@ static int launch_paged(const PagedAttnParams& p, bool bc, unsigned grid, hipStr
 }
 
 int paged_set_shape(int v) {
-    if (v < 0 || v > 3) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_shape must be 0..3");
+    if (v < 0 || v > 4) return fail(DLM_ERR_INVALID_ARG, "set_option: paged_shape must be 0..4");
     g_paged_shape = v;
     return DLM_OK;
 }
@@ -1064,6 +1078,7 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
     const PagedPlan pl = plan_paged(a);
     p.rows_wg = pl.rows;
     p.row_groups = pl.row_groups;
+    p.thin_waves = pl.thin_waves;
     if (pl.shares && p.max_kv_len > 0 && a->workspace && a->workspace_bytes >= pl.bytes() && aligned16(a->workspace)) {
         p.shares = pl.shares;
         p.part_o = (float*)a->workspace;

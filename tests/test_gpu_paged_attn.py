@@ -121,7 +121,7 @@ def options():
 
 
 @pytest.mark.parametrize("shares", [0, -1, 1, 2, 7, 64, 1000])
-@pytest.mark.parametrize("shape", [1, 2, 3])
+@pytest.mark.parametrize("shape", [1, 2, 3, 4])
 @pytest.mark.parametrize("d", [64, 128])
 def test_every_shape_of_workgroup(options, shape, shares, d):
     """16, 32 and 128 rows a workgroup, keys dealt out to few workgroups and to more than there are, for few rows and many, every mask and type."""
@@ -135,7 +135,7 @@ def test_every_shape_of_workgroup(options, shape, shares, d):
                 c.check(**mask)
 
 
-@pytest.mark.parametrize("shape", [1, 2, 3])
+@pytest.mark.parametrize("shape", [1, 2, 3, 4])
 def test_more_than_32_tiles_a_wavefront(options, shape):
     """The look-ups of pages go on past the first 32 tiles."""
     options("paged_shape", shape)
@@ -216,7 +216,7 @@ def test_what_is_not_finite():
     assert c.out[3].isfinite().all()
 
 
-@pytest.mark.parametrize("shape", [1, 2, 3])
+@pytest.mark.parametrize("shape", [1, 2, 3, 4])
 def test_every_8_bit_value(options, shape):
     """One key: the output is its value, every e4m3 there is, exactly (powers of two as scales); NaN stays NaN."""
     options("paged_shape", shape)
