@@ -35,7 +35,7 @@ struct PagedAttnParams {
     int max_kv_len;
     const int32_t* q_len;
     int bs;                        // block size of the block-causal mask
-    FastDiv by_g, by_bs;
+    FastDiv by_g, by_bs, by_shares;
     float scale_log2;              // scale * log2(e): the softmax is evaluated with exp2
     int rows_wg, row_groups;       // rows of a workgroup; row groups that Lq rows make
     int thin_waves;                // wavefronts of a workgroup of 16 rows
@@ -112,12 +112,13 @@ struct Work {
 constexpr int SMALLEST_SHARE = 8;           // tiles: two a wavefront
 
 // Even shares.  The tiles of all row groups, sequence by sequence, KV head by KV head, make one line of N (a row group has at least one, so that somebody
-// writes its zeros; under a block-causal mask each has as many as its sequence's last); workgroup w of W takes [w N / W, (w + 1) N / W).  So one long
-// sequence among short ones, or too few sequences for the chip, cost nothing but the joins, and the host need not know the lengths.  A share is the end of one
-// row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began elsewhere) and 2w + 1.
+// writes its zeros; under a block-causal mask each has as many as its sequence's last); with S = max(ceil(N / shares), 8) workgroup w takes tiles
+// [w S, (w + 1) S).  So one long sequence among short ones, or too few sequences for the chip, cost nothing but the joins, and the host need not
+// know the lengths.  A share is the end of one row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began
+// elsewhere) and 2w + 1.
 template <int RT, bool BC>
 struct Shares {
-    int w, W, N, at, end;                   // its tiles: at .. end - 1
+    int w, N, S, at, end;                   // its tiles: at .. end - 1
     int b, base, len, ql;                   // the sequence of `at`, its first tile, its lengths as given
     // tiles of each row group of a sequence, and the row groups
     static __device__ __forceinline__ int tiles_of(const PagedAttnParams& p, int len_, int ql_, int& groups) {
@@ -125,21 +126,15 @@ struct Shares {
         groups = p.Hkv * ((ql * p.g + RT - 1) / RT);
         return ql > 0 ? max((visible_keys<BC>(p, len, ql, ql - 1) + 31) >> 5, 1) : 0;
     }
-    // (v, W <= 65536, so the remainders' product fits 32 bits; a quotient of whole numbers below 2^47 by N < 2^31 that is under 2^17 is at least 2^-31 from
-    // the next whole one unless it is one, which 53 bits tell apart)
-    __device__ __forceinline__ int start_of(uint32_t v) const {
-        const uint32_t q = (uint32_t)N / (uint32_t)W, r = (uint32_t)N - q * W;
-        return __builtin_amdgcn_readfirstlane(v * q + v * r / (uint32_t)W);
-    }
-    __device__ __forceinline__ int owner_of(int tile) const { return (int)((((double)tile + 1.0) * W - 1.0) / N); }
     // false: no share for this workgroup.  smem: 8 ints
     __device__ bool find(const PagedAttnParams& p, int* smem) {
         const int tid = threadIdx.x & 255, lane = lane_id(), wave = tid >> 6;        // (a second 256 threads do the same)
         const int each = (p.B + 255) / 256, from = min(tid * each, p.B), to = min(from + each, p.B);
-        int own = 0, groups;
+        int own = 0, groups, l = 0, q = 0;
         for (int i = from; i < to; ++i) {
-            const int u = tiles_of(p, p.kv_len[i], p.q_len ? p.q_len[i] : 0, groups);
-            own += u * groups;
+            l = p.kv_len[i];
+            q = p.q_len ? p.q_len[i] : 0;
+            own += tiles_of(p, l, q, groups) * groups;
         }
         int sum = own;
 #pragma unroll
@@ -151,24 +146,28 @@ struct Shares {
         __syncthreads();
         const int s0 = smem[0], s1 = smem[1], s2 = smem[2], s3 = smem[3];
         N = __builtin_amdgcn_readfirstlane(s0 + s1 + s2 + s3);
-        W = __builtin_amdgcn_readfirstlane(min(p.shares, max(N / SMALLEST_SHARE, 1)));
+        if (N == 0) return false;           // nobody asks (and there is no N - 1 to divide)
+        S = max((int)quotient(N - 1, p.by_shares) + 1, SMALLEST_SHARE);
         w = blockIdx.x;
-        if (w >= W || N == 0) return false;
-        at = start_of(w);
-        end = start_of(w + 1);
+        if ((int64_t)w * S >= N) return false;
+        at = w * S;
+        end = min(N - at, S) + at;
         int first = sum - own + (wave > 0 ? s0 : 0) + (wave > 1 ? s1 : 0) + (wave > 2 ? s2 : 0);
         if (at >= first && at < first + own) {
-            for (int i = from; i < to; ++i) {
-                const int l = p.kv_len[i], q = p.q_len ? p.q_len[i] : 0, u = tiles_of(p, l, q, groups);
-                if (at < first + u * groups) {
-                    smem[4] = i;
-                    smem[5] = first;
-                    smem[6] = l;
-                    smem[7] = q;
-                    break;
+            int i = from;
+            if (each > 1) {                 // (with one sequence a thread l and q are its)
+                for (;; ++i) {
+                    l = p.kv_len[i];
+                    q = p.q_len ? p.q_len[i] : 0;
+                    const int u = tiles_of(p, l, q, groups) * groups;
+                    if (at < first + u) break;
+                    first += u;
                 }
-                first += u * groups;
             }
+            smem[4] = i;
+            smem[5] = first;
+            smem[6] = l;
+            smem[7] = q;
         }
         __syncthreads();
         b = __builtin_amdgcn_readfirstlane(smem[4]);
@@ -204,7 +203,7 @@ struct Shares {
         if (wk.t0 == 0 && threadIdx.x == 0) {
             int32_t* m = p.meta + 2 * (((int64_t)b * p.Hkv + wk.kvh) * p.row_groups + wk.r0 / RT);
             m[0] = w;
-            m[1] = owner_of(first + units - 1) - w + 1;
+            m[1] = (first + units - 1) / S - w + 1;
         }
         at = stop;
         return true;
@@ -864,10 +863,10 @@ __global__ __launch_bounds__(512, 1) void paged_tall_kernel(PagedAttnParams p) {
 
 // Joins the sums of each (sequence, head, row) whose keys were shared out: M = max m_s, w_s = 2^(m_s - M), out = sum w_s o_s / sum w_s l_s,
 // lse = (M + log2 sum w_s l_s) ln 2.  D / 4 threads a row and group of shares, G groups: group k takes shares k, k + G, .. in their order, four
-// requested at a time, and the groups are added up in theirs.
+// requested at a time (eight with several groups), and the groups are added up in theirs.
 template <int D, bool F8, int G>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
-    constexpr int TPR = D / 4, RPW = 256 / TPR / G;
+    constexpr int TPR = D / 4, RPW = 256 / TPR / G, U = G > 1 ? 8 : 4;
     __shared__ float part[G > 1 ? 256 / TPR : 1][D + 2];
     const int64_t rows = (int64_t)p.B * p.Hq * p.Lq, row = min((int64_t)blockIdx.x * RPW + threadIdx.x / (TPR * G), rows - 1);
     const int c4 = threadIdx.x % TPR, gi = threadIdx.x / TPR, k = gi % G;
@@ -877,24 +876,23 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
     const int32_t* m = p.meta + 2 * (((int64_t)b * p.Hkv + h / p.g) * p.row_groups + r / p.rows_wg);
     const int w0 = m[0], n = i < ql && m[1] > 1 ? m[1] : 0;                // 0: nothing to join here (rows behind q_len: nobody has written m)
     float M = -INFINITY, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = k; s0 < n; s0 += 4 * G) {
-        float m[4], l[4];
-        f32x4 v[4];
+    for (int s0 = k; s0 < n; s0 += U * G) {
+        f32x2 ml[U];
+        f32x4 v[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int s = min(s0 + u * G, n - 1);                          // (past the last one it is loaded again and not used)
             const int64_t at = (int64_t)(2 * (w0 + s) + (s == 0)) * p.rows_wg + rr;
-            m[u] = p.part_ml[at * 2];
-            l[u] = p.part_ml[at * 2 + 1];
+            ml[u] = *reinterpret_cast<const f32x2*>(p.part_ml + at * 2);
             v[u] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + 4 * c4);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             if (s0 + u * G >= n) continue;
-            const float m_new = __builtin_fmaxf(M, m[u]), m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float a = fast_exp2(M - m_use), w = fast_exp2(m[u] - m_use);
+            const float m_new = __builtin_fmaxf(M, ml[u][0]), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float a = fast_exp2(M - m_use), w = fast_exp2(ml[u][0] - m_use);
             M = m_new;
-            den = den * a + l[u] * w;
+            den = den * a + ml[u][1] * w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = o[e] * a + v[u][e] * w;
         }
@@ -1081,6 +1079,7 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
     p.thin_waves = pl.thin_waves;
     if (pl.shares && p.max_kv_len > 0 && a->workspace && a->workspace_bytes >= pl.bytes() && aligned16(a->workspace)) {
         p.shares = pl.shares;
+        p.by_shares = fast_div(pl.shares);
         p.part_o = (float*)a->workspace;
         p.part_ml = p.part_o + (size_t)2 * pl.shares * pl.rows * a->d;
         p.meta = (int32_t*)(p.part_o + pl.sums);
