@@ -938,21 +938,22 @@ struct PagedPlan {
 // T = the longest sequence's tiles; the lengths themselves are not known here.
 // Up to 16 rows: two wavefronts for sequences of a few tiles (T <= 4; 64 sequences of up to 120 tokens, 32/32 heads: 23 us, four wavefronts and 32 rows
 // 27), eight for few row groups whose keys a CU streams quickly (16 sequences of 1100 tokens, 32/8 heads: 15.3 / 16.3, in 8 bits 10 / 16), else
-// 32 rows; 128 for blocks of many heads.
+// 32 rows.  128 for blocks of many heads, where workgroups of 32 would not all be resident at once (two a CU, at d = 64 three): sharing tiles among the rows makes
+// more of a full chip, and a longer chain of steps (32 rows of 28/4 heads, 1024 tokens, 8 sequences: 15 us with 32 rows, 25 with 128; 32 sequences: 43 / 29).
 // One workgroup a row group costs least where the row groups fill the chip; it leaves CUs idle where they are few, and one that is much longer than the
 // others runs on alone.  Even shares cost a second launch, a scan of the lengths and what is left half done at each border.  Estimates, in
 // microseconds:
 //   32 rows:  a CU streams 49 GB/s, the chip 6.6 TB/s; 4.5 for the launch, with shares 11 and at least 17.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168
 //             with shares, of 2048 - 4096 134 / 142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.
 //             From 256 tiles on always shares.
-//   128 rows: a tile takes a CU 0.7, shares cost 20.  32 x 32 rows of 28/4 heads, 1024 tokens: 29 / 38.
+//   128 rows: a tile takes a CU 0.7, shares cost 20.  32 sequences of 1024 tokens, 32 rows of 28/4 heads: 29 / 38.
 static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
     static const int shape_rows[5] = {0, 16, 32, 128, 16};
     PagedPlan pl = {};
     const int64_t R = (int64_t)a->Lq * (a->Hq / a->Hkv), T = ((int64_t)a->max_kv_len + 31) / 32, heads = (int64_t)a->B * a->Hkv;
     const int64_t tile = (int64_t)64 * a->d * (a->cache.type == DLM_KV_E4M3 ? 1 : 2);      // bytes
     pl.thin_waves = T <= 4 ? 2 : 8;
-    pl.rows = R <= 16 && (T <= 4 || (heads <= 128 && T * tile <= 560 << 10)) ? 16 : R <= 64 ? 32 : 128;
+    pl.rows = R <= 16 && (T <= 4 || (heads <= 128 && T * tile <= 560 << 10)) ? 16 : R <= 64 || heads * ((R + 31) / 32) <= (a->d == 64 ? 768 : 512) ? 32 : 128;
     if (g_paged_shape > 0) {
         pl.rows = shape_rows[g_paged_shape];
         pl.thin_waves = g_paged_shape == 4 ? 2 : 8;
