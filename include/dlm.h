@@ -438,7 +438,8 @@ typedef struct dlm_head_map {
 /* dlm_qk_norm_rope -- dlm_head_map for the T tokens of a batch: training, and prompts whose keys go to a dense cache.
  *   q [T, Hq, d], k [T, Hkv, d] bf16, token and head strides of their own (views of one projection are fine); Hq or Hkv may be
  *   0 (that tensor absent).  q_out, k_out likewise; an output may be its input itself (same pointer and strides).
- * Supported: d in {64, 128}; bases 16-byte aligned, strides multiples of 8; T * max(Hq, Hkv) < 2^31. */
+ * Supported: d in {64, 128}; bases 16-byte aligned, strides multiples of 8; T * max(Hq, Hkv) < 2^31, and up to 2^28 heads of all tensors together
+ * (more are refused where they do not fit a launch; the gradient takes them). */
 typedef struct dlm_qk_args {
     uint32_t struct_size;
     int32_t T, Hq, Hkv, d;
@@ -533,7 +534,7 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
  * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,
  * a call runs one workgroup for each sequence and KV head; results then differ by the rounding of another summation order only.
- * Values that a row does not see have to be finite where another of the 32 rows of its tile sees them (they are multiplied by zero).
+ * Values that a row does not see have to be finite where another query row of its sequence sees them (they are multiplied by zero).
  * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8; stride_t of the cache below 2^26. */
 typedef struct dlm_paged_attn_args {
     uint32_t struct_size;

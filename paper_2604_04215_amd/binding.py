@@ -1,8 +1,9 @@
-"""ctypes binding to libdlm.so: argument marshalling only.
+"""Binding to libdlm.so: argument marshalling only.
 
 Every function here fills the C structs of include/dlm.h from torch tensors
 (device pointers, element strides) and calls the library on the current torch
-HIP stream.  There is no fallback: if the HIP library has not been built, or a
+HIP stream: with ctypes, the calls of a paged cache in the module _marshal
+(csrc/marshal.cpp).  There is no fallback: if the HIP library has not been built, or a
 tensor is not on the GPU, the call raises.
 """
 from __future__ import annotations

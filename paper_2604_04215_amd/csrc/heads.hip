@@ -470,10 +470,11 @@ static uint32_t deal(Walk** walk, int n, uint32_t most) {
     return groups;
 }
 
-static int launch_head_map(HeadParams& p, int d, int style, hipStream_t st) {
+static int launch_head_map(HeadParams& p, int d, int style, const char* who, hipStream_t st) {
     Walk* walks[3] = {&p.part[0].walk, &p.part[1].walk, &p.part[2].walk};
     const uint32_t groups = deal(walks, 3, 1u << 29);            // one step a wavefront: loops over several were 5 - 12 % slower
     if (groups == 0) return DLM_OK;
+    if (groups >= 1u << 24) return fail(DLM_ERR_UNSUPPORTED, "%s: too many heads for one launch", who);      // (2^32 threads)
     const bool pairs = p.rotation.rope && style == DLM_ROPE_PAIRS;
     if (d == 128) {
         if (pairs) hipLaunchKernelGGL((head_map_kernel<128, true>), dim3(groups), dim3(256), 0, st, p);
@@ -517,7 +518,7 @@ extern "C" int dlm_qk_norm_rope(const dlm_qk_args* a, void* stream) {
     p.part[2].walk = walk_of(0, 0, a->d);
     p.rotation = rotation_of(a->map);
     p.eps = a->map.eps;
-    return launch_head_map(p, a->d, a->map.rope_style, (hipStream_t)stream);
+    return launch_head_map(p, a->d, a->map.rope_style, who, (hipStream_t)stream);
 }
 
 extern "C" int dlm_paged_append(const dlm_append_args* a, void* stream) {
@@ -546,7 +547,7 @@ extern "C" int dlm_paged_append(const dlm_append_args* a, void* stream) {
     p.slots = a->slots;
     p.n_slots = (uint32_t)c.n_pages * (uint32_t)c.page_size;
     p.page_shift = log2_of(c.page_size);
-    return launch_head_map(p, a->d, a->map.rope_style, (hipStream_t)stream);
+    return launch_head_map(p, a->d, a->map.rope_style, who, (hipStream_t)stream);
 }
 
 extern "C" size_t dlm_qk_norm_rope_bwd_workspace_bytes(const dlm_qk_bwd_args* a) {

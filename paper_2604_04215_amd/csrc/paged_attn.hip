@@ -960,7 +960,8 @@ static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
     }
     pl.row_groups = (int)((R + pl.rows - 1) / pl.rows);
     const int64_t groups = heads * pl.row_groups, rounds = (groups + 255) / 256;
-    if (pl.rows == 16 || groups > 0x7fffffff / (T + 1)) return pl;          // (the line of tiles is counted in 32 bits)
+    // (the line of tiles is counted in 32 bits, and the joins are one launch)
+    if (pl.rows == 16 || groups > 0x7fffffff / (T + 1) || (int64_t)a->B * a->Lq * a->Hq > 1 << 26) return pl;
     const int most = pl.rows == 128 ? 256 : 512;
     if (g_paged_shares) pl.shares = g_paged_shares > 0 ? g_paged_shares : 0;
     else if (T > 256) pl.shares = most;
@@ -1086,7 +1087,8 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
         p.meta = (int32_t*)(p.part_o + pl.sums);
     }
     const int64_t grid = set_remap(p.remap, (int64_t)a->B * a->Hkv, pl.row_groups, false);
-    if (grid == 0 || (int64_t)a->B * a->Hkv > 0x7fffffff || (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
+    const int64_t threads = pl.rows == 128 ? 512 : pl.rows == 16 ? 64 * pl.thin_waves : 256;
+    if (grid == 0 || grid * threads > 0xffffffffll || (int64_t)a->B * a->Hkv > 0x7fffffff || (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
     hipStream_t st = (hipStream_t)stream;
     const bool f8 = c.type == DLM_KV_E4M3, bc = a->mask_mode == DLM_MASK_BLOCK_CAUSAL;
     if (a->d == 128) return f8 ? launch_paged<128, true>(p, bc, (unsigned)grid, st) : launch_paged<128, false>(p, bc, (unsigned)grid, st);

@@ -76,7 +76,7 @@ def compare(c, out, lse, mag, top):
     assert (np.abs(got - out)[~left] <= bound[~left]).all(), (np.abs(got - out)[~left] / (bound[~left] + 1e-300)).max()
     live = np.isfinite(lse)
     assert np.array_equal(got_lse[lse == -np.inf], lse[lse == -np.inf])
-    assert (np.abs(got_lse - lse)[live] <= (e + 2 * n * U + 4 * U * np.abs(np.where(live, lse, 0)))[live]).all()
+    assert (np.abs(got_lse[live] - lse[live]) <= (e + 2 * n * U)[live] + 4 * U * np.abs(lse[live])).all()
 
 
 SHAPES = [([1], 1, 1, 1, 64, 16), ([1, 31, 32, 33], 1, 14, 2, 64, 16), ([400, 17, 3], 1, 32, 8, 128, 64), ([0, 5, 64, 65], 1, 4, 4, 128, 16),
@@ -175,6 +175,20 @@ def test_long_sequence_split_and_not():
     c.run(max_kv_len=2900)
     c.lengths = [2900, 0]
     c.check()
+
+
+def test_no_keys_at_all():
+    """Tables without entries, caches without pages, sequences without tokens: zeros, and a log-sum-exp of -inf."""
+    c = Case([0, 0], 2, 4, 2, 64, 16)
+    for table, pages in ((c.table[:, :0], c.pages), (c.table, [x[:0] for x in c.pages]), (c.table, c.pages)):
+        c.out.fill_(7.0), c.lse.fill_(7.0)
+        c.lens.fill_(5 if table.shape[1] else 0)
+        if pages is c.pages:
+            c.lens.zero_()
+        dlm.paged_attn(c.q, c.out, *pages, table, c.lens, lse=c.lse)
+        assert (c.out == 0).all() and (c.lse == -float("inf")).all()
+    dlm.paged_attn(c.q[:0], c.out[:0], *c.pages, c.table[:0], c.lens[:0])
+    dlm.paged_attn(c.q[:, :0], c.out[:, :0], *c.pages, c.table, c.lens)
 
 
 def test_absent_pages():

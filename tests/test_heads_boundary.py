@@ -89,18 +89,19 @@ REFUSED = (
     + [("dlm_paged_attn", _attn, dict(cache=_cache(**c)), code) for c, code in CACHE]
     + [("dlm_qk_norm_rope", _qk, kw, code) for kw, code in [
         (dict(struct_size=8), BAD), (dict(T=-1), BAD), (dict(d=96), UNSUPPORTED), (dict(q=None), BAD), (dict(q=P + 4), UNSUPPORTED), (dict(k_out=None), BAD),
-        (dict(q_stride_t=516), UNSUPPORTED), (dict(qo_stride_t=256), BAD), (dict(qo_stride_h=64), BAD), (dict(ko_stride_t=0), BAD), (dict(T=1 << 30), UNSUPPORTED)]]
+        (dict(q_stride_t=516), UNSUPPORTED), (dict(qo_stride_t=256), BAD), (dict(qo_stride_h=64), BAD), (dict(ko_stride_t=0), BAD), (dict(T=1 << 30), UNSUPPORTED), (dict(T=1 << 28), UNSUPPORTED)]]
     + [("dlm_qk_norm_rope_bwd", _bwd, kw, code) for kw, code in [
         (dict(struct_size=8), BAD), (dict(d_q_out=None), BAD), (dict(q=None), BAD), (dict(d_k=P + 2), UNSUPPORTED), (dict(dk_stride_t=128), BAD),
         (dict(map=_map(q_weight=None)), BAD), (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=16), WORKSPACE), (dict(workspace=P + 4), WORKSPACE)]]
     + [("dlm_paged_append", _append, kw, code) for kw, code in [
         (dict(struct_size=8), BAD), (dict(Hkv=0), BAD), (dict(v=None), BAD), (dict(slots=None), BAD), (dict(q_out=None), BAD), (dict(v_stride_h=100), UNSUPPORTED),
-        (dict(cache=_cache(stride_h=128)), BAD), (dict(cache=_cache(stride_page=2048)), BAD)]]
+        (dict(cache=_cache(stride_h=128)), BAD), (dict(cache=_cache(stride_page=2048)), BAD), (dict(T=1 << 28), UNSUPPORTED)]]
     + [("dlm_paged_attn", _attn, kw, code) for kw, code in [
         (dict(struct_size=8), BAD), (dict(Hkv=3), BAD), (dict(Hkv=0), BAD), (dict(d=256), UNSUPPORTED), (dict(mask_mode=2), BAD), (dict(mask_mode=1), BAD),
         (dict(scale=float("nan")), BAD), (dict(max_kv_len=-1), BAD), (dict(max_kv_len=65), BAD), (dict(table_stride=-1), BAD), (dict(q=None), BAD),
         (dict(kv_len=None), BAD), (dict(block_table=None), BAD), (dict(out=P + 8), UNSUPPORTED), (dict(q_stride_b=516), UNSUPPORTED), (dict(o_stride_h=64), BAD),
-        (dict(o_stride_b=128), BAD), (dict(Lq=1 << 30, Hq=8), UNSUPPORTED)]])
+        (dict(o_stride_b=128), BAD), (dict(Lq=1 << 30, Hq=8), UNSUPPORTED),
+        (dict(B=1, Lq=1 << 28, Hkv=1), UNSUPPORTED)]])
 
 
 @pytest.mark.parametrize("name,make,fields,code", REFUSED)
@@ -131,6 +132,52 @@ def test_workspace_sizes():
     many = L.dlm_paged_attn_workspace_bytes(C.byref(_attn(table_stride=1 << 20, max_kv_len=65536)))
     assert 0 < many < 64 << 20
     assert L.dlm_paged_attn_workspace_bytes(None) == 0
+
+
+def test_options():
+    L = dlm.lib()
+    for name, good, bad in (("paged_shape", (1, 2, 3, 4, 0), (-1, 5)), ("paged_shares", (-1, 1, 65536, 0), (-2, 65537))):
+        for v in good:
+            assert L.dlm_set_option(name.encode(), v) == dlm.DLM_OK
+        for v in bad:
+            assert L.dlm_set_option(name.encode(), v) == BAD and name in dlm.last_error()
+
+
+def test_shares_give_every_tile_one_owner():
+    """The arithmetic by which workgroups share out the tiles of a batch (sizes, pieces, slots of sums, counts to be joined), over random batches."""
+    import random
+    rng = random.Random(5)
+    for _ in range(3000):
+        B, H, shares = rng.randint(1, 9), rng.randint(1, 4), rng.choice([1, 2, 3, 7, 64, 512, 1000])
+        tiles = [rng.choice([0, 0, 1, 2, rng.randint(1, 70)]) for _ in range(B)]                # of each row group of a sequence
+        groups = [H * rng.randint(1, 3) for _ in range(B)]
+        total = sum(t * g for t, g in zip(tiles, groups))
+        if total == 0:
+            continue
+        size = max((total - 1) // shares + 1, 8)
+        owned, joined, sums = [0] * total, {}, {}
+        for w in range(shares):
+            if w * size >= total:
+                continue
+            at, end, b, base, used = w * size, min(total, (w + 1) * size), 0, 0, set()
+            while at < end:
+                while at >= base + tiles[b] * groups[b]:
+                    base += tiles[b] * groups[b]
+                    b += 1
+                first = base + (at - base) // tiles[b] * tiles[b]
+                stop = min(end, first + tiles[b])
+                owned[at:stop] = [n + 1 for n in owned[at:stop]]
+                if at == first:
+                    joined[first] = (w, (first + tiles[b] - 1) // size - w + 1)
+                if not (at == first and stop == first + tiles[b]):
+                    slot = 2 * w + (at == first)
+                    assert slot not in used and slot < 2 * shares
+                    used.add(slot)
+                    sums.setdefault(first, []).append(slot)
+                at = stop
+        assert owned == [1] * total
+        for first, (w, n) in joined.items():
+            assert sums.get(first, []) == ([2 * (w + s) + (s == 0) for s in range(n)] if n > 1 else [])
 
 
 def test_binding_refuses_what_is_not_on_the_gpu():
