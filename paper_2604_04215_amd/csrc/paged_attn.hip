@@ -938,38 +938,53 @@ struct PagedPlan {
 // T = the longest sequence's tiles; the lengths themselves are not known here.
 // Up to 16 rows: two wavefronts for sequences of a few tiles (T <= 4; 64 sequences of up to 120 tokens, 32/32 heads: 23 us, four wavefronts and 32 rows
 // 27), eight for few row groups whose keys a CU streams quickly (16 sequences of 1100 tokens, 32/8 heads: 15.3 / 16.3, in 8 bits 10 / 16), else
-// 32 rows.  128 for blocks of many heads, where workgroups of 32 would not all be resident at once (two a CU, at d = 64 three): sharing tiles among the rows makes
-// more of a full chip, and a longer chain of steps (32 rows of 28/4 heads, 1024 tokens, 8 sequences: 15 us with 32 rows, 25 with 128; 32 sequences: 43 / 29).
-// One workgroup a row group costs least where the row groups fill the chip; it leaves CUs idle where they are few, and one that is much longer than the
-// others runs on alone.  Even shares cost a second launch, a scan of the lengths and what is left half done at each border.  Estimates, in
-// microseconds:
-//   32 rows:  a CU streams 49 GB/s, the chip 6.6 TB/s; 4.5 for the launch, with shares 11 and at least 17.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168
-//             with shares, of 2048 - 4096 134 / 142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.
-//             From 256 tiles on always shares.
-//   128 rows: a tile takes a CU 0.7, shares cost 20.  32 sequences of 1024 tokens, 32 rows of 28/4 heads: 29 / 38.
+// 32 rows.  Above 32 rows 32 or 128, one workgroup a row group or even shares, whichever is estimated to take least.  One workgroup a row group costs least
+// where the row groups fill the chip (and of one sequence and KV head they run on one XCD, whose L2 they share); it leaves CUs idle where they are few, and one that is
+// much longer than the others runs on alone.  Even shares cost a second launch, a scan of the lengths and what is left half done at each border, and their row
+// groups do not meet in an L2.  From 256 tiles on always shares, however equal the lengths may be, unless the row groups of one sequence fill the chip by themselves.
+// Estimates, in microseconds:
+//   up to 32 rows: a CU streams 49 GB/s, the chip 6.6 TB/s; 4.5 for the launch, with shares 11 and at least 17.  64 sequences of 4096 tokens, 32/8 heads: 164 / 168
+//                  with shares, of 2048 - 4096 134 / 142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.
+//   above:         a tile of 32 rows takes 0.28 (d = 64: 0.19) in a chain of its own and 0.29 (0.16) of a CU, with shares what its bytes take the chip (8-bit entries
+//                  count as 12 bits), one of 128 rows 0.56 (0.44) and 0.78 (0.44), with shares 0.9 (0.53).  Over 998 calls of equal lengths (33 - 896 rows,
+//                  1 - 64 sequences of 300 - 12000 tokens) the choice takes 1.4 % longer than the best of the four in the mean, at most 34 % (up to 256 tiles).
+//                  32 rows of 28/4 heads, 32 rows / 128 / with shares 32 / 128: 8 sequences of 1000 tokens 17 / 27 / 36 / 26, of 4000 44 / 78 / 82 / 50, of 12000
+//                  121 / 221 / 220 / 98; 32 sequences of 1000 43 / 31 / 89 / 41.
+//   causal masks:  row groups see half of the new tokens' keys in the middle, which shares do not know (one prompt of 8192 tokens, 28/4 heads: 680 / with shares 1217).
 static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
     static const int shape_rows[5] = {0, 16, 32, 128, 16};
     PagedPlan pl = {};
     const int64_t R = (int64_t)a->Lq * (a->Hq / a->Hkv), T = ((int64_t)a->max_kv_len + 31) / 32, heads = (int64_t)a->B * a->Hkv;
     const int64_t tile = (int64_t)64 * a->d * (a->cache.type == DLM_KV_E4M3 ? 1 : 2);      // bytes
+    auto larger = [](double x, double y) { return x > y ? x : y; };
+    auto time = [&](int rows, bool shared) {
+        const int64_t groups = heads * ((R + rows - 1) / rows);
+        const double stream = (double)groups * T * tile / 6.6e6, once = (double)heads * T * tile / 6.4e6;
+        const double mean = T - (a->mask_mode == DLM_MASK_BLOCK_CAUSAL ? a->Lq / 64.0 : 0);          // tiles that a row group sees
+        const bool d64 = a->d == 64;
+        if (rows == 32) {
+            if (shared) return larger(R <= 32 ? stream + 11 : stream * (a->cache.type == DLM_KV_E4M3 ? 1.5 : 1) + 13, 17);
+            if (R <= 32) return larger((double)T * ((groups + 255) / 256) * tile / 49e3, stream) + 4.5;
+            return larger(once, larger(T * (d64 ? 0.19 : 0.28), mean * groups / 256 * (d64 ? 0.16 : 0.29))) + 7;
+        }
+        if (shared) return (double)T * groups / 256 * (d64 ? 0.53 : 0.9) + 20;
+        return larger(once, larger(T * (d64 ? 0.44 : 0.56), groups > 128 ? mean * ((groups + 255) / 256) * (d64 ? 0.44 : 0.78) : 0)) + 9;
+    };
+    // whether a workgroup a row group is out of the question
+    const bool never_alone = T > 256 && (int64_t)a->Hkv * ((R + 127) / 128) < 256;
+    auto shares = [&](int rows) { return never_alone || time(rows, true) < time(rows, false); };
     pl.thin_waves = T <= 4 ? 2 : 8;
-    pl.rows = R <= 16 && (T <= 4 || (heads <= 128 && T * tile <= 560 << 10)) ? 16 : R <= 64 || heads * ((R + 31) / 32) <= (a->d == 64 ? 768 : 512) ? 32 : 128;
+    if (R <= 16 && (T <= 4 || (heads <= 128 && T * tile <= 560 << 10))) pl.rows = 16;
+    else pl.rows = R <= 32 || time(32, shares(32)) <= time(128, shares(128)) ? 32 : 128;
     if (g_paged_shape > 0) {
         pl.rows = shape_rows[g_paged_shape];
         pl.thin_waves = g_paged_shape == 4 ? 2 : 8;
     }
     pl.row_groups = (int)((R + pl.rows - 1) / pl.rows);
-    const int64_t groups = heads * pl.row_groups, rounds = (groups + 255) / 256;
+    const int64_t groups = heads * pl.row_groups;
     // (the line of tiles is counted in 32 bits, and the joins are one launch)
     if (pl.rows == 16 || groups > 0x7fffffff / (T + 1) || (int64_t)a->B * a->Lq * a->Hq > 1 << 26) return pl;
-    const int most = pl.rows == 128 ? 256 : 512;
-    if (g_paged_shares) pl.shares = g_paged_shares > 0 ? g_paged_shares : 0;
-    else if (T > 256) pl.shares = most;
-    else if (pl.rows == 128) pl.shares = 0.7 * T * rounds > 0.7 * T * groups / 256 + 20 ? most : 0;
-    else {
-        const double all = (double)groups * T * tile / 6.6e6, alone = (double)T * rounds * tile / 49e3;
-        pl.shares = (alone > all ? alone : all) + 4.5 > (all + 11 > 17 ? all + 11 : 17) ? most : 0;
-    }
+    pl.shares = g_paged_shares ? (g_paged_shares > 0 ? g_paged_shares : 0) : !shares(pl.rows) ? 0 : pl.rows == 128 ? 256 : 512;
     if (pl.shares > groups * T / SMALLEST_SHARE) pl.shares = (int)(groups * T / SMALLEST_SHARE);
     pl.sums = (size_t)2 * pl.shares * pl.rows * (a->d + 2);
     pl.meta = (size_t)2 * groups;
@@ -1086,7 +1101,7 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
         p.part_ml = p.part_o + (size_t)2 * pl.shares * pl.rows * a->d;
         p.meta = (int32_t*)(p.part_o + pl.sums);
     }
-    const int64_t grid = set_remap(p.remap, (int64_t)a->B * a->Hkv, pl.row_groups, false);
+    const int64_t grid = set_remap(p.remap, (int64_t)a->B * a->Hkv, pl.row_groups, a->mask_mode == DLM_MASK_BLOCK_CAUSAL);      // (longest first)
     const int64_t threads = pl.rows == 128 ? 512 : pl.rows == 16 ? 64 * pl.thin_waves : 256;
     if (grid == 0 || grid * threads > 0xffffffffll || (int64_t)a->B * a->Hkv > 0x7fffffff || (int64_t)a->B * a->Hq * a->Lq > 0x7fffffff) return fail(DLM_ERR_UNSUPPORTED, "paged_attn: too many workgroups");
     hipStream_t st = (hipStream_t)stream;
