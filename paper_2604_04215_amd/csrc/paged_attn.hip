@@ -210,43 +210,54 @@ struct Shares {
     }
 };
 
-// Pages of a wavefront's next 32 tiles, `step` apart: lane 2j + h holds the one of half h (16 keys, a page is no smaller) of its j-th tile.  One
-// load for 32 tiles, requested 32 tiles ahead: a look-up a tile was a trip to memory in front of every fetch.  The first one travels with the
-// sequence's lengths, so it may look at entries behind the sequence's end (but inside the table's row): whatever they hold, a page outside the
-// cache is not read and a key behind the end not seen.
+// Where a wavefront's next 32 tiles lie, `step` apart: lane 2j + h holds half h (16 keys, a page is no smaller) of its j-th tile.  One load of page numbers
+// for 32 tiles, requested 32 tiles ahead (a look-up a tile was a trip to memory in front of every fetch), and all 64 places are computed at once, one a lane (64-bit
+// products a tile were some 50 scalar instructions in the chain of each wavefront: 128 rows, 32 sequences of 1024 tokens in 8 bits 29.8 -> 27.1 us).  The first load travels with the sequence's lengths, so it may look
+// at entries behind the sequence's end (but inside the table's row): whatever they hold, a page outside the cache is not read and a key behind the end
+// not seen.
 template <int ES>
 struct Pages {
     const int32_t* table;
-    int first, step, last, now, next;
+    int first, step, last, next;
+    uint32_t lo, hi;                        // byte offset in the cache
+    uint64_t there;                         // one bit a half: whether there is such a page
     __device__ __forceinline__ int look(const PagedAttnParams& p, int j) const {
         const int lane = lane_id();
         return table[min((int)(((int64_t)(first + step * (j + (lane >> 1))) * 32 + 16 * (lane & 1)) >> p.page_shift), last)];
+    }
+    __device__ __forceinline__ void settle(const PagedAttnParams& p, int j) {
+        const int lane = lane_id();
+        const bool in = (unsigned)next < (unsigned)p.n_pages;
+        const uint32_t row = ((uint32_t)(first + step * (j + (lane >> 1))) * 32 + 16 * (lane & 1)) & ((1u << p.page_shift) - 1);
+        const uint64_t at = ((uint64_t)(in ? (uint32_t)next : 0u) * (uint64_t)p.sp + (uint64_t)row * (uint32_t)p.st) * ES;
+        lo = (uint32_t)at;
+        hi = (uint32_t)(at >> 32);
+        there = __ballot(in);
     }
     __device__ __forceinline__ Pages(const PagedAttnParams& p, int b, int first_tile, int step_) {
         table = p.table + b * p.table_stride;
         first = first_tile;
         step = step_;
         last = (max(p.max_kv_len, 1) - 1) >> p.page_shift;
-        now = p.max_kv_len > 0 ? look(p, 0) : 0;
-        next = 0;
+        next = p.max_kv_len > 0 ? look(p, 0) : 0;
     }
     // before tile 0: `n` tiles in all
     __device__ __forceinline__ void begin(const PagedAttnParams& p, int n) {
+        settle(p, 0);
         if (n > 32) next = look(p, 32);
     }
     // before tile j > 0 of n
     __device__ __forceinline__ void advance(const PagedAttnParams& p, int j, int n) {
         if ((j & 31) == 0) {
-            now = next;
+            settle(p, j);
             if (j + 32 < n) next = look(p, j + 32);
         }
     }
     // byte offset of half h of tile j in the cache; false: there is no such page
-    __device__ __forceinline__ bool half(const PagedAttnParams& p, int j, int h, int64_t& base) const {
-        const int page = __builtin_amdgcn_readlane(now, 2 * (j & 31) + h), key = (first + step * j) * 32 + 16 * h;
-        const bool there = (unsigned)page < (unsigned)p.n_pages;
-        base = ((int64_t)(there ? page : 0) * p.sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.st) * ES;
-        return there;
+    __device__ __forceinline__ bool half(int j, int h, int64_t& base) const {
+        const int at = 2 * (j & 31) + h;
+        base = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, at) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, at));
+        return there >> at & 1;
     }
 };
 
@@ -312,10 +323,10 @@ __device__ __forceinline__ void hide(V& S, int at, int limit, bool here0, bool h
         if (at + STEP * (i >> 2) + (i & 3) >= limit || !(i < N / 2 ? here0 : here1)) S[i] = -INFINITY;
 }
 
-// One 32-key tile in LDS (K rows KP bytes apart, V rows VP) for the 32 rows of a wavefront: scores, softmax, P V.
-template <int D, int KP, int VP>
-__device__ __forceinline__ void tile32(const unsigned char* Kl, const unsigned char* Vl, const bf16x8 (&qf)[D / 16], int key0, int limit, int limit_min,
-                                       bool here0, bool here1, float scale_log2, Running& run, f32x16 (&O)[D / 32], int lane) {
+// One 32-key tile in LDS (K rows KP bytes apart, V rows VP) for the 32 rows of a wavefront, in four parts:
+// scores S^T = K Q^T
+template <int D, int KP>
+__device__ __forceinline__ f32x16 scores32(const unsigned char* Kl, const bf16x8 (&qf)[D / 16], int lane) {
     const int n = lane & 31, hi = lane >> 5;
     f32x16 S;
 #pragma unroll
@@ -323,19 +334,18 @@ __device__ __forceinline__ void tile32(const unsigned char* Kl, const unsigned c
 #pragma unroll
     for (int c = 0; c < D / 16; ++c)
         S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Kl + n * KP + (16 * c + 8 * hi) * 2), qf[c], S, 0, 0, 0);
-    if (key0 + 32 > limit_min || !here0 || !here1) hide<16, 8>(S, key0 + 4 * hi, limit, here0, here1);
-    float mx = -INFINITY, m_use, rs = 0.f;
+    return S;
+}
+// masks and the running maximum; returns what exponentials are relative to
+template <int D>
+__device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limit_min, bool here0, bool here1, float scale_log2, Running& run,
+                                        f32x16 (&O)[D / 32], int lane) {
+    if (key0 + 32 > limit_min || !here0 || !here1) hide<16, 8>(S, key0 + 4 * (lane >> 5), limit, here0, here1);
+    float mx = -INFINITY, m_use;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2, m_use);
-    uint32_t pk[8];
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-        const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
-        rs += p0 + p1;
-        pk[i >> 1] = pack_bf16x2(p0, p1);
-    }
     if (__any(alpha != 1.0f)) {
         run.l *= alpha;
 #pragma unroll
@@ -343,10 +353,27 @@ __device__ __forceinline__ void tile32(const unsigned char* Kl, const unsigned c
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
     }
+    return m_use;
+}
+// probabilities, and their sum
+__device__ __forceinline__ void weights32(const f32x16& S, float scale_log2, float m_use, Running& run, bf16x8 (&pf)[2]) {
+    float rs = 0.f;
+    uint32_t pk[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
+        rs += p0 + p1;
+        pk[i >> 1] = pack_bf16x2(p0, p1);
+    }
     run.l += rs;
     const u32x4 plo = {pk[0], pk[1], pk[2], pk[3]}, phi = {pk[4], pk[5], pk[6], pk[7]};
-    const bf16x8 pf[2] = {as_bf16x8(plo), as_bf16x8(phi)};
-    const int s16 = lane & 15, blk = (lane >> 4) & 1;
+    pf[0] = as_bf16x8(plo);
+    pf[1] = as_bf16x8(phi);
+}
+// O^T += V^T P^T
+template <int D, int VP>
+__device__ __forceinline__ void values32(const unsigned char* Vl, const bf16x8 (&pf)[2], f32x16 (&O)[D / 32], int lane) {
+    const int hi = lane >> 5, s16 = lane & 15, blk = (lane >> 4) & 1;
     const unsigned char* vbase = Vl + (4 * hi + (s16 >> 2)) * VP + (16 * blk + 4 * (s16 & 3)) * 2;
 #pragma unroll
     for (int e = 0; e < 2 * (D / 32); ++e) {
@@ -472,7 +499,7 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             int64_t base;
-            there[h] = pages.half(p, j, h, base);
+            there[h] = pages.half(j, h, base);
             ks[h] = kb + base;
             vs[h] = vb + base;
         }
@@ -628,7 +655,7 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             int64_t base;
-            there[h] = pages.half(p, j, h, base);
+            there[h] = pages.half(j, h, base);
             ks[h] = kb + base;
             vs[h] = vb + base;
         }
@@ -661,7 +688,11 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
             pages.advance(p, j + 1, J);
             fetch(j + 1);
         }
-        tile32<D, KP, VP>(Kl, Vl, qf, key0, limit, limit_min, here0, here1, scale_log2, run, O, lane);
+        f32x16 S = scores32<D, KP>(Kl, qf, lane);
+        const float m_use = lead32<D>(S, key0, limit, limit_min, here0, here1, scale_log2, run, O, lane);
+        bf16x8 pf[2];
+        weights32(S, scale_log2, m_use, run, pf);
+        values32<D, VP>(Vl, pf, O, lane);
     }
     float* mb = reinterpret_cast<float*>(smem);
     __syncthreads();
@@ -687,15 +718,23 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedAttnParams p) {
     run_rows<32, BC, EVEN, F8 ? 1 : 2, 4>(p, smem, [&](const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_wide_rows<D, F8, BC, NT>(p, wk, pages, smem); });
 }
 
+template <int N>
+struct Const {
+    static constexpr int value = N;
+};
+
 // ---- 128 rows -----------------------------------------------------------------------------------------------
 // Two key groups of four wavefronts take every second tile; wavefront w of a group has rows 32 w .. 32 w + 31.  A group's t-th tile sits in its LDS
-// buffer t % 2: while it is multiplied, tile t + 1 is stored into the other one and tile t + 3 requested, one barrier a tile.
+// buffer t % 2.  Step t: the scores of tile t + 1 are formed among the exponentials of tile t, then O takes its values; meanwhile K of tile t + 2 and V of
+// tile t + 1 go into the places of K of tile t and V of tile t - 1, and K of tile t + 4 and V of tile t + 3 are requested.  One barrier a step.
+// One workgroup a CU at d = 128 (235 registers), two at d = 64.  A step of two tiles takes 1.1 us (d = 128), of which the matrix units work 0.43, the vector units
+// 0.5 and LDS 0.4: what they overlap is the two wavefronts of a SIMD and the woven products.  4 prompts of 4096 tokens, 32/8 heads, 8-bit cache: 1218 us, 0.9 PFLOP/s.
 template <int D, bool F8, bool BC>
 __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
     constexpr int RT = 128, PF = 2, MP = D + 4;
     constexpr int KP = D * 2 + 16, VP = D * 2 + 64, TILE = 32 * KP + 32 * VP;
     constexpr int ES = F8 ? 1 : 2;
-    constexpr int C = D * ES / 16, RPL = 256 / C, NLD = RPL > 32 ? 1 : 32 / RPL;      // rows that one load of the workgroup covers (64 at d = 64, e4m3: half the threads)
+    constexpr int C = D * ES / 16, RPL = 256 / C, NLD = RPL > 32 ? 1 : 32 / RPL;      // rows that one load of the workgroup covers (64 at d = 64, e4m3: every row twice)
     constexpr int OPB = D * 2 + 16;
     static_assert(4 * 32 * OPB <= 4 * TILE && RT * MP * 4 <= 4 * TILE, "sums and results pass through the tiles' place");
 
@@ -724,65 +763,89 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[dt][i] = 0.f;
 
-    const int lrow = tid / C, lc = tid % C;
-    const bool loads = lrow < 32;
+    const int lrow = tid / C & 31, lc = tid % C;
     const unsigned char* kb = (const unsigned char*)p.k + (int64_t)wk.kvh * p.sh * ES;
     const unsigned char* vb = (const unsigned char*)p.v + (int64_t)wk.kvh * p.sh * ES;
     const uint32_t off = (uint32_t)((lrow & 15) * (int)p.st * ES + lc * 16);      // (a load covers 16 rows or 32)
     u32x4 kr[PF][NLD], vr[PF][NLD];
-    bool there[4][2];                       // of the tiles in flight and the one at work: tile t's are there[t % 4]
-    auto fetch = [&](int slot, int flag, int t) {
-        int64_t base[2];
+    int64_t base[2] = {0, 0};               // of the two halves of the newest tile that was looked up
+    uint32_t here = 0;                      // whether its pages exist, two bits; those of the tiles before it in the bits above
+    auto look = [&](int t) {
+        uint32_t both = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) there[flag][h] = pages.half(p, t, h, base[h]);
-        if (loads) {
-#pragma unroll
-            for (int q = 0; q < NLD; ++q) {
-                const int64_t where = (NLD == 1 ? (lrow < 16 ? base[0] : base[1]) : base[q]) + off;
-                kr[slot][q] = load16<false>(kb + where);
-                vr[slot][q] = load16<false>(vb + where);
-            }
-        }
+        for (int h = 0; h < 2; ++h) both |= (uint32_t)pages.half(t, h, base[h]) << h;
+        here = here << 2 | both;
     };
-    auto store = [&](int slot, int flag, int t) {
-        if (!loads) return;
-        unsigned char* Kl = smem + (t & 1) * TILE;
-        unsigned char* Vl = Kl + 32 * KP;
+    auto fetch = [&](u32x4 (&to)[NLD], const unsigned char* from) {
+#pragma unroll
+        for (int q = 0; q < NLD; ++q) to[q] = load16<false>(from + (NLD == 1 ? (lrow < 16 ? base[0] : base[1]) : base[q]) + off);
+    };
+    auto store_k = [&](int slot, int buffer) {
+#pragma unroll
+        for (int q = 0; q < NLD; ++q) stage16<F8>(smem + buffer * TILE + (q * RPL + lrow) * KP + lc * 16 * (2 / ES), kr[slot][q]);
+    };
+    auto store_v = [&](int slot, int buffer, int t, uint32_t both) {
         const int key0 = (wk.t0 + 2 * t + wg) * 32;
-        const bool whole = key0 + 32 <= wk.seen && there[flag][0] && there[flag][1];
+        const bool whole = key0 + 32 <= wk.seen && both == 3;
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
             const int row = q * RPL + lrow;
             u32x4 v = vr[slot][q];
-            if (!whole && !(key0 + row < wk.seen && (row < 16 ? there[flag][0] : there[flag][1]))) v = u32x4{0, 0, 0, 0};
-            stage16<F8>(Kl + row * KP + lc * 16 * (2 / ES), kr[slot][q]);
-            stage16<F8>(Vl + row * VP + lc * 16 * (2 / ES), v);
+            if (!whole && !(key0 + row < wk.seen && (both >> (row < 16 ? 0 : 1) & 1))) v = u32x4{0, 0, 0, 0};
+            stage16<F8>(smem + buffer * TILE + 32 * KP + row * VP + lc * 16 * (2 / ES), v);
         }
     };
     const int Tn = (wk.Tn - wg + 1) / 2, steps = (wk.Tn + 1) / 2;     // tiles of this key group, and of the other one if it has more
-    if (Tn > 0) {
+    f32x16 S;
+    if (steps > 0) {
+        // What is requested and stored behind the last tile is the last tile again and nobody's: without conditions around them the compiler knows how many
+        // loads are in flight and waits for the oldest only.  (A second group without any tile has its first one, behind the end.)
+        const int ends = max(Tn, 1) - 1;
         pages.begin(p, Tn);
-        fetch(0, 0, 0);
-        if (Tn > 1) fetch(1, 1, 1);
-        store(0, 0, 0);
-        if (Tn > 2) fetch(0, 2, 2);
-    }
-    __syncthreads();
-    for (int t4 = 0; t4 < steps; t4 += 4) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int t = t4 + u;
-            if (t >= steps) break;          // (uniform)
-            if (t + 1 < Tn) {
-                store((u + 1) % PF, (u + 1) % 4, t + 1);
-                if (t + 3 < Tn) {
-                    pages.advance(p, t + 3, Tn);
-                    fetch((u + 1) % PF, (u + 3) % 4, t + 3);
+        for (int t = 0; t < 4; ++t) {
+            if (t == 2) {
+                store_k(0, 0);
+                store_v(0, 0, 0, here >> 2 & 3);
+                store_k(1, 1);
+            }
+            look(min(t, ends));
+            fetch(kr[t & 1], kb);
+            asm volatile("" ::: "memory");          // (in this order, as in the steps)
+            if (t < 3) fetch(vr[t & 1], vb);
+            asm volatile("" ::: "memory");
+        }
+        __syncthreads();
+        S = scores32<D, KP>(smem, qf, lane);
+        __syncthreads();
+        auto step = [&](int t, auto parity) {
+            constexpr int u = decltype(parity)::value;         // t % 2
+            store_k(u, u);
+            store_v(1 - u, 1 - u, t + 1, here >> 4 & 3);
+            fetch(vr[1 - u], vb);
+            if (t + 4 < Tn) pages.advance(p, t + 4, Tn);
+            look(min(t + 4, ends));
+            fetch(kr[u], kb);
+            if (mine && t < Tn) {
+                const float m_use = lead32<D>(S, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, here >> 8 & 1, here >> 9 & 1, scale_log2, run, O, lane);
+                bf16x8 pf[2];
+                if constexpr (D == 128) {
+                    const f32x16 next = scores32<D, KP>(smem + (1 - u) * TILE, qf, lane);
+                    weights32(S, scale_log2, m_use, run, pf);
+                    values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
+                    S = next;
+                } else {                        // (four wavefronts a SIMD overlap by themselves if their registers, 128 each, suffice)
+                    weights32(S, scale_log2, m_use, run, pf);
+                    __builtin_amdgcn_sched_barrier(0);
+                    values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
+                    S = scores32<D, KP>(smem + (1 - u) * TILE, qf, lane);
                 }
             }
-            const unsigned char* Kl = smem + (t & 1) * TILE;
-            if (mine && t < Tn) tile32<D, KP, VP>(Kl, Kl + 32 * KP, qf, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, there[u][0], there[u][1], scale_log2, run, O, lane);
             __syncthreads();
+        };
+        for (int t = 0; t < steps; t += 2) {    // (an odd number of steps: one more with nothing to multiply; an exit between the two would hide what is in flight)
+            step(t, Const<0>());
+            step(t + 1, Const<1>());
         }
     }
     // the second key group hands its sums to the first, lane for lane
@@ -855,7 +918,7 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
 }
 
 template <int D, bool F8, bool BC, bool EVEN>
-__global__ __launch_bounds__(512, 1) void paged_tall_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(512, D == 64 && !EVEN ? 4 : 2) void paged_tall_kernel(PagedAttnParams p) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[tall_smem(D)];
     fetch_args<sizeof(PagedAttnParams)>();
     run_rows<128, BC, EVEN, F8 ? 1 : 2, 2>(p, smem, [&](const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_tall_rows<D, F8, BC>(p, wk, pages, smem); });
@@ -947,10 +1010,10 @@ struct PagedPlan {
 //                  with shares, of 2048 - 4096 134 / 142, of 100 - 16000 371 / 316; 8 sequences of 500 - 2000, 28/4 heads 22 / 17; one of 65536 579 / 50.
 //   above:         a tile of 32 rows takes 0.28 (d = 64: 0.19) in a chain of its own and 0.29 (0.16) of a CU, with shares what its bytes take the chip (8-bit entries
 //                  count as 12 bits), one of 128 rows 0.56 (0.44) and 0.78 (0.44), with shares 0.9 (0.53).  Over 998 calls of equal lengths (33 - 896 rows,
-//                  1 - 64 sequences of 300 - 12000 tokens) the choice takes 1.4 % longer than the best of the four in the mean, at most 34 % (up to 256 tiles).
-//                  32 rows of 28/4 heads, 32 rows / 128 / with shares 32 / 128: 8 sequences of 1000 tokens 17 / 27 / 36 / 26, of 4000 44 / 78 / 82 / 50, of 12000
-//                  121 / 221 / 220 / 98; 32 sequences of 1000 43 / 31 / 89 / 41.
-//   causal masks:  row groups see half of the new tokens' keys in the middle, which shares do not know (one prompt of 8192 tokens, 28/4 heads: 680 / with shares 1217).
+//                  1 - 64 sequences of 300 - 12000 tokens) the choice takes 1.2 % longer than the best of the four in the mean, at most 35 %.
+//                  32 rows of 28/4 heads, 32 rows / 128 / with shares 32 / 128: 8 sequences of 1000 tokens 17 / 26 / 36 / 27, of 4000 43 / 72 / 84 / 50, of 12000
+//                  124 / 198 / 218 / 95; 32 sequences of 1000 43 / 30 / 88 / 40.
+//   causal masks:  row groups see half of the new tokens' keys in the middle, which shares do not know (one prompt of 8192 tokens, 28/4 heads, blocks of 32: 640 / with shares 1088).
 static PagedPlan plan_paged(const dlm_paged_attn_args* a) {
     static const int shape_rows[5] = {0, 16, 32, 128, 16};
     PagedPlan pl = {};
