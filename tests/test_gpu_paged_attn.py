@@ -291,3 +291,78 @@ def test_pages_past_32_bits_of_offset():
     c.pages = pages
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("bs", [0, 1, 32])
+def test_whole_prompts(bs):
+    """As many queries as keys, and more or fewer of them: many row groups a sequence, the later ones with more keys."""
+    mask = dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=bs) if bs else {}
+    for Hq, Hkv, d, e4m3 in ((7, 1, 64, False), (2, 1, 128, False), (2, 2, 128, True)):
+        c = Case([401, 90, 400, 800], 400, Hq, Hkv, d, 32, e4m3, q_len=[400, 90, 33, 399])
+        c.run(**mask)
+        c.check(**mask)
+
+
+@pytest.mark.parametrize("shape", [0, 2, 3])
+def test_pages_that_sequences_share(options, shape):
+    """A common beginning in the same pages, a page twice in one sequence, two sequences of the same pages throughout."""
+    options("paged_shape", shape)
+    c = Case([500, 300, 300, 64], 3, 8, 2, 64, 32)
+    t = c.table
+    t[1, :5] = t[0, :5]
+    t[2] = t[1]
+    t[3, 1] = t[3, 0]
+    for mask in ({}, dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=1)):
+        c.run(**mask)
+        c.check(**mask)
+
+
+@pytest.mark.parametrize("shape", [2, 3])
+def test_two_calls_at_once(options, shape):
+    """Two streams, a workspace each: what each gives alone."""
+    options("paged_shape", shape)
+    options("paged_shares", 300)
+    a, b = Case([6000, 100], 4, 8, 2, 64, 64, seed=1), Case([300, 5000, 2000], 8, 4, 4, 128, 16, seed=2)
+    want = []
+    for c in (a, b):
+        assert c.run() > 0
+        want.append((c.out.clone(), c.lse.clone()))
+    spaces, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for c in (a, b):
+        given = (c.q, c.out, *c.pages, c.table, c.lens)
+        spaces.append(torch.empty(dlm.paged_attn_workspace_bytes(*given, lse=c.lse), dtype=torch.uint8, device=DEV))
+        c.out.zero_(), c.lse.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, ws, s in zip((a, b), spaces, streams):
+            with torch.cuda.stream(s):
+                dlm.paged_attn(c.q, c.out, *c.pages, c.table, c.lens, lse=c.lse, workspace=ws)
+    torch.cuda.synchronize()
+    for c, (out, lse) in zip((a, b), want):
+        assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+
+
+@pytest.mark.parametrize("shape", [2, 3])
+def test_captured_and_replayed(options, shape):
+    """Shares in a graph: replays with other lengths, numbers of rows and pages, eager calls in between."""
+    options("paged_shape", shape)
+    options("paged_shares", 64)
+    c = Case([900, 2000, 40], 5, 8, 2, 128, 32, q_len=[5, 5, 5])
+    given, how = (c.q, c.out, *c.pages, c.table, c.lens), dict(q_len=c.q_len, lse=c.lse)
+    ws = torch.empty(dlm.paged_attn_workspace_bytes(*given, **how), dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dlm.paged_attn(*given, workspace=ws, **how)
+    for lens, rows in (([900, 2000, 40], [5, 5, 5]), ([2000, 0, 1], [1, 0, 5]), ([33, 32, 31], [0, 0, 0]), ([1, 2000, 1999], [5, 3, 4])):
+        c.lens.copy_(torch.tensor(lens, dtype=I32)), c.q_len.copy_(torch.tensor(rows, dtype=I32))
+        c.table.clamp_(min=0)
+        c.out.fill_(7.0), c.lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.lengths = lens
+        c.check()
+        got = c.out.clone(), c.lse.clone()
+        c.out.fill_(7.0), c.lse.fill_(7.0)
+        c.run()
+        assert torch.equal(c.out, got[0]) and torch.equal(c.lse, got[1])
