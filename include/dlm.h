@@ -533,7 +533,7 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it the keys of all sequences are dealt out evenly to the
  * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
  * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,
- * a call runs one workgroup for each sequence and KV head; results then differ by the rounding of another summation order only.
+ * a call runs one workgroup for each sequence, KV head and group of rows; results then differ by the rounding of another summation order only.
  * Values that a row does not see have to be finite where another query row of its sequence sees them (they are multiplied by zero).
  * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8; stride_t of the cache below 2^26. */
 typedef struct dlm_paged_attn_args {
