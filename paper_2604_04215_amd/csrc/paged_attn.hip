@@ -310,7 +310,8 @@ struct Running {
     float m, l;
     // mx: largest score of the tile in log2 units.  Returns the factor for what has been summed up; m_use: what to subtract.
     __device__ __forceinline__ float follow(float mx, float& m_use) {
-        const bool grow = mx > m + 8.0f;
+#pragma clang fp contract(off)
+        const bool grow = mx - m > 8.0f;                 // (a difference: exact where mx and m are so large that m + 8 would be rounded)
         const float m_new = grow ? mx : m;
         m_use = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = grow ? fast_exp2(m - m_use) : 1.0f;
@@ -318,6 +319,20 @@ struct Running {
         return alpha;
     }
 };
+
+// exp2(S factor - m_use) is one fused operation an entry, with the product unrounded while m_use is rounded: from 2^30 on they may lie so far apart that the
+// row's largest p is 0 or infinite.  From 2^20 on the product is rounded as m_use was, and S becomes the exponent itself.
+constexpr float FAR = 0x1p20f;
+template <int N, typename V>
+__device__ __forceinline__ void far_scores(V& S, float& factor, float& m_use) {
+#pragma clang fp contract(off)
+    if (__any(__builtin_fabsf(m_use) >= FAR)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) S[i] = S[i] * factor - m_use;
+        factor = 1.0f;
+        m_use = 0.f;
+    }
+}
 
 // scores of keys that the lane's row does not see; entry i of S is key at + STEP * (i / 4) + i % 4, entries from N/2 on lie in the second half
 template <int N, int STEP, typename V>
@@ -340,32 +355,33 @@ __device__ __forceinline__ f32x16 scores32(const unsigned char* Kl, const bf16x8
         S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Kl + n * KP + 32 * c + 16 * (F8 && c >= 4 ? 1 - hi : hi)), qf[c], S, 0, 0, 0);
     return S;
 }
-// masks and the running maximum; returns what exponentials are relative to
+// Masks and the running maximum; returns what exponentials are relative to.  factor: from scores to log2 units
 template <int D>
-__device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limit_min, bool here0, bool here1, float scale_log2, Running& run,
+__device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limit_min, bool here0, bool here1, float& factor, Running& run,
                                         f32x16 (&O)[D / 32], int lane) {
     if (key0 + 32 > limit_min || !here0 || !here1) hide<16, 8>(S, key0 + 4 * (lane >> 5), limit, here0, here1);
     float mx = -INFINITY, m_use;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, S[i]), S[i + 1]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2, m_use);
-    if (__any(alpha != 1.0f)) {
+    const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * factor, m_use);
+    if (__any(alpha != 1.0f || __builtin_fabsf(m_use) >= FAR)) {
         run.l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[dt][i] *= alpha;
+        far_scores<16>(S, factor, m_use);
     }
     return m_use;
 }
 // probabilities, and their sum
-__device__ __forceinline__ void weights32(const f32x16& S, float scale_log2, float m_use, Running& run, bf16x8 (&pf)[2]) {
+__device__ __forceinline__ void weights32(const f32x16& S, float factor, float m_use, Running& run, bf16x8 (&pf)[2]) {
     float rs = 0.f;
     uint32_t pk[8];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
+        const float p0 = fast_exp2(fmaf(S[i], factor, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], factor, -m_use));
         rs += p0 + p1;
         pk[i >> 1] = pack_bf16x2(p0, p1);
     }
@@ -566,19 +582,21 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
         mx = __builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
         sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         const float alpha = run.follow(__builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2, m_use);
-        u32x4 pk;
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float p0 = fast_exp2(fmaf(S[i], scale_log2, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], scale_log2, -m_use));
-            rs += p0 + p1;
-            pk[i >> 1] = pack_bf16x2(p0, p1);
-        }
-        if (__any(alpha != 1.0f)) {
+        float factor = scale_log2;
+        if (__any(alpha != 1.0f || __builtin_fabsf(m_use) >= FAR)) {
             run.l *= alpha;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) O[dt][i] *= alpha;
+            far_scores<8>(S, factor, m_use);
+        }
+        u32x4 pk;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float p0 = fast_exp2(fmaf(S[i], factor, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], factor, -m_use));
+            rs += p0 + p1;
+            pk[i >> 1] = pack_bf16x2(p0, p1);
         }
         run.l += rs;
         const unsigned char* vbase = Vl + (4 * q4 + (n >> 2)) * VP + 8 * (n & 3);
@@ -696,9 +714,10 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
             fetch(j + 1);
         }
         f32x16 S = scores32<D, F8, KP>(Kl, qf, lane);
-        const float m_use = lead32<D>(S, key0, limit, limit_min, here0, here1, scale_log2, run, O, lane);
+        float factor = scale_log2;
+        const float m_use = lead32<D>(S, key0, limit, limit_min, here0, here1, factor, run, O, lane);
         bf16x8 pf[2];
-        weights32(S, scale_log2, m_use, run, pf);
+        weights32(S, factor, m_use, run, pf);
         values32<D, F8, VP>(Vl, pf, O, lane);
     }
     float* mb = reinterpret_cast<float*>(smem);
@@ -834,15 +853,16 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
             look(min(t + 4, ends));
             fetch(kr[u], kb);
             if (mine && t < Tn) {
-                const float m_use = lead32<D>(S, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, here >> 8 & 1, here >> 9 & 1, scale_log2, run, O, lane);
+                float factor = scale_log2;
+                const float m_use = lead32<D>(S, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, here >> 8 & 1, here >> 9 & 1, factor, run, O, lane);
                 bf16x8 pf[2];
                 if constexpr (D == 128) {
                     const f32x16 next = scores32<D, F8, KP>(smem + (1 - u) * TILE, qf, lane);
-                    weights32(S, scale_log2, m_use, run, pf);
+                    weights32(S, factor, m_use, run, pf);
                     values32<D, F8, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
                     S = next;
                 } else {                        // (four wavefronts a SIMD overlap by themselves if their registers, 128 each, suffice)
-                    weights32(S, scale_log2, m_use, run, pf);
+                    weights32(S, factor, m_use, run, pf);
                     __builtin_amdgcn_sched_barrier(0);
                     values32<D, F8, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
                     S = scores32<D, F8, KP>(smem + (1 - u) * TILE, qf, lane);
