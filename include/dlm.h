@@ -528,8 +528,9 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  *   mask_mode    DLM_MASK_FULL: every row sees all kv_len keys.  DLM_MASK_BLOCK_CAUSAL: row i stands at position
  *                kv_len - q_len + i and sees the keys whose position / block_size is at most its own (block_size 1: causal)
  *   scale        <= 0 selects 1/sqrt(d)
- * A row that sees no key, or only scores of -inf, gets out = 0 and lse = -inf.  Arithmetic as dlm_block_attn; e4m3 entries are exact in bf16, their scales
- * are applied in fp32.
+ * A row that sees no key, or only scores of -inf, gets out = 0 and lse = -inf.  Arithmetic as dlm_block_attn, but that probabilities keep more than 8 bits for
+ * the product with V: 15 up to 32 rows (Lq * Hq / Hkv) and a bf16 cache, 11 with an e4m3 cache.  e4m3 entries are exact in 16 bits, their scales are applied in
+ * fp32.
  * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it the keys of all sequences are dealt out evenly to the
  * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
  * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,

@@ -7,9 +7,8 @@
 //   paged_wide_kernel   32 rows, keys split over the wavefronts (single tokens, small blocks): bound by HBM
 //   paged_tall_kernel   128 rows, 32 a wavefront, which share the tiles of keys in LDS (blocks with many heads a KV head): bound by the products
 //                       and what stands between them
-// Per 32-key tile: S^T = K Q^T (a lane then has 8 or 16 keys of one row: maximum and sum are in-lane but for one or two swaps), p rounded to bf16
-// for the second product (its relative error 2^-9 an entry averages out; the sum uses the unrounded p), O^T += V^T P^T with V^T from the
-// transposing LDS read.  Everything else is fp32.
+// Per 32-key tile: S^T = K Q^T (a lane then has 8 or 16 keys of one row: maximum and sum are in-lane but for one or two swaps), O^T += V^T P^T with V^T from
+// the transposing LDS read.  The second product takes 16-bit operands too, so p is rounded for it (never for the sum): see Weights.  Everything else is fp32.
 #include "paged.hpp"
 
 namespace dlm {
@@ -17,6 +16,7 @@ namespace dlm {
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 
 struct PagedAttnParams {
     int B, Lq, Hq, Hkv, g;
@@ -54,13 +54,27 @@ __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) {
 }
 __device__ __forceinline__ int clamped(int v, int hi) { return min(max(v, 0), hi); }
 
-// eight e4m3 entries as bf16 (exact: bf16 has more of both exponent and mantissa)
+__device__ __forceinline__ f16x8 as_f16x8(u32x4 v) {
+    union { u32x4 u; f16x8 h; } x;
+    x.u = v;
+    return x.h;
+}
+
+// eight e4m3 entries as bf16 or fp16 (exact: both have more exponents, 2^-9 .. 448 are normal numbers, and more mantissa)
+template <bool HALF>
 __device__ __forceinline__ u32x4 widen_e4m3(uint32_t lo, uint32_t hi) {
     auto pair = [](uint32_t w, bool upper) {
-        union { __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 b; uint32_t u; } x;
-        if (upper) x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-        else x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-        return x.u;
+        if constexpr (HALF) {
+            union { __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 h; uint32_t u; } x;
+            if (upper) x.h = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
+            else x.h = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+            return x.u;
+        } else {
+            union { __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 b; uint32_t u; } x;
+            if (upper) x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+            else x.b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+            return x.u;
+        }
     };
     return u32x4{pair(lo, false), pair(lo, true), pair(hi, false), pair(hi, true)};
 }
@@ -290,12 +304,13 @@ __device__ __forceinline__ u32x4 load16(const unsigned char* a) {
     return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a)) : *reinterpret_cast<const u32x4*>(a);
 }
 
-// 16 bytes of cache into LDS as bf16, 16 or 32 bytes from base + off on; an off with bit 4 set: the 16-byte halves of the 32 change places
-template <bool F8>
+// 16 bytes of cache into LDS as bf16 (8-bit values, HALF: as fp16), 16 or 32 bytes from base + off on; an off with bit 4 set: the 16-byte halves of the 32
+// change places
+template <bool F8, bool HALF>
 __device__ __forceinline__ void stage16(unsigned char* base, uint32_t off, u32x4 v) {
     if constexpr (F8) {
-        *reinterpret_cast<u32x4*>(base + off) = widen_e4m3(v[0], v[1]);
-        *reinterpret_cast<u32x4*>(base + (off ^ 16)) = widen_e4m3(v[2], v[3]);
+        *reinterpret_cast<u32x4*>(base + off) = widen_e4m3<HALF>(v[0], v[1]);
+        *reinterpret_cast<u32x4*>(base + (off ^ 16)) = widen_e4m3<HALF>(v[2], v[3]);
     } else *reinterpret_cast<u32x4*>(base + off) = v;
 }
 
@@ -304,15 +319,18 @@ __device__ __forceinline__ void stage16(unsigned char* base, uint32_t off, u32x4
 template <bool F8>
 __device__ __forceinline__ constexpr uint32_t turned(uint32_t off) { return F8 ? off ^ (off >> 3 & 16) : off; }
 
-// The maximum that exponentials are relative to follows the running one only when that has grown by 2^8 (p stays in range of bf16 and of the
-// sums): the accumulators are rescaled a few times a row instead of at every tile.
+// The maximum that exponentials are relative to follows the running one only when that has grown by 2^8 (p stays in range of its type and of the
+// sums): the accumulators are rescaled a few times a row instead of at every tile.  With an 8-bit cache it lies 2^7 below the largest score, which
+// leaves small p more of fp16's range: p is at most 2^15 and loses bits of its 11 below 2^-14, that is 2^-21 times the row's largest.
+template <bool F8>
 struct Running {
+    static constexpr float LIFT = F8 ? 7.0f : 0.0f;
     float m, l;
     // mx: largest score of the tile in log2 units.  Returns the factor for what has been summed up; m_use: what to subtract.
     __device__ __forceinline__ float follow(float mx, float& m_use) {
 #pragma clang fp contract(off)
-        const bool grow = mx - m > 8.0f;                 // (a difference: exact where mx and m are so large that m + 8 would be rounded)
-        const float m_new = grow ? mx : m;
+        const bool grow = mx - m > 8.0f + LIFT;          // (a difference: exact where mx and m are so large that m + 8 would be rounded)
+        const float m_new = grow ? mx - LIFT : m;
         m_use = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = grow ? fast_exp2(m - m_use) : 1.0f;
         m = m_new;
@@ -356,8 +374,8 @@ __device__ __forceinline__ f32x16 scores32(const unsigned char* Kl, const bf16x8
     return S;
 }
 // Masks and the running maximum; returns what exponentials are relative to.  factor: from scores to log2 units
-template <int D>
-__device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limit_min, bool here0, bool here1, float& factor, Running& run,
+template <int D, bool F8>
+__device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limit_min, bool here0, bool here1, float& factor, Running<F8>& run,
                                         f32x16 (&O)[D / 32], int lane) {
     if (key0 + 32 > limit_min || !here0 || !here1) hide<16, 8>(S, key0 + 4 * (lane >> 5), limit, here0, here1);
     float mx = -INFINITY, m_use;
@@ -375,34 +393,64 @@ __device__ __forceinline__ float lead32(f32x16& S, int key0, int limit, int limi
     }
     return m_use;
 }
+// How probabilities go into the second product, whose operands have 16 bits:
+//   FP16  8-bit caches: fp16, in which the values are exact; each p within 2^-11, as many products
+//   BOTH  up to 32 rows: the upper half of p's bits and the nearest bf16 of what they leave, twice the products; each p within 2^-15.  Neither is negative and the
+//         second is not zero where p is not (2^-23 of p more see to it), so an infinite value stays what it is.
+//   BF16  above 32 rows: bf16, each p within 2^-8, as in dlm_block_attn
+// The result's error against 64 bits, relative to its norm, is 0.0016 - 0.0017 with FP16 and BOTH, which is its own rounding, and 0.0022 - 0.0023 with BF16.  BOTH
+// costs 0 - 2 % where memory bounds, but above 32 rows, where the products do, 8 - 31 % (32 sequences of 1000 tokens, 32 rows of 28/4 heads 28.1 -> 33.3 us; 4 prompts of 4096
+// tokens, 32/8 heads 1299 -> 1605; 16384 causal ones of 14/2 heads of 64 609 -> 798).
+enum { BF16, BOTH, FP16 };
+template <int KIND, int N>
+struct Weights {
+    uint32_t hi[N / 2], lo[KIND == BOTH ? N / 2 : 1];
+    __device__ __forceinline__ void set(int i, float p0, float p1) {        // entries 2i, 2i + 1
+        if constexpr (KIND == FP16) {
+            union { __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 h; uint32_t u; } x;
+            x.h[0] = (_Float16)p0;
+            x.h[1] = (_Float16)p1;
+            hi[i] = x.u;
+        } else if constexpr (KIND == BOTH) {
+            auto left = [](float p) { return fmaf(p, 1.0f + 0x1p-23f, -__uint_as_float(__float_as_uint(p) & 0xffff0000u)); };
+            hi[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+            lo[i] = pack_bf16x2(left(p0), left(p1));
+        } else hi[i] = pack_bf16x2(p0, p1);
+    }
+    // entries 8k .. 8k + 7
+    __device__ __forceinline__ u32x4 upper(int k) const { return u32x4{hi[4 * k], hi[4 * k + 1], hi[4 * k + 2], hi[4 * k + 3]}; }
+    __device__ __forceinline__ u32x4 lower(int k) const { return u32x4{lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]}; }
+};
 // probabilities, and their sum
-__device__ __forceinline__ void weights32(const f32x16& S, float factor, float m_use, Running& run, bf16x8 (&pf)[2]) {
+template <bool F8, int KIND>
+__device__ __forceinline__ void weights32(const f32x16& S, float factor, float m_use, Running<F8>& run, Weights<KIND, 16>& pf) {
     float rs = 0.f;
-    uint32_t pk[8];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
         const float p0 = fast_exp2(fmaf(S[i], factor, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], factor, -m_use));
         rs += p0 + p1;
-        pk[i >> 1] = pack_bf16x2(p0, p1);
+        pf.set(i >> 1, p0, p1);
     }
     run.l += rs;
-    const u32x4 plo = {pk[0], pk[1], pk[2], pk[3]}, phi = {pk[4], pk[5], pk[6], pk[7]};
-    pf[0] = as_bf16x8(plo);
-    pf[1] = as_bf16x8(phi);
 }
 // O^T += V^T P^T
-template <int D, bool F8, int VP>
-__device__ __forceinline__ void values32(const unsigned char* Vl, const bf16x8 (&pf)[2], f32x16 (&O)[D / 32], int lane) {
+template <int D, int VP, int KIND>
+__device__ __forceinline__ void values32(const unsigned char* Vl, const Weights<KIND, 16>& pf, f32x16 (&O)[D / 32], int lane) {
+    constexpr bool F8 = KIND == FP16;
     const int hi = lane >> 5, s16 = lane & 15, blk = (lane >> 4) & 1;
     const unsigned char* vbase = Vl + (4 * hi + (s16 >> 2)) * VP + (16 * blk + 4 * (s16 & 3)) * 2;
     const unsigned char* vturned = Vl + (4 * hi + (s16 >> 2)) * VP + ((16 * blk + 4 * (s16 & 3)) * 2 ^ 16);
 #pragma unroll
     for (int e = 0; e < 2 * (D / 32); ++e) {
-        union { s16x4 h[2]; bf16x8 v; } f;
+        union { s16x4 h[2]; bf16x8 v; f16x8 f; } f;
 #pragma unroll
         for (int q = 0; q < 2; ++q)
             f.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((F8 && e >= 4 ? vturned : vbase) + (16 * (e & 1) + 8 * q) * VP + 32 * (e >> 1) * 2));
-        O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[e & 1], O[e >> 1], 0, 0, 0);
+        if constexpr (KIND == FP16) O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.f, as_f16x8(pf.upper(e & 1)), O[e >> 1], 0, 0, 0);
+        else {
+            if constexpr (KIND == BOTH) O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, as_bf16x8(pf.lower(e & 1)), O[e >> 1], 0, 0, 0);
+            O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, as_bf16x8(pf.upper(e & 1)), O[e >> 1], 0, 0, 0);
+        }
     }
 }
 
@@ -500,7 +548,7 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
     const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
 
     f32x4 O[D / 16];
-    Running run = {-INFINITY, 0.f};
+    Running<F8> run = {-INFINITY, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
@@ -544,8 +592,8 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
         for (int c = 0; c < D / 32; ++c) {
             bf16x8 k0, k1;
             if constexpr (F8) {
-                k0 = as_bf16x8(widen_e4m3(kr[0][c >> 1][2 * (c & 1)], kr[0][c >> 1][2 * (c & 1) + 1]));
-                k1 = as_bf16x8(widen_e4m3(kr[1][c >> 1][2 * (c & 1)], kr[1][c >> 1][2 * (c & 1) + 1]));
+                k0 = as_bf16x8(widen_e4m3<false>(kr[0][c >> 1][2 * (c & 1)], kr[0][c >> 1][2 * (c & 1) + 1]));
+                k1 = as_bf16x8(widen_e4m3<false>(kr[1][c >> 1][2 * (c & 1)], kr[1][c >> 1][2 * (c & 1) + 1]));
             } else {
                 k0 = as_bf16x8(kr[0][c]);
                 k1 = as_bf16x8(kr[1][c]);
@@ -560,7 +608,7 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
             u32x4 v = vr[q];
             // rows behind the end hold anything, NaN too: as values they have to be zeros (as keys their scores are replaced)
             if (!whole && !(key0 + row < wk.seen && (q * RPL < 16 ? here0 : here1))) v = u32x4{0, 0, 0, 0};
-            stage16<F8>(Vl + row * VP, lc * 16 * (2 / ES), v);
+            stage16<F8, true>(Vl + row * VP, lc * 16 * (2 / ES), v);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (j + 1 < J) {
@@ -591,21 +639,25 @@ __device__ __forceinline__ void paged_thin_rows(const PagedAttnParams& p, const 
                 for (int i = 0; i < 4; ++i) O[dt][i] *= alpha;
             far_scores<8>(S, factor, m_use);
         }
-        u32x4 pk;
+        Weights<F8 ? FP16 : BOTH, 8> pf;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const float p0 = fast_exp2(fmaf(S[i], factor, -m_use)), p1 = fast_exp2(fmaf(S[i + 1], factor, -m_use));
             rs += p0 + p1;
-            pk[i >> 1] = pack_bf16x2(p0, p1);
+            pf.set(i >> 1, p0, p1);
         }
         run.l += rs;
         const unsigned char* vbase = Vl + (4 * q4 + (n >> 2)) * VP + 8 * (n & 3);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
-            union { s16x4 h[2]; bf16x8 v; } f;
+            union { s16x4 h[2]; bf16x8 v; f16x8 f; } f;
 #pragma unroll
             for (int q = 0; q < 2; ++q) f.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vbase + 16 * q * VP + 32 * dt));
-            O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, as_bf16x8(pk), O[dt], 0, 0, 0);
+            if constexpr (F8) O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.f, as_f16x8(pf.upper(0)), O[dt], 0, 0, 0);
+            else {
+                O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, as_bf16x8(pf.lower(0)), O[dt], 0, 0, 0);
+                O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, as_bf16x8(pf.upper(0)), O[dt], 0, 0, 0);
+            }
         }
     }
     float* mb = reinterpret_cast<float*>(smem);
@@ -633,7 +685,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_thin_kernel(PagedAttnParams 
 // ---- 32 rows ------------------------------------------------------------------------------------------------
 // Four wavefronts take every fourth tile, each with a place of its own in LDS (no barriers before the join) and the next tile in flight in registers; two workgroups
 // a CU.  Bound by HBM: 64 sequences of 4096 tokens, 32/8 heads of 128: 167 us, 6.4 TB/s (8-bit cache 91, 5.9); one of 65536 with shares 44 + 4.6 for the joins.
-template <int D, bool F8, bool BC, bool NT>
+// ONE: one row group a sequence and KV head, whose keys nobody else reads
+template <int D, bool F8, bool BC, bool ONE>
 __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
     constexpr int NW = 4, RT = 32;
     constexpr int KP = D * 2 + 16;          // pitch of a K row in LDS: 16-byte reads of 16 rows hit distinct banks
@@ -658,7 +711,7 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
     const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
 
     f32x16 O[D / 32];
-    Running run = {-INFINITY, 0.f};
+    Running<F8> run = {-INFINITY, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -686,8 +739,8 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
         }
 #pragma unroll
         for (int q = 0; q < NLD; ++q) {
-            kr[q] = load16<NT>(ks[q * RPL / 16] + off[q]);
-            vr[q] = load16<NT>(vs[q * RPL / 16] + off[q]);
+            kr[q] = load16<ONE>(ks[q * RPL / 16] + off[q]);
+            vr[q] = load16<ONE>(vs[q * RPL / 16] + off[q]);
         }
     };
     const int J = (wk.Tn - w + NW - 1) / NW;        // tiles of this wavefront
@@ -705,8 +758,8 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
             u32x4 v = vr[q];
             // rows behind the end hold anything, NaN too: as values they have to be zeros (as keys their scores are replaced)
             if (!whole && !(key0 + row < wk.seen && (q * RPL < 16 ? here0 : here1))) v = u32x4{0, 0, 0, 0};
-            stage16<F8>(Kl + row * KP, turned<F8>(lc * 16 * (2 / ES)), kr[q]);
-            stage16<F8>(Vl + row * VP, turned<F8>(lc * 16 * (2 / ES)), v);
+            stage16<F8, false>(Kl + row * KP, turned<F8>(lc * 16 * (2 / ES)), kr[q]);
+            stage16<F8, true>(Vl + row * VP, turned<F8>(lc * 16 * (2 / ES)), v);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (j + 1 < J) {
@@ -715,10 +768,10 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
         }
         f32x16 S = scores32<D, F8, KP>(Kl, qf, lane);
         float factor = scale_log2;
-        const float m_use = lead32<D>(S, key0, limit, limit_min, here0, here1, factor, run, O, lane);
-        bf16x8 pf[2];
+        const float m_use = lead32<D, F8>(S, key0, limit, limit_min, here0, here1, factor, run, O, lane);
+        Weights<F8 ? FP16 : ONE ? BOTH : BF16, 16> pf;
         weights32(S, factor, m_use, run, pf);
-        values32<D, F8, VP>(Vl, pf, O, lane);
+        values32<D, VP>(Vl, pf, O, lane);
     }
     float* mb = reinterpret_cast<float*>(smem);
     __syncthreads();
@@ -737,11 +790,11 @@ __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const 
     join_rows<D, F8, RT, NW, MP>(p, wk, mb, tid);
 }
 
-template <int D, bool F8, bool BC, bool NT, bool EVEN>
+template <int D, bool F8, bool BC, bool ONE, bool EVEN>
 __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedAttnParams p) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[wide_smem(D)];
     fetch_args<sizeof(PagedAttnParams)>();
-    run_rows<32, BC, EVEN, F8 ? 1 : 2, 4>(p, smem, [&](const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_wide_rows<D, F8, BC, NT>(p, wk, pages, smem); });
+    run_rows<32, BC, EVEN, F8 ? 1 : 2, 4>(p, smem, [&](const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages) { paged_wide_rows<D, F8, BC, ONE>(p, wk, pages, smem); });
 }
 
 template <int N>
@@ -783,7 +836,7 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
     const float scale_log2 = F8 && p.k_scale ? p.scale_log2 * p.k_scale[wk.kvh] : p.scale_log2;
 
     f32x16 O[D / 32];
-    Running run = {-INFINITY, 0.f};
+    Running<F8> run = {-INFINITY, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -808,7 +861,7 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
     };
     auto store_k = [&](int slot, int buffer) {
 #pragma unroll
-        for (int q = 0; q < NLD; ++q) stage16<F8>(smem + buffer * TILE + (q * RPL + lrow) * KP, turned<F8>(lc * 16 * (2 / ES)), kr[slot][q]);
+        for (int q = 0; q < NLD; ++q) stage16<F8, false>(smem + buffer * TILE + (q * RPL + lrow) * KP, turned<F8>(lc * 16 * (2 / ES)), kr[slot][q]);
     };
     auto store_v = [&](int slot, int buffer, int t, uint32_t both) {
         const int key0 = (wk.t0 + 2 * t + wg) * 32;
@@ -818,7 +871,7 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
             const int row = q * RPL + lrow;
             u32x4 v = vr[slot][q];
             if (!whole && !(key0 + row < wk.seen && (both >> (row < 16 ? 0 : 1) & 1))) v = u32x4{0, 0, 0, 0};
-            stage16<F8>(smem + buffer * TILE + 32 * KP + row * VP, turned<F8>(lc * 16 * (2 / ES)), v);
+            stage16<F8, true>(smem + buffer * TILE + 32 * KP + row * VP, turned<F8>(lc * 16 * (2 / ES)), v);
         }
     };
     const int Tn = (wk.Tn - wg + 1) / 2, steps = (wk.Tn + 1) / 2;     // tiles of this key group, and of the other one if it has more
@@ -854,17 +907,17 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
             fetch(kr[u], kb);
             if (mine && t < Tn) {
                 float factor = scale_log2;
-                const float m_use = lead32<D>(S, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, here >> 8 & 1, here >> 9 & 1, factor, run, O, lane);
-                bf16x8 pf[2];
+                const float m_use = lead32<D, F8>(S, (wk.t0 + 2 * t + wg) * 32, limit, limit_min, here >> 8 & 1, here >> 9 & 1, factor, run, O, lane);
+                Weights<F8 ? FP16 : BF16, 16> pf;
                 if constexpr (D == 128) {
                     const f32x16 next = scores32<D, F8, KP>(smem + (1 - u) * TILE, qf, lane);
                     weights32(S, factor, m_use, run, pf);
-                    values32<D, F8, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
+                    values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
                     S = next;
                 } else {                        // (four wavefronts a SIMD overlap by themselves if their registers, 128 each, suffice)
                     weights32(S, factor, m_use, run, pf);
                     __builtin_amdgcn_sched_barrier(0);
-                    values32<D, F8, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
+                    values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
                     S = scores32<D, F8, KP>(smem + (1 - u) * TILE, qf, lane);
                 }
             }

@@ -1,5 +1,5 @@
 """Attention over a paged cache, every shape of workgroup, alone and with shares, on inputs that separate right from nearly
-right: huge scores (GPU)."""
+right: probabilities whose roundings add up, huge scores (GPU)."""
 import numpy as np
 import pytest
 import torch
@@ -44,6 +44,36 @@ def fill(c, which, b, rows, values):
     x = c.pages[which].float()
     x.transpose(1, 2)[at[0], at[1], :, :values.shape[-1]] = values.to(DEV).float()[:, None]
     c.pages[which].copy_(x.to(c.pages[which].dtype))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_probabilities_keep_their_bits(form, d, e4m3):
+    """Two kinds of keys whose values nearly cancel, so that what a probability loses is not averaged out: even ones with score 0 and value 1, odd ones with
+    score -m / 8 in head m and value -x in column x.  Every score is exact, so a probability is within e = (4 m / 8 + 8) u of its own.  For the second product it is
+    rounded, bf16: to 2^-15 of itself (two bf16 of it: half of its bits, and the nearest of what they leave, which is under 2^-7), with 128 rows a workgroup to 2^-8; 8-bit cache: to 2^-11
+    or 2^-32 of the row's largest (fp16 of 128 times it or more)."""
+    lens = [40] if form[0] in (1, 4) else [900, 64]
+    c = Case(lens, 3, 16, 2, d, 16, e4m3)
+    m = torch.arange(16, device=DEV) % 8 + 1.0 + torch.arange(16, device=DEV) // 8 * 8
+    c.q.zero_()
+    c.q[..., 0] = m
+    x = torch.tensor([(1 + i / 8) * 2 ** k for k in range(3) for i in range(8)])
+    values = -x[torch.arange(d) % len(x)]
+    for b, n in enumerate(lens):
+        odd = (torch.arange(n) % 2)[:, None]
+        fill(c, 0, b, np.arange(n), -odd.expand(n, d).float())
+        fill(c, 1, b, np.arange(n), torch.where(odd == 1, values, torch.ones(d)))
+    if e4m3:
+        c.scales[0].fill_(1.0), c.scales[1].fill_(1.0)
+    run(form, c, scale=0.125)
+    out, lse, mag, _ = heads.paged_attention(wide(c.q), *c.values(), c.table.cpu().numpy(), lens, scale=0.125)
+    e = (4 * m.cpu().numpy() / 8 + 8) * U
+    p = 2.0 ** -11 + max(lens) * 2.0 ** -32 * 7.5 if e4m3 else H if form[0] == 3 else 2.0 ** -15 + 2.0 ** -23
+    bound = (p + 2 * e[None, None, :, None] + 2 * max(lens) * U) * mag * (1 + H) + H * np.abs(out) * (1 + H)
+    err = np.abs(wide(c.out) - out)
+    assert (err <= bound).all(), (err / bound).max()
+    assert (np.abs(wide(c.lse) - lse) <= e[None, :, None] + 2 * max(lens) * U + 4 * U * np.abs(lse)).all()
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
