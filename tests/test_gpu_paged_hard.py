@@ -1,5 +1,5 @@
-"""Attention over a paged cache, every shape of workgroup, alone and with shares, on inputs that separate right from nearly
-right: probabilities whose roundings add up, huge scores (GPU)."""
+"""Attention over a paged cache, every shape of workgroup, alone and with shares, on inputs that separate right from nearly right: probabilities whose
+roundings add up, scores that rise from tile to tile or are huge, absent pages, what is not finite (GPU)."""
 import numpy as np
 import pytest
 import torch
@@ -13,6 +13,7 @@ pytestmark = pytest.mark.gpu
 
 # (paged_shape, paged_shares): 16, 32, 128, 16 rows; 16 rows are never shared out
 FORMS = [(0, 0), (1, 0), (4, 0), (2, -1), (2, 5), (2, 40), (3, -1), (3, 5), (3, 40)]
+CAUSAL = dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=1)
 
 
 @pytest.fixture(params=FORMS, ids=lambda f: "shape%d-shares%d" % f)
@@ -76,6 +77,31 @@ def test_probabilities_keep_their_bits(form, d, e4m3):
     assert (np.abs(wide(c.lse) - lse) <= e[None, :, None] + 2 * max(lens) * U + 4 * U * np.abs(lse)).all()
 
 
+# whole numbers that both types of cache hold
+LEVELS = list(range(-16, 17)) + list(range(18, 33, 2)) + list(range(36, 65, 4))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("Lq", [2, 9])
+def test_scores_that_rise_from_tile_to_tile(form, Lq, e4m3):
+    """Every tile's scores lie 12 above those of the tile before for some rows, below for others, in a random order for a second sequence: what has been summed up is scaled down again and again."""
+    n = 32 * len(LEVELS) - 7
+    c = Case([n, n], Lq, 8, 2, 64, 16, e4m3)
+    if e4m3:
+        c.scales[0].fill_(1.0), c.scales[1].fill_(1.0)
+    for b in range(2):
+        level = torch.tensor(LEVELS, dtype=torch.float32)
+        if b:
+            level = level[torch.from_numpy(c.rng.permutation(len(LEVELS)))]
+        fill(c, 0, b, np.arange(n), torch.stack([level[torch.arange(n) // 32], torch.from_numpy(c.rng.standard_normal(n)).float()], 1))
+    c.q[..., 2:] = 0
+    c.q[..., 1] = 1
+    c.q[..., 0] = torch.tensor([12.0, -12.0, 0.0, 6.0, 12.0, 0.5, -12.0, 12.0], device=DEV)
+    for mask in ({}, CAUSAL):
+        run(form, c, scale=1.0, **mask)
+        c.check(**mask, scale=1.0)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("power", [21, 25, 31, 40, 60])
 def test_huge_scores(form, power, e4m3):
@@ -101,3 +127,107 @@ def test_huge_scores(form, power, e4m3):
         assert (np.abs(got - want) <= (2.0 ** -11 + 2 * n * U + 32 * U) * mag + H * np.abs(want) * (1 + H)).all()
         lse = np.log(len(picked)) + abs(float(q0[h]))
         assert (np.abs(wide(c.lse)[0, h] - lse) <= 8 * U * lse + 2 * n * U).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("page", [16, 64])
+def test_absent_pages_all_over(form, page, e4m3):
+    """A quarter of the pages of long sequences is not there: every parity of tile, either half of one, first and last ones, a sequence without any."""
+    c = Case([1500, 1490, 700, 300], 9, 8, 2, 128, page, e4m3)
+    gone = c.rng.random(c.table.shape) < 0.25
+    gone[0, 0] = gone[0, 1500 // page] = gone[1, 1] = True
+    gone[3] = True
+    lost = torch.from_numpy(np.where(c.rng.random(gone.shape) < 0.5, -1, 1 << 30).astype(np.int32)).to(DEV)
+    c.table.copy_(torch.where(torch.from_numpy(gone).to(DEV), lost, c.table))
+    for mask in ({}, dict(mask_mode=dlm.MASK_BLOCK_CAUSAL, block_size=4)):
+        run(form, c, **mask)
+        c.check(**mask)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_nan_where_nobody_looks(form, e4m3):
+    """NaN in rows behind the end of a sequence, in pages that nobody owns, and in keys that a causal mask hides."""
+    c = Case([1301, 21, 64, 700, 0], 9, 8, 2, 64, 32, e4m3)
+    owned = torch.zeros(c.pages[0].shape[0], 32, dtype=torch.bool, device=DEV)
+    for b, n in enumerate(c.lengths):
+        for t in range(n):
+            owned[where(c, b, t)] = True
+    for x in c.pages:
+        x.view(torch.uint8 if e4m3 else torch.int16).transpose(1, 2)[~owned] = 0x7f if e4m3 else 0x7fc0
+    for mask in ({}, CAUSAL):
+        run(form, c, **mask)
+        c.check(**mask)
+    run(form, c, **CAUSAL)
+    before = c.out.clone(), c.lse.clone()
+    page, row = where(c, 0, 1296)                   # the key of query row 4
+    raw = c.pages[0].view(torch.uint8 if e4m3 else torch.int16)
+    raw[page, 1, row, 7] = 0x7f if e4m3 else 0x7fc0
+    run(form, c, **CAUSAL)
+    assert c.out[0, 4:, 4:].isnan().all() and c.lse[0, 4:, 4:].isnan().all()
+    c.out[0, 4:, 4:], c.lse[0, 4:, 4:] = before[0][0, 4:, 4:], before[1][0, 4:, 4:]
+    assert torch.equal(c.out, before[0]) and torch.equal(c.lse, before[1])
+
+
+def test_what_is_not_finite_stays_where_it_is(form):
+    """NaN in a key reaches every row of its KV head, NaN or an infinity in a value its column only, NaN in a query its row; scores of -inf count as not seen, all of a
+    row's or those of some tiles."""
+    c = Case([1000, 1000, 1000, 1000, 1000], 9, 8, 2, 64, 16)
+    page, row = where(c, 0, 707)
+    c.pages[0][page, 0, row, 3] = float("nan")
+    page, row = where(c, 1, 209)
+    c.pages[1][page, 0, row, 5], c.pages[1][page, 1, row, 6] = float("nan"), float("inf")
+    c.q[2:4, ..., 0] = 1.0
+    for b, hidden in ((2, range(1000)), (3, [*range(0, 40), *range(100, 612), 999])):
+        for t in hidden:
+            page, row = where(c, b, t)
+            c.pages[0][page, :, row, 0] = float("-inf")
+    c.q[4, 3, 2, 9] = float("nan")
+    run(form, c)
+    out, lse = c.out, c.lse
+    assert out[0, :, :4].isnan().all() and lse[0, :4].isnan().all()
+    assert out[1, :, :4, 5].isnan().all() and (out[1, :, 4:, 6] == float("inf")).all()
+    assert (out[2] == 0).all() and (lse[2] == -float("inf")).all()
+    assert out[4, 3, 2].isnan().all() and lse[4, 2, 3].isnan()
+    # the rest as without them
+    clean = Case([1000, 1000, 1000, 1000, 1000], 9, 8, 2, 64, 16)
+    clean.q[2:4, ..., 0] = 1.0
+    clean.q[4, 3, 2, 9] = 0
+    want, want_lse, mag, top = heads.paged_attention(wide(clean.q), *clean.values(), clean.table.cpu().numpy(), clean.lengths)
+    k, v = clean.values()
+    seen = [t for t in range(1000) if not (t < 40 or 100 <= t < 612 or t == 999)]
+    at = [where(c, 3, t) for t in seen]
+    for i in range(9):
+        for h in range(8):
+            s = np.array([k[p, h // 4, r] for p, r in at]) @ wide(clean.q)[3, i, h] / 8
+            p = np.exp(s - s.max())
+            vv = np.array([v[pg, h // 4, r] for pg, r in at])
+            want_lse[3, h, i] = s.max() + np.log(p.sum())
+            want[3, i, h], mag[3, i, h] = p @ vv / p.sum(), p @ np.abs(vv) / p.sum()
+    e = 2 * (64 + 16) * U * top + 8 * U
+    bound = (H + 2 * np.moveaxis(e, 1, 2)[..., None] + 2000 * U) * mag + H * np.abs(want) * (1 + H)
+    fine = np.ones(want.shape, dtype=bool)
+    fine[0, :, :4] = fine[1, :, :4, 5] = fine[1, :, 4:, 6] = fine[2] = fine[4, 3, 2] = False
+    assert (np.abs(wide(out) - want)[fine] <= bound[fine]).all()
+    assert (np.abs(wide(lse) - want_lse)[3] <= e[3] + 2000 * U + 4 * U * np.abs(want_lse[3])).all()
+
+
+def test_shares_are_taken_where_they_are_asked_for():
+    """n workgroups share keys with 32 and 128 rows a workgroup (at least 8 tiles each), never with 16 rows."""
+    c = Case([4000, 3000], 2, 8, 2, 64, 16)
+    given = (c.q, c.out, *c.pages, c.table, c.lens)
+    try:
+        for shape, some in ((1, False), (2, True), (3, True), (4, False)):
+            dlm.set_option("paged_shape", shape)
+            sizes = []
+            for n in (1, 7, 10 ** 4):
+                dlm.set_option("paged_shares", n)
+                sizes.append(dlm.paged_attn_workspace_bytes(*given))
+                c.run()
+                c.check()
+            assert all((s > 0) == some for s in sizes)
+            if some:                                # 125 tiles of 4 row groups: 62 shares at most
+                rows = 32 if shape == 2 else 128
+                assert sizes == [2 * s * rows * 66 * 4 + 2 * 4 * 4 for s in (1, 7, 62)]
+    finally:
+        dlm.set_option("paged_shape", 0)
+        dlm.set_option("paged_shares", 0)
