@@ -535,6 +535,8 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
  * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,
  * a call runs one workgroup for each sequence, KV head and group of rows; results then differ by the rounding of another summation order only.
+ * The size belongs to exactly these arguments: it may rise where B or max_kv_len falls (a small batch is shared out, a large one not).  It is at most
+ * 2^18 (d + 2) + 8 B Hkv ceil(Lq Hq / (32 Hkv)) bytes (34 MB and a little for d = 128), what a program with calls of many sizes allocates.
  * Values that a row does not see have to be finite where another query row of its sequence sees them (they are multiplied by zero).
  * Supported: d in {64, 128}; Hq % Hkv == 0; q / out 16-byte aligned, strides multiples of 8; stride_t of the cache below 2^26. */
 typedef struct dlm_paged_attn_args {

@@ -1158,6 +1158,7 @@ static int validate_paged_attn(const dlm_paged_attn_args* a) {
     if (!a->q || !a->out || !a->kv_len) return fail(DLM_ERR_INVALID_ARG, "%s: null q/out/kv_len", who);
     if (a->max_kv_len > 0 && !a->block_table) return fail(DLM_ERR_INVALID_ARG, "%s: null block_table", who);
     if (!aligned16(a->q) || !aligned16(a->out)) return fail(DLM_ERR_UNSUPPORTED, "%s: q/out not 16-byte aligned", who);
+    if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
     const int64_t n[3] = {a->B, a->Lq, a->Hq}, qs[3] = {a->q_stride_b, a->q_stride_t, a->q_stride_h}, os[3] = {a->o_stride_b, a->o_stride_t, a->o_stride_h};
     for (int i = 0; i < 3; ++i)
         if (n[i] > 1 && (qs[i] % 8 || os[i] % 8)) return fail(DLM_ERR_UNSUPPORTED, "%s: q/out strides must be multiples of 8", who);
@@ -1237,7 +1238,7 @@ extern "C" int dlm_paged_attn(const dlm_paged_attn_args* a, void* stream) {
     p.rows_wg = pl.rows;
     p.row_groups = pl.row_groups;
     p.thin_waves = pl.thin_waves;
-    if (pl.shares && p.max_kv_len > 0 && a->workspace && a->workspace_bytes >= pl.bytes() && aligned16(a->workspace)) {
+    if (pl.shares && p.max_kv_len > 0 && a->workspace && a->workspace_bytes >= pl.bytes()) {
         p.shares = pl.shares;
         p.by_shares = fast_div(pl.shares);
         p.part_o = (float*)a->workspace;
