@@ -531,10 +531,12 @@ int dlm_paged_append(const dlm_append_args *args, void *stream);
  * A row that sees no key, or only scores of -inf, gets out = 0 and lse = -inf.  Arithmetic as dlm_block_attn, but that probabilities keep more than 8 bits for
  * the product with V: 15 up to 32 rows (Lq * Hq / Hkv) and a bf16 cache, 11 with an e4m3 cache.  e4m3 entries are exact in 16 bits, their scales are applied in
  * fp32.
- * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes, 16-byte aligned: with it the keys of all sequences are dealt out evenly to the
- * workgroups, long and short ones alike (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend
- * on the lengths of all sequences of the batch, in rounding only); calls that may overlap need one each.  Without one, or with a smaller one,
- * a call runs one workgroup for each sequence, KV head and group of rows; results then differ by the rounding of another summation order only.
+ * workspace: optional, dlm_paged_attn_workspace_bytes(args) bytes (0: none wanted), 16-byte aligned.  Without one, or with a smaller one, a call runs one workgroup for
+ * each sequence, KV head and group of rows, so that a sequence much longer than the others runs on alone.  With it the keys of all sequences are dealt out evenly to a fixed
+ * number of workgroups (fp32 partial results, joined in a fixed order by a second launch: deterministic; they depend on the lengths of all sequences of the batch, in rounding
+ * only).  Whether they are is decided on the host, which knows no lengths, as if every sequence had max_kv_len tokens: where there are few
+ * sequences for their keys, and whenever max_kv_len is above 8192 (unless the rows of one sequence fill the chip); many sequences under a lower bound are not shared out,
+ * however unequal they are.  Calls that may overlap need a workspace each.  The two ways differ by the rounding of another summation order only.
  * The size belongs to exactly these arguments: it may rise where B or max_kv_len falls (a small batch is shared out, a large one not).  It is at most
  * 2^18 (d + 2) + 8 B Hkv ceil(Lq Hq / (32 Hkv)) bytes (34 MB and a little for d = 128), what a program with calls of many sizes allocates.
  * Values that a row does not see have to be finite where another query row of its sequence sees them (they are multiplied by zero).
@@ -605,8 +607,9 @@ size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
  *                   key range is dispatched first, 4 = the same grouping for the dK / dV passes; 0 = plain
  *                   (tile, KV head, sequence) grids.
  *   "paged_shares"  0 = the library decides whether the keys of a dlm_paged_attn with a workspace are dealt out evenly to a number of workgroups
- *                   whatever the sequences' lengths (default); -1 = one workgroup for each sequence, KV head and group of rows; n >= 1 = n
- *                   workgroups share them (the workspace's size depends on it).
+ *                   (default); -1 = one workgroup for each sequence, KV head and group of rows; n >= 1 = n workgroups share them, or as many as
+ *                   max_kv_len leaves 8 tiles of 32 keys each (none: unshared), and never with 16 rows a workgroup, the library's own choice for short sequences among
+ *                   them (the workspace's size depends on it).
  *   "paged_shape"   0 = the library picks dlm_paged_attn's workgroups from the rows a KV head has (default); 1, 2, 3, 4 = 16, 32, 128, 16
  *                   rows (of 8, 4, 8, 2 wavefronts; the workspace's size depends on it).
  * The knobs exist for tests and tuning sweeps. */

@@ -1,8 +1,8 @@
 // dlm_paged_attn: a block of new tokens, or one, against the pages of its sequence.
 //
 // The g = Hq/Hkv query heads of a KV head and the sequence's query rows are packed into R = g * q_len rows (row = i*g + head), and a workgroup
-// takes some of them, a "row group" of one (sequence, KV head).  With a workspace the 32-key tiles of all row groups are dealt
-// out evenly whatever the lengths (see Shares), and paged_merge_kernel joins what belongs together.  Three shapes, by R (see plan_rows):
+// takes some of them, a "row group" of one (sequence, KV head).  With a workspace the 32-key tiles of all row groups may be dealt
+// out evenly (see Shares), and paged_merge_kernel joins what belongs together.  Three shapes, by R; which, and whether shares, see plan_paged:
 //   paged_thin_kernel   16 rows, keys split over the wavefronts (a few short sequences): bound by latency
 //   paged_wide_kernel   32 rows, keys split over the wavefronts (single tokens, small blocks): bound by HBM
 //   paged_tall_kernel   128 rows, 32 a wavefront, which share the tiles of keys in LDS (blocks with many heads a KV head): bound by the products
@@ -128,7 +128,9 @@ constexpr int SMALLEST_SHARE = 8;           // tiles: two a wavefront
 // Even shares.  The tiles of all row groups, sequence by sequence, KV head by KV head, make one line of N (a row group has at least one, so that somebody
 // writes its zeros; under a block-causal mask each has as many as its sequence's last); with S = max(ceil(N / shares), 8) workgroup w takes tiles
 // [w S, (w + 1) S).  So one long sequence among short ones, or too few sequences for the chip, cost nothing but the joins, and the host need not
-// know the lengths.  A share is the end of one row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began
+// know the lengths.  (What a workgroup keeps of this while it works on a piece is dear: every form with shares spills 34 - 62 scalar registers into vector ones, the
+// 32-row one of d = 128, bf16 and a causal mask two vector registers into scratch; without shares 0 - 4 and none.  With equal lengths, 32 sequences of 1000 tokens, 32 rows of
+// 28/4 heads: 29 us alone, 40 with shares.)  A share is the end of one row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began
 // elsewhere) and 2w + 1.
 template <int RT, bool BC>
 struct Shares {
@@ -806,7 +808,7 @@ struct Const {
 // Two key groups of four wavefronts take every second tile; wavefront w of a group has rows 32 w .. 32 w + 31.  A group's t-th tile sits in its LDS
 // buffer t % 2.  Step t: the scores of tile t + 1 are formed among the exponentials of tile t, then O takes its values; meanwhile K of tile t + 2 and V of
 // tile t + 1 go into the places of K of tile t and V of tile t - 1, and K of tile t + 4 and V of tile t + 3 are requested.  One barrier a step.
-// One workgroup a CU at d = 128 (235 registers), two at d = 64.  A step of two tiles takes 1.1 us (d = 128), of which the matrix units work 0.43, the vector units
+// One workgroup a CU at d = 128 (235 registers), two at d = 64 (125; with shares 159 - 167, one).  A step of two tiles takes 1.1 us (d = 128), of which the matrix units work 0.43, the vector units
 // 0.5 and LDS 0.4: what they overlap is the two wavefronts of a SIMD and the woven products.  4 prompts of 4096 tokens, 32/8 heads, 8-bit cache: 1218 us, 0.9 PFLOP/s.
 template <int D, bool F8, bool BC>
 __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
@@ -914,7 +916,7 @@ __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const 
                     weights32(S, factor, m_use, run, pf);
                     values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
                     S = next;
-                } else {                        // (four wavefronts a SIMD overlap by themselves if their registers, 128 each, suffice)
+                } else {                        // (four wavefronts a SIMD, of 128 registers each, overlap by themselves; with shares there are two, for which this order has not been chosen)
                     weights32(S, factor, m_use, run, pf);
                     __builtin_amdgcn_sched_barrier(0);
                     values32<D, VP>(smem + u * TILE + 32 * KP, pf, O, lane);
@@ -1078,7 +1080,9 @@ struct PagedPlan {
     size_t sums, meta;      // of the workspace: floats of sums and (maximum, sum) pairs, ints behind them
     size_t bytes() const { return shares ? sums * sizeof(float) + meta * sizeof(int32_t) : 0; }
 };
-// T = the longest sequence's tiles; the lengths themselves are not known here.
+// T = the longest sequence's tiles; the lengths themselves are not known here, and every sequence is taken to be as long as max_kv_len.  Where they are not that shows: one
+// token of 64 sequences, 32/8 heads of 128, one of 8192 tokens and 63 of 100 under a bound of 8192: 85 us alone, which is chosen, 28 with shares; 64 of 100 under a bound of
+// 32768: 17 with shares, which are chosen, 9.5 alone.
 // Up to 16 rows: two wavefronts for sequences of a few tiles (T <= 4; 64 sequences of up to 120 tokens, 32/32 heads: 23 us, four wavefronts and 32 rows
 // 27), eight for few row groups whose keys a CU streams quickly (16 sequences of 1100 tokens, 32/8 heads: 15.3 / 16.3, in 8 bits 10 / 16), else
 // 32 rows.  Above 32 rows 32 or 128, one workgroup a row group or even shares, whichever is estimated to take least.  One workgroup a row group costs least
