@@ -21,7 +21,6 @@ MASK_FULL, MASK_BLOCK_CAUSAL = 0, 1
 RULE_THRESHOLD, RULE_TOPK = 0, 1
 CONF_TOKEN_PROB, CONF_MARGIN, CONF_NEG_ENTROPY = 0, 1, 2
 WB_NONE, WB_BLOCK_WHEN_DONE, WB_COMMITTED_ROWS, WB_WHILE_ACTIVE = 0, 1, 2, 3
-KV_BF16, KV_E4M3 = 0, 1
 ROPE_HALVES, ROPE_PAIRS = 0, 1
 
 EXPORTS = ["dlm_block_attn", "dlm_block_attn_workspace_bytes", "dlm_lmhead_confidence",
