@@ -426,7 +426,7 @@ typedef struct dlm_paged_kv {
  *   positions  int32 [T], needed with rope: row of the table for each token.  The rotated entries of a token whose position
  *              is outside [0, rope_len) come out as NaN.
  *   rot_dim    a multiple of 16, at most d
- * All in fp32, rounded once at the end. */
+ * All in fp32, rounded once at the end: the mean overflows for entries from 2^60 on (a head of zeros comes out, gradients likewise). */
 typedef struct dlm_head_map {
     const void *q_weight, *k_weight;
     float eps;

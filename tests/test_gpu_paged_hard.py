@@ -77,6 +77,28 @@ def test_probabilities_keep_their_bits(form, d, e4m3):
     assert (np.abs(wide(c.lse) - lse) <= e[None, :, None] + 2 * max(lens) * U + 4 * U * np.abs(lse)).all()
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_small_probabilities(form, e4m3):
+    """One key of score 0 and value 0 and 20000 of score -18 and value 1: each has 2^-26 of the largest probability, in fp16 a number without its full 11 bits, and their
+    sum decides.  Bound as above: 2^-32 of the largest for each of them, 2 e + 2 n u and the output's rounding of the sum."""
+    n = 20001
+    c = Case([n], 3, 8, 2, 64, 64, e4m3)
+    if e4m3:
+        c.scales[0].fill_(1.0), c.scales[1].fill_(1.0)
+    first, value = torch.full((n, 1), -18.0), torch.ones(n, 64)
+    first[11111], value[11111] = 0, 0
+    fill(c, 0, 0, np.arange(n), first)
+    fill(c, 1, 0, np.arange(n), value)
+    c.q.zero_()
+    c.q[..., 0] = 1
+    run(form, c, scale=1.0)
+    small = 20000 * np.exp(-18.0)
+    want, e = small / (1 + small), (4 * 18 + 8) * U
+    p = n * 2.0 ** -32 if e4m3 else H * want if form[0] == 3 else 2.0 ** -14 * want
+    assert (np.abs(wide(c.out) - want) <= p + (2 * e + 2 * n * U) * want + H * want * (1 + H)).all()
+    assert (np.abs(wide(c.lse) - np.log1p(small)) <= e + 2 * n * U).all()
+
+
 # whole numbers that both types of cache hold
 LEVELS = list(range(-16, 17)) + list(range(18, 33, 2)) + list(range(36, 65, 4))
 
