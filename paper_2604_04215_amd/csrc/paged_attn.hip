@@ -686,7 +686,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_thin_kernel(PagedAttnParams 
 
 // ---- 32 rows ------------------------------------------------------------------------------------------------
 // Four wavefronts take every fourth tile, each with a place of its own in LDS (no barriers before the join) and the next tile in flight in registers; two workgroups
-// a CU.  Bound by HBM: 64 sequences of 4096 tokens, 32/8 heads of 128: 167 us, 6.4 TB/s (8-bit cache 91, 5.9); one of 65536 with shares 44 + 4.6 for the joins.
+// a CU.  Bound by HBM: 64 sequences of 4096 tokens, 32/8 heads of 128: 169 us, 6.3 TB/s (8-bit cache 90, 6.0); one of 65536 with shares 45 + 4.6 for the joins.
 // ONE: one row group a sequence and KV head, whose keys nobody else reads
 template <int D, bool F8, bool BC, bool ONE>
 __device__ __forceinline__ void paged_wide_rows(const PagedAttnParams& p, const Work<32, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
@@ -809,7 +809,7 @@ struct Const {
 // buffer t % 2.  Step t: the scores of tile t + 1 are formed among the exponentials of tile t, then O takes its values; meanwhile K of tile t + 2 and V of
 // tile t + 1 go into the places of K of tile t and V of tile t - 1, and K of tile t + 4 and V of tile t + 3 are requested.  One barrier a step.
 // One workgroup a CU at d = 128 (235 registers), two at d = 64 (125; with shares 159 - 167, one).  A step of two tiles takes 1.1 us (d = 128), of which the matrix units work 0.43, the vector units
-// 0.5 and LDS 0.4: what they overlap is the two wavefronts of a SIMD and the woven products.  4 prompts of 4096 tokens, 32/8 heads, 8-bit cache: 1218 us, 0.9 PFLOP/s.
+// 0.5 and LDS 0.4: what they overlap is the two wavefronts of a SIMD and the woven products.  4 prompts of 4096 tokens, 32/8 heads, 8-bit cache: 1228 us, 0.9 PFLOP/s.
 template <int D, bool F8, bool BC>
 __device__ __forceinline__ void paged_tall_rows(const PagedAttnParams& p, const Work<128, BC>& wk, Pages<F8 ? 1 : 2>& pages, unsigned char* smem) {
     constexpr int RT = 128, PF = 2, MP = D + 4;
