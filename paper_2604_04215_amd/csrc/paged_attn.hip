@@ -127,7 +127,7 @@ constexpr int SMALLEST_SHARE = 8;           // tiles: two a wavefront
 
 // Even shares.  The tiles of all row groups, sequence by sequence, KV head by KV head, make one line of N (a row group has at least one, so that somebody
 // writes its zeros; under a block-causal mask each has as many as its sequence's last); with S = max(ceil(N / shares), 8) workgroup w takes tiles
-// [w S, (w + 1) S).  So one long sequence among short ones, or too few sequences for the chip, cost nothing but the joins, and the host need not
+// [w S, (w + 1) S).  So one long sequence among short ones, or too few sequences for the chip, leave no CU idle, and the host need not
 // know the lengths.  (What a workgroup keeps of this while it works on a piece is dear: every form with shares spills 34 - 62 scalar registers into vector ones, the
 // 32-row one of d = 128, bf16 and a causal mask two vector registers into scratch; without shares 0 - 4 and none.  With equal lengths, 32 sequences of 1000 tokens, 32 rows of
 // 28/4 heads: 29 us alone, 40 with shares.)  A share is the end of one row group, some whole ones, the beginning of another: at most two sets of sums, slots 2w (for rows that began
