@@ -564,6 +564,124 @@ typedef struct dlm_paged_attn_args {
 int dlm_paged_attn(const dlm_paged_attn_args *args, void *stream);
 size_t dlm_paged_attn_workspace_bytes(const dlm_paged_attn_args *args);
 
+/* ------------------------------------------------------------------------- *
+ * Embedding and the norms between layers: with the LM head, the ends of a training step.
+ *
+ * Rows here are bf16, or fp32 where a program keeps its residual stream or its gradients in 32 bits (DLM_ROW_*).  Bases 16-byte aligned, row
+ * strides multiples of 16 bytes, not negative; rows of an output do not overlap.
+ * ------------------------------------------------------------------------- */
+#define DLM_ROW_BF16           0
+#define DLM_ROW_F32            1
+
+/* dlm_embed -- out[t] = scale * table[tokens[t]]   (in fp32, rounded once)
+ *   tokens  int32 [T]; one outside [0, V) has no row (the padding of a batch): out[t] is zeros
+ *   table   bf16 [V, Dh], row stride table_stride
+ *   out     [T, Dh] of out_type, row stride out_stride
+ * Supported: Dh % 8 == 0; finite scale. */
+typedef struct dlm_embed_args {
+    uint32_t struct_size;
+    int32_t T, V, Dh;
+    const int32_t *tokens;
+    const void *table;
+    int64_t table_stride;
+    float scale;
+    void *out;
+    int64_t out_stride;
+    int32_t out_type;
+} dlm_embed_args;
+
+int dlm_embed(const dlm_embed_args *args, void *stream);
+
+/* dlm_embed_bwd -- gradient of dlm_embed: d_table[v] = scale * sum of d_out[t] over the t with tokens[t] == v
+ *   d_out       [T, Dh] of d_out_type; rows of tokens outside [0, V) count for nothing
+ *   d_table     [V, Dh] of d_table_type
+ *   accumulate  0: every row of d_table is written, zeros where no token names it.  Not 0: the sums are added to the rows that tokens name, all
+ *               other rows are neither read nor written (micro-batches; a table that is the LM head's weight as well).
+ * fp32 sums in an order that tokens and T decide, no atomics: deterministic.
+ * workspace: dlm_embed_bwd_workspace_bytes(args) bytes (they depend on T and Dh), 16-byte aligned.
+ * Supported: Dh % 8 == 0; V < 2^21 - 1; T <= 2^28.  d_out and d_table do not overlap. */
+typedef struct dlm_embed_bwd_args {
+    uint32_t struct_size;
+    int32_t T, V, Dh;
+    const int32_t *tokens;
+    const void *d_out;
+    int64_t d_out_stride;
+    int32_t d_out_type;
+    float scale;
+    void *d_table;
+    int64_t d_table_stride;
+    int32_t d_table_type;
+    int32_t accumulate;
+    void *workspace;
+    size_t workspace_bytes;
+} dlm_embed_bwd_args;
+
+int dlm_embed_bwd(const dlm_embed_bwd_args *args, void *stream);
+size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args *args);
+
+#define DLM_NORM_RMS           0    /* y = s / sqrt(mean(s^2) + eps) * weight + bias            */
+#define DLM_NORM_LAYER         1    /* y = (s - mean(s)) / sqrt(var(s) + eps) * weight + bias   */
+
+/* dlm_row_norm -- norm of rows, with the residual stream's sum in the same pass: s = x + residual, out = norm(s)
+ *   x            [T, D] of x_type (also the type of residual and sum_out)
+ *   residual     optional [T, D]; NULL: s = x.  The sum is rounded to x_type, and what is normalised is the rounded sum, which the
+ *                backward pass finds in sum_out.
+ *   sum_out      optional [T, D], with residual only: s
+ *   weight, bias optional bf16 [D]; NULL: 1, 0
+ *   out          bf16 [T, D]
+ * sum_out may be x or residual itself, out may be a bf16 x (same pointer and stride).  All in fp32; squares overflow for entries from 2^60 on (the
+ * row then comes out as its bias).  eps >= 2^-126.
+ * Supported: D a multiple of 8, up to 16384. */
+typedef struct dlm_row_norm_args {
+    uint32_t struct_size;
+    int32_t T, D, kind;
+    const void *x;
+    int64_t x_stride;
+    int32_t x_type;
+    const void *residual;
+    int64_t residual_stride;
+    void *sum_out;
+    int64_t sum_stride;
+    const void *weight, *bias;
+    float eps;
+    void *out;
+    int64_t out_stride;
+} dlm_row_norm_args;
+
+int dlm_row_norm(const dlm_row_norm_args *args, void *stream);
+
+/* dlm_row_norm_bwd -- gradients of dlm_row_norm.  With n the normalised row, r the factor that made it so and g = d_out * weight:
+ *   d_x = r (g - n mean(g n)) + d_sum   (layer norm: r (g - mean(g) - n mean(g n)) + d_sum);   d_weight = sum over rows of d_out n;   d_bias = sum of d_out
+ *   d_out   bf16 [T, D]
+ *   x       [T, D] of x_type: what was normalised (sum_out of a forward call with a residual, else x)
+ *   d_sum   optional [T, D] of x_type: the gradient of sum_out from where else it went
+ *   d_x     [T, D] of x_type: gradient of s, that is of x and of residual; may be d_sum or x itself, or a d_out of its type (same pointer and
+ *           stride)
+ *   d_weight, d_bias  optional fp32 [D], 16-byte aligned, written (not added to)
+ * fp32 sums in a fixed order, no atomics: deterministic.
+ * workspace: dlm_row_norm_bwd_workspace_bytes(args) bytes (they depend on T and D), 16-byte aligned; needed for d_weight and d_bias only. */
+typedef struct dlm_row_norm_bwd_args {
+    uint32_t struct_size;
+    int32_t T, D, kind;
+    const void *d_out;
+    int64_t d_out_stride;
+    const void *x;
+    int64_t x_stride;
+    int32_t x_type;
+    const void *d_sum;
+    int64_t d_sum_stride;
+    const void *weight;
+    float eps;
+    void *d_x;
+    int64_t d_x_stride;
+    float *d_weight, *d_bias;
+    void *workspace;
+    size_t workspace_bytes;
+} dlm_row_norm_bwd_args;
+
+int dlm_row_norm_bwd(const dlm_row_norm_bwd_args *args, void *stream);
+size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
+
 /* dlm_set_option -- process-wide tuning / test knobs (not thread-safe against running calls).  These integers are the
  * ONLY mutable state the library keeps between calls (besides the per-device address of the built-in scratch of
  * dlm_lmhead_confidence_static); every default is the planner's choice, and every setting computes the same function.

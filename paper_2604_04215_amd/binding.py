@@ -22,12 +22,14 @@ RULE_THRESHOLD, RULE_TOPK = 0, 1
 CONF_TOKEN_PROB, CONF_MARGIN, CONF_NEG_ENTROPY = 0, 1, 2
 WB_NONE, WB_BLOCK_WHEN_DONE, WB_COMMITTED_ROWS, WB_WHILE_ACTIVE = 0, 1, 2, 3
 ROPE_HALVES, ROPE_PAIRS = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
 
 EXPORTS = ["dlm_block_attn", "dlm_block_attn_workspace_bytes", "dlm_lmhead_confidence",
            "dlm_lmhead_workspace_bytes", "dlm_lmhead_confidence_static", "dlm_lmhead_static_scratch_bytes", "dlm_unmask_commit", "dlm_mask_compact", "dlm_kv_refresh",
            "dlm_block_attn_bwd", "dlm_block_attn_bwd_workspace_bytes", "dlm_seq_logprob", "dlm_set_option", "dlm_last_error", "dlm_version",
            "dlm_qk_norm_rope", "dlm_qk_norm_rope_bwd", "dlm_qk_norm_rope_bwd_workspace_bytes", "dlm_paged_append", "dlm_paged_attn",
-           "dlm_paged_attn_workspace_bytes"]
+           "dlm_paged_attn_workspace_bytes", "dlm_embed", "dlm_embed_bwd", "dlm_embed_bwd_workspace_bytes", "dlm_row_norm", "dlm_row_norm_bwd",
+           "dlm_row_norm_bwd_workspace_bytes"]
 
 
 class KvSeg(C.Structure):
@@ -575,3 +577,37 @@ def paged_attn(q, out, cache_k, cache_v, block_table, kv_len, *, max_kv_len: Opt
     tensor of paged_attn_workspace_bytes(...) bytes when that is not 0)."""
     _enqueue((_native or _load_native()).paged_attn, q, stream, q, out, cache_k, cache_v, block_table, kv_len, max_kv_len, q_len, mask_mode, block_size, scale,
              lse, k_scale, v_scale, workspace)
+
+
+# ---- embedding and the norms between layers -------------------------------------------------------------------------
+def embed(tokens, table, out, *, scale: float = 1.0, stream=None) -> None:
+    """out[t] = scale * table[tokens[t]], zeros for a token outside the table.  tokens int32 [T]; table bf16 [V, Dh]; out bf16 or fp32 [T, Dh]."""
+    _enqueue((_native or _load_native()).embed, tokens, stream, tokens, table, out, scale)
+
+
+def embed_bwd_workspace_bytes(T: int, V: int, Dh: int) -> int:
+    return (_native or _load_native()).embed_bwd_workspace(T, V, Dh)
+
+
+def embed_bwd(tokens, d_out, d_table, *, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """Gradient of embed: d_table[v] = scale * the sum of the rows of d_out whose token is v (zeros where there is none), or, with accumulate, that
+    sum added to the rows of d_table that tokens name.  d_out [T, Dh] and d_table [V, Dh] bf16 or fp32; workspace: a uint8 tensor of
+    embed_bwd_workspace_bytes(...) bytes."""
+    _enqueue((_native or _load_native()).embed_bwd, tokens, stream, tokens, d_out, d_table, scale, int(accumulate), workspace)
+
+
+def row_norm(x, out, *, kind: int = NORM_RMS, weight=None, bias=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None) -> None:
+    """out = norm of x, or of x + residual (which goes to sum_out, if given), times weight, plus bias.  x, residual, sum_out bf16 or fp32 [T, D], all of
+    one type; weight, bias bf16 [D]; out bf16 [T, D].  kind: NORM_RMS or NORM_LAYER.  sum_out may be x or residual."""
+    _enqueue((_native or _load_native()).row_norm, x, stream, x, out, kind, weight, bias, eps, residual, sum_out)
+
+
+def row_norm_bwd_workspace_bytes(T: int, D: int) -> int:
+    return (_native or _load_native()).row_norm_bwd_workspace(T, D)
+
+
+def row_norm_bwd(d_out, x, d_x, *, kind: int = NORM_RMS, weight=None, eps: float = 1e-6, d_sum=None, d_weight=None, d_bias=None, workspace=None,
+                 stream=None) -> None:
+    """Gradients of row_norm: d_out bf16 [T, D] and x (what was normalised) into d_x, to which d_sum, the gradient of the sum from elsewhere, is
+    added; d_weight, d_bias fp32 [D] are overwritten and need a workspace of row_norm_bwd_workspace_bytes(...) bytes."""
+    _enqueue((_native or _load_native()).row_norm_bwd, x, stream, d_out, x, d_x, kind, weight, eps, d_sum, d_weight, d_bias, workspace)

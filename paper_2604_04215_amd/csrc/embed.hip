@@ -1,0 +1,431 @@
+// dlm_embed and its gradient: rows of the embedding table for a batch of tokens, and rows of equal tokens summed.
+//
+// The lookup is a copy, bound by what it writes.  The gradient is a sum over rows that lie anywhere: tokens are sorted first (with their positions,
+// so that the sum of a token's rows has one order and no atomics are needed), then every row is read once.  In a masked batch one token has half of
+// the rows, so the sorted list is cut into chunks of equal length whatever tokens they hold; the sums of a token that goes over the end
+// of a chunk are joined by a last launch.
+#include "rows.hpp"
+
+namespace dlm {
+
+struct EmbedParams {
+    int T, V, Dh;
+    const int32_t* tokens;
+    const uint16_t* table;
+    int64_t table_st;
+    float scale;
+    void* out;
+    int64_t out_st;
+};
+
+// TPR threads a row
+template <bool F32, int TPR>
+__global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
+    constexpr int ROWS = 256 / TPR;
+    const int l = threadIdx.x % TPR;
+    const int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (t >= p.T) return;
+    const int token = p.tokens[t];
+    const bool known = (uint32_t)token < (uint32_t)p.V;
+    const uint16_t* src = p.table + (int64_t)(known ? token : 0) * p.table_st;
+#pragma unroll 4
+    for (int c = 8 * l; c < p.Dh; c += 8 * TPR) {
+        float f[8];
+        Piece<false>::open(known ? *reinterpret_cast<const u32x4*>(src + c) : u32x4{0, 0, 0, 0}, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = known ? f[e] * p.scale : 0.f;
+        if constexpr (F32) {
+            const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
+            Piece<true>::stream_out(p.out, t * p.out_st + c, Piece<true>::close(lo));
+            Piece<true>::stream_out(p.out, t * p.out_st + c + 4, Piece<true>::close(hi));
+        } else {
+            Piece<false>::stream_out(p.out, t * p.out_st + c, Piece<false>::close(f));
+        }
+    }
+}
+
+// ---- gradient: sorting --------------------------------------------------------------------------------------
+// Runs of RUN tokens are sorted by themselves, a workgroup each, then up to MERGE runs at a time become one: an entry's place in the merged
+// run is its place in its own plus, for every other run, the number of entries there that go before it (a binary search each; equal
+// tokens stay in the order of their positions, since earlier runs hold earlier ones).
+constexpr int RUN = 2048, RUN_BITS = 11, MERGE = 32;
+constexpr int EMBED_MAX_V = (1 << (32 - RUN_BITS)) - 2;       // a token (or V: none) and a place in its run share 32 bits
+
+struct SortParams {
+    int T, V;
+    const int32_t* tokens;
+    int32_t *token, *pos;          // sorted within each run
+    int runs;                      // workgroups behind these clear the table
+    // what is cleared: `rows` of `pieces` 16-byte pieces each, `pitch` bytes apart, `total` pieces in all (a table without gaps: rows of 4096 pieces)
+    void* table;
+    int64_t rows, pitch, total;
+    int pieces;
+};
+
+__global__ __launch_bounds__(256) void embed_sort_kernel(SortParams p) {
+    __shared__ uint32_t lds[RUN];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= p.runs) {
+        for (int64_t row = blockIdx.x - p.runs; row < p.rows; row += gridDim.x - p.runs) {
+            const int n = (int)min((int64_t)p.pieces, p.total - row * p.pieces);
+            for (int i = tid; i < n; i += 256) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>((char*)p.table + row * p.pitch) + i);
+        }
+        return;
+    }
+    const int64_t t0 = (int64_t)blockIdx.x * RUN;
+    const int n = (int)min((int64_t)RUN, p.T - t0);
+    // key: token, then place; behind the end the largest
+    uint32_t k[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = 8 * tid + e;
+        uint32_t token = 0xffffffffu >> RUN_BITS;
+        if (i < n) {
+            const int32_t x = p.tokens[t0 + i];
+            token = (uint32_t)x < (uint32_t)p.V ? x : p.V;
+        }
+        k[e] = token << RUN_BITS | i;
+    }
+    // Bitonic network over element numbers i = 8 tid + e: partners by the bits of i below 3 are in the thread's own registers, below 9 in the
+    // wavefront, above in another one.
+#pragma unroll
+    for (int size = 1; size <= RUN_BITS; ++size) {
+#pragma unroll
+        for (int bit = size - 1; bit >= 0; --bit) {
+            if (bit < 3) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e >> bit & 1) continue;
+                    const int o = e | 1 << bit;
+                    const bool up = size >= 3 ? !(tid >> (size - 3) & 1) : !(e >> size & 1);
+                    const uint32_t lo = min(k[e], k[o]), hi = max(k[e], k[o]);
+                    k[e] = up ? lo : hi;
+                    k[o] = up ? hi : lo;
+                }
+            } else {
+                const int mask = 1 << (bit - 3);
+                const bool up = size == RUN_BITS || !(tid >> (size - 3) & 1), lower = !(tid & mask);
+                uint32_t other[8];
+                if (mask < WAVE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) other[e] = shfl_xor(k[e], mask);
+                } else {
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) lds[e * 256 + tid] = k[e];
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) other[e] = lds[e * 256 + (tid ^ mask)];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) k[e] = up == lower ? min(k[e], other[e]) : max(k[e], other[e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = 8 * tid + e;
+        if (i < n) {
+            p.token[t0 + i] = k[e] >> RUN_BITS;
+            p.pos[t0 + i] = (int32_t)t0 + (k[e] & (RUN - 1));
+        }
+    }
+}
+
+// Runs of `len` entries, MERGE of them into one
+__global__ __launch_bounds__(256) void embed_merge_kernel(const int32_t* token, const int32_t* pos, int32_t* token_out, int32_t* pos_out, int T, int64_t len) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= T) return;
+    const int x = token[i], at = pos[i];
+    const int64_t run = i / len, group = run / MERGE * MERGE;
+    int64_t to = group * len + (i - run * len);
+    for (int j = 0; j < MERGE; ++j) {
+        const int64_t r = group + j, r0 = r * len;
+        if (r0 >= T) break;
+        if (r == run) continue;
+        // entries of run r with a token below x, or, in an earlier run, at most x
+        const int y = x + (r < run ? 1 : 0);
+        int64_t lo = r0, hi = r0 + len < T ? r0 + len : T;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (token[mid] < y) lo = mid + 1;
+            else hi = mid;
+        }
+        to += lo - r0;
+    }
+    token_out[to] = x;
+    pos_out[to] = at;
+}
+
+// ---- gradient: sums -----------------------------------------------------------------------------------------
+constexpr int GROUP = 16;          // chunks of a workgroup, one a wavefront
+struct EmbedGradParams {
+    int T, V, Dh;
+    const int32_t *token, *pos;    // sorted
+    const void* dy;
+    int64_t dy_st;
+    float scale;
+    void* table;
+    int64_t table_st;
+    int accumulate;
+    int chunk, groups;             // sorted entries a wavefront takes, workgroups of a slice of columns
+    float* part;                   // [groups][2][Dh]: the sum of a token that began in an earlier group; of one that goes on in the next
+};
+
+// the sum of a token's rows into the table
+template <bool F32>
+__device__ __forceinline__ void embed_store(const EmbedGradParams& p, int token, int c, const f32x4& a) {
+    const int64_t at = (int64_t)token * p.table_st + c;
+    float f[4] = {a[0] * p.scale, a[1] * p.scale, a[2] * p.scale, a[3] * p.scale};
+    if constexpr (F32) {
+        float* dst = (float*)p.table + at;
+        if (p.accumulate) {
+            const f32x4 old = *reinterpret_cast<const f32x4*>(dst);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] += old[e];
+        }
+        *reinterpret_cast<f32x4*>(dst) = f32x4{f[0], f[1], f[2], f[3]};
+    } else {
+        uint16_t* dst = (uint16_t*)p.table + at;
+        if (p.accumulate) {
+            float old[4];
+            load_bf16<4>(dst, old);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] += old[e];
+        }
+        *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+    }
+}
+
+// A wavefront adds the rows of one chunk, 64 pieces of each; at the end of a token it stores the sum.  The sums of a token that lies in several
+// chunks of the workgroup meet in LDS and are added in order by the wavefront that has its first row; those of one that lies in several
+// groups go to `part`.
+template <bool F32IN, bool F32>
+__global__ __launch_bounds__(GROUP * WAVE) void embed_grad_kernel(EmbedGradParams p) {
+    using P = Piece<F32IN>;
+    constexpr int E = P::E, Q = E / 4, AHEAD = 8;
+    __shared__ f32x4 lds[GROUP][2][Q][WAVE];       // [0]: of a token that began in an earlier chunk, [1]: of one that goes on in the next
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
+    const int slices = gridDim.x / p.groups, group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
+    const int c0 = (slice * WAVE + lane) * E, c = c0 < p.Dh ? c0 : 0;          // (lanes behind the row read its beginning, and store nothing)
+    const bool live = c0 < p.Dh;
+    const int64_t first = (int64_t)group * GROUP * p.chunk, i0 = first + (int64_t)wave * p.chunk;
+    const int n = (int)max((int64_t)0, min((int64_t)p.chunk, p.T - i0));
+    const int32_t *token = p.token + i0, *pos = p.pos + i0;
+    const int x_first = n > 0 ? token[0] : p.V;
+    int x_last = p.V;                              // the token of the chunk's end, where it began here and goes on
+    if (x_first < p.V) {                           // (else the chunk holds no token: V sorts last)
+        const int before = i0 > 0 ? token[-1] : -1, behind = i0 + n < p.T ? token[n] : -1;
+        typename P::Raw ring[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) ring[k] = P::stream(p.dy, (int64_t)pos[min(k, n - 1)] * p.dy_st + c);
+        float a[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) a[e] = 0.f;
+        bool began = x_first != before;            // the token at hand began in this chunk
+        for (int k0 = 0; k0 < n; k0 += AHEAD) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = k0 + k;
+                if (i >= n) break;
+                float f[E];
+                P::open(ring[k], f);
+                ring[k] = P::stream(p.dy, (int64_t)pos[min(i + AHEAD, n - 1)] * p.dy_st + c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) a[e] += f[e];
+                const int x = token[i], next = i + 1 < n ? token[i + 1] : behind;
+                if (x == next && i + 1 < n) continue;
+                const bool goes_on = x == next;    // into the next chunk
+                if (goes_on && began) x_last = x;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const f32x4 sum = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                    if (!began || goes_on) lds[wave][began ? 1 : 0][q][lane] = sum;
+                    else if (x < p.V && live) embed_store<F32>(p, x, c + 4 * q, sum);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) a[e] = 0.f;
+                began = true;
+            }
+        }
+    }
+    __syncthreads();
+    // from this wavefront's chunk on: the token that began in it, and, the first wavefront, one that began in an earlier group
+#pragma unroll 1
+    for (int which = wave == 0 ? 0 : 1; which < 2; ++which) {
+        const int x = which ? x_last : (group > 0 && x_first == p.token[first - 1] ? x_first : p.V);
+        if (x >= p.V) continue;
+        f32x4 sum[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) sum[q] = lds[wave][which][q][lane];
+        int64_t end = i0 + n;                      // behind the last entry added
+        for (int k = wave + 1; k < GROUP && end < p.T && p.token[end] == x && p.token[end - 1] == x; ++k) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) sum[q] += lds[k][0][q][lane];
+            end = min(end + p.chunk, (int64_t)p.T);
+        }
+        const bool goes_on = end < p.T && p.token[end] == x && p.token[end - 1] == x;
+        if (!live) continue;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (which && !goes_on) embed_store<F32>(p, x, c + 4 * q, sum[q]);
+            else *reinterpret_cast<f32x4*>(p.part + ((int64_t)group * 2 + which) * p.Dh + c + 4 * q) = sum[q];
+        }
+    }
+}
+
+// For every group whose last token goes on: its sums of that token, one a group, joined in their order.
+template <bool F32>
+__global__ __launch_bounds__(WAVE) void embed_join_kernel(EmbedGradParams p) {
+    const int group = blockIdx.x;
+    const int64_t size = (int64_t)GROUP * p.chunk, i0 = group * size, end = i0 + size;      // (the last group is not among them)
+    const int x = p.token[end - 1];
+    if (x >= p.V || p.token[end] != x) return;
+    if (i0 > 0 && p.token[i0] == x && p.token[i0 - 1] == x) return;      // began earlier
+    // the group that holds the token's last entry
+    int64_t lo = end + 1, hi = p.T;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (p.token[mid] == x) lo = mid + 1;
+        else hi = mid;
+    }
+    const int last = (int)((lo - 1) / size);
+    const int c = (blockIdx.y * WAVE + lane_id()) * 4;
+    if (c >= p.Dh) return;
+    f32x4 a = *reinterpret_cast<const f32x4*>(p.part + ((int64_t)group * 2 + 1) * p.Dh + c);
+#pragma unroll 8
+    for (int k = group + 1; k <= last; ++k) a += *reinterpret_cast<const f32x4*>(p.part + (int64_t)k * 2 * p.Dh + c);
+    embed_store<F32>(p, x, c, a);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------
+static int validate_embed(int T, int V, int Dh, const int32_t* tokens, float scale, const char* who) {
+    if (T < 0 || V <= 0 || Dh <= 0) return fail(DLM_ERR_INVALID_ARG, "%s: bad sizes T=%d V=%d Dh=%d", who, T, V, Dh);
+    if (Dh % 8) return fail(DLM_ERR_UNSUPPORTED, "%s: Dh=%d is not a multiple of 8", who, Dh);
+    if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return fail(DLM_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    if (T > 0 && !tokens) return fail(DLM_ERR_INVALID_ARG, "%s: null tokens", who);
+    return DLM_OK;
+}
+
+template <bool F32>
+static void launch_embed(const EmbedParams& all, hipStream_t st) {
+    constexpr int MOST = 1 << 22;                   // rows a launch: its threads stay below 2^32
+    for (int64_t t0 = 0; t0 < all.T; t0 += MOST) {
+        EmbedParams p = all;
+        p.T = (int)(all.T - t0 < MOST ? all.T - t0 : MOST);
+        p.tokens = all.tokens + t0;
+        p.out = (char*)all.out + t0 * all.out_st * (F32 ? 4 : 2);
+        if (p.Dh <= 64) hipLaunchKernelGGL((embed_kernel<F32, 8>), dim3((p.T + 31) / 32), dim3(256), 0, st, p);
+        else if (p.Dh <= 512) hipLaunchKernelGGL((embed_kernel<F32, 64>), dim3((p.T + 3) / 4), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((embed_kernel<F32, 256>), dim3(p.T), dim3(256), 0, st, p);
+    }
+}
+
+// How the gradient is cut up, and where its workspace holds what
+struct EmbedPlan {
+    int runs, levels, chunk, groups;
+    size_t list_bytes, part_at, bytes;              // one list of T; the sums behind the lists
+};
+static EmbedPlan plan_embed(int T, int Dh) {
+    EmbedPlan p = {};
+    p.runs = (int)(((int64_t)T + RUN - 1) / RUN);
+    for (int64_t n = p.runs; n > 1; n = (n + MERGE - 1) / MERGE) ++p.levels;
+    // some 8192 wavefronts, of chunks that are neither so short that their borders cost more than their rows nor so long that a few run on alone
+    const int64_t slices = (Dh + 511) / 512;
+    int64_t chunk = T * slices / 8192;
+    chunk = chunk < 8 ? 8 : chunk > 128 ? 128 : chunk;
+    p.chunk = (int)chunk;
+    p.groups = (int)((T + GROUP * chunk - 1) / (GROUP * chunk));
+    p.list_bytes = ((size_t)T * 4 + 15) / 16 * 16;
+    p.part_at = p.list_bytes * (p.levels > 0 ? 4 : 2);
+    p.bytes = p.part_at + (size_t)p.groups * 2 * Dh * sizeof(float);
+    return p;
+}
+
+}  // namespace dlm
+
+using namespace dlm;
+
+extern "C" int dlm_embed(const dlm_embed_args* a, void* stream) {
+    static const char who[] = "embed";
+    if (!a) return fail(DLM_ERR_INVALID_ARG, "%s: null args", who);
+    if (a->struct_size != sizeof(dlm_embed_args)) return fail(DLM_ERR_INVALID_ARG, "%s: struct_size %u != %zu", who, a->struct_size, sizeof(dlm_embed_args));
+    int rc;
+    if ((rc = validate_embed(a->T, a->V, a->Dh, a->tokens, a->scale, who)) != DLM_OK) return rc;
+    if ((rc = validate_row_type(a->out_type, who, "out")) != DLM_OK) return rc;
+    if (a->T == 0) return DLM_OK;
+    if ((rc = validate_rows(a->table, a->table_stride, a->V, a->Dh, 2, false, who, "table")) != DLM_OK) return rc;
+    if ((rc = validate_rows(a->out, a->out_stride, a->T, a->Dh, row_bytes(a->out_type), true, who, "out")) != DLM_OK) return rc;
+    const EmbedParams p = {a->T, a->V, a->Dh, a->tokens, (const uint16_t*)a->table, a->table_stride, a->scale, a->out, a->out_stride};
+    if (a->out_type == DLM_ROW_F32) launch_embed<true>(p, (hipStream_t)stream);
+    else launch_embed<false>(p, (hipStream_t)stream);
+    return check_hip(hipGetLastError(), "embed_kernel launch");
+}
+
+extern "C" size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args* a) {
+    if (!a || a->struct_size != sizeof(dlm_embed_bwd_args) || a->T <= 0 || a->Dh <= 0) return 0;
+    return plan_embed(a->T, a->Dh).bytes;
+}
+
+extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
+    static const char who[] = "embed_bwd";
+    if (!a) return fail(DLM_ERR_INVALID_ARG, "%s: null args", who);
+    if (a->struct_size != sizeof(dlm_embed_bwd_args))
+        return fail(DLM_ERR_INVALID_ARG, "%s: struct_size %u != %zu", who, a->struct_size, sizeof(dlm_embed_bwd_args));
+    int rc;
+    if ((rc = validate_embed(a->T, a->V, a->Dh, a->tokens, a->scale, who)) != DLM_OK) return rc;
+    if (a->V > EMBED_MAX_V) return fail(DLM_ERR_UNSUPPORTED, "%s: V=%d (supported: up to %d)", who, a->V, EMBED_MAX_V);
+    if (a->T > 1 << 28) return fail(DLM_ERR_UNSUPPORTED, "%s: T=%d (supported: up to 2^28)", who, a->T);
+    if ((rc = validate_row_type(a->d_out_type, who, "d_out")) != DLM_OK) return rc;
+    if ((rc = validate_row_type(a->d_table_type, who, "d_table")) != DLM_OK) return rc;
+    if ((rc = validate_rows(a->d_out, a->d_out_stride, a->T, a->Dh, row_bytes(a->d_out_type), false, who, "d_out")) != DLM_OK) return rc;
+    const int bytes = row_bytes(a->d_table_type);
+    if ((rc = validate_rows(a->d_table, a->d_table_stride, a->V, a->Dh, bytes, true, who, "d_table")) != DLM_OK) return rc;
+    const size_t need = dlm_embed_bwd_workspace_bytes(a);
+    if (need > 0) {
+        if (!a->workspace || a->workspace_bytes < need) return fail(DLM_ERR_WORKSPACE, "%s: workspace of %zu bytes required", who, need);
+        if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const EmbedPlan plan = plan_embed(a->T, a->Dh);
+    char* ws = (char*)a->workspace;
+    int32_t* list[4];
+    for (int i = 0; i < 4; ++i) list[i] = (int32_t*)(ws + i * plan.list_bytes);
+    const int64_t row_bytes_ = (int64_t)a->Dh * bytes, pitch = a->V > 1 ? a->d_table_stride * bytes : row_bytes_;
+    SortParams s = {a->T, a->V, a->tokens, list[0], list[1], plan.runs, a->d_table, 0, 0, a->V * row_bytes_ / 16, 0};
+    if (!a->accumulate) {
+        const bool gaps = pitch != row_bytes_;
+        s.pieces = gaps ? (int)(row_bytes_ / 16) : 4096;
+        s.pitch = gaps ? pitch : 4096 * 16;
+        s.rows = (s.total + s.pieces - 1) / s.pieces;
+    }
+    const int clear = (int)(s.rows < 2048 ? s.rows : 2048);
+    if (plan.runs + clear == 0) return DLM_OK;
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(plan.runs + clear), dim3(256), 0, st, s);
+    if ((rc = check_hip(hipGetLastError(), "embed_sort_kernel launch")) != DLM_OK) return rc;
+    if (a->T == 0) return DLM_OK;
+    int from = 0;
+    int64_t len = RUN;
+    for (int level = 0; level < plan.levels; ++level) {
+        const int to = from ^ 2;
+        hipLaunchKernelGGL(embed_merge_kernel, dim3((unsigned)(((int64_t)a->T + 255) / 256)), dim3(256), 0, st, list[from], list[from + 1], list[to], list[to + 1], a->T, len);
+        if ((rc = check_hip(hipGetLastError(), "embed_merge_kernel launch")) != DLM_OK) return rc;
+        from = to;
+        len *= MERGE;
+    }
+    const EmbedGradParams p = {a->T, a->V, a->Dh, list[from], list[from + 1], a->d_out, a->d_out_stride, a->scale, a->d_table, a->d_table_stride,
+                               a->accumulate, plan.chunk, plan.groups, (float*)(ws + plan.part_at)};
+    const bool in32 = a->d_out_type == DLM_ROW_F32, out32 = a->d_table_type == DLM_ROW_F32;
+    const int per = in32 ? 256 : 512;
+    const dim3 grid((unsigned)((int64_t)plan.groups * ((a->Dh + per - 1) / per))), threads(GROUP * WAVE);
+    if (in32 && out32) hipLaunchKernelGGL((embed_grad_kernel<true, true>), grid, threads, 0, st, p);
+    else if (in32) hipLaunchKernelGGL((embed_grad_kernel<true, false>), grid, threads, 0, st, p);
+    else if (out32) hipLaunchKernelGGL((embed_grad_kernel<false, true>), grid, threads, 0, st, p);
+    else hipLaunchKernelGGL((embed_grad_kernel<false, false>), grid, threads, 0, st, p);
+    if ((rc = check_hip(hipGetLastError(), "embed_grad_kernel launch")) != DLM_OK) return rc;
+    if (plan.groups < 2) return DLM_OK;
+    const dim3 join(plan.groups - 1, (a->Dh + 255) / 256);
+    if (out32) hipLaunchKernelGGL((embed_join_kernel<true>), join, dim3(WAVE), 0, st, p);
+    else hipLaunchKernelGGL((embed_join_kernel<false>), join, dim3(WAVE), 0, st, p);
+    return check_hip(hipGetLastError(), "embed_join_kernel launch");
+}

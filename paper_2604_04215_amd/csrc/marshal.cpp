@@ -260,6 +260,118 @@ size_t paged_attn_workspace(Args& a) {
     return dlm_paged_attn_workspace_bytes(&s);
 }
 
+// rows [n, D] of bf16 or fp32 into a pointer, its stride and its type
+template <typename P>
+void rows(Args& a, int i, const char* name, int64_t n, int64_t D, P& ptr, int64_t& stride, int32_t& type) {
+    if (a.v[i] == Py_None) return;
+    if (!THPVariable_Check(a.v[i])) refuse(name, "a tensor expected");
+    const bool wide = THPVariable_Unpack(a.v[i]).scalar_type() == at::kFloat;
+    const at::Tensor& t = a.needed(i, name, wide ? at::kFloat : at::kBFloat16, 2);
+    a.fits(t, name, {n, D});
+    ptr = t.data_ptr();
+    stride = t.stride(0);
+    type = wide ? DLM_ROW_F32 : DLM_ROW_BF16;
+}
+// the same of a type that is given
+template <typename P>
+void rows_of(Args& a, int i, const char* name, int64_t n, int64_t D, int32_t type, P& ptr, int64_t& stride) {
+    const at::Tensor* t = a.tensor(i, name, type == DLM_ROW_F32 ? at::kFloat : at::kBFloat16, 2);
+    if (!t) return;
+    a.fits(*t, name, {n, D});
+    ptr = t->data_ptr();
+    stride = t->stride(0);
+}
+int64_t axis(Args& a, int i, const char* name, int64_t dim, int64_t which) {
+    if (!THPVariable_Check(a.v[i])) refuse(name, "a tensor expected");
+    const at::Tensor& t = THPVariable_Unpack(a.v[i]);
+    if (t.dim() != dim) refuse(name, (std::to_string(t.dim()) + " axes, expected " + std::to_string(dim)).c_str());
+    return t.size(which);
+}
+
+// (stream, tokens, table, out, scale)
+int embed(Args& a) {
+    dlm_embed_args s = {};
+    s.struct_size = sizeof s;
+    s.T = size32(axis(a, 1, "tokens", 1, 0), "tokens");
+    s.V = size32(axis(a, 2, "table", 2, 0), "table");
+    s.Dh = size32(axis(a, 2, "table", 2, 1), "table");
+    rows_of(a, 2, "table", s.V, s.Dh, DLM_ROW_BF16, s.table, s.table_stride);
+    rows(a, 3, "out", s.T, s.Dh, s.out, s.out_stride, s.out_type);
+    s.tokens = a.flat<int32_t>(1, "tokens", at::kInt, {s.T});
+    s.scale = (float)a.number(4);
+    return dlm_embed(&s, a.stream());
+}
+// (stream, tokens, d_out, d_table, scale, accumulate, workspace)
+int embed_bwd(Args& a) {
+    dlm_embed_bwd_args s = {};
+    s.struct_size = sizeof s;
+    s.T = size32(axis(a, 1, "tokens", 1, 0), "tokens");
+    s.V = size32(axis(a, 3, "d_table", 2, 0), "d_table");
+    s.Dh = size32(axis(a, 3, "d_table", 2, 1), "d_table");
+    rows(a, 2, "d_out", s.T, s.Dh, s.d_out, s.d_out_stride, s.d_out_type);
+    rows(a, 3, "d_table", s.V, s.Dh, s.d_table, s.d_table_stride, s.d_table_type);
+    s.tokens = a.flat<int32_t>(1, "tokens", at::kInt, {s.T});
+    s.scale = (float)a.number(4);
+    s.accumulate = a.whole(5);
+    a.workspace(6, s.workspace, s.workspace_bytes);
+    return dlm_embed_bwd(&s, a.stream());
+}
+// (T, V, Dh)
+size_t embed_bwd_workspace(Args& a) {
+    dlm_embed_bwd_args s = {};
+    s.struct_size = sizeof s;
+    s.T = a.whole(0);
+    s.V = a.whole(1);
+    s.Dh = a.whole(2);
+    return dlm_embed_bwd_workspace_bytes(&s);
+}
+
+// (stream, x, out, kind, weight, bias, eps, residual, sum_out)
+int row_norm(Args& a) {
+    dlm_row_norm_args s = {};
+    s.struct_size = sizeof s;
+    s.T = size32(axis(a, 1, "x", 2, 0), "x");
+    s.D = size32(axis(a, 1, "x", 2, 1), "x");
+    rows(a, 1, "x", s.T, s.D, s.x, s.x_stride, s.x_type);
+    a.needed(2, "out", at::kBFloat16, 2);
+    rows_of(a, 2, "out", s.T, s.D, DLM_ROW_BF16, s.out, s.out_stride);
+    s.kind = a.whole(3);
+    s.weight = a.flat<void>(4, "weight", at::kBFloat16, {s.D});
+    s.bias = a.flat<void>(5, "bias", at::kBFloat16, {s.D});
+    s.eps = (float)a.number(6);
+    rows_of(a, 7, "residual", s.T, s.D, s.x_type, s.residual, s.residual_stride);
+    rows_of(a, 8, "sum_out", s.T, s.D, s.x_type, s.sum_out, s.sum_stride);
+    return dlm_row_norm(&s, a.stream());
+}
+// (stream, d_out, x, d_x, kind, weight, eps, d_sum, d_weight, d_bias, workspace)
+int row_norm_bwd(Args& a) {
+    dlm_row_norm_bwd_args s = {};
+    s.struct_size = sizeof s;
+    s.T = size32(axis(a, 2, "x", 2, 0), "x");
+    s.D = size32(axis(a, 2, "x", 2, 1), "x");
+    rows(a, 2, "x", s.T, s.D, s.x, s.x_stride, s.x_type);
+    a.needed(1, "d_out", at::kBFloat16, 2);
+    rows_of(a, 1, "d_out", s.T, s.D, DLM_ROW_BF16, s.d_out, s.d_out_stride);
+    if (a.v[3] == Py_None) refuse("d_x", "is needed");
+    rows_of(a, 3, "d_x", s.T, s.D, s.x_type, s.d_x, s.d_x_stride);
+    s.kind = a.whole(4);
+    s.weight = a.flat<void>(5, "weight", at::kBFloat16, {s.D});
+    s.eps = (float)a.number(6);
+    rows_of(a, 7, "d_sum", s.T, s.D, s.x_type, s.d_sum, s.d_sum_stride);
+    s.d_weight = a.flat<float>(8, "d_weight", at::kFloat, {s.D});
+    s.d_bias = a.flat<float>(9, "d_bias", at::kFloat, {s.D});
+    a.workspace(10, s.workspace, s.workspace_bytes);
+    return dlm_row_norm_bwd(&s, a.stream());
+}
+// (T, D)
+size_t row_norm_bwd_workspace(Args& a) {
+    dlm_row_norm_bwd_args s = {};
+    s.struct_size = sizeof s;
+    s.T = a.whole(0);
+    s.D = a.whole(1);
+    return dlm_row_norm_bwd_workspace_bytes(&s);
+}
+
 template <auto F, int N>
 PyObject* entry(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n != N) return PyErr_Format(PyExc_TypeError, "%d arguments expected", N);
@@ -280,6 +392,12 @@ PyMethodDef methods[] = {
     {"paged_append", (PyCFunction)(void*)entry<paged_append, 16>, METH_FASTCALL, nullptr},
     {"paged_attn", (PyCFunction)(void*)entry<paged_attn, 16>, METH_FASTCALL, nullptr},
     {"paged_attn_workspace", (PyCFunction)(void*)entry<paged_attn_workspace, 16>, METH_FASTCALL, nullptr},
+    {"embed", (PyCFunction)(void*)entry<embed, 5>, METH_FASTCALL, nullptr},
+    {"embed_bwd", (PyCFunction)(void*)entry<embed_bwd, 7>, METH_FASTCALL, nullptr},
+    {"embed_bwd_workspace", (PyCFunction)(void*)entry<embed_bwd_workspace, 3>, METH_FASTCALL, nullptr},
+    {"row_norm", (PyCFunction)(void*)entry<row_norm, 9>, METH_FASTCALL, nullptr},
+    {"row_norm_bwd", (PyCFunction)(void*)entry<row_norm_bwd, 11>, METH_FASTCALL, nullptr},
+    {"row_norm_bwd_workspace", (PyCFunction)(void*)entry<row_norm_bwd_workspace, 2>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
