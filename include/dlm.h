@@ -682,6 +682,53 @@ typedef struct dlm_row_norm_bwd_args {
 int dlm_row_norm_bwd(const dlm_row_norm_bwd_args *args, void *stream);
 size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
 
+/* ------------------------------------------------------------------------- *
+ * dlm_lmhead_bwd -- gradients through the lse and ztarget of dlm_lmhead_confidence, the log-likelihood terms of Eq. 2 and Eq. 3.  With
+ * p = exp(z - lse), 0 at forbid_token, for each selected row:
+ *   dz_v = inv_temperature * (d_lse * p_v + d_ztarget * [v == target]);   d_hidden[row] = sum_v dz_v w[v];   d_w[v] = sum_rows dz_v hidden[row]
+ * (a log-probability log p(target) = ztarget - lse with gradient g: d_ztarget = g, d_lse = -g).
+ *   M, Dh, V, hidden, row_idx, m_dev, w, inv_temperature, forbid_token, out_scatter   as in the forward call
+ *   lse        fp32, the forward call's; target, d_lse, d_ztarget are indexed like it (by r, or by row(r) with out_scatter).  d_lse or d_ztarget may be
+ *              NULL: zero.  d_ztarget needs target; a target outside [0, V), or forbid_token, has no gradient.
+ *              A row whose d_lse is zero may have any lse.
+ *   d_hidden   optional, rows of d_hidden_type indexed like `hidden`: row(r) is written for every r, other rows are left as they are.  Rows named
+ *              twice count twice for d_w; in d_hidden such a row holds the gradient of one of the two.
+ *   d_w        optional [V, Dh] of d_w_type; accumulate 0: written, else added to
+ * The logits are not stored.  bf16 operands and fp32 sums; dz is rounded to bf16 for a product whose result is bf16 and to two bf16 terms (16 bits) for
+ * one whose result is fp32.  No atomics: deterministic (the order of sums depends on the sizes alone).  hidden and w have to be finite: other rows'
+ * values are multiplied by dz that may be zero.
+ * workspace: dlm_lmhead_bwd_workspace_bytes(args) bytes, 16-byte aligned; they depend on M, Dh, V, the types and which gradients are wanted.
+ * Supported: Dh % 64 == 0, up to 65536; M up to 2^20; V up to 2^24; rows 16-byte aligned, strides multiples of 16 bytes, w_stride_row < 2^23.
+ * ------------------------------------------------------------------------- */
+typedef struct dlm_lmhead_bwd_args {
+    uint32_t struct_size;
+    int32_t M, Dh, V;
+    const void *hidden;
+    int64_t hidden_stride_row;
+    const int32_t *row_idx;
+    const int32_t *m_dev;
+    const void *w;
+    int64_t w_stride_row;
+    float inv_temperature;
+    int32_t forbid_token;
+    int32_t out_scatter;
+    const float *lse;
+    const int32_t *target;
+    const float *d_lse, *d_ztarget;
+    void *d_hidden;
+    int64_t d_hidden_stride_row;
+    int32_t d_hidden_type;
+    void *d_w;
+    int64_t d_w_stride_row;
+    int32_t d_w_type;
+    int32_t accumulate;
+    void *workspace;
+    size_t workspace_bytes;
+} dlm_lmhead_bwd_args;
+
+int dlm_lmhead_bwd(const dlm_lmhead_bwd_args *args, void *stream);
+size_t dlm_lmhead_bwd_workspace_bytes(const dlm_lmhead_bwd_args *args);
+
 /* dlm_set_option -- process-wide tuning / test knobs (not thread-safe against running calls).  These integers are the
  * ONLY mutable state the library keeps between calls (besides the per-device address of the built-in scratch of
  * dlm_lmhead_confidence_static); every default is the planner's choice, and every setting computes the same function.
@@ -730,6 +777,8 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *                   them (the workspace's size depends on it).
  *   "paged_shape"   0 = the library picks dlm_paged_attn's workgroups from the rows a KV head has (default); 1, 2, 3, 4 = 16, 32, 128, 16
  *                   rows (of 8, 4, 8, 2 wavefronts; the workspace's size depends on it).
+ *   "lmhead_bwd_columns" 0 = dlm_lmhead_bwd takes as many columns of the vocabulary at a time as fit 2 GiB of dz (default); n, a multiple of 256 =
+ *                   at most n (the workspace's size depends on it).
  * The knobs exist for tests and tuning sweeps. */
 int dlm_set_option(const char *name, int value);
 

@@ -29,7 +29,7 @@ EXPORTS = ["dlm_block_attn", "dlm_block_attn_workspace_bytes", "dlm_lmhead_confi
            "dlm_block_attn_bwd", "dlm_block_attn_bwd_workspace_bytes", "dlm_seq_logprob", "dlm_set_option", "dlm_last_error", "dlm_version",
            "dlm_qk_norm_rope", "dlm_qk_norm_rope_bwd", "dlm_qk_norm_rope_bwd_workspace_bytes", "dlm_paged_append", "dlm_paged_attn",
            "dlm_paged_attn_workspace_bytes", "dlm_embed", "dlm_embed_bwd", "dlm_embed_bwd_workspace_bytes", "dlm_row_norm", "dlm_row_norm_bwd",
-           "dlm_row_norm_bwd_workspace_bytes"]
+           "dlm_row_norm_bwd_workspace_bytes", "dlm_lmhead_bwd", "dlm_lmhead_bwd_workspace_bytes"]
 
 
 class KvSeg(C.Structure):
@@ -611,3 +611,21 @@ def row_norm_bwd(d_out, x, d_x, *, kind: int = NORM_RMS, weight=None, eps: float
     """Gradients of row_norm: d_out bf16 [T, D] and x (what was normalised) into d_x, to which d_sum, the gradient of the sum from elsewhere, is
     added; d_weight, d_bias fp32 [D] are overwritten and need a workspace of row_norm_bwd_workspace_bytes(...) bytes."""
     _enqueue((_native or _load_native()).row_norm_bwd, x, stream, d_out, x, d_x, kind, weight, eps, d_sum, d_weight, d_bias, workspace)
+
+
+def lmhead_bwd_workspace_bytes(hidden, w, lse, *, target=None, d_ztarget=None, d_lse=None, d_hidden=None, d_w=None, accumulate: bool = False,
+                               M: Optional[int] = None, row_idx=None, m_dev=None, inv_temperature: float = 1.0, forbid_token: int = -1,
+                               out_scatter: bool = False) -> int:
+    """Bytes of workspace lmhead_bwd wants for this call."""
+    return (_native or _load_native()).lmhead_bwd_workspace(0, hidden, w, lse, target, d_ztarget, d_lse, d_hidden, d_w, int(accumulate), M, row_idx, m_dev,
+                                                            inv_temperature, forbid_token, int(out_scatter), None)
+
+
+def lmhead_bwd(hidden, w, lse, *, target=None, d_ztarget=None, d_lse=None, d_hidden=None, d_w=None, accumulate: bool = False, M: Optional[int] = None,
+               row_idx=None, m_dev=None, inv_temperature: float = 1.0, forbid_token: int = -1, out_scatter: bool = False, workspace=None, stream=None) -> None:
+    """Gradients through lmhead_confidence's lse and ztarget (d_lse, d_ztarget fp32, either may be None) into d_hidden (shaped like hidden; the selected
+    rows are written) and d_w (shaped like w; written, or added to with accumulate), each bf16 or fp32 or None.  hidden, w, row_idx, m_dev,
+    inv_temperature, forbid_token, out_scatter as in the forward call; lse its output; lse, target, d_ztarget, d_lse are indexed alike.
+    workspace: a uint8 tensor of lmhead_bwd_workspace_bytes(...) bytes."""
+    _enqueue((_native or _load_native()).lmhead_bwd, hidden, stream, hidden, w, lse, target, d_ztarget, d_lse, d_hidden, d_w, int(accumulate), M, row_idx, m_dev,
+             inv_temperature, forbid_token, int(out_scatter), workspace)

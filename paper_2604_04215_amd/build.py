@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdlm.so")
 PEAKS_LIB = os.path.join(HERE, "libdlm_peaks.so")     # achievable-peak micro-benchmarks (bench.py --kernel peaks)
-SOURCES = ["core.hip", "commit.hip", "attn.hip", "attn_bwd.hip", "lmhead.hip", "heads.hip", "paged_attn.hip", "embed.hip", "norm.hip"]
+SOURCES = ["core.hip", "commit.hip", "attn.hip", "attn_bwd.hip", "lmhead.hip", "heads.hip", "paged_attn.hip", "embed.hip", "norm.hip", "lmhead_bwd.hip"]
 PEAKS_SOURCES = ["peaks.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE,
          # packed-fp32 code generation off (hipcc-only flag; the host pass warns that it ignores it)

@@ -1,0 +1,645 @@
+// dlm_lmhead_bwd: gradient of the LM head's log-sum-exp and target logit.
+//
+// With z = inv_t h w^T and p = exp(z - lse) (lse from the forward pass, so that no row has to be reduced again):
+//   dz = inv_t (d_lse p + d_ztarget [v = target]);   d_hidden = dz W;   d_w = dz^T H.
+// Three products of 2 M V Dh operations, all bound by the matrix pipes from a few hundred rows on, below that by reading W twice and writing d_w once.
+// The logits themselves are never stored; dz is, in 16 bits, for as many columns at a time as the workspace holds (a "chunk"): d_hidden sums over the
+// vocabulary and d_w over the rows, so that one of the two would otherwise form all of dz again, a fourth product.
+//
+// One loop serves the three: C[i][j] = sum over k of A(i, k) B(j, k), on 32 x 32 x 16 MFMA tiles.  An operand comes either with k along its
+// rows (hidden and W for the logits; dz for d_hidden) or with k across them (W for d_hidden; dz and hidden for d_w), which is
+// turned on the way from LDS into registers by the transposing read, so that nothing is transposed in memory.
+//
+// Rounding of dz: bf16 where the gradient is bf16 (half a step of dz beside half a step of the result: 1.4 times the error of rounding the
+// result alone; a second term would be another product), two bf16 terms, 16 bits, for a product whose result is fp32.
+#include "rows.hpp"
+
+namespace dlm {
+
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+
+struct LmbRow {                    // what the logits' kernel knows of a row
+    float lse, a, c;               // a = inv_t d_lse, c = inv_t d_ztarget
+    int target;                    // -1: none
+};
+
+struct LmbParams {
+    int M, Dh, V;
+    const int32_t* m_dev;
+    const uint16_t* hidden;        // as the caller has them
+    int64_t h_stride;
+    const int32_t* row_idx;
+    const uint16_t* w;
+    int64_t w_stride;
+    float inv_t;
+    int forbid, scatter;
+    const float *lse, *d_lse, *d_zt;
+    const int32_t* target;
+    // workspace
+    LmbRow* rows;                  // [M rounded up to 64]
+    uint16_t* h;                   // the selected hidden rows, [M rounded up to 64][Dh], zeros behind the last
+    uint16_t* w_tail;              // [64][Dh]: the last V % 64 rows of W, zeros behind them
+    uint16_t* dz;                  // [terms][M rounded up to 64][ldz]
+    int64_t dz_term;               // entries of a term
+    int ldz;
+    float* part;                   // [splits][M][Dh]
+    // the chunk: columns v0 .. v0 + n of dz, n a multiple of 64 but for the end of the vocabulary
+    int v0, n, terms_h, terms_w, add;      // add: d_hidden's partial sums are there already
+    int ni, nj, splits;            // tiles of d_hidden: along Dh, along the rows; parts of its sum
+    int n2;                        // workgroups of d_hidden (a multiple of 8)
+    int wi, wj;                    // tiles of d_w: along Dh, along the chunk
+    void* d_hidden;
+    int64_t dh_stride;
+    int dh_f32;
+    void* d_w;
+    int64_t dw_stride;
+    int dw_f32, accumulate;
+};
+
+__device__ __forceinline__ int lmb_rows(const LmbParams& p) { return p.m_dev ? min(p.M, max(*p.m_dev, 0)) : p.M; }
+
+// Selected hidden rows side by side, what belongs to them, and the rows of W behind the last whole 64: the products then read whole tiles.
+__global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
+    const int M = lmb_rows(p), bound = (p.M + 63) & ~63, r = blockIdx.x;
+    if (r >= bound) {
+        const int t = r - bound, v = (p.V & ~63) + t;
+        for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
+            *reinterpret_cast<u32x4*>(p.w_tail + (int64_t)t * p.Dh + c) =
+                v < p.V ? *reinterpret_cast<const u32x4*>(p.w + v * p.w_stride + c) : u32x4{0, 0, 0, 0};
+        return;
+    }
+    if (r >= ((M + 63) & ~63)) return;
+    const bool live = r < M;
+    const int row = !live ? 0 : p.row_idx ? p.row_idx[r] : r;
+    for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
+        *reinterpret_cast<u32x4*>(p.h + (int64_t)r * p.Dh + c) =
+            live ? *reinterpret_cast<const u32x4*>(p.hidden + row * p.h_stride + c) : u32x4{0, 0, 0, 0};
+    if (threadIdx.x == 0) {
+        LmbRow o = {0.f, 0.f, 0.f, -1};
+        if (live) {
+            const int at = p.scatter ? row : r;
+            o.lse = p.lse[at];
+            if (p.d_lse) o.a = p.d_lse[at] * p.inv_t;
+            if (p.d_zt) {
+                o.c = p.d_zt[at] * p.inv_t;
+                o.target = p.target[at];
+            }
+        }
+        p.rows[r] = o;
+    }
+}
+
+// Tile number -> tile, so that neighbouring numbers form blocks of gi x gj tiles, which share their panels through one XCD's L2 (see lmb_slot).
+__device__ __forceinline__ void lmb_tile(int t, int ni, int nj, int gi, int gj, int& i, int& j) {
+    const int band = t / (gi * nj), bi = min(gi, ni - band * gi);
+    int r = t - band * gi * nj;
+    const int col = r / (bi * gj), bj = min(gj, nj - col * gj);
+    r -= col * bi * gj;
+    j = r / bi;
+    i = band * gi + r - j * bi;
+    j += col * gj;
+    (void)bj;
+}
+// Workgroups go round the 8 XCDs: each gets a stretch of the tile numbers.  -1: none
+__device__ __forceinline__ int lmb_slot(int block, int tiles) {
+    const int per = (tiles + 7) >> 3, slot = block >> 3, t = (block & 7) * per + slot;
+    return slot < per && t < tiles ? t : -1;
+}
+
+__device__ __forceinline__ void lmb_load_lds16(const void* base, uint32_t offset, uint32_t dst) {   // base: wave-uniform
+    uint64_t a;
+    // (scalars are read by scalar instructions alone, which wait for whatever wrote them)
+    asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %1, %0"
+                 : "=&s"(a) : "v"(offset), "s"(__builtin_amdgcn_readfirstlane(dst)), "s"(base) : "memory");
+}
+
+// The shape of a workgroup: WV x WH wavefronts of TVW x THW tiles of 32 x 32.
+//
+// Memory to registers goes through a ring of five LDS stages of 32 k each, without registers in between.  Requests come in pairs of stages, two pairs
+// ahead, spread evenly over the MFMAs, and fragments are read one MFMA step ahead, across the barriers (lmhead.hip has the measurements).
+// Images of an operand's stage (TILE x 32 entries, 64 TILE bytes):
+//   k along the rows: rows of 64 bytes; 16-byte piece c of row r in place c ^ (r / 4 % 4).
+//   k across the rows: 32 rows of 2 TILE bytes; 64-byte piece c of row k in place c ^ (k % 4) (TILE = 64: c ^ (k / 2 % 2), TILE = 32: c), so that the four
+//   rows that a transposing read touches lie in different banks.
+template <bool AROW, bool BROW, int WV, int WH, int TVW, int THW>
+struct LmbLoop {
+    static constexpr int NW = WV * WH, TI = 32 * TVW * WV, TJ = 32 * THW * WH, STAGE = (TI + TJ) * 64, NS = 5, RING = NS * STAGE;
+    static constexpr int IPA = TI / 16 / NW, IPB = TJ / 16 / NW, IPW = IPA + IPB;      // requests of a wavefront and stage
+    static_assert(TI / 16 % NW == 0 && TJ / 16 % NW == 0, "requests split evenly over the wavefronts");
+    static_assert(RING <= 160 * 1024, "five stages within the 160 KB of LDS");
+
+    unsigned char* ring;
+    uint32_t lds0;
+    int w, lane;
+    uint32_t voff[IPW];            // a lane's place in each request, from the wave-uniform base of its stage
+    f32x16 acc[TVW][THW];
+
+    __device__ __forceinline__ LmbLoop(unsigned char* r) : ring(r) {
+        lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)r;
+        lane = lane_id();
+        w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    }
+    static __device__ __forceinline__ int swz(int tile, int k) { return tile >= 128 ? k & 3 : tile == 64 ? k >> 1 & 1 : 0; }
+    // Places of operand A's (B's) requests: entry (e, k) of the stage is `pitch` bytes a row from the base.  `last`: the last index along the
+    // tile that may be read (rows), or the last multiple of 8 (columns).
+    template <bool ROW, int TILE, int IP>
+    __device__ __forceinline__ void place(uint32_t (&v)[IPW], int first, uint32_t pitch, int last) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+#pragma unroll
+        for (int j = 0; j < IP; ++j) {
+            const int g = w * IP + j;
+            if constexpr (ROW) {
+                constexpr int LPR = TILE / 8, RPI = 64 / LPR;          // lanes a row, rows a request
+                const int k = g * RPI + l / LPR, c = l % LPR;
+                const int col = ((c >> 2 ^ swz(TILE, k)) << 2 | (c & 3)) * 8;
+                v[first + j] = (uint32_t)k * pitch + (uint32_t)min(col, last) * 2;
+            } else {
+                const int row = g * 16 + (l >> 2), piece = (l & 3) ^ (l >> 4 & 3);
+                v[first + j] = (uint32_t)min(row, last) * pitch + piece * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void place_a(uint32_t pitch, int last) { place<AROW, TI, IPA>(voff, 0, pitch, last); }
+    __device__ __forceinline__ void place_b(uint32_t pitch, int last) { place<BROW, TJ, IPB>(voff, IPA, pitch, last); }
+
+    struct Bases {
+        const char *a0, *a1, *b0, *b1;                                 // of a pair's two stages
+    };
+    // request jj of a pair (0 .. 2 IPW): even ones into its first stage
+    __device__ __forceinline__ void issue(const Bases& s, int jj, uint32_t st0, uint32_t st1) {
+        const int j = jj >> 1;
+        const char* base = j < IPA ? (jj & 1 ? s.a1 : s.a0) : (jj & 1 ? s.b1 : s.b0);
+        const uint32_t at = j < IPA ? (uint32_t)(w * IPA + j) * 1024 : TI * 64 + (uint32_t)(w * IPB + j - IPA) * 1024;
+        lmb_load_lds16(base, voff[j], lds0 + (jj & 1 ? st1 : st0) + at);
+    }
+
+    // np pairs of stages; pair(q, Bases&): the bases of pair q, asked for 0, 1, 2 .. in order (and again for the last one)
+    template <typename Pair>
+    __device__ __forceinline__ void run(int np, Pair&& pair) {
+        const int n = lane & 31, hi = lane >> 5, s16 = lane & 15, blk = lane >> 4 & 1, wv = w % WV, wh = w / WV;
+        // lane offsets of the fragments: one a step (k along the rows), or one a tile
+        uint32_t la[AROW ? TVW : 2], lb[BROW ? THW : 2];
+#pragma unroll
+        for (int h = 0; h < (AROW ? TVW : 2); ++h) {
+            if constexpr (AROW) la[h] = lds0 + (8 * hi + (s16 >> 2)) * TI * 2 + ((wv * TVW + h ^ swz(TI, s16 >> 2)) << 6) + 32 * blk + 8 * (s16 & 3);
+            else la[h] = lds0 + (wv * TVW * 32 + n) * 64 + ((2 * h + hi ^ (n >> 2 & 3)) << 4);
+        }
+#pragma unroll
+        for (int h = 0; h < (BROW ? THW : 2); ++h) {
+            if constexpr (BROW) lb[h] = lds0 + TI * 64 + (8 * hi + (s16 >> 2)) * TJ * 2 + ((wh * THW + h ^ swz(TJ, s16 >> 2)) << 6) + 32 * blk + 8 * (s16 & 3);
+            else lb[h] = lds0 + TI * 64 + (wh * THW * 32 + n) * 64 + ((2 * h + hi ^ (n >> 2 & 3)) << 4);
+        }
+        union Frag {
+            s16x4 q[2];
+            bf16x8 v;
+        };
+        Frag fa[2][TVW], fb[2][THW];
+        const auto read = [&](int h, uint32_t sb, int f) {
+            if (f < TVW) {
+                if constexpr (AROW) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        fa[h][f].q[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(la[f % (AROW ? TVW : 2)] + sb + (16 * h + 4 * q) * TI * 2));
+                } else {
+                    fa[h][f].v = *(const lds_bf16x8*)(uintptr_t)(la[h] + sb + f * 2048);
+                }
+            } else {
+                const int t = f - TVW;
+                if constexpr (BROW) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        fb[h][t].q[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(lb[t % (BROW ? THW : 2)] + sb + (16 * h + 4 * q) * TJ * 2));
+                } else {
+                    fb[h][t].v = *(const lds_bf16x8*)(uintptr_t)(lb[h] + sb + t * 2048);
+                }
+            }
+        };
+        constexpr int NF = TVW + THW, NM = TVW * THW;
+#pragma unroll
+        for (int a = 0; a < TVW; ++a)
+#pragma unroll
+            for (int c = 0; c < THW; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][c][i] = 0.f;
+        if (np == 0) return;
+        // half a stage: the products of one MFMA step, behind the first ones the fragments of the next step, between them requests
+        Bases src;
+        const auto half = [&](auto H, uint32_t rsb, auto PART, uint32_t st0, uint32_t st1) {
+            constexpr int h = decltype(H)::value, part = decltype(PART)::value;
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                acc[i % TVW][i / TVW] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][i % TVW].v, fb[h][i / TVW].v, acc[i % TVW][i / TVW], 0, 0, 0);
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+                    if (f * NM / (2 * NF) == i) read(1 - h, rsb, f);
+                if constexpr (part != 0) {
+#pragma unroll
+                    for (int j = 0; j < IPW; ++j)
+                        if (j * NM / IPW == i) issue(src, j + (part == 2 ? IPW : 0), st0, st1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        using I0 = std::integral_constant<int, 0>;
+        using I1 = std::integral_constant<int, 1>;
+        using I2 = std::integral_constant<int, 2>;
+        const auto next = [](uint32_t s) { return s + STAGE == NS * STAGE ? 0u : s + STAGE; };
+        // (a pair past the last one is the last one again, into stages that nobody reads)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            pair(min(q, np - 1), src);
+#pragma unroll
+            for (int jj = 0; jj < 2 * IPW; ++jj) issue(src, jj, 2 * q * STAGE, (2 * q + 1) * STAGE);
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        uint32_t sb = 0;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) read(0, sb, f);
+        for (int q = 0; q < np; ++q) {
+            const uint32_t s1 = next(sb), s2 = next(s1), s3 = next(s2), s4 = next(s3);
+            pair(min(q + 2, np - 1), src);
+            half(I0(), sb, I0(), 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();          // every wavefront has read the pair's first stage to the end: it is free
+            asm volatile("" ::: "memory");
+            half(I1(), s1, I1(), s4, sb);
+            half(I0(), s1, I2(), s4, sb);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPW) : "memory");      // all but the pair just requested has landed
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            half(I1(), s2, I0(), 0, 0);
+            sb = s2;
+        }
+#pragma unroll
+        for (int a = 0; a < TVW; ++a)
+#pragma unroll
+            for (int c = 0; c < THW; ++c) asm volatile("" : "+a"(acc[a][c]));
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // requests into the ring end before the workgroup does
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+};
+
+// ---- dz of a chunk: rows of W along i, hidden rows along j -----------------------------------------------------
+template <int WV, int WH, int TVW, int THW, int TERMS>
+__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
+    using Loop = LmbLoop<false, false, WV, WH, TVW, THW>;
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[Loop::RING];
+    const int M = lmb_rows(p), padded = (M + 63) & ~63;
+    const int ni = (p.n + Loop::TI - 1) / Loop::TI, nj = (padded + Loop::TJ - 1) / Loop::TJ;
+    const int t = lmb_slot(blockIdx.x, ni * nj);
+    if (t < 0) return;
+    int ti, tj;
+    const int gj = min(nj, 8);
+    lmb_tile(t, ni, nj, 32 / gj, gj, ti, tj);
+    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
+    Loop loop(ring);
+    const char* wb = (const char*)(p.w + (int64_t)(p.v0 + i0) * p.w_stride);
+    const char* hb = (const char*)(p.h + (int64_t)j0 * p.Dh);
+    loop.place_a((uint32_t)p.w_stride * 2, p.V - 1 - p.v0 - i0);
+    loop.place_b((uint32_t)p.Dh * 2, padded - 1 - j0);
+    loop.run(p.Dh / 64, [&](int q, typename Loop::Bases& s) {
+        s.a0 = wb + q * 128;
+        s.a1 = s.a0 + 64;
+        s.b0 = hb + q * 128;
+        s.b1 = s.b0 + 64;
+    });
+    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+#pragma unroll
+    for (int c = 0; c < THW; ++c) {
+        const int m = j0 + (wh * THW + c) * 32 + n;
+        if (m >= padded) continue;
+        const LmbRow row = p.rows[m];
+        uint16_t* dst = p.dz + (int64_t)m * p.ldz;
+#pragma unroll
+        for (int a = 0; a < TVW; ++a)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                float d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int v = p.v0 + i + e;
+                    // (the difference first: a logit and lse are large where their difference is not)
+                    const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row.lse) * 1.4426950408889634f);
+                    d[e] = (row.a != 0.f ? row.a * x : 0.f) + (v == row.target ? row.c : 0.f);
+                    if (v == p.forbid || v >= p.V) d[e] = 0.f;
+                }
+                if (i >= p.ldz) continue;
+                const u32x2 top = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
+                *reinterpret_cast<u32x2*>(dst + i) = top;
+                if constexpr (TERMS == 2) {
+                    u32x2 rest;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        rest[e] = pack_bf16x2(d[2 * e] - __uint_as_float(top[e] << 16), d[2 * e + 1] - __uint_as_float(top[e] & 0xffff0000u));
+                    *reinterpret_cast<u32x2*>(dst + p.dz_term + i) = rest;
+                }
+            }
+    }
+}
+
+// ---- d_hidden's and d_w's products of a chunk ----------------------------------------------------------------
+// d_hidden: columns of Dh along i, rows along j, the vocabulary is summed over, in `splits` parts.
+template <int WV, int WH, int TVW, int THW>
+__device__ __forceinline__ void lmb_hidden(const LmbParams& p, unsigned char* ring, int block) {
+    using Loop = LmbLoop<true, false, WV, WH, TVW, THW>;
+    const int M = lmb_rows(p), padded = (M + 63) & ~63;
+    int t = lmb_slot(block, p.ni * p.nj * p.splits);
+    if (t < 0) return;
+    const int s = t / (p.ni * p.nj);
+    int ti, tj;
+    const int gj = min(p.nj, 8);
+    lmb_tile(t - s * p.ni * p.nj, p.ni, p.nj, 32 / gj, gj, ti, tj);
+    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
+    if (j0 >= M) return;
+    const int all = (p.n + 63) >> 6, whole = p.n >> 6;                  // pairs of stages of a term; those that W itself holds
+    const int64_t total = (int64_t)all * p.terms_h;
+    const int q0 = (int)(total * s / p.splits), q1 = (int)(total * (s + 1) / p.splits);
+    Loop loop(ring);
+    bool tail = false;
+    loop.place_a((uint32_t)p.w_stride * 2, p.Dh - 8 - i0);
+    loop.place_b((uint32_t)p.ldz * 2, padded - 1 - j0);
+    loop.run(q1 - q0, [&](int q, typename Loop::Bases& b) {
+        q += q0;
+        const int term = q >= all ? 1 : 0;
+        const int k = q - term * all;
+        if ((k >= whole) != tail) {                                     // into the rows behind the last whole 64, or back
+            tail = !tail;
+            loop.place_a((uint32_t)(tail ? p.Dh : p.w_stride) * 2, p.Dh - 8 - i0);
+        }
+        const int64_t pitch = tail ? p.Dh : p.w_stride;
+        b.a0 = (const char*)(tail ? p.w_tail + i0 : p.w + (int64_t)(p.v0 + 64 * k) * p.w_stride + i0);
+        b.a1 = b.a0 + 64 * pitch;
+        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)j0 * p.ldz + 64 * k);
+        b.b1 = b.b0 + 64;
+    });
+    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+#pragma unroll
+    for (int c = 0; c < THW; ++c) {
+        const int m = j0 + (wh * THW + c) * 32 + n;
+        if (m >= M) continue;
+        float* dst = p.part + ((int64_t)s * p.M + m) * p.Dh;
+#pragma unroll
+        for (int a = 0; a < TVW; ++a)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                if (i >= p.Dh) continue;
+                f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
+                if (p.add) x += *reinterpret_cast<const f32x4*>(dst + i);
+                *reinterpret_cast<f32x4*>(dst + i) = x;
+            }
+    }
+}
+
+// d_w: columns of Dh along i, the chunk's along j, rows are summed over.
+template <int WV, int WH, int TVW, int THW>
+__device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ring, int block) {
+    using Loop = LmbLoop<true, true, WV, WH, TVW, THW>;
+    const int t = lmb_slot(block, p.wi * p.wj);
+    if (t < 0) return;
+    int ti, tj;
+    lmb_tile(t, p.wi, p.wj, 4, 8, ti, tj);
+    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
+    const int all = (lmb_rows(p) + 63) >> 6;
+    Loop loop(ring);
+    loop.place_a((uint32_t)p.Dh * 2, p.Dh - 8 - i0);
+    loop.place_b((uint32_t)p.ldz * 2, p.ldz - 8 - j0);
+    loop.run(all * p.terms_w, [&](int q, typename Loop::Bases& b) {
+        const int term = q >= all ? 1 : 0, k = q - term * all;
+        b.a0 = (const char*)(p.h + (int64_t)64 * k * p.Dh + i0);
+        b.a1 = b.a0 + (int64_t)64 * p.Dh;
+        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)64 * k * p.ldz + j0);
+        b.b1 = b.b0 + (int64_t)64 * p.ldz;
+    });
+    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+#pragma unroll
+    for (int c = 0; c < THW; ++c) {
+        const int v = p.v0 + j0 + (wh * THW + c) * 32 + n;
+        if (v >= p.V || j0 + (wh * THW + c) * 32 + n >= p.n) continue;
+#pragma unroll
+        for (int a = 0; a < TVW; ++a)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                if (i >= p.Dh) continue;
+                f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
+                if (p.dw_f32) {
+                    float* dst = (float*)p.d_w + v * p.dw_stride + i;
+                    if (p.accumulate) x += *reinterpret_cast<const f32x4*>(dst);
+                    *reinterpret_cast<f32x4*>(dst) = x;
+                } else {
+                    uint16_t* dst = (uint16_t*)p.d_w + v * p.dw_stride + i;
+                    if (p.accumulate) {
+                        float old[4];
+                        load_bf16<4>(dst, old);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] += old[e];
+                    }
+                    *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                }
+            }
+    }
+}
+
+// Both in one launch: the workgroups of the second fill the CUs that the last round of the first leaves idle.
+template <int HV, int HH, int HTV, int HTH, int WV, int WH, int WTV, int WTH>
+__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_grad_kernel(LmbParams p) {
+    using A = LmbLoop<true, false, HV, HH, HTV, HTH>;
+    using B = LmbLoop<true, true, WV, WH, WTV, WTH>;
+    static_assert(HV * HH == WV * WH, "one workgroup size");
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[A::RING > B::RING ? A::RING : B::RING];
+    if ((int)blockIdx.x < p.n2) lmb_hidden<HV, HH, HTV, HTH>(p, ring, blockIdx.x);
+    else lmb_weight<WV, WH, WTV, WTH>(p, ring, blockIdx.x - p.n2);
+}
+
+// The parts of d_hidden's sum, in order, into the rows that were selected
+__global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
+    const int r = blockIdx.x;
+    if (r >= lmb_rows(p)) return;
+    const int64_t row = p.row_idx ? p.row_idx[r] : r;
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < p.Dh; c += 1024 * gridDim.y) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
+        if (p.dh_f32) *reinterpret_cast<f32x4*>((float*)p.d_hidden + row * p.dh_stride + c) = x;
+        else *reinterpret_cast<u32x2*>((uint16_t*)p.d_hidden + row * p.dh_stride + c) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------
+constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more rows, fewer columns at a time
+static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
+
+int lmb_set_columns(int v) {
+    if (v < 0 || v % 256) return fail(DLM_ERR_INVALID_ARG, "set_option: lmhead_bwd_columns must be a multiple of 256, or 0");
+    g_lmb_columns = v;
+    return DLM_OK;
+}
+
+struct LmbPlan {
+    int padded, terms, chunk, splits, ni, nj, tj;
+    size_t rows_at, h_at, tail_at, dz_at, part_at, bytes;
+};
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
+    LmbPlan p = {};
+    p.padded = a->M > 0 ? (a->M + 63) & ~63 : 64;
+    const bool two_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32, two_w = a->d_w && a->d_w_type == DLM_ROW_F32;
+    p.terms = two_h || two_w ? 2 : 1;
+    const int64_t whole = ((int64_t)a->V + 255) & ~(int64_t)255;
+    int64_t most = (int64_t)(LMB_DZ_BYTES / ((size_t)p.padded * 2 * p.terms)) & ~(int64_t)255;
+    if (most < 256) most = 256;
+    if (g_lmb_columns > 0 && most > g_lmb_columns) most = g_lmb_columns;
+    p.chunk = (int)(whole < most ? whole : most);
+    p.tj = 256;
+    p.ni = (a->Dh + 255) / 256;
+    p.nj = (p.padded + p.tj - 1) / p.tj;
+    // parts of d_hidden's sum: the number that wastes least of the last round of CUs, each part with some work
+    const int tiles = p.ni * p.nj, pairs = (int)((p.chunk + 63) / 64);
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s <= 64 && s * 4 <= pairs; ++s) {
+        const double rounds = (double)((int64_t)(tiles * s + 255) / 256) / s;       // in times of an undivided tile
+        const double cost = rounds * pairs + 0.02 * s * a->M * (double)a->Dh / 65536;
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    p.splits = best;
+    size_t at = 0;
+    p.rows_at = at;
+    at += up256((size_t)p.padded * sizeof(LmbRow));
+    p.h_at = at;
+    at += up256((size_t)p.padded * a->Dh * 2);
+    p.tail_at = at;
+    at += up256((size_t)64 * a->Dh * 2);
+    p.dz_at = at;
+    at += up256((size_t)p.terms * p.padded * p.chunk * 2);
+    p.part_at = at;
+    if (a->d_hidden) at += up256((size_t)p.splits * a->M * a->Dh * 4);
+    p.bytes = at;
+    return p;
+}
+
+static int validate_lmb(const dlm_lmhead_bwd_args* a, const char* who) {
+    if (!a) return fail(DLM_ERR_INVALID_ARG, "%s: null args", who);
+    if (a->struct_size != sizeof(dlm_lmhead_bwd_args))
+        return fail(DLM_ERR_INVALID_ARG, "%s: struct_size %u != %zu", who, a->struct_size, sizeof(dlm_lmhead_bwd_args));
+    if (a->M < 0 || a->Dh <= 0 || a->V <= 0) return fail(DLM_ERR_INVALID_ARG, "%s: bad sizes M=%d Dh=%d V=%d", who, a->M, a->Dh, a->V);
+    if (a->Dh % 64) return fail(DLM_ERR_UNSUPPORTED, "%s: Dh=%d is not a multiple of 64", who, a->Dh);
+    if (a->M > 1 << 20 || a->Dh > 1 << 16 || a->V > 1 << 24)
+        return fail(DLM_ERR_UNSUPPORTED, "%s: M=%d Dh=%d V=%d (supported: up to 2^20, 2^16, 2^24)", who, a->M, a->Dh, a->V);
+    if (a->forbid_token >= a->V) return fail(DLM_ERR_INVALID_ARG, "%s: forbid_token %d >= V", who, a->forbid_token);
+    if (!(a->inv_temperature > 0.f) || a->inv_temperature > 3.0e38f) return fail(DLM_ERR_INVALID_ARG, "%s: inv_temperature must be positive and finite", who);
+    int rc;
+    if (a->d_hidden) {
+        if ((rc = validate_row_type(a->d_hidden_type, who, "d_hidden")) != DLM_OK) return rc;
+        if ((rc = validate_rows(a->d_hidden, a->d_hidden_stride_row, a->M > 0 ? 2 : 0, a->Dh, row_bytes(a->d_hidden_type), true, who, "d_hidden")) != DLM_OK) return rc;
+    }
+    if (a->d_w) {
+        if ((rc = validate_row_type(a->d_w_type, who, "d_w")) != DLM_OK) return rc;
+        if ((rc = validate_rows(a->d_w, a->d_w_stride_row, a->V, a->Dh, row_bytes(a->d_w_type), true, who, "d_w")) != DLM_OK) return rc;
+    }
+    if (a->M == 0) return DLM_OK;
+    if (!a->d_hidden && !a->d_w) return fail(DLM_ERR_INVALID_ARG, "%s: neither d_hidden nor d_w", who);
+    if (!a->d_lse && !a->d_ztarget) return fail(DLM_ERR_INVALID_ARG, "%s: neither d_lse nor d_ztarget", who);
+    if (a->d_ztarget && !a->target) return fail(DLM_ERR_INVALID_ARG, "%s: d_ztarget needs target", who);
+    if (!a->lse) return fail(DLM_ERR_INVALID_ARG, "%s: null lse", who);
+    if ((rc = validate_rows(a->hidden, a->hidden_stride_row, 2, a->Dh, 2, false, who, "hidden")) != DLM_OK) return rc;
+    if ((rc = validate_rows(a->w, a->w_stride_row, a->V, a->Dh, 2, false, who, "w")) != DLM_OK) return rc;
+    if (a->hidden_stride_row < a->Dh || (a->V > 1 && a->w_stride_row < a->Dh)) return fail(DLM_ERR_INVALID_ARG, "%s: row stride < Dh", who);
+    if (a->V > 1 && a->w_stride_row >= 1 << 23) return fail(DLM_ERR_UNSUPPORTED, "%s: w_stride_row >= 2^23", who);
+    return DLM_OK;
+}
+
+}  // namespace dlm
+
+using namespace dlm;
+
+extern "C" size_t dlm_lmhead_bwd_workspace_bytes(const dlm_lmhead_bwd_args* a) {
+    if (!a || a->struct_size != sizeof(dlm_lmhead_bwd_args) || a->M < 0 || a->Dh <= 0 || a->V <= 0) return 0;
+    return plan_lmb(a).bytes;
+}
+
+extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
+    static const char who[] = "lmhead_bwd";
+    int rc;
+    if ((rc = validate_lmb(a, who)) != DLM_OK) return rc;
+    if (a->M == 0 && (!a->d_w || a->accumulate)) return DLM_OK;
+    const LmbPlan plan = plan_lmb(a);
+    if (!a->workspace || a->workspace_bytes < plan.bytes) return fail(DLM_ERR_WORKSPACE, "%s: workspace of %zu bytes required", who, plan.bytes);
+    if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
+    hipStream_t st = (hipStream_t)stream;
+    char* ws = (char*)a->workspace;
+    LmbParams p = {};
+    p.M = a->M;
+    p.Dh = a->Dh;
+    p.V = a->V;
+    p.m_dev = a->m_dev;
+    p.hidden = (const uint16_t*)a->hidden;
+    p.h_stride = a->hidden_stride_row;
+    p.row_idx = a->row_idx;
+    p.w = (const uint16_t*)a->w;
+    p.w_stride = a->V > 1 ? a->w_stride_row : a->Dh;
+    p.inv_t = a->inv_temperature;
+    p.forbid = a->forbid_token < 0 ? -1 : a->forbid_token;
+    p.scatter = a->out_scatter;
+    p.lse = a->lse;
+    p.d_lse = a->d_lse;
+    p.d_zt = a->d_ztarget;
+    p.target = a->target;
+    p.rows = (LmbRow*)(ws + plan.rows_at);
+    p.h = (uint16_t*)(ws + plan.h_at);
+    p.w_tail = (uint16_t*)(ws + plan.tail_at);
+    p.dz = (uint16_t*)(ws + plan.dz_at);
+    p.ldz = plan.chunk;
+    p.dz_term = (int64_t)plan.padded * plan.chunk;
+    p.part = (float*)(ws + plan.part_at);
+    p.terms_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32 ? 2 : 1;
+    p.terms_w = a->d_w && a->d_w_type == DLM_ROW_F32 ? 2 : 1;
+    p.splits = plan.splits;
+    p.d_hidden = a->d_hidden;
+    p.dh_stride = a->d_hidden_stride_row;
+    p.dh_f32 = a->d_hidden_type == DLM_ROW_F32;
+    p.d_w = a->d_w;
+    p.dw_stride = a->V > 1 ? a->d_w_stride_row : a->Dh;
+    p.dw_f32 = a->d_w_type == DLM_ROW_F32;
+    p.accumulate = a->accumulate;
+    if (a->M > 0) {
+        hipLaunchKernelGGL(lmb_gather_kernel, dim3(plan.padded + (a->V % 64 ? 64 : 0)), dim3(256), 0, st, p);
+        if ((rc = check_hip(hipGetLastError(), "lmb_gather_kernel launch")) != DLM_OK) return rc;
+    }
+    const bool hidden = a->d_hidden && a->M > 0;
+    for (int64_t v0 = 0; v0 < a->V; v0 += plan.chunk) {
+        p.v0 = (int)v0;
+        p.n = (int)(a->V - v0 < plan.chunk ? a->V - v0 : plan.chunk);
+        p.add = v0 > 0;
+        const int vt = (p.n + 255) / 256;
+        if (a->M > 0) {
+            const dim3 grid((unsigned)(((int64_t)vt * ((plan.padded + 255) / 256) + 7) / 8 * 8));
+            if (plan.terms == 2) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 2>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 1>), grid, dim3(256), 0, st, p);
+            if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
+        }
+        p.ni = plan.ni;
+        p.nj = plan.nj;
+        p.n2 = hidden ? (p.ni * p.nj * p.splits + 7) / 8 * 8 : 0;
+        p.wi = plan.ni;
+        p.wj = a->d_w ? vt : 0;
+        const int64_t n3 = ((int64_t)p.wi * p.wj + 7) / 8 * 8;
+        if (p.n2 + n3 == 0) continue;
+        hipLaunchKernelGGL((lmb_grad_kernel<2, 2, 4, 4, 2, 2, 4, 4>), dim3((unsigned)(p.n2 + n3)), dim3(256), 0, st, p);
+        if ((rc = check_hip(hipGetLastError(), "lmb_grad_kernel launch")) != DLM_OK) return rc;
+    }
+    if (!hidden) return DLM_OK;
+    hipLaunchKernelGGL(lmb_join_kernel, dim3(a->M, (a->Dh + 1023) / 1024), dim3(256), 0, st, p);
+    return check_hip(hipGetLastError(), "lmb_join_kernel launch");
+}

@@ -372,6 +372,54 @@ size_t row_norm_bwd_workspace(Args& a) {
     return dlm_row_norm_bwd_workspace_bytes(&s);
 }
 
+// (stream, hidden, w, lse, target, d_ztarget, d_lse, d_hidden, d_w, accumulate, M, row_idx, m_dev, inv_temperature, forbid_token, out_scatter, workspace)
+void lmhead_bwd_args(Args& a, dlm_lmhead_bwd_args& s) {
+    s.struct_size = sizeof s;
+    const at::Tensor &hidden = a.needed(1, "hidden", at::kBFloat16, 2), &w = a.needed(2, "w", at::kBFloat16, 2);
+    a.needed(3, "lse", at::kFloat, 1);
+    const int64_t n = hidden.size(0);
+    s.Dh = size32(hidden.size(1), "hidden");
+    s.V = size32(w.size(0), "w");
+    a.fits(w, "w", {-1, s.Dh});
+    s.hidden = hidden.data_ptr();
+    s.hidden_stride_row = n > 1 ? hidden.stride(0) : s.Dh;
+    s.w = w.data_ptr();
+    s.w_stride_row = w.stride(0);
+    s.row_idx = a.flat<int32_t>(11, "row_idx", at::kInt, {-1});
+    const int64_t listed = s.row_idx ? THPVariable_Unpack(a.v[11]).size(0) : n;
+    s.M = a.v[10] == Py_None ? size32(listed, "row_idx") : a.whole(10);
+    if (s.M > listed) refuse("M", "more rows than there are");
+    s.out_scatter = a.whole(15);
+    const int64_t held = s.out_scatter ? n : s.M;       // entries that are read of the arrays that go with the rows
+    const auto with_rows = [&](int i, const char* name, at::ScalarType type) -> const void* {
+        const void* ptr = a.flat<void>(i, name, type, {-1});
+        if (ptr && THPVariable_Unpack(a.v[i]).size(0) < held) refuse(name, ("at least " + std::to_string(held) + " entries expected").c_str());
+        return ptr;
+    };
+    s.lse = (const float*)with_rows(3, "lse", at::kFloat);
+    s.target = (const int32_t*)with_rows(4, "target", at::kInt);
+    s.d_ztarget = (const float*)with_rows(5, "d_ztarget", at::kFloat);
+    s.d_lse = (const float*)with_rows(6, "d_lse", at::kFloat);
+    rows(a, 7, "d_hidden", n, s.Dh, s.d_hidden, s.d_hidden_stride_row, s.d_hidden_type);
+    if (s.d_hidden && n <= 1) s.d_hidden_stride_row = s.Dh;
+    rows(a, 8, "d_w", s.V, s.Dh, s.d_w, s.d_w_stride_row, s.d_w_type);
+    s.accumulate = a.whole(9);
+    s.m_dev = a.flat<int32_t>(12, "m_dev", at::kInt, {1});
+    s.inv_temperature = (float)a.number(13);
+    s.forbid_token = a.whole(14);
+    a.workspace(16, s.workspace, s.workspace_bytes);
+}
+int lmhead_bwd(Args& a) {
+    dlm_lmhead_bwd_args s = {};
+    lmhead_bwd_args(a, s);
+    return dlm_lmhead_bwd(&s, a.stream());
+}
+size_t lmhead_bwd_workspace(Args& a) {
+    dlm_lmhead_bwd_args s = {};
+    lmhead_bwd_args(a, s);
+    return dlm_lmhead_bwd_workspace_bytes(&s);
+}
+
 template <auto F, int N>
 PyObject* entry(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n != N) return PyErr_Format(PyExc_TypeError, "%d arguments expected", N);
@@ -398,6 +446,8 @@ PyMethodDef methods[] = {
     {"row_norm", (PyCFunction)(void*)entry<row_norm, 9>, METH_FASTCALL, nullptr},
     {"row_norm_bwd", (PyCFunction)(void*)entry<row_norm_bwd, 11>, METH_FASTCALL, nullptr},
     {"row_norm_bwd_workspace", (PyCFunction)(void*)entry<row_norm_bwd_workspace, 2>, METH_FASTCALL, nullptr},
+    {"lmhead_bwd", (PyCFunction)(void*)entry<lmhead_bwd, 17>, METH_FASTCALL, nullptr},
+    {"lmhead_bwd_workspace", (PyCFunction)(void*)entry<lmhead_bwd_workspace, 17>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
