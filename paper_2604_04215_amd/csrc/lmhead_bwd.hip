@@ -10,8 +10,12 @@
 // rows (hidden and W for the logits; dz for d_hidden) or with k across them (W for d_hidden; dz and hidden for d_w), which is
 // turned on the way from LDS into registers by the transposing read, so that nothing is transposed in memory.
 //
-// Rounding of dz: bf16 where the gradient is bf16 (half a step of dz beside half a step of the result: 1.4 times the error of rounding the
-// result alone; a second term would be another product), two bf16 terms, 16 bits, for a product whose result is fp32.
+// Rounding of dz.  One bf16 (8 bits) would make the error of a bf16 gradient 1.4 times that of rounding the gradient alone.  So:
+//   bf16 gradients, many rows: one fp16 term, 11 bits, at the same rate.  Its other operands are fp16 too, exact copies of hidden rows and of W
+//     but for powers of two (see LmbScale), which costs a pass over W: 3 % of the time of 4096 rows.
+//   bf16 gradients, few rows: two bf16 terms, 16 bits: twice the products where reading W takes longest, and no copy of it.
+//   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products added up in two floats (the logits too: an error of one is one of the
+//     probability).  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
 #include "rows.hpp"
 
 namespace dlm {
@@ -19,11 +23,28 @@ namespace dlm {
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 
 struct LmbRow {                    // what the logits' kernel knows of a row
     float lse, a, c;               // a = inv_t d_lse, c = inv_t d_ztarget
     int target;                    // -1: none
 };
+
+// fp16 operands.  With e(x) the exponent of the largest entry of a row (its size lies in [2^e, 2^(e+1))):
+//   h16[m] = h[m] 2^(14 - up[m]),  up[m] = e(h[m]) + u;   w16[v] = w[v] 2^(14 - e(w[v]));   D[m][v] = dz[m][v] 2^(up[m] + e(w[v]) - K)
+//   d_hidden[m] = 2^(K - 14 - up[m]) sum_v D w16;   d_w[v] = 2^(K - 14 - e(w[v])) sum_m D h16
+// K = L + max_v e(w[v]) - 13 keeps D below 2^15, where L = max_m (e(h[m]) + c[m]) and 2^(c + 1) exceeds a row's |d_lse| + |d_ztarget|, inv_t included.
+// u = min(L - e(h[m]) - c[m], 20) brings rows of small gradients up (h keeps its 8 bits in entries of 2^-11 of its largest and more): dz of 2^-8 of the largest
+// of its row keeps all 11 bits while the row's gradient is at most 2^40 below the largest.
+struct LmbScale {
+    int *row_e, *row_c, *up;       // [M rounded up to 64]
+    int* w_e;                      // [V rounded up to 256]
+    int *row_max, *w_max;          // by workgroup
+    int* out;                      // max_v e(w[v]), K
+    uint16_t *h16, *w16, *tail16;
+};
+constexpr int LMB_STATS = 256;     // workgroups that look for a largest exponent
+constexpr int LMB_NONE = -100000;  // exponent of a row of zeros
 
 struct LmbParams {
     int M, Dh, V;
@@ -41,6 +62,8 @@ struct LmbParams {
     LmbRow* rows;                  // [M rounded up to 64]
     uint16_t* h;                   // the selected hidden rows, [M rounded up to 64][Dh], zeros behind the last
     uint16_t* w_tail;              // [64][Dh]: the last V % 64 rows of W, zeros behind them
+    int f16;                       // dz is fp16 and scaled
+    LmbScale sc;
     uint16_t* dz;                  // [terms][M rounded up to 64][ldz]
     int64_t dz_term;               // entries of a term
     int ldz;
@@ -60,10 +83,80 @@ struct LmbParams {
 
 __device__ __forceinline__ int lmb_rows(const LmbParams& p) { return p.m_dev ? min(p.M, max(*p.m_dev, 0)) : p.M; }
 
+// exponent of a row's largest entry, over the 256 threads of a workgroup; NaN and infinities count for nothing
+__device__ __forceinline__ int lmb_exponent(const uint16_t* row, int Dh, float* meet) {
+    float most = 0.f;
+    for (int c = threadIdx.x * 8; c < Dh; c += 2048) {
+        float f[8];
+        load_bf16<8>(row + c, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]) < INFINITY ? fabsf(f[e]) : 0.f);
+    }
+#pragma unroll
+    for (int off = 1; off < WAVE; off *= 2) most = fmaxf(most, shfl_xor(most, off));
+    __syncthreads();
+    if (lane_id() == 0) meet[threadIdx.x >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(meet[0], meet[1]), fmaxf(meet[2], meet[3]));
+    return most > 0.f ? max((int)(__float_as_uint(most) >> 23) - 127, -126) : LMB_NONE;
+}
+// eight entries times 2^k
+__device__ __forceinline__ u32x4 lmb_half8(const uint16_t* src, int k) {
+    float f[8];
+    load_bf16<8>(src, f);
+    f16x8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)ldexpf(f[e], k);
+    return __builtin_bit_cast(u32x4, h);
+}
+
+// fp16 operands, first pass: exponents of the selected rows and of their gradients
+__global__ __launch_bounds__(256) void lmb_stat_kernel(LmbParams p) {
+    __shared__ float meet[4];
+    const int M = lmb_rows(p);
+    int most = LMB_NONE;
+    for (int r = blockIdx.x; r < M; r += gridDim.x) {
+        const int row = p.row_idx ? p.row_idx[r] : r, at = p.scatter ? row : r;
+        const float a = p.d_lse ? fabsf(p.d_lse[at] * p.inv_t) : 0.f, b = p.d_zt ? fabsf(p.d_zt[at] * p.inv_t) : 0.f, g = a + b;
+        const int e = lmb_exponent(p.hidden + row * p.h_stride, p.Dh, meet);
+        const int c = g > 0.f && g < INFINITY ? max((int)(__float_as_uint(g) >> 23) - 127, -126) : LMB_NONE;
+        if (threadIdx.x == 0) {
+            p.sc.row_e[r] = e;
+            p.sc.row_c[r] = c;
+        }
+        if (e != LMB_NONE && c != LMB_NONE) most = max(most, e + c);
+    }
+    if (threadIdx.x == 0) p.sc.row_max[blockIdx.x] = most;
+}
+__device__ __forceinline__ int lmb_most(const int* v, int n) {
+    int m = LMB_NONE;
+    for (int i = threadIdx.x & 63; i < n; i += WAVE) m = max(m, v[i]);
+#pragma unroll
+    for (int off = 1; off < WAVE; off *= 2) m = max(m, shfl_xor(m, off));
+    return m;
+}
+
 // Selected hidden rows side by side, what belongs to them, and the rows of W behind the last whole 64: the products then read whole tiles.
+// fp16: the scaled copies of both, and of all of W.
 __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
+    __shared__ float meet[4];
     const int M = lmb_rows(p), bound = (p.M + 63) & ~63, r = blockIdx.x;
     if (r >= bound) {
+        if (p.f16) {
+            int most = LMB_NONE;
+            const int padded = (p.V + 63) & ~63, whole = p.V & ~63;
+            for (int v = r - bound; v < padded; v += LMB_STATS * 8) {
+                uint16_t* dst = v < whole ? p.sc.w16 + (int64_t)v * p.Dh : p.sc.tail16 + (int64_t)(v - whole) * p.Dh;
+                const uint16_t* src = p.w + min(v, p.V - 1) * p.w_stride;
+                const int e = v < p.V ? lmb_exponent(src, p.Dh, meet) : LMB_NONE;
+                if (v < p.V && threadIdx.x == 0) p.sc.w_e[v] = e;
+                most = max(most, e);
+                for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
+                    *reinterpret_cast<u32x4*>(dst + c) = e != LMB_NONE ? lmb_half8(src + c, 14 - e) : u32x4{0, 0, 0, 0};
+            }
+            if (threadIdx.x == 0) p.sc.w_max[r - bound] = most;
+            return;
+        }
         const int t = r - bound, v = (p.V & ~63) + t;
         for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
             *reinterpret_cast<u32x4*>(p.w_tail + (int64_t)t * p.Dh + c) =
@@ -73,9 +166,16 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     if (r >= ((M + 63) & ~63)) return;
     const bool live = r < M;
     const int row = !live ? 0 : p.row_idx ? p.row_idx[r] : r;
-    for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
-        *reinterpret_cast<u32x4*>(p.h + (int64_t)r * p.Dh + c) =
-            live ? *reinterpret_cast<const u32x4*>(p.hidden + row * p.h_stride + c) : u32x4{0, 0, 0, 0};
+    int up = 0;
+    if (p.f16 && live) {
+        const int e = p.sc.row_e[r], c = p.sc.row_c[r], most = lmb_most(p.sc.row_max, LMB_STATS);
+        up = e == LMB_NONE ? 0 : e + (c == LMB_NONE ? 0 : min(max(most - e - c, 0), 20));
+    }
+    for (int c = threadIdx.x * 8; c < p.Dh; c += 2048) {
+        const uint16_t* src = p.hidden + row * p.h_stride + c;
+        *reinterpret_cast<u32x4*>(p.h + (int64_t)r * p.Dh + c) = live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0};
+        if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = live ? lmb_half8(src, 14 - up) : u32x4{0, 0, 0, 0};
+    }
     if (threadIdx.x == 0) {
         LmbRow o = {0.f, 0.f, 0.f, -1};
         if (live) {
@@ -88,6 +188,15 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
             }
         }
         p.rows[r] = o;
+        if (p.f16) p.sc.up[r] = up;
+    }
+}
+// K, from what the workgroups found
+__global__ __launch_bounds__(WAVE) void lmb_scale_kernel(LmbParams p) {
+    const int L = lmb_most(p.sc.row_max, LMB_STATS), S = lmb_most(p.sc.w_max, LMB_STATS * 8);
+    if (threadIdx.x == 0) {
+        p.sc.out[0] = S == LMB_NONE ? 0 : S;
+        p.sc.out[1] = (L == LMB_NONE ? 0 : L) + (S == LMB_NONE ? 0 : S) - 13;
     }
 }
 
@@ -123,7 +232,9 @@ __device__ __forceinline__ void lmb_load_lds16(const void* base, uint32_t offset
 //   k along the rows: rows of 64 bytes; 16-byte piece c of row r in place c ^ (r / 4 % 4).
 //   k across the rows: 32 rows of 2 TILE bytes; 64-byte piece c of row k in place c ^ (k % 4) (TILE = 64: c ^ (k / 2 % 2), TILE = 32: c), so that the four
 //   rows that a transposing read touches lie in different banks.
-template <bool AROW, bool BROW, int WV, int WH, int TVW, int THW>
+//
+// BLOCK > 0: the sums of so many pairs of stages are added up in two floats (a sum, and what its roundings lost).
+template <bool AROW, bool BROW, bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 struct LmbLoop {
     static constexpr int NW = WV * WH, TI = 32 * TVW * WV, TJ = 32 * THW * WH, STAGE = (TI + TJ) * 64, NS = 5, RING = NS * STAGE;
     static constexpr int IPA = TI / 16 / NW, IPB = TJ / 16 / NW, IPW = IPA + IPB;      // requests of a wavefront and stage
@@ -195,6 +306,7 @@ struct LmbLoop {
         union Frag {
             s16x4 q[2];
             bf16x8 v;
+            f16x8 f;
         };
         Frag fa[2][TVW], fb[2][THW];
         const auto read = [&](int h, uint32_t sb, int f) {
@@ -224,6 +336,14 @@ struct LmbLoop {
             for (int c = 0; c < THW; ++c)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[a][c][i] = 0.f;
+        constexpr int BV = BLOCK > 0 ? TVW : 1, BH = BLOCK > 0 ? THW : 1;
+        f32x16 sum[BV][BH], lost[BV][BH];
+        if constexpr (BLOCK > 0) {
+#pragma unroll
+            for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                for (int c = 0; c < THW; ++c) sum[a][c] = lost[a][c] = acc[a][c];
+        }
         if (np == 0) return;
         // half a stage: the products of one MFMA step, behind the first ones the fragments of the next step, between them requests
         Bases src;
@@ -231,7 +351,9 @@ struct LmbLoop {
             constexpr int h = decltype(H)::value, part = decltype(PART)::value;
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
-                acc[i % TVW][i / TVW] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][i % TVW].v, fb[h][i / TVW].v, acc[i % TVW][i / TVW], 0, 0, 0);
+                f32x16& x = acc[i % TVW][i / TVW];
+                if constexpr (F16) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[h][i % TVW].f, fb[h][i / TVW].f, x, 0, 0, 0);
+                else x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][i % TVW].v, fb[h][i / TVW].v, x, 0, 0, 0);
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
                     if (f * NM / (2 * NF) == i) read(1 - h, rsb, f);
@@ -260,20 +382,43 @@ struct LmbLoop {
         uint32_t sb = 0;
 #pragma unroll
         for (int f = 0; f < NF; ++f) read(0, sb, f);
-        for (int q = 0; q < np; ++q) {
-            const uint32_t s1 = next(sb), s2 = next(s1), s3 = next(s2), s4 = next(s3);
-            pair(min(q + 2, np - 1), src);
-            half(I0(), sb, I0(), 0, 0);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();          // every wavefront has read the pair's first stage to the end: it is free
-            asm volatile("" ::: "memory");
-            half(I1(), s1, I1(), s4, sb);
-            half(I0(), s1, I2(), s4, sb);
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPW) : "memory");      // all but the pair just requested has landed
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            half(I1(), s2, I0(), 0, 0);
-            sb = s2;
+        for (int q = 0; q < np;) {
+            const int end = BLOCK > 0 ? min(q + BLOCK, np) : np;
+#pragma unroll 1
+            for (; q < end; ++q) {
+                const uint32_t s1 = next(sb), s2 = next(s1), s3 = next(s2), s4 = next(s3);
+                pair(min(q + 2, np - 1), src);
+                half(I0(), sb, I0(), 0, 0);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();      // every wavefront has read the pair's first stage to the end: it is free
+                asm volatile("" ::: "memory");
+                half(I1(), s1, I1(), s4, sb);
+                half(I0(), s1, I2(), s4, sb);
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPW) : "memory");      // all but the pair just requested has landed
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                half(I1(), s2, I0(), 0, 0);
+                sb = s2;
+            }
+            if constexpr (BLOCK > 0) {
+#pragma unroll
+                for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                    for (int c = 0; c < THW; ++c)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = acc[a][c][i], s = sum[a][c][i], t = s + x, y = t - s;
+                            lost[a][c][i] += (s - (t - y)) + (x - y);
+                            sum[a][c][i] = t;
+                            acc[a][c][i] = 0.f;
+                        }
+            }
+        }
+        if constexpr (BLOCK > 0) {
+#pragma unroll
+            for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                for (int c = 0; c < THW; ++c) acc[a][c] = sum[a][c] + lost[a][c];
         }
 #pragma unroll
         for (int a = 0; a < TVW; ++a)
@@ -286,9 +431,10 @@ struct LmbLoop {
 };
 
 // ---- dz of a chunk: rows of W along i, hidden rows along j -----------------------------------------------------
-template <int WV, int WH, int TVW, int THW, int TERMS>
+// TERMS bf16 terms; 0: one scaled fp16.
+template <int WV, int WH, int TVW, int THW, int TERMS, int BLOCK>
 __global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
-    using Loop = LmbLoop<false, false, WV, WH, TVW, THW>;
+    using Loop = LmbLoop<false, false, false, BLOCK, WV, WH, TVW, THW>;
     __shared__ __attribute__((aligned(1024))) unsigned char ring[Loop::RING];
     const int M = lmb_rows(p), padded = (M + 63) & ~63;
     const int ni = (p.n + Loop::TI - 1) / Loop::TI, nj = (padded + Loop::TJ - 1) / Loop::TJ;
@@ -310,45 +456,67 @@ __global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
         s.b1 = s.b0 + 64;
     });
     const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+    const int none = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
+    LmbRow row[THW];
+    int up[THW];
 #pragma unroll
     for (int c = 0; c < THW; ++c) {
-        const int m = j0 + (wh * THW + c) * 32 + n;
-        if (m >= padded) continue;
-        const LmbRow row = p.rows[m];
-        uint16_t* dst = p.dz + (int64_t)m * p.ldz;
+        const int m = min(j0 + (wh * THW + c) * 32 + n, padded - 1);
+        row[c] = p.rows[m];
+        up[c] = TERMS == 0 ? p.sc.up[m] - K : 0;
+    }
 #pragma unroll
-        for (int a = 0; a < TVW; ++a)
+    for (int a = 0; a < TVW; ++a)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+        for (int g = 0; g < 4; ++g) {
+            const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+            if (i >= p.ldz) continue;
+            typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+            i32x4 we = {0, 0, 0, 0};
+            if constexpr (TERMS == 0) {
+                we = *reinterpret_cast<const i32x4*>(p.sc.w_e + p.v0 + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) we[e] = we[e] == LMB_NONE ? none : we[e];
+            }
+#pragma unroll
+            for (int c = 0; c < THW; ++c) {
+                const int m = j0 + (wh * THW + c) * 32 + n;
+                uint16_t* dst = p.dz + (int64_t)m * p.ldz + i;
                 float d[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int v = p.v0 + i + e;
                     // (the difference first: a logit and lse are large where their difference is not)
-                    const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row.lse) * 1.4426950408889634f);
-                    d[e] = (row.a != 0.f ? row.a * x : 0.f) + (v == row.target ? row.c : 0.f);
+                    const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row[c].lse) * 1.4426950408889634f);
+                    d[e] = (row[c].a != 0.f ? row[c].a * x : 0.f) + (v == row[c].target ? row[c].c : 0.f);
                     if (v == p.forbid || v >= p.V) d[e] = 0.f;
                 }
-                if (i >= p.ldz) continue;
-                const u32x2 top = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
-                *reinterpret_cast<u32x2*>(dst + i) = top;
-                if constexpr (TERMS == 2) {
-                    u32x2 rest;
+                if (m >= padded) continue;
+                if constexpr (TERMS == 0) {
+                    typedef __attribute__((__vector_size__(4 * sizeof(_Float16)))) _Float16 f16x4;
+                    f16x4 q;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        rest[e] = pack_bf16x2(d[2 * e] - __uint_as_float(top[e] << 16), d[2 * e + 1] - __uint_as_float(top[e] & 0xffff0000u));
-                    *reinterpret_cast<u32x2*>(dst + p.dz_term + i) = rest;
+                    for (int e = 0; e < 4; ++e) q[e] = (_Float16)ldexpf(d[e], up[c] + we[e]);
+                    *reinterpret_cast<u32x2*>(dst) = __builtin_bit_cast(u32x2, q);
+                } else {
+                    // every term what the ones before it leave, which fp32 holds exactly
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {
+                        const u32x2 q = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
+                        *reinterpret_cast<u32x2*>(dst + k * p.dz_term) = q;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) d[e] -= __uint_as_float(e & 1 ? q[e / 2] & 0xffff0000u : q[e / 2] << 16);
+                    }
                 }
             }
-    }
+        }
 }
 
 // ---- d_hidden's and d_w's products of a chunk ----------------------------------------------------------------
 // d_hidden: columns of Dh along i, rows along j, the vocabulary is summed over, in `splits` parts.
-template <int WV, int WH, int TVW, int THW>
+template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 __device__ __forceinline__ void lmb_hidden(const LmbParams& p, unsigned char* ring, int block) {
-    using Loop = LmbLoop<true, false, WV, WH, TVW, THW>;
+    using Loop = LmbLoop<true, false, F16, BLOCK, WV, WH, TVW, THW>;
     const int M = lmb_rows(p), padded = (M + 63) & ~63;
     int t = lmb_slot(block, p.ni * p.nj * p.splits);
     if (t < 0) return;
@@ -363,18 +531,20 @@ __device__ __forceinline__ void lmb_hidden(const LmbParams& p, unsigned char* ri
     const int q0 = (int)(total * s / p.splits), q1 = (int)(total * (s + 1) / p.splits);
     Loop loop(ring);
     bool tail = false;
-    loop.place_a((uint32_t)p.w_stride * 2, p.Dh - 8 - i0);
+    const uint16_t *w = F16 ? p.sc.w16 : p.w, *w_tail = F16 ? p.sc.tail16 : p.w_tail;
+    const int64_t w_stride = F16 ? p.Dh : p.w_stride;
+    loop.place_a((uint32_t)w_stride * 2, p.Dh - 8 - i0);
     loop.place_b((uint32_t)p.ldz * 2, padded - 1 - j0);
     loop.run(q1 - q0, [&](int q, typename Loop::Bases& b) {
         q += q0;
-        const int term = q >= all ? 1 : 0;
+        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0);
         const int k = q - term * all;
         if ((k >= whole) != tail) {                                     // into the rows behind the last whole 64, or back
             tail = !tail;
-            loop.place_a((uint32_t)(tail ? p.Dh : p.w_stride) * 2, p.Dh - 8 - i0);
+            loop.place_a((uint32_t)(tail ? p.Dh : w_stride) * 2, p.Dh - 8 - i0);
         }
-        const int64_t pitch = tail ? p.Dh : p.w_stride;
-        b.a0 = (const char*)(tail ? p.w_tail + i0 : p.w + (int64_t)(p.v0 + 64 * k) * p.w_stride + i0);
+        const int64_t pitch = tail ? p.Dh : w_stride;
+        b.a0 = (const char*)(tail ? w_tail + i0 : w + (int64_t)(p.v0 + 64 * k) * w_stride + i0);
         b.a1 = b.a0 + 64 * pitch;
         b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)j0 * p.ldz + 64 * k);
         b.b1 = b.b0 + 64;
@@ -399,21 +569,22 @@ __device__ __forceinline__ void lmb_hidden(const LmbParams& p, unsigned char* ri
 }
 
 // d_w: columns of Dh along i, the chunk's along j, rows are summed over.
-template <int WV, int WH, int TVW, int THW>
+template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 __device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ring, int block) {
-    using Loop = LmbLoop<true, true, WV, WH, TVW, THW>;
+    using Loop = LmbLoop<true, true, F16, BLOCK, WV, WH, TVW, THW>;
     const int t = lmb_slot(block, p.wi * p.wj);
     if (t < 0) return;
     int ti, tj;
     lmb_tile(t, p.wi, p.wj, 4, 8, ti, tj);
     const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
     const int all = (lmb_rows(p) + 63) >> 6;
+    const uint16_t* h = F16 ? p.sc.h16 : p.h;
     Loop loop(ring);
     loop.place_a((uint32_t)p.Dh * 2, p.Dh - 8 - i0);
     loop.place_b((uint32_t)p.ldz * 2, p.ldz - 8 - j0);
     loop.run(all * p.terms_w, [&](int q, typename Loop::Bases& b) {
-        const int term = q >= all ? 1 : 0, k = q - term * all;
-        b.a0 = (const char*)(p.h + (int64_t)64 * k * p.Dh + i0);
+        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
+        b.a0 = (const char*)(h + (int64_t)64 * k * p.Dh + i0);
         b.a1 = b.a0 + (int64_t)64 * p.Dh;
         b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)64 * k * p.ldz + j0);
         b.b1 = b.b0 + (int64_t)64 * p.ldz;
@@ -423,6 +594,11 @@ __device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ri
     for (int c = 0; c < THW; ++c) {
         const int v = p.v0 + j0 + (wh * THW + c) * 32 + n;
         if (v >= p.V || j0 + (wh * THW + c) * 32 + n >= p.n) continue;
+        int scale = 0;
+        if (F16 && all > 0) {
+            const int e = p.sc.w_e[v];
+            scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
+        }
 #pragma unroll
         for (int a = 0; a < TVW; ++a)
 #pragma unroll
@@ -430,6 +606,10 @@ __device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ri
                 const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
                 if (i >= p.Dh) continue;
                 f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
+                if constexpr (F16) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
+                }
                 if (p.dw_f32) {
                     float* dst = (float*)p.d_w + v * p.dw_stride + i;
                     if (p.accumulate) x += *reinterpret_cast<const f32x4*>(dst);
@@ -449,14 +629,11 @@ __device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ri
 }
 
 // Both in one launch: the workgroups of the second fill the CUs that the last round of the first leaves idle.
-template <int HV, int HH, int HTV, int HTH, int WV, int WH, int WTV, int WTH>
+template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 __global__ __launch_bounds__(64 * WV * WH, 1) void lmb_grad_kernel(LmbParams p) {
-    using A = LmbLoop<true, false, HV, HH, HTV, HTH>;
-    using B = LmbLoop<true, true, WV, WH, WTV, WTH>;
-    static_assert(HV * HH == WV * WH, "one workgroup size");
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[A::RING > B::RING ? A::RING : B::RING];
-    if ((int)blockIdx.x < p.n2) lmb_hidden<HV, HH, HTV, HTH>(p, ring, blockIdx.x);
-    else lmb_weight<WV, WH, WTV, WTH>(p, ring, blockIdx.x - p.n2);
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[LmbLoop<true, true, F16, BLOCK, WV, WH, TVW, THW>::RING];
+    if ((int)blockIdx.x < p.n2) lmb_hidden<F16, BLOCK, WV, WH, TVW, THW>(p, ring, blockIdx.x);
+    else lmb_weight<F16, BLOCK, WV, WH, TVW, THW>(p, ring, blockIdx.x - p.n2);
 }
 
 // The parts of d_hidden's sum, in order, into the rows that were selected
@@ -467,6 +644,11 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < p.Dh; c += 1024 * gridDim.y) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
+        if (p.f16) {
+            const int scale = p.sc.out[1] - 14 - p.sc.up[r];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
+        }
         if (p.dh_f32) *reinterpret_cast<f32x4*>((float*)p.d_hidden + row * p.dh_stride + c) = x;
         else *reinterpret_cast<u32x2*>((uint16_t*)p.d_hidden + row * p.dh_stride + c) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
     }
@@ -474,6 +656,8 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 
 // ---- host ---------------------------------------------------------------------------------------------------
 constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more rows, fewer columns at a time
+// Up to so many rows two bf16 terms take less time than the pass over W that fp16 needs
+constexpr int LMB_FEW = 256;
 static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
 
 int lmb_set_columns(int v) {
@@ -483,30 +667,33 @@ int lmb_set_columns(int v) {
 }
 
 struct LmbPlan {
-    int padded, terms, chunk, splits, ni, nj, tj;
-    size_t rows_at, h_at, tail_at, dz_at, part_at, bytes;
+    int padded, terms_h, terms_w, terms, f16, tile, chunk, splits, ni, nj;
+    size_t rows_at, h_at, tail_at, dz_at, part_at, h16_at, w16_at, ints_at, bytes;
 };
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     LmbPlan p = {};
     p.padded = a->M > 0 ? (a->M + 63) & ~63 : 64;
-    const bool two_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32, two_w = a->d_w && a->d_w_type == DLM_ROW_F32;
-    p.terms = two_h || two_w ? 2 : 1;
+    const bool wide_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32, wide_w = a->d_w && a->d_w_type == DLM_ROW_F32, wide = wide_h || wide_w;
+    p.f16 = !wide && a->M > LMB_FEW;
+    p.terms_h = p.f16 ? 1 : wide_h ? 3 : 2;
+    p.terms_w = p.f16 ? 1 : wide_w ? 3 : 2;
+    p.terms = p.f16 ? 1 : wide ? 3 : 2;
+    p.tile = wide ? 128 : 256;
     const int64_t whole = ((int64_t)a->V + 255) & ~(int64_t)255;
     int64_t most = (int64_t)(LMB_DZ_BYTES / ((size_t)p.padded * 2 * p.terms)) & ~(int64_t)255;
     if (most < 256) most = 256;
     if (g_lmb_columns > 0 && most > g_lmb_columns) most = g_lmb_columns;
     p.chunk = (int)(whole < most ? whole : most);
-    p.tj = 256;
-    p.ni = (a->Dh + 255) / 256;
-    p.nj = (p.padded + p.tj - 1) / p.tj;
+    p.ni = (a->Dh + p.tile - 1) / p.tile;
+    p.nj = (p.padded + p.tile - 1) / p.tile;
     // parts of d_hidden's sum: the number that wastes least of the last round of CUs, each part with some work
     const int tiles = p.ni * p.nj, pairs = (int)((p.chunk + 63) / 64);
     int best = 1;
     double least = 1e30;
     for (int s = 1; s <= 64 && s * 4 <= pairs; ++s) {
-        const double rounds = (double)((int64_t)(tiles * s + 255) / 256) / s;       // in times of an undivided tile
+        const double rounds = (double)(((int64_t)tiles * s + 255) / 256) / s;       // in times of an undivided tile
         const double cost = rounds * pairs + 0.02 * s * a->M * (double)a->Dh / 65536;
         if (cost < least) {
             least = cost;
@@ -515,16 +702,21 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     }
     p.splits = best;
     size_t at = 0;
-    p.rows_at = at;
-    at += up256((size_t)p.padded * sizeof(LmbRow));
-    p.h_at = at;
-    at += up256((size_t)p.padded * a->Dh * 2);
-    p.tail_at = at;
-    at += up256((size_t)64 * a->Dh * 2);
-    p.dz_at = at;
-    at += up256((size_t)p.terms * p.padded * p.chunk * 2);
-    p.part_at = at;
-    if (a->d_hidden) at += up256((size_t)p.splits * a->M * a->Dh * 4);
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    p.rows_at = take((size_t)p.padded * sizeof(LmbRow));
+    p.h_at = take((size_t)p.padded * a->Dh * 2);
+    p.tail_at = take((size_t)64 * a->Dh * 2);
+    p.dz_at = take((size_t)p.terms * p.padded * p.chunk * 2);
+    if (a->d_hidden) p.part_at = take((size_t)p.splits * a->M * a->Dh * 4);
+    if (p.f16) {
+        p.h16_at = take((size_t)p.padded * a->Dh * 2);
+        p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
+        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 9 + 2) * 4);
+    }
     p.bytes = at;
     return p;
 }
@@ -603,8 +795,22 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
     p.ldz = plan.chunk;
     p.dz_term = (int64_t)plan.padded * plan.chunk;
     p.part = (float*)(ws + plan.part_at);
-    p.terms_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32 ? 2 : 1;
-    p.terms_w = a->d_w && a->d_w_type == DLM_ROW_F32 ? 2 : 1;
+    p.terms_h = plan.terms_h;
+    p.terms_w = plan.terms_w;
+    p.f16 = plan.f16;
+    if (plan.f16) {
+        int* ints = (int*)(ws + plan.ints_at);
+        p.sc.row_e = ints;
+        p.sc.row_c = ints + plan.padded;
+        p.sc.up = ints + 2 * (int64_t)plan.padded;
+        p.sc.w_e = ints + 3 * (int64_t)plan.padded;
+        p.sc.row_max = p.sc.w_e + ((int64_t)a->V + 255) / 256 * 256;
+        p.sc.w_max = p.sc.row_max + LMB_STATS;
+        p.sc.out = p.sc.w_max + LMB_STATS * 8;
+        p.sc.h16 = (uint16_t*)(ws + plan.h16_at);
+        p.sc.w16 = (uint16_t*)(ws + plan.w16_at);
+        p.sc.tail16 = p.w_tail;
+    }
     p.splits = plan.splits;
     p.d_hidden = a->d_hidden;
     p.dh_stride = a->d_hidden_stride_row;
@@ -614,19 +820,29 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
     p.dw_f32 = a->d_w_type == DLM_ROW_F32;
     p.accumulate = a->accumulate;
     if (a->M > 0) {
-        hipLaunchKernelGGL(lmb_gather_kernel, dim3(plan.padded + (a->V % 64 ? 64 : 0)), dim3(256), 0, st, p);
+        if (plan.f16) {
+            hipLaunchKernelGGL(lmb_stat_kernel, dim3(LMB_STATS), dim3(256), 0, st, p);
+            if ((rc = check_hip(hipGetLastError(), "lmb_stat_kernel launch")) != DLM_OK) return rc;
+        }
+        const int more = plan.f16 ? LMB_STATS * 8 : a->V % 64 ? 64 : 0;
+        hipLaunchKernelGGL(lmb_gather_kernel, dim3(plan.padded + more), dim3(256), 0, st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_gather_kernel launch")) != DLM_OK) return rc;
+        if (plan.f16) {
+            hipLaunchKernelGGL(lmb_scale_kernel, dim3(1), dim3(WAVE), 0, st, p);
+            if ((rc = check_hip(hipGetLastError(), "lmb_scale_kernel launch")) != DLM_OK) return rc;
+        }
     }
     const bool hidden = a->d_hidden && a->M > 0;
     for (int64_t v0 = 0; v0 < a->V; v0 += plan.chunk) {
         p.v0 = (int)v0;
         p.n = (int)(a->V - v0 < plan.chunk ? a->V - v0 : plan.chunk);
         p.add = v0 > 0;
-        const int vt = (p.n + 255) / 256;
+        const int vt = (p.n + plan.tile - 1) / plan.tile;
         if (a->M > 0) {
-            const dim3 grid((unsigned)(((int64_t)vt * ((plan.padded + 255) / 256) + 7) / 8 * 8));
-            if (plan.terms == 2) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 2>), grid, dim3(256), 0, st, p);
-            else hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 1>), grid, dim3(256), 0, st, p);
+            const dim3 grid((unsigned)(((int64_t)vt * plan.nj + 7) / 8 * 8));
+            if (plan.terms == 3) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 2, 2, 3, 4>), grid, dim3(256), 0, st, p);
+            else if (plan.terms == 2) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 2, 0>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 0, 0>), grid, dim3(256), 0, st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
         }
         p.ni = plan.ni;
@@ -636,7 +852,10 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.wj = a->d_w ? vt : 0;
         const int64_t n3 = ((int64_t)p.wi * p.wj + 7) / 8 * 8;
         if (p.n2 + n3 == 0) continue;
-        hipLaunchKernelGGL((lmb_grad_kernel<2, 2, 4, 4, 2, 2, 4, 4>), dim3((unsigned)(p.n2 + n3)), dim3(256), 0, st, p);
+        const dim3 grid((unsigned)(p.n2 + n3));
+        if (plan.terms == 3) hipLaunchKernelGGL((lmb_grad_kernel<false, 4, 2, 2, 2, 2>), grid, dim3(256), 0, st, p);
+        else if (plan.terms == 2) hipLaunchKernelGGL((lmb_grad_kernel<false, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((lmb_grad_kernel<true, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_grad_kernel launch")) != DLM_OK) return rc;
     }
     if (!hidden) return DLM_OK;
