@@ -39,7 +39,7 @@ struct LmbRow {                    // what the logits' kernel knows of a row
 struct LmbScale {
     int *row_e, *row_c, *up;       // [M rounded up to 64]
     int* w_e;                      // [V rounded up to 256]
-    int *row_max, *w_max;          // by workgroup
+    int *row_max, *w_max;          // by workgroup, by wavefront
     int* out;                      // max_v e(w[v]), K
     uint16_t *h16, *w16, *tail16;
 };
@@ -70,9 +70,10 @@ struct LmbParams {
     float* part;                   // [splits][M][Dh]
     // the chunk: columns v0 .. v0 + n of dz, n a multiple of 64 but for the end of the vocabulary
     int v0, n, terms_h, terms_w, add;      // add: d_hidden's partial sums are there already
-    int ni, nj, splits;            // tiles of d_hidden: along Dh, along the rows; parts of its sum
-    int n2;                        // workgroups of d_hidden (a multiple of 8)
-    int wi, wj;                    // tiles of d_w: along Dh, along the chunk
+    int splits;                    // parts of d_hidden's sum
+    int n2;                        // workgroups of d_hidden (a multiple of 8), where each takes one tile; 0: it is not wanted
+    int queued;                    // workgroups take one tile after the other
+    int* counters;                 // of three lists of tiles: dz, d_hidden, d_w
     void* d_hidden;
     int64_t dh_stride;
     int dh_f32;
@@ -81,55 +82,59 @@ struct LmbParams {
     int dw_f32, accumulate;
 };
 
-__device__ __forceinline__ int lmb_rows(const LmbParams& p) { return p.m_dev ? min(p.M, max(*p.m_dev, 0)) : p.M; }
+__device__ __forceinline__ int lmb_rows(const LmbParams& p) { return p.m_dev ? min(p.M, max(__builtin_amdgcn_readfirstlane(*p.m_dev), 0)) : p.M; }
 
-// exponent of a row's largest entry, over the 256 threads of a workgroup; NaN and infinities count for nothing
-__device__ __forceinline__ int lmb_exponent(const uint16_t* row, int Dh, float* meet) {
-    float most = 0.f;
-    for (int c = threadIdx.x * 8; c < Dh; c += 2048) {
-        float f[8];
-        load_bf16<8>(row + c, f);
+// the largest size of eight entries; NaN and infinities count for nothing
+__device__ __forceinline__ float lmb_top8(u32x4 v) {
+    float f[8], top = 0.f;
+    Piece<false>::open(v, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]) < INFINITY ? fabsf(f[e]) : 0.f);
-    }
-#pragma unroll
-    for (int off = 1; off < WAVE; off *= 2) most = fmaxf(most, shfl_xor(most, off));
-    __syncthreads();
-    if (lane_id() == 0) meet[threadIdx.x >> 6] = most;
-    __syncthreads();
-    most = fmaxf(fmaxf(meet[0], meet[1]), fmaxf(meet[2], meet[3]));
-    return most > 0.f ? max((int)(__float_as_uint(most) >> 23) - 127, -126) : LMB_NONE;
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]) < INFINITY ? fabsf(f[e]) : 0.f);
+    return top;
 }
-// eight entries times 2^k
-__device__ __forceinline__ u32x4 lmb_half8(const uint16_t* src, int k) {
+// the exponent of the largest of a wavefront's sizes
+__device__ __forceinline__ int lmb_exponent(float top) {
+#pragma unroll
+    for (int off = 1; off < WAVE; off *= 2) top = fmaxf(top, shfl_xor(top, off));
+    return top > 0.f ? max((int)(__float_as_uint(top) >> 23) - 127, -126) : LMB_NONE;
+}
+// eight entries times 2^k, zeros if not `any`
+__device__ __forceinline__ u32x4 lmb_half8(u32x4 v, bool any, int k) {
     float f[8];
-    load_bf16<8>(src, f);
+    Piece<false>::open(v, f);
     f16x8 h;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = (_Float16)ldexpf(f[e], k);
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)(any ? ldexpf(f[e], k) : 0.f);
     return __builtin_bit_cast(u32x4, h);
 }
 
-// fp16 operands, first pass: exponents of the selected rows and of their gradients
+// fp16 operands, first pass: exponents of the selected rows and of their gradients, a wavefront a row
 __global__ __launch_bounds__(256) void lmb_stat_kernel(LmbParams p) {
-    __shared__ float meet[4];
-    const int M = lmb_rows(p);
+    __shared__ int meet[4];
+    const int M = lmb_rows(p), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int most = LMB_NONE;
-    for (int r = blockIdx.x; r < M; r += gridDim.x) {
+    for (int r = blockIdx.x * 4 + wave; r < M; r += gridDim.x * 4) {
         const int row = p.row_idx ? p.row_idx[r] : r, at = p.scatter ? row : r;
         const float a = p.d_lse ? fabsf(p.d_lse[at] * p.inv_t) : 0.f, b = p.d_zt ? fabsf(p.d_zt[at] * p.inv_t) : 0.f, g = a + b;
-        const int e = lmb_exponent(p.hidden + row * p.h_stride, p.Dh, meet);
+        float top = 0.f;
+#pragma unroll 8
+        for (int c = lane * 8; c < p.Dh; c += 512) top = fmaxf(top, lmb_top8(*reinterpret_cast<const u32x4*>(p.hidden + row * p.h_stride + c)));
+        const int e = lmb_exponent(top);
         const int c = g > 0.f && g < INFINITY ? max((int)(__float_as_uint(g) >> 23) - 127, -126) : LMB_NONE;
-        if (threadIdx.x == 0) {
+        if (lane == 0) {
             p.sc.row_e[r] = e;
             p.sc.row_c[r] = c;
         }
         if (e != LMB_NONE && c != LMB_NONE) most = max(most, e + c);
     }
-    if (threadIdx.x == 0) p.sc.row_max[blockIdx.x] = most;
+    if (lane == 0) meet[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) p.sc.row_max[blockIdx.x] = max(max(meet[0], meet[1]), max(meet[2], meet[3]));
 }
+// largest of n numbers, over the wavefront
 __device__ __forceinline__ int lmb_most(const int* v, int n) {
     int m = LMB_NONE;
+#pragma unroll 8
     for (int i = threadIdx.x & 63; i < n; i += WAVE) m = max(m, v[i]);
 #pragma unroll
     for (int off = 1; off < WAVE; off *= 2) m = max(m, shfl_xor(m, off));
@@ -139,22 +144,38 @@ __device__ __forceinline__ int lmb_most(const int* v, int n) {
 // Selected hidden rows side by side, what belongs to them, and the rows of W behind the last whole 64: the products then read whole tiles.
 // fp16: the scaled copies of both, and of all of W.
 __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
-    __shared__ float meet[4];
     const int M = lmb_rows(p), bound = (p.M + 63) & ~63, r = blockIdx.x;
+    if (r == 0 && threadIdx.x < 24) p.counters[threadIdx.x * 16] = 0;
     if (r >= bound) {
         if (p.f16) {
+            // a wavefront a row, its first 4096 entries kept in registers
             int most = LMB_NONE;
-            const int padded = (p.V + 63) & ~63, whole = p.V & ~63;
-            for (int v = r - bound; v < padded; v += LMB_STATS * 8) {
+            const int padded = (p.V + 63) & ~63, whole = p.V & ~63, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            for (int v = (r - bound) * 4 + wave; v < padded; v += LMB_STATS * 8 * 4) {
                 uint16_t* dst = v < whole ? p.sc.w16 + (int64_t)v * p.Dh : p.sc.tail16 + (int64_t)(v - whole) * p.Dh;
                 const uint16_t* src = p.w + min(v, p.V - 1) * p.w_stride;
-                const int e = v < p.V ? lmb_exponent(src, p.Dh, meet) : LMB_NONE;
-                if (v < p.V && threadIdx.x == 0) p.sc.w_e[v] = e;
+                u32x4 kept[8];
+                float top = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int c = (k * WAVE + lane) * 8;
+                    kept[k] = c < p.Dh ? *reinterpret_cast<const u32x4*>(src + c) : u32x4{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = fmaxf(top, lmb_top8(kept[k]));
+                for (int c = 4096 + lane * 8; c < p.Dh; c += 512) top = fmaxf(top, lmb_top8(*reinterpret_cast<const u32x4*>(src + c)));
+                const int e = v < p.V ? lmb_exponent(top) : LMB_NONE;
+                if (v < p.V && lane == 0) p.sc.w_e[v] = e;
                 most = max(most, e);
-                for (int c = threadIdx.x * 8; c < p.Dh; c += 2048)
-                    *reinterpret_cast<u32x4*>(dst + c) = e != LMB_NONE ? lmb_half8(src + c, 14 - e) : u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int c = (k * WAVE + lane) * 8;
+                    if (c < p.Dh) __builtin_nontemporal_store(lmb_half8(kept[k], e != LMB_NONE, 14 - e), reinterpret_cast<u32x4*>(dst + c));
+                }
+                for (int c = 4096 + lane * 8; c < p.Dh; c += 512)
+                    *reinterpret_cast<u32x4*>(dst + c) = lmb_half8(*reinterpret_cast<const u32x4*>(src + c), e != LMB_NONE, 14 - e);
             }
-            if (threadIdx.x == 0) p.sc.w_max[r - bound] = most;
+            if (lane == 0) p.sc.w_max[(r - bound) * 4 + wave] = most;
             return;
         }
         const int t = r - bound, v = (p.V & ~63) + t;
@@ -174,7 +195,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     for (int c = threadIdx.x * 8; c < p.Dh; c += 2048) {
         const uint16_t* src = p.hidden + row * p.h_stride + c;
         *reinterpret_cast<u32x4*>(p.h + (int64_t)r * p.Dh + c) = live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0};
-        if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = live ? lmb_half8(src, 14 - up) : u32x4{0, 0, 0, 0};
+        if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = lmb_half8(live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0}, live, 14 - up);
     }
     if (threadIdx.x == 0) {
         LmbRow o = {0.f, 0.f, 0.f, -1};
@@ -192,9 +213,14 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     }
 }
 // K, from what the workgroups found
-__global__ __launch_bounds__(WAVE) void lmb_scale_kernel(LmbParams p) {
-    const int L = lmb_most(p.sc.row_max, LMB_STATS), S = lmb_most(p.sc.w_max, LMB_STATS * 8);
+__global__ __launch_bounds__(512) void lmb_scale_kernel(LmbParams p) {
+    __shared__ int meet[8];
+    const int wave = threadIdx.x >> 6, L = lmb_most(p.sc.row_max, LMB_STATS), S0 = lmb_most(p.sc.w_max + wave * LMB_STATS * 4, LMB_STATS * 4);
+    if (lane_id() == 0) meet[wave] = S0;
+    __syncthreads();
     if (threadIdx.x == 0) {
+        int S = meet[0];
+        for (int k = 1; k < 8; ++k) S = max(S, meet[k]);
         p.sc.out[0] = S == LMB_NONE ? 0 : S;
         p.sc.out[1] = (L == LMB_NONE ? 0 : L) + (S == LMB_NONE ? 0 : S) - 13;
     }
@@ -211,11 +237,23 @@ __device__ __forceinline__ void lmb_tile(int t, int ni, int nj, int gi, int gj, 
     j += col * gj;
     (void)bj;
 }
-// Workgroups go round the 8 XCDs: each gets a stretch of the tile numbers.  -1: none
-__device__ __forceinline__ int lmb_slot(int block, int tiles) {
-    const int per = (tiles + 7) >> 3, slot = block >> 3, t = (block & 7) * per + slot;
-    return slot < per && t < tiles ? t : -1;
-}
+// Workgroups go round the 8 XCDs: each XCD has a stretch of the tile numbers.  With a counter a workgroup takes one tile after the other, in order;
+// `ahead` is the one behind the tile at hand, whose operands are requested before that one is done.
+struct LmbList {
+    int t0, len, index, ahead, later;      // later: what a number from the counter is short of the list's index
+    int* counter;                          // NULL: one tile
+    __device__ __forceinline__ LmbList(int tiles, int block) {
+        const int per = (tiles + 7) >> 3;
+        t0 = (block & 7) * per;
+        len = max(0, min(per, tiles - t0));
+        index = block >> 3;
+        ahead = len;
+        later = 0;
+        counter = nullptr;
+    }
+};
+constexpr int LMB_COUNTERS = 8 * 16;       // of one list: one an XCD, lines apart
+__device__ __forceinline__ int lmb_take(int* counter) { return __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ __forceinline__ void lmb_load_lds16(const void* base, uint32_t offset, uint32_t dst) {   // base: wave-uniform
     uint64_t a;
@@ -279,6 +317,15 @@ struct LmbLoop {
     struct Bases {
         const char *a0, *a1, *b0, *b1;                                 // of a pair's two stages
     };
+    static __device__ __forceinline__ const char* uniform(const char* x) {
+        const uint64_t v = (uint64_t)x;
+        return (const char*)((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v));
+    }
+    template <typename Job>
+    __device__ __forceinline__ void bases(Job& job, int q, Bases& s) {
+        job.pair(*this, q, s);
+        s = Bases{uniform(s.a0), uniform(s.a1), uniform(s.b0), uniform(s.b1)};      // (which the compiler does not always see)
+    }
     // request jj of a pair (0 .. 2 IPW): even ones into its first stage
     __device__ __forceinline__ void issue(const Bases& s, int jj, uint32_t st0, uint32_t st1) {
         const int j = jj >> 1;
@@ -287,9 +334,13 @@ struct LmbLoop {
         lmb_load_lds16(base, voff[j], lds0 + (jj & 1 ? st1 : st0) + at);
     }
 
-    // np pairs of stages; pair(q, Bases&): the bases of pair q, asked for 0, 1, 2 .. in order (and again for the last one)
-    template <typename Pair>
-    __device__ __forceinline__ void run(int np, Pair&& pair) {
+    // The tiles of a list.  The job knows them: open(t) makes t the tile that requests are for, of np pairs of stages; place(loop) its places; pair(loop, q,
+    // bases) the bases of its pair q, asked for in order (and again for the last one); at: what store(loop, at) needs to know of a tile.
+    // The requests of a tile's last two pairs are the next tile's first two, so that its first trip to memory hides behind the end of this one; every
+    // tile of a list with a counter has two pairs or more.
+    template <typename Job>
+    __device__ __forceinline__ void run(Job& job, LmbList list) {
+        if (list.index >= list.len) return;
         const int n = lane & 31, hi = lane >> 5, s16 = lane & 15, blk = lane >> 4 & 1, wv = w % WV, wh = w / WV;
         // lane offsets of the fragments: one a step (k along the rows), or one a tile
         uint32_t la[AROW ? TVW : 2], lb[BROW ? THW : 2];
@@ -329,22 +380,7 @@ struct LmbLoop {
                 }
             }
         };
-        constexpr int NF = TVW + THW, NM = TVW * THW;
-#pragma unroll
-        for (int a = 0; a < TVW; ++a)
-#pragma unroll
-            for (int c = 0; c < THW; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[a][c][i] = 0.f;
-        constexpr int BV = BLOCK > 0 ? TVW : 1, BH = BLOCK > 0 ? THW : 1;
-        f32x16 sum[BV][BH], lost[BV][BH];
-        if constexpr (BLOCK > 0) {
-#pragma unroll
-            for (int a = 0; a < TVW; ++a)
-#pragma unroll
-                for (int c = 0; c < THW; ++c) sum[a][c] = lost[a][c] = acc[a][c];
-        }
-        if (np == 0) return;
+        constexpr int NF = TVW + THW, NM = TVW * THW, BV = BLOCK > 0 ? TVW : 1, BH = BLOCK > 0 ? THW : 1;
         // half a stage: the products of one MFMA step, behind the first ones the fragments of the next step, between them requests
         Bases src;
         const auto half = [&](auto H, uint32_t rsb, auto PART, uint32_t st0, uint32_t st1) {
@@ -369,62 +405,99 @@ struct LmbLoop {
         using I1 = std::integral_constant<int, 1>;
         using I2 = std::integral_constant<int, 2>;
         const auto next = [](uint32_t s) { return s + STAGE == NS * STAGE ? 0u : s + STAGE; };
-        // (a pair past the last one is the last one again, into stages that nobody reads)
+        job.open(list.t0 + __builtin_amdgcn_readfirstlane(list.index));
+        job.place(*this);
+        if (job.np > 0) {
+            // (a pair past the last one is the last one again, into stages that nobody reads)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            pair(min(q, np - 1), src);
+            for (int q = 0; q < 2; ++q) {
+                bases(job, min(q, job.np - 1), src);
 #pragma unroll
-            for (int jj = 0; jj < 2 * IPW; ++jj) issue(src, jj, 2 * q * STAGE, (2 * q + 1) * STAGE);
+                for (int jj = 0; jj < 2 * IPW; ++jj) issue(src, jj, 2 * q * STAGE, (2 * q + 1) * STAGE);
+            }
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
         }
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * IPW) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        uint32_t sb = 0;
+        uint32_t sb = 0;           // the stage of the pair at hand; the one in front of it is free between tiles
+        for (;;) {
+            const bool more = list.counter && list.ahead < list.len;
+            int taken = 0;
+            if (more && threadIdx.x == 0) taken = lmb_take(list.counter);
+            const auto at = job.at;
+            const int np = job.np;
+            f32x16 sum[BV][BH], lost[BV][BH];
 #pragma unroll
-        for (int f = 0; f < NF; ++f) read(0, sb, f);
-        for (int q = 0; q < np;) {
-            const int end = BLOCK > 0 ? min(q + BLOCK, np) : np;
+            for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                for (int c = 0; c < THW; ++c) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[a][c][i] = 0.f;
+                    if constexpr (BLOCK > 0) sum[a][c] = lost[a][c] = acc[a][c];
+                }
+            if (np > 0) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f) read(0, sb, f);
+            }
+            int ask = 2;
+            for (int q = 0; q < np;) {
+                const int end = BLOCK > 0 ? min(q + BLOCK, np) : np;
 #pragma unroll 1
-            for (; q < end; ++q) {
-                const uint32_t s1 = next(sb), s2 = next(s1), s3 = next(s2), s4 = next(s3);
-                pair(min(q + 2, np - 1), src);
-                half(I0(), sb, I0(), 0, 0);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                __builtin_amdgcn_s_barrier();      // every wavefront has read the pair's first stage to the end: it is free
-                asm volatile("" ::: "memory");
-                half(I1(), s1, I1(), s4, sb);
-                half(I0(), s1, I2(), s4, sb);
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPW) : "memory");      // all but the pair just requested has landed
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                half(I1(), s2, I0(), 0, 0);
-                sb = s2;
+                for (; q < end; ++q) {
+                    const uint32_t s1 = next(sb), s2 = next(s1), s3 = next(s2), s4 = next(s3);
+                    if (more && q + 2 == np) {
+                        job.open(list.t0 + list.ahead);
+                        job.place(*this);
+                        ask = 0;
+                    }
+                    bases(job, min(ask, job.np - 1), src);
+                    ++ask;
+                    half(I0(), sb, I0(), 0, 0);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();      // every wavefront has read the pair's first stage to the end: it is free
+                    asm volatile("" ::: "memory");
+                    half(I1(), s1, I1(), s4, sb);
+                    half(I0(), s1, I2(), s4, sb);
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPW) : "memory");      // all but the pair just requested has landed
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    half(I1(), s2, I0(), 0, 0);
+                    sb = s2;
+                }
+                if constexpr (BLOCK > 0) {
+#pragma unroll
+                    for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                        for (int c = 0; c < THW; ++c)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float x = acc[a][c][i], s = sum[a][c][i], t = s + x, y = t - s;
+                                lost[a][c][i] += (s - (t - y)) + (x - y);
+                                sum[a][c][i] = t;
+                                acc[a][c][i] = 0.f;
+                            }
+                }
             }
             if constexpr (BLOCK > 0) {
 #pragma unroll
                 for (int a = 0; a < TVW; ++a)
 #pragma unroll
-                    for (int c = 0; c < THW; ++c)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float x = acc[a][c][i], s = sum[a][c][i], t = s + x, y = t - s;
-                            lost[a][c][i] += (s - (t - y)) + (x - y);
-                            sum[a][c][i] = t;
-                            acc[a][c][i] = 0.f;
-                        }
+                    for (int c = 0; c < THW; ++c) acc[a][c] = sum[a][c] + lost[a][c];
             }
-        }
-        if constexpr (BLOCK > 0) {
 #pragma unroll
             for (int a = 0; a < TVW; ++a)
 #pragma unroll
-                for (int c = 0; c < THW; ++c) acc[a][c] = sum[a][c] + lost[a][c];
+                for (int c = 0; c < THW; ++c) asm volatile("" : "+a"(acc[a][c]));
+            job.store(*this, at);
+            if (!more) break;
+            const uint32_t box = sb == 0 ? (NS - 1) * STAGE : sb - STAGE;
+            if (threadIdx.x == 0) *reinterpret_cast<int*>(ring + box) = taken;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            list.ahead = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const int*>(ring + box)) + list.later;
         }
-#pragma unroll
-        for (int a = 0; a < TVW; ++a)
-#pragma unroll
-            for (int c = 0; c < THW; ++c) asm volatile("" : "+a"(acc[a][c]));
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // requests into the ring end before the workgroup does
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // requests into the ring end before anything else is put there
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     }
@@ -433,207 +506,304 @@ struct LmbLoop {
 // ---- dz of a chunk: rows of W along i, hidden rows along j -----------------------------------------------------
 // TERMS bf16 terms; 0: one scaled fp16.
 template <int WV, int WH, int TVW, int THW, int TERMS, int BLOCK>
-__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
+struct LmbDz {
     using Loop = LmbLoop<false, false, false, BLOCK, WV, WH, TVW, THW>;
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[Loop::RING];
-    const int M = lmb_rows(p), padded = (M + 63) & ~63;
-    const int ni = (p.n + Loop::TI - 1) / Loop::TI, nj = (padded + Loop::TJ - 1) / Loop::TJ;
-    const int t = lmb_slot(blockIdx.x, ni * nj);
-    if (t < 0) return;
-    int ti, tj;
-    const int gj = min(nj, 8);
-    lmb_tile(t, ni, nj, 32 / gj, gj, ti, tj);
-    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
-    Loop loop(ring);
-    const char* wb = (const char*)(p.w + (int64_t)(p.v0 + i0) * p.w_stride);
-    const char* hb = (const char*)(p.h + (int64_t)j0 * p.Dh);
-    loop.place_a((uint32_t)p.w_stride * 2, p.V - 1 - p.v0 - i0);
-    loop.place_b((uint32_t)p.Dh * 2, padded - 1 - j0);
-    loop.run(p.Dh / 64, [&](int q, typename Loop::Bases& s) {
-        s.a0 = wb + q * 128;
-        s.a1 = s.a0 + 64;
-        s.b0 = hb + q * 128;
-        s.b1 = s.b0 + 64;
-    });
-    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
-    const int none = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
-    LmbRow row[THW];
-    int up[THW];
-#pragma unroll
-    for (int c = 0; c < THW; ++c) {
-        const int m = min(j0 + (wh * THW + c) * 32 + n, padded - 1);
-        row[c] = p.rows[m];
-        up[c] = TERMS == 0 ? p.sc.up[m] - K : 0;
+    struct At {
+        int i0, j0;
+    };
+    const LmbParams& p;
+    int padded, ni, nj, gj, np;
+    At at;
+    const char *wb, *hb;
+    __device__ __forceinline__ LmbDz(const LmbParams& q) : p(q) {
+        padded = (lmb_rows(p) + 63) & ~63;
+        ni = (p.n + Loop::TI - 1) / Loop::TI;
+        nj = (padded + Loop::TJ - 1) / Loop::TJ;
+        gj = max(min(nj, 8), 1);
+        np = p.Dh / 64;
     }
+    __device__ __forceinline__ void open(int t) {
+        int ti, tj;
+        lmb_tile(t, ni, nj, 32 / gj, gj, ti, tj);
+        at = At{ti * Loop::TI, tj * Loop::TJ};
+        wb = (const char*)(p.w + (int64_t)(p.v0 + at.i0) * p.w_stride);
+        hb = (const char*)(p.h + (int64_t)at.j0 * p.Dh);
+    }
+    __device__ __forceinline__ void place(Loop& loop) const {
+        loop.place_a((uint32_t)p.w_stride * 2, p.V - 1 - p.v0 - at.i0);
+        loop.place_b((uint32_t)p.Dh * 2, padded - 1 - at.j0);
+    }
+    __device__ __forceinline__ void pair(Loop&, int q, typename Loop::Bases& b) const {
+        b.a0 = wb + q * 128;
+        b.a1 = b.a0 + 64;
+        b.b0 = hb + q * 128;
+        b.b1 = b.b0 + 64;
+    }
+    __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
+        const int i0 = tile.i0, j0 = tile.j0;
+        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+        const int none = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
+        LmbRow row[THW];
+        int up[THW];
 #pragma unroll
-    for (int a = 0; a < TVW; ++a)
+        for (int c = 0; c < THW; ++c) {
+            const int m = min(j0 + (wh * THW + c) * 32 + n, padded - 1);
+            row[c] = p.rows[m];
+            up[c] = TERMS == 0 ? p.sc.up[m] - K : 0;
+        }
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
-            if (i >= p.ldz) continue;
-            typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
-            i32x4 we = {0, 0, 0, 0};
-            if constexpr (TERMS == 0) {
-                we = *reinterpret_cast<const i32x4*>(p.sc.w_e + p.v0 + i);
+        for (int a = 0; a < TVW; ++a)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) we[e] = we[e] == LMB_NONE ? none : we[e];
-            }
-#pragma unroll
-            for (int c = 0; c < THW; ++c) {
-                const int m = j0 + (wh * THW + c) * 32 + n;
-                uint16_t* dst = p.dz + (int64_t)m * p.ldz + i;
-                float d[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int v = p.v0 + i + e;
-                    // (the difference first: a logit and lse are large where their difference is not)
-                    const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row[c].lse) * 1.4426950408889634f);
-                    d[e] = (row[c].a != 0.f ? row[c].a * x : 0.f) + (v == row[c].target ? row[c].c : 0.f);
-                    if (v == p.forbid || v >= p.V) d[e] = 0.f;
-                }
-                if (m >= padded) continue;
+            for (int g = 0; g < 4; ++g) {
+                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                if (i >= p.ldz) continue;
+                typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+                i32x4 we = {0, 0, 0, 0};
                 if constexpr (TERMS == 0) {
-                    typedef __attribute__((__vector_size__(4 * sizeof(_Float16)))) _Float16 f16x4;
-                    f16x4 q;
+                    we = *reinterpret_cast<const i32x4*>(p.sc.w_e + p.v0 + i);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) q[e] = (_Float16)ldexpf(d[e], up[c] + we[e]);
-                    *reinterpret_cast<u32x2*>(dst) = __builtin_bit_cast(u32x2, q);
-                } else {
-                    // every term what the ones before it leave, which fp32 holds exactly
+                    for (int e = 0; e < 4; ++e) we[e] = we[e] == LMB_NONE ? none : we[e];
+                }
 #pragma unroll
-                    for (int k = 0; k < TERMS; ++k) {
-                        const u32x2 q = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
-                        *reinterpret_cast<u32x2*>(dst + k * p.dz_term) = q;
+                for (int c = 0; c < THW; ++c) {
+                    const int m = j0 + (wh * THW + c) * 32 + n;
+                    uint16_t* dst = p.dz + (int64_t)m * p.ldz + i;
+                    float d[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) d[e] -= __uint_as_float(e & 1 ? q[e / 2] & 0xffff0000u : q[e / 2] << 16);
+                    for (int e = 0; e < 4; ++e) {
+                        const int v = p.v0 + i + e;
+                        // (the difference first: a logit and lse are large where their difference is not)
+                        const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row[c].lse) * 1.4426950408889634f);
+                        d[e] = (row[c].a != 0.f ? row[c].a * x : 0.f) + (v == row[c].target ? row[c].c : 0.f);
+                        if (v == p.forbid || v >= p.V) d[e] = 0.f;
+                    }
+                    if (m >= padded) continue;
+                    if constexpr (TERMS == 0) {
+                        typedef __attribute__((__vector_size__(4 * sizeof(_Float16)))) _Float16 f16x4;
+                        f16x4 q;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q[e] = (_Float16)ldexpf(d[e], up[c] + we[e]);
+                        *reinterpret_cast<u32x2*>(dst) = __builtin_bit_cast(u32x2, q);
+                    } else {
+                        // every term what the ones before it leave, which fp32 holds exactly
+#pragma unroll
+                        for (int k = 0; k < TERMS; ++k) {
+                            const u32x2 q = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
+                            *reinterpret_cast<u32x2*>(dst + k * p.dz_term) = q;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[e] -= __uint_as_float(e & 1 ? q[e / 2] & 0xffff0000u : q[e / 2] << 16);
+                        }
                     }
                 }
             }
-        }
+    }
+};
+template <int WV, int WH, int TVW, int THW, int TERMS, int BLOCK>
+__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
+    using Job = LmbDz<WV, WH, TVW, THW, TERMS, BLOCK>;
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[Job::Loop::RING];
+    if (blockIdx.x == 0 && threadIdx.x < 16) p.counters[LMB_COUNTERS + threadIdx.x * 16] = 0;      // the gradients' two lists
+    Job job(p);
+    LmbList list(job.ni * job.nj, blockIdx.x);
+    if (p.queued) {
+        list.counter = p.counters + (blockIdx.x & 7) * 16;
+        list.later = 2 * (gridDim.x >> 3);
+        list.ahead = list.index + (gridDim.x >> 3);
+    }
+    typename Job::Loop loop(ring);
+    loop.run(job, list);
 }
 
 // ---- d_hidden's and d_w's products of a chunk ----------------------------------------------------------------
 // d_hidden: columns of Dh along i, rows along j, the vocabulary is summed over, in `splits` parts.
 template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
-__device__ __forceinline__ void lmb_hidden(const LmbParams& p, unsigned char* ring, int block) {
+struct LmbHidden {
     using Loop = LmbLoop<true, false, F16, BLOCK, WV, WH, TVW, THW>;
-    const int M = lmb_rows(p), padded = (M + 63) & ~63;
-    int t = lmb_slot(block, p.ni * p.nj * p.splits);
-    if (t < 0) return;
-    const int s = t / (p.ni * p.nj);
-    int ti, tj;
-    const int gj = min(p.nj, 8);
-    lmb_tile(t - s * p.ni * p.nj, p.ni, p.nj, 32 / gj, gj, ti, tj);
-    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
-    if (j0 >= M) return;
-    const int all = (p.n + 63) >> 6, whole = p.n >> 6;                  // pairs of stages of a term; those that W itself holds
-    const int64_t total = (int64_t)all * p.terms_h;
-    const int q0 = (int)(total * s / p.splits), q1 = (int)(total * (s + 1) / p.splits);
-    Loop loop(ring);
-    bool tail = false;
-    const uint16_t *w = F16 ? p.sc.w16 : p.w, *w_tail = F16 ? p.sc.tail16 : p.w_tail;
-    const int64_t w_stride = F16 ? p.Dh : p.w_stride;
-    loop.place_a((uint32_t)w_stride * 2, p.Dh - 8 - i0);
-    loop.place_b((uint32_t)p.ldz * 2, padded - 1 - j0);
-    loop.run(q1 - q0, [&](int q, typename Loop::Bases& b) {
-        q += q0;
-        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0);
-        const int k = q - term * all;
-        if ((k >= whole) != tail) {                                     // into the rows behind the last whole 64, or back
-            tail = !tail;
-            loop.place_a((uint32_t)(tail ? p.Dh : w_stride) * 2, p.Dh - 8 - i0);
-        }
-        const int64_t pitch = tail ? p.Dh : w_stride;
-        b.a0 = (const char*)(tail ? w_tail + i0 : w + (int64_t)(p.v0 + 64 * k) * w_stride + i0);
-        b.a1 = b.a0 + 64 * pitch;
-        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)j0 * p.ldz + 64 * k);
-        b.b1 = b.b0 + 64;
-    });
-    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
-#pragma unroll
-    for (int c = 0; c < THW; ++c) {
-        const int m = j0 + (wh * THW + c) * 32 + n;
-        if (m >= M) continue;
-        float* dst = p.part + ((int64_t)s * p.M + m) * p.Dh;
-#pragma unroll
-        for (int a = 0; a < TVW; ++a)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
-                if (i >= p.Dh) continue;
-                f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
-                if (p.add) x += *reinterpret_cast<const f32x4*>(dst + i);
-                *reinterpret_cast<f32x4*>(dst + i) = x;
-            }
+    struct At {
+        int i0, j0, s;
+    };
+    const LmbParams& p;
+    int M, padded, ni, nj, gj, np;
+    At at;
+    int all, whole, q0;                            // pairs of stages of a term; those that W itself holds; the tile's first
+    bool tail;
+    __device__ __forceinline__ LmbHidden(const LmbParams& q) : p(q) {
+        M = lmb_rows(p);
+        padded = (M + 63) & ~63;
+        ni = (p.Dh + Loop::TI - 1) / Loop::TI;
+        nj = (M + Loop::TJ - 1) / Loop::TJ;
+        gj = max(min(nj, 8), 1);
+        all = (p.n + 63) >> 6;
+        whole = p.n >> 6;
     }
-}
+    __device__ __forceinline__ int tiles() const { return ni * nj * p.splits; }
+    __device__ __forceinline__ void open(int t) {
+        const int s = t / (ni * nj);
+        int ti, tj;
+        lmb_tile(t - s * ni * nj, ni, nj, 32 / gj, gj, ti, tj);
+        at = At{ti * Loop::TI, tj * Loop::TJ, s};
+        const int total = all * p.terms_h;         // (at most 3 2^18, of at most 64 parts)
+        q0 = total * s / p.splits;
+        np = total * (s + 1) / p.splits - q0;
+        tail = false;
+    }
+    __device__ __forceinline__ void place_w(Loop& loop) const { loop.place_a((uint32_t)(F16 || tail ? p.Dh : p.w_stride) * 2, p.Dh - 8 - at.i0); }
+    __device__ __forceinline__ void place(Loop& loop) const {
+        place_w(loop);
+        loop.place_b((uint32_t)p.ldz * 2, padded - 1 - at.j0);
+    }
+    __device__ __forceinline__ void pair(Loop& loop, int q, typename Loop::Bases& b) {
+        q += q0;
+        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
+        if ((k >= whole) != tail) {                // into the rows behind the last whole 64, or back
+            tail = !tail;
+            if (!F16) place_w(loop);
+        }
+        const uint16_t *w = F16 ? p.sc.w16 : p.w, *w_tail = F16 ? p.sc.tail16 : p.w_tail;
+        const int64_t pitch = F16 || tail ? p.Dh : p.w_stride;
+        b.a0 = (const char*)(tail ? w_tail + at.i0 : w + (int64_t)(p.v0 + 64 * k) * pitch + at.i0);
+        b.a1 = b.a0 + 64 * pitch;
+        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)at.j0 * p.ldz + 64 * k);
+        b.b1 = b.b0 + 64;
+    }
+    __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
+        const int i0 = tile.i0, j0 = tile.j0, s = tile.s;
+        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+#pragma unroll
+        for (int c = 0; c < THW; ++c) {
+            const int m = j0 + (wh * THW + c) * 32 + n;
+            if (m >= M) continue;
+            float* dst = p.part + ((int64_t)s * p.M + m) * p.Dh;
+#pragma unroll
+            for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                    if (i >= p.Dh) continue;
+                    f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
+                    if (p.add) x += *reinterpret_cast<const f32x4*>(dst + i);
+                    *reinterpret_cast<f32x4*>(dst + i) = x;
+                }
+        }
+    }
+};
 
 // d_w: columns of Dh along i, the chunk's along j, rows are summed over.
 template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
-__device__ __forceinline__ void lmb_weight(const LmbParams& p, unsigned char* ring, int block) {
+struct LmbWeight {
     using Loop = LmbLoop<true, true, F16, BLOCK, WV, WH, TVW, THW>;
-    const int t = lmb_slot(block, p.wi * p.wj);
-    if (t < 0) return;
-    int ti, tj;
-    lmb_tile(t, p.wi, p.wj, 4, 8, ti, tj);
-    const int i0 = ti * Loop::TI, j0 = tj * Loop::TJ;
-    const int all = (lmb_rows(p) + 63) >> 6;
-    const uint16_t* h = F16 ? p.sc.h16 : p.h;
-    Loop loop(ring);
-    loop.place_a((uint32_t)p.Dh * 2, p.Dh - 8 - i0);
-    loop.place_b((uint32_t)p.ldz * 2, p.ldz - 8 - j0);
-    loop.run(all * p.terms_w, [&](int q, typename Loop::Bases& b) {
-        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
-        b.a0 = (const char*)(h + (int64_t)64 * k * p.Dh + i0);
-        b.a1 = b.a0 + (int64_t)64 * p.Dh;
-        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)64 * k * p.ldz + j0);
-        b.b1 = b.b0 + (int64_t)64 * p.ldz;
-    });
-    const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
-#pragma unroll
-    for (int c = 0; c < THW; ++c) {
-        const int v = p.v0 + j0 + (wh * THW + c) * 32 + n;
-        if (v >= p.V || j0 + (wh * THW + c) * 32 + n >= p.n) continue;
-        int scale = 0;
-        if (F16 && all > 0) {
-            const int e = p.sc.w_e[v];
-            scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
-        }
-#pragma unroll
-        for (int a = 0; a < TVW; ++a)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
-                if (i >= p.Dh) continue;
-                f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
-                if constexpr (F16) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
-                }
-                if (p.dw_f32) {
-                    float* dst = (float*)p.d_w + v * p.dw_stride + i;
-                    if (p.accumulate) x += *reinterpret_cast<const f32x4*>(dst);
-                    *reinterpret_cast<f32x4*>(dst) = x;
-                } else {
-                    uint16_t* dst = (uint16_t*)p.d_w + v * p.dw_stride + i;
-                    if (p.accumulate) {
-                        float old[4];
-                        load_bf16<4>(dst, old);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] += old[e];
-                    }
-                    *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-                }
-            }
+    struct At {
+        int i0, j0;
+    };
+    const LmbParams& p;
+    int ni, nj, all, np;
+    At at;
+    __device__ __forceinline__ LmbWeight(const LmbParams& q) : p(q) {
+        all = (lmb_rows(p) + 63) >> 6;
+        np = all * p.terms_w;
+        ni = (p.Dh + Loop::TI - 1) / Loop::TI;
+        nj = (p.n + Loop::TJ - 1) / Loop::TJ;
     }
-}
+    __device__ __forceinline__ int tiles() const { return ni * nj; }
+    __device__ __forceinline__ void open(int t) {
+        int ti, tj;
+        lmb_tile(t, ni, nj, 4, 8, ti, tj);
+        at = At{ti * Loop::TI, tj * Loop::TJ};
+    }
+    __device__ __forceinline__ void place(Loop& loop) const {
+        loop.place_a((uint32_t)p.Dh * 2, p.Dh - 8 - at.i0);
+        loop.place_b((uint32_t)p.ldz * 2, p.ldz - 8 - at.j0);
+    }
+    __device__ __forceinline__ void pair(Loop&, int q, typename Loop::Bases& b) const {
+        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
+        b.a0 = (const char*)((F16 ? p.sc.h16 : p.h) + (int64_t)64 * k * p.Dh + at.i0);
+        b.a1 = b.a0 + (int64_t)64 * p.Dh;
+        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)64 * k * p.ldz + at.j0);
+        b.b1 = b.b0 + (int64_t)64 * p.ldz;
+    }
+    __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
+        const int i0 = tile.i0, j0 = tile.j0;
+        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+#pragma unroll
+        for (int c = 0; c < THW; ++c) {
+            const int v = p.v0 + j0 + (wh * THW + c) * 32 + n;
+            if (v >= p.V || j0 + (wh * THW + c) * 32 + n >= p.n) continue;
+            int scale = 0;
+            if (F16 && all > 0) {
+                const int e = p.sc.w_e[v];
+                scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
+            }
+#pragma unroll
+            for (int a = 0; a < TVW; ++a)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                    if (i >= p.Dh) continue;
+                    f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
+                    if constexpr (F16) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
+                    }
+                    if (p.dw_f32) {
+                        float* dst = (float*)p.d_w + v * p.dw_stride + i;
+                        if (p.accumulate) x += *reinterpret_cast<const f32x4*>(dst);
+                        *reinterpret_cast<f32x4*>(dst) = x;
+                    } else {
+                        uint16_t* dst = (uint16_t*)p.d_w + v * p.dw_stride + i;
+                        if (p.accumulate) {
+                            float old[4];
+                            load_bf16<4>(dst, old);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[e] += old[e];
+                        }
+                        *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                    }
+                }
+        }
+    }
+};
 
-// Both in one launch: the workgroups of the second fill the CUs that the last round of the first leaves idle.
+// Both in one launch: what a workgroup of the first has left over it spends on the second.
 template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 __global__ __launch_bounds__(64 * WV * WH, 1) void lmb_grad_kernel(LmbParams p) {
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[LmbLoop<true, true, F16, BLOCK, WV, WH, TVW, THW>::RING];
-    if ((int)blockIdx.x < p.n2) lmb_hidden<F16, BLOCK, WV, WH, TVW, THW>(p, ring, blockIdx.x);
-    else lmb_weight<F16, BLOCK, WV, WH, TVW, THW>(p, ring, blockIdx.x - p.n2);
+    using Hidden = LmbHidden<F16, BLOCK, WV, WH, TVW, THW>;
+    using Weight = LmbWeight<F16, BLOCK, WV, WH, TVW, THW>;
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[Hidden::Loop::RING];
+    if (blockIdx.x == 0 && threadIdx.x < 8) p.counters[threadIdx.x * 16] = 0;          // the next chunk's list of dz
+    const int block = blockIdx.x, xcd = block & 7, wgs = gridDim.x >> 3;
+    if (p.n2 > 0 && (p.queued || block < p.n2)) {
+        Hidden job(p);
+        LmbList list(job.tiles(), block);
+        if (p.queued) {
+            list.counter = p.counters + LMB_COUNTERS + xcd * 16;
+            list.later = 2 * wgs;
+            list.ahead = list.index + wgs;
+        }
+        typename Hidden::Loop loop(ring);
+        loop.run(job, list);
+    }
+    if (!p.d_w || (!p.queued && block < p.n2)) return;
+    Weight job(p);
+    LmbList list(job.tiles(), p.queued ? block : block - p.n2);
+    const bool one_pair = p.queued && job.np < 2;      // (few rows, which the device alone knows: tiles by themselves)
+    if (p.queued && !one_pair) {
+        // in the order in which workgroups come here
+        list.counter = p.counters + 2 * LMB_COUNTERS + xcd * 16;
+        if (threadIdx.x == 0) {
+            const int first = lmb_take(list.counter);
+            reinterpret_cast<int*>(ring)[0] = first;
+            reinterpret_cast<int*>(ring)[1] = first < list.len ? lmb_take(list.counter) : first;
+        }
+        __syncthreads();
+        list.index = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(ring)[0]);
+        list.ahead = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(ring)[1]);
+        __syncthreads();
+    }
+    typename Weight::Loop loop(ring);
+    do {
+        loop.run(job, list);
+        list.index += wgs;
+    } while (one_pair && list.index < list.len);
 }
 
 // The parts of d_hidden's sum, in order, into the rows that were selected
@@ -666,9 +836,21 @@ int lmb_set_columns(int v) {
     return DLM_OK;
 }
 
+// Workgroups that fit the chip, a multiple of 8
+static int device_wgs(int a_cu) {
+    static int cus[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256 * a_cu;
+    if (cus[dev] == 0) {
+        int n = 0;
+        cus[dev] = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n >= 8 ? n & ~7 : 256;
+    }
+    return cus[dev] * a_cu;
+}
+
 struct LmbPlan {
     int padded, terms_h, terms_w, terms, f16, tile, chunk, splits, ni, nj;
-    size_t rows_at, h_at, tail_at, dz_at, part_at, h16_at, w16_at, ints_at, bytes;
+    size_t rows_at, h_at, tail_at, dz_at, part_at, h16_at, w16_at, ints_at, counters_at, bytes;
 };
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -688,13 +870,15 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     p.chunk = (int)(whole < most ? whole : most);
     p.ni = (a->Dh + p.tile - 1) / p.tile;
     p.nj = (p.padded + p.tile - 1) / p.tile;
-    // parts of d_hidden's sum: the number that wastes least of the last round of CUs, each part with some work
-    const int tiles = p.ni * p.nj, pairs = (int)((p.chunk + 63) / 64);
+    // Parts of d_hidden's sum.  In times of a pair of stages (1.8 us of a 256 x 256 tile): the launch takes what all its tiles take together, but no
+    // less than d_hidden's rounds of tiles; a part costs its rows written and read again.
+    const int64_t tiles = (int64_t)p.ni * p.nj, pairs = (p.chunk + 63) / 64 * p.terms_h, wgs = p.tile == 128 ? 512 : 256;
+    const double rest = a->d_w ? (double)p.ni * ((p.chunk + p.tile - 1) / p.tile) * (p.padded / 64) * p.terms_w : 0.0;
+    const double part = (double)a->M * a->Dh * 8e-7 * (p.tile == 128 ? 4 : 1);
     int best = 1;
-    double least = 1e30;
+    double least = 1e300;
     for (int s = 1; s <= 64 && s * 4 <= pairs; ++s) {
-        const double rounds = (double)(((int64_t)tiles * s + 255) / 256) / s;       // in times of an undivided tile
-        const double cost = rounds * pairs + 0.02 * s * a->M * (double)a->Dh / 65536;
+        const double all = (tiles * pairs + rest) / wgs, rounds = (double)((tiles * s + wgs - 1) / wgs) * pairs / s, cost = (all > rounds ? all : rounds) + part * s;
         if (cost < least) {
             least = cost;
             best = s;
@@ -707,6 +891,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
         at += up256(bytes);
         return here;
     };
+    p.counters_at = take(3 * LMB_COUNTERS * sizeof(int));
     p.rows_at = take((size_t)p.padded * sizeof(LmbRow));
     p.h_at = take((size_t)p.padded * a->Dh * 2);
     p.tail_at = take((size_t)64 * a->Dh * 2);
@@ -715,7 +900,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     if (p.f16) {
         p.h16_at = take((size_t)p.padded * a->Dh * 2);
         p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
-        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 9 + 2) * 4);
+        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 33 + 2) * 4);
     }
     p.bytes = at;
     return p;
@@ -806,12 +991,12 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.sc.w_e = ints + 3 * (int64_t)plan.padded;
         p.sc.row_max = p.sc.w_e + ((int64_t)a->V + 255) / 256 * 256;
         p.sc.w_max = p.sc.row_max + LMB_STATS;
-        p.sc.out = p.sc.w_max + LMB_STATS * 8;
+        p.sc.out = p.sc.w_max + LMB_STATS * 32;
         p.sc.h16 = (uint16_t*)(ws + plan.h16_at);
         p.sc.w16 = (uint16_t*)(ws + plan.w16_at);
         p.sc.tail16 = p.w_tail;
     }
-    p.splits = plan.splits;
+    p.counters = (int*)(ws + plan.counters_at);
     p.d_hidden = a->d_hidden;
     p.dh_stride = a->d_hidden_stride_row;
     p.dh_f32 = a->d_hidden_type == DLM_ROW_F32;
@@ -828,7 +1013,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         hipLaunchKernelGGL(lmb_gather_kernel, dim3(plan.padded + more), dim3(256), 0, st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_gather_kernel launch")) != DLM_OK) return rc;
         if (plan.f16) {
-            hipLaunchKernelGGL(lmb_scale_kernel, dim3(1), dim3(WAVE), 0, st, p);
+            hipLaunchKernelGGL(lmb_scale_kernel, dim3(1), dim3(512), 0, st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_scale_kernel launch")) != DLM_OK) return rc;
         }
     }
@@ -837,28 +1022,30 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.v0 = (int)v0;
         p.n = (int)(a->V - v0 < plan.chunk ? a->V - v0 : plan.chunk);
         p.add = v0 > 0;
-        const int vt = (p.n + plan.tile - 1) / plan.tile;
+        const int64_t vt = (p.n + plan.tile - 1) / plan.tile, all = (p.n + 63) / 64;
+        p.splits = v0 > 0 && all * p.terms_h < 2 * plan.splits ? 1 : plan.splits;          // (parts that the last chunk has no work for stay as they are)
+        p.n2 = hidden ? (plan.ni * plan.nj * p.splits + 7) / 8 * 8 : 0;
+        const int64_t n1 = (vt * plan.nj + 7) / 8 * 8, n3 = a->d_w ? (plan.ni * vt + 7) / 8 * 8 : 0;
+        // A list of tiles where they are more than the workgroups that fit the chip, and long enough to request the next one behind (see LmbLoop)
+        const int wgs = device_wgs(plan.tile == 128 ? 2 : 1);
         if (a->M > 0) {
-            const dim3 grid((unsigned)(((int64_t)vt * plan.nj + 7) / 8 * 8));
+            p.queued = n1 > wgs && a->Dh >= 128;
+            const dim3 grid((unsigned)(p.queued ? wgs : n1));
             if (plan.terms == 3) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 2, 2, 3, 4>), grid, dim3(256), 0, st, p);
             else if (plan.terms == 2) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 2, 0>), grid, dim3(256), 0, st, p);
             else hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 0, 0>), grid, dim3(256), 0, st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
         }
-        p.ni = plan.ni;
-        p.nj = plan.nj;
-        p.n2 = hidden ? (p.ni * p.nj * p.splits + 7) / 8 * 8 : 0;
-        p.wi = plan.ni;
-        p.wj = a->d_w ? vt : 0;
-        const int64_t n3 = ((int64_t)p.wi * p.wj + 7) / 8 * 8;
         if (p.n2 + n3 == 0) continue;
-        const dim3 grid((unsigned)(p.n2 + n3));
+        p.queued = a->M > 0 && p.n2 + n3 > wgs && (!hidden || all * p.terms_h >= 2 * p.splits);
+        const dim3 grid((unsigned)(p.queued ? wgs : p.n2 + n3));
         if (plan.terms == 3) hipLaunchKernelGGL((lmb_grad_kernel<false, 4, 2, 2, 2, 2>), grid, dim3(256), 0, st, p);
         else if (plan.terms == 2) hipLaunchKernelGGL((lmb_grad_kernel<false, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL((lmb_grad_kernel<true, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_grad_kernel launch")) != DLM_OK) return rc;
     }
     if (!hidden) return DLM_OK;
+    p.splits = plan.splits;
     hipLaunchKernelGGL(lmb_join_kernel, dim3(a->M, (a->Dh + 1023) / 1024), dim3(256), 0, st, p);
     return check_hip(hipGetLastError(), "lmb_join_kernel launch");
 }
