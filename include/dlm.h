@@ -694,7 +694,8 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *   d_hidden   optional, rows of d_hidden_type indexed like `hidden`: row(r) is written for every r, other rows are left as they are.  Rows named
  *              twice count twice for d_w; in d_hidden such a row holds the gradient of one of the two.
  *   d_w        optional [V, Dh] of d_w_type; accumulate 0: written, else added to
- * The logits are not stored.  No atomics: deterministic (the order of sums depends on the sizes alone).  hidden and w have to be finite: other rows'
+ * The logits are not stored.  No atomics: deterministic (the order of sums depends on the sizes, the types and which
+ * gradients are wanted).  hidden and w have to be finite: other rows'
  * values are multiplied by dz that may be zero.
  * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 11 bits, as an fp16 scaled by row and column (rows whose |d_lse| + |d_ztarget| times
  * their largest entry is less than 2^-40 of the largest such product of the call lose bits), or, up to 256 rows, 16 bits.  Where a gradient is
@@ -781,6 +782,8 @@ size_t dlm_lmhead_bwd_workspace_bytes(const dlm_lmhead_bwd_args *args);
  *                   rows (of 8, 4, 8, 2 wavefronts; the workspace's size depends on it).
  *   "lmhead_bwd_columns" 0 = dlm_lmhead_bwd takes as many columns of the vocabulary at a time as fit 2 GiB of dz (default); n, a multiple of 256 =
  *                   at most n (the workspace's size depends on it).
+ *   "lmhead_bwd_workgroups" workgroups of the launches of dlm_lmhead_bwd that take their tiles from a list: 0 = as fit the device (default); n, a multiple of 8 =
+ *                   n (tests: makes small calls take the list).
  * The knobs exist for tests and tuning sweeps. */
 int dlm_set_option(const char *name, int value);
 

@@ -26,9 +26,10 @@ typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 
 struct LmbRow {                    // what the logits' kernel knows of a row
-    float lse, a, c;               // a = inv_t d_lse, c = inv_t d_ztarget
-    int target;                    // -1: none
+    float lse, a, c;               // a = inv_t d_lse, c = inv_t d_ztarget; a row without a has an infinite lse, and so probabilities of zero
+    int target;
 };
+constexpr int LMB_NO_TARGET = -(1 << 28);
 
 // fp16 operands.  With e(x) the exponent of the largest entry of a row (its size lies in [2^e, 2^(e+1))):
 //   h16[m] = h[m] 2^(14 - up[m]),  up[m] = e(h[m]) + u;   w16[v] = w[v] 2^(14 - e(w[v]));   D[m][v] = dz[m][v] 2^(up[m] + e(w[v]) - K)
@@ -64,10 +65,11 @@ struct LmbParams {
     uint16_t* w_tail;              // [64][Dh]: the last V % 64 rows of W, zeros behind them
     int f16;                       // dz is fp16 and scaled
     LmbScale sc;
+    int last_e;                    // the last four of w_e
     uint16_t* dz;                  // [terms][M rounded up to 64][ldz]
     int64_t dz_term;               // entries of a term
     int ldz;
-    float* part;                   // [splits][M][Dh]
+    float* part;                   // [splits][terms][M][Dh]
     // the chunk: columns v0 .. v0 + n of dz, n a multiple of 64 but for the end of the vocabulary
     int v0, n, terms_h, terms_w, add;      // add: d_hidden's partial sums are there already
     int splits;                    // parts of d_hidden's sum
@@ -198,14 +200,15 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
         if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = lmb_half8(live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0}, live, 14 - up);
     }
     if (threadIdx.x == 0) {
-        LmbRow o = {0.f, 0.f, 0.f, -1};
+        LmbRow o = {INFINITY, 0.f, 0.f, LMB_NO_TARGET};
         if (live) {
             const int at = p.scatter ? row : r;
-            o.lse = p.lse[at];
             if (p.d_lse) o.a = p.d_lse[at] * p.inv_t;
+            if (o.a != 0.f) o.lse = p.lse[at];
             if (p.d_zt) {
                 o.c = p.d_zt[at] * p.inv_t;
-                o.target = p.target[at];
+                const int t = p.target[at];
+                o.target = t >= 0 && t < p.V && t != p.forbid ? t : LMB_NO_TARGET;
             }
         }
         p.rows[r] = o;
@@ -262,6 +265,23 @@ __device__ __forceinline__ void lmb_load_lds16(const void* base, uint32_t offset
                  : "=&s"(a) : "v"(offset), "s"(__builtin_amdgcn_readfirstlane(dst)), "s"(base) : "memory");
 }
 
+// Of 16 columns of an accumulator a lane has 0 .. 3 and 8 .. 11 (w[0 .. 1], w[2 .. 3], two a word), lane + 32 the others: eight in a row for each, 0 .. 7
+// and 8 .. 15.
+__device__ __forceinline__ u32x4 lmb_eight(const uint32_t (&w)[4]) {
+    const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    return u32x4{x[0], y[0], x[1], y[1]};
+}
+
+template <int V, int H, int TV, int TH>
+struct LmbShape {
+    static constexpr int WV = V, WH = H, TVW = TV, THW = TH;
+};
+using Lmb256 = LmbShape<2, 2, 4, 4>;       // 256 x 256, one workgroup a CU
+using Lmb256x128 = LmbShape<4, 1, 2, 4>;   // one
+using Lmb256x64 = LmbShape<4, 1, 2, 2>;    // one
+using Lmb128 = LmbShape<2, 2, 2, 2>;       // 128 x 128, two
+using Lmb64 = LmbShape<2, 2, 1, 1>;        // 64 x 64, four
+
 // The shape of a workgroup: WV x WH wavefronts of TVW x THW tiles of 32 x 32.
 //
 // Memory to registers goes through a ring of five LDS stages of 32 k each, without registers in between.  Requests come in pairs of stages, two pairs
@@ -290,29 +310,32 @@ struct LmbLoop {
         lane = lane_id();
         w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     }
-    static __device__ __forceinline__ int swz(int tile, int k) { return tile >= 128 ? k & 3 : tile == 64 ? k >> 1 & 1 : 0; }
-    // Places of operand A's (B's) requests: entry (e, k) of the stage is `pitch` bytes a row from the base.  `last`: the last index along the
-    // tile that may be read (rows), or the last multiple of 8 (columns).
-    template <bool ROW, int TILE, int IP>
-    __device__ __forceinline__ void place(uint32_t (&v)[IPW], int first, uint32_t pitch, int last) {
+    // the lane, formed where it stands: what follows from it is not kept in registers over the loop
+    __device__ __forceinline__ int lane_here() const {
         int l = lane;
         asm volatile("" : "+v"(l));
+        return l;
+    }
+    static __device__ __forceinline__ int swz(int tile, int k) { return tile >= 128 ? k & 3 : tile == 64 ? k >> 1 & 1 : 0; }
+    // Places of operand A's (B's) requests.  k across the rows: row k is `pitch` bytes behind row k - 1, columns end at `last` (a multiple of 8);
+    // k along the rows: row r begins at place(r).
+    template <int TILE, int IP>
+    __device__ __forceinline__ void place_columns(int first, uint32_t pitch, int last) {
+        const int l = lane_here();
+        constexpr int LPR = TILE / 8, RPI = 64 / LPR;                  // lanes a row, rows a request
 #pragma unroll
         for (int j = 0; j < IP; ++j) {
-            const int g = w * IP + j;
-            if constexpr (ROW) {
-                constexpr int LPR = TILE / 8, RPI = 64 / LPR;          // lanes a row, rows a request
-                const int k = g * RPI + l / LPR, c = l % LPR;
-                const int col = ((c >> 2 ^ swz(TILE, k)) << 2 | (c & 3)) * 8;
-                v[first + j] = (uint32_t)k * pitch + (uint32_t)min(col, last) * 2;
-            } else {
-                const int row = g * 16 + (l >> 2), piece = (l & 3) ^ (l >> 4 & 3);
-                v[first + j] = (uint32_t)min(row, last) * pitch + piece * 16;
-            }
+            const int k = (w * IP + j) * RPI + l / LPR, c = l % LPR;
+            const int col = ((c >> 2 ^ swz(TILE, k)) << 2 | (c & 3)) * 8;
+            voff[first + j] = (uint32_t)k * pitch + (uint32_t)min(col, last) * 2;
         }
     }
-    __device__ __forceinline__ void place_a(uint32_t pitch, int last) { place<AROW, TI, IPA>(voff, 0, pitch, last); }
-    __device__ __forceinline__ void place_b(uint32_t pitch, int last) { place<BROW, TJ, IPB>(voff, IPA, pitch, last); }
+    template <int IP, typename Place>
+    __device__ __forceinline__ void place_rows(int first, Place&& place) {
+        const int l = lane_here();
+#pragma unroll
+        for (int j = 0; j < IP; ++j) voff[first + j] = place((w * IP + j) * 16 + (l >> 2)) + ((l & 3) ^ (l >> 4 & 3)) * 16;
+    }
 
     struct Bases {
         const char *a0, *a1, *b0, *b1;                                 // of a pair's two stages
@@ -530,8 +553,9 @@ struct LmbDz {
         hb = (const char*)(p.h + (int64_t)at.j0 * p.Dh);
     }
     __device__ __forceinline__ void place(Loop& loop) const {
-        loop.place_a((uint32_t)p.w_stride * 2, p.V - 1 - p.v0 - at.i0);
-        loop.place_b((uint32_t)p.Dh * 2, padded - 1 - at.j0);
+        const int last_w = p.V - 1 - p.v0 - at.i0, last_h = padded - 1 - at.j0;
+        loop.template place_rows<Loop::IPA>(0, [&](int r) { return (uint32_t)min(r, last_w) * (uint32_t)p.w_stride * 2; });
+        loop.template place_rows<Loop::IPB>(Loop::IPA, [&](int r) { return (uint32_t)min(r, last_h) * (uint32_t)p.Dh * 2; });
     }
     __device__ __forceinline__ void pair(Loop&, int q, typename Loop::Bases& b) const {
         b.a0 = wb + q * 128;
@@ -539,68 +563,93 @@ struct LmbDz {
         b.b0 = hb + q * 128;
         b.b1 = b.b0 + 64;
     }
-    __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
-        const int i0 = tile.i0, j0 = tile.j0;
-        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
-        const int none = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
-        LmbRow row[THW];
-        int up[THW];
+    // One exponential an entry, and little beside it: the matrix pipes stand still meanwhile.  What few tiles or entries need, the end of the
+    // vocabulary, the forbidden token and the target, is behind branches.
+    __device__ __forceinline__ void store(Loop& loop, const At& tile) const {
+        const int lane = loop.lane_here(), n = lane & 31, hi = lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+        const int first = tile.i0 + wv * TVW * 32 + 4 * hi, v_first = p.v0 + first;                // the lane's first column
+        const bool edge = p.v0 + tile.i0 + Loop::TI > p.V || (p.forbid >= p.v0 + tile.i0 && p.forbid < p.v0 + tile.i0 + Loop::TI);
+        const float log2e = 1.4426950408889634f, k = p.inv_t * log2e;
+        const int S = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
+        float off[THW], ra[THW], rc[THW];
+        int target[THW], m[THW];
 #pragma unroll
         for (int c = 0; c < THW; ++c) {
-            const int m = min(j0 + (wh * THW + c) * 32 + n, padded - 1);
-            row[c] = p.rows[m];
-            up[c] = TERMS == 0 ? p.sc.up[m] - K : 0;
+            m[c] = tile.j0 + (wh * THW + c) * 32 + n;
+            const LmbRow row = p.rows[min(m[c], padded - 1)];
+            off[c] = TERMS == 3 ? -row.lse : -row.lse * log2e;
+            const int up = TERMS == 0 ? p.sc.up[min(m[c], padded - 1)] - K + S : 0;
+            ra[c] = TERMS == 0 ? ldexpf(row.a, up) : row.a;
+            rc[c] = TERMS == 0 ? ldexpf(row.c, up) : row.c;
+            target[c] = row.target - v_first;
         }
 #pragma unroll
         for (int a = 0; a < TVW; ++a)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
-                if (i >= p.ldz) continue;
-                typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
-                i32x4 we = {0, 0, 0, 0};
+            for (int g = 0; g < 4; g += 2) {
+                const int i = first + a * 32 + 8 * g;
+                float f[8];
                 if constexpr (TERMS == 0) {
-                    we = *reinterpret_cast<const i32x4*>(p.sc.w_e + p.v0 + i);
+                    typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) we[e] = we[e] == LMB_NONE ? none : we[e];
+                    for (int q = 0; q < 2; ++q) {
+                        const i32x4 we = *reinterpret_cast<const i32x4*>(p.sc.w_e + min(p.v0 + i + 8 * q, p.last_e));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) f[4 * q + e] = ldexpf(1.f, we[e] == LMB_NONE ? 0 : we[e] - S);
+                    }
                 }
 #pragma unroll
                 for (int c = 0; c < THW; ++c) {
-                    const int m = j0 + (wh * THW + c) * 32 + n;
-                    uint16_t* dst = p.dz + (int64_t)m * p.ldz + i;
-                    float d[4];
+                    float d[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int v = p.v0 + i + e;
-                        // (the difference first: a logit and lse are large where their difference is not)
-                        const float x = fast_exp2(fmaf(loop.acc[a][c][4 * g + e], p.inv_t, -row[c].lse) * 1.4426950408889634f);
-                        d[e] = (row[c].a != 0.f ? row[c].a * x : 0.f) + (v == row[c].target ? row[c].c : 0.f);
-                        if (v == p.forbid || v >= p.V) d[e] = 0.f;
-                    }
-                    if (m >= padded) continue;
-                    if constexpr (TERMS == 0) {
-                        typedef __attribute__((__vector_size__(4 * sizeof(_Float16)))) _Float16 f16x4;
-                        f16x4 q;
+                    for (int q = 0; q < 2; ++q) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) q[e] = (_Float16)ldexpf(d[e], up[c] + we[e]);
-                        *reinterpret_cast<u32x2*>(dst) = __builtin_bit_cast(u32x2, q);
-                    } else {
-                        // every term what the ones before it leave, which fp32 holds exactly
-#pragma unroll
-                        for (int k = 0; k < TERMS; ++k) {
-                            const u32x2 q = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3])};
-                            *reinterpret_cast<u32x2*>(dst + k * p.dz_term) = q;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) d[e] -= __uint_as_float(e & 1 ? q[e / 2] & 0xffff0000u : q[e / 2] << 16);
+                        for (int e = 0; e < 4; ++e) {
+                            const float z = loop.acc[a][c][4 * (g + q) + e];
+                            // fp32 results: the difference first, a logit and lse are large where their difference is not
+                            const float x = TERMS == 3 ? fast_exp2(fmaf(z, p.inv_t, off[c]) * log2e) : fast_exp2(fmaf(z, k, off[c]));
+                            d[4 * q + e] = ra[c] * x;
                         }
+                        const uint32_t t = (uint32_t)(target[c] - a * 32 - 8 * (g + q));
+                        if (t < 4) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[4 * q + e] += t == e ? rc[c] : 0.f;
+                        }
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int v = p.v0 + i + e / 4 * 8 + e % 4;
+                            if (v == p.forbid || v >= p.V) d[e] = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < (TERMS == 0 ? 1 : TERMS); ++t) {
+                        uint32_t w[4];
+                        if constexpr (TERMS == 0) {
+                            typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(d[2 * e] * f[2 * e]), (_Float16)(d[2 * e + 1] * f[2 * e + 1])});
+                        } else {
+                            // every term what the ones before it leave, which fp32 holds exactly
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                w[e] = pack_bf16x2(d[2 * e], d[2 * e + 1]);
+                                d[2 * e] -= __uint_as_float(w[e] << 16);
+                                d[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+                            }
+                        }
+                        const u32x4 out = lmb_eight(w);
+                        const int at8 = i + 4 * hi;                     // (lane and lane + 32 share 16 columns, lmb_eight gives each eight of them)
+                        if (m[c] < padded && at8 < p.ldz) *reinterpret_cast<u32x4*>(p.dz + t * p.dz_term + (int64_t)m[c] * p.ldz + at8) = out;
                     }
                 }
             }
     }
 };
-template <int WV, int WH, int TVW, int THW, int TERMS, int BLOCK>
-__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
-    using Job = LmbDz<WV, WH, TVW, THW, TERMS, BLOCK>;
+template <typename S, int TERMS, int BLOCK>
+__global__ __launch_bounds__(64 * S::WV * S::WH, 1) void lmb_dz_kernel(LmbParams p) {
+    using Job = LmbDz<S::WV, S::WH, S::TVW, S::THW, TERMS, BLOCK>;
     __shared__ __attribute__((aligned(1024))) unsigned char ring[Job::Loop::RING];
     if (blockIdx.x == 0 && threadIdx.x < 16) p.counters[LMB_COUNTERS + threadIdx.x * 16] = 0;      // the gradients' two lists
     Job job(p);
@@ -615,7 +664,8 @@ __global__ __launch_bounds__(64 * WV * WH, 1) void lmb_dz_kernel(LmbParams p) {
 }
 
 // ---- d_hidden's and d_w's products of a chunk ----------------------------------------------------------------
-// d_hidden: columns of Dh along i, rows along j, the vocabulary is summed over, in `splits` parts.
+// d_hidden: columns of Dh along i, rows along j (all of the first term of dz, then the second's, so that W is read once for all), the vocabulary is
+// summed over, in `splits` parts.
 template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
 struct LmbHidden {
     using Loop = LmbLoop<true, false, F16, BLOCK, WV, WH, TVW, THW>;
@@ -623,15 +673,16 @@ struct LmbHidden {
         int i0, j0, s;
     };
     const LmbParams& p;
-    int M, padded, ni, nj, gj, np;
+    int M, padded, rows, ni, nj, gj, np;
     At at;
-    int all, whole, q0;                            // pairs of stages of a term; those that W itself holds; the tile's first
+    int all, whole, q0;                            // pairs of stages; those that W itself holds; the tile's first
     bool tail;
     __device__ __forceinline__ LmbHidden(const LmbParams& q) : p(q) {
         M = lmb_rows(p);
         padded = (M + 63) & ~63;
+        rows = padded * p.terms_h;
         ni = (p.Dh + Loop::TI - 1) / Loop::TI;
-        nj = (M + Loop::TJ - 1) / Loop::TJ;
+        nj = (rows + Loop::TJ - 1) / Loop::TJ;
         gj = max(min(nj, 8), 1);
         all = (p.n + 63) >> 6;
         whole = p.n >> 6;
@@ -642,20 +693,31 @@ struct LmbHidden {
         int ti, tj;
         lmb_tile(t - s * ni * nj, ni, nj, 32 / gj, gj, ti, tj);
         at = At{ti * Loop::TI, tj * Loop::TJ, s};
-        const int total = all * p.terms_h;         // (at most 3 2^18, of at most 64 parts)
-        q0 = total * s / p.splits;
-        np = total * (s + 1) / p.splits - q0;
+        q0 = all * s / p.splits;                   // (at most 2^18 pairs in at most 64 parts)
+        np = all * (s + 1) / p.splits - q0;
         tail = false;
     }
-    __device__ __forceinline__ void place_w(Loop& loop) const { loop.place_a((uint32_t)(F16 || tail ? p.Dh : p.w_stride) * 2, p.Dh - 8 - at.i0); }
+    __device__ __forceinline__ void place_w(Loop& loop) const {
+        loop.template place_columns<Loop::TI, Loop::IPA>(0, (uint32_t)(F16 || tail ? p.Dh : p.w_stride) * 2, p.Dh - 8 - at.i0);
+    }
+    // a row and its term
+    __device__ __forceinline__ int split_row(int r, int& m) const {
+        const int term = (r >= padded ? 1 : 0) + (r >= 2 * padded ? 1 : 0);
+        m = r - term * padded;
+        return term;
+    }
     __device__ __forceinline__ void place(Loop& loop) const {
         place_w(loop);
-        loop.place_b((uint32_t)p.ldz * 2, padded - 1 - at.j0);
+        // (dz as a whole is less than 2^32 bytes)
+        loop.template place_rows<Loop::IPB>(Loop::IPA, [&](int r) {
+            int m;
+            const int term = split_row(min(at.j0 + r, rows - 1), m);
+            return ((uint32_t)term * (uint32_t)p.dz_term + (uint32_t)m * (uint32_t)p.ldz) * 2;
+        });
     }
     __device__ __forceinline__ void pair(Loop& loop, int q, typename Loop::Bases& b) {
-        q += q0;
-        const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
-        if ((k >= whole) != tail) {                // into the rows behind the last whole 64, or back
+        const int k = q + q0;
+        if ((k >= whole) != tail) {                // into the rows behind the last whole 64
             tail = !tail;
             if (!F16) place_w(loop);
         }
@@ -663,22 +725,23 @@ struct LmbHidden {
         const int64_t pitch = F16 || tail ? p.Dh : p.w_stride;
         b.a0 = (const char*)(tail ? w_tail + at.i0 : w + (int64_t)(p.v0 + 64 * k) * pitch + at.i0);
         b.a1 = b.a0 + 64 * pitch;
-        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)at.j0 * p.ldz + 64 * k);
+        b.b0 = (const char*)(p.dz + 64 * k);
         b.b1 = b.b0 + 64;
     }
     __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
-        const int i0 = tile.i0, j0 = tile.j0, s = tile.s;
-        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+        const int lane = loop.lane_here(), n = lane & 31, hi = lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
 #pragma unroll
         for (int c = 0; c < THW; ++c) {
-            const int m = j0 + (wh * THW + c) * 32 + n;
-            if (m >= M) continue;
-            float* dst = p.part + ((int64_t)s * p.M + m) * p.Dh;
+            const int r = tile.j0 + (wh * THW + c) * 32 + n;
+            int m;
+            const int term = split_row(r, m);
+            if (r >= rows || m >= M) continue;
+            float* dst = p.part + ((int64_t)(tile.s * p.terms_h + term) * p.M + m) * p.Dh;
 #pragma unroll
             for (int a = 0; a < TVW; ++a)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
+                    const int i = tile.i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
                     if (i >= p.Dh) continue;
                     f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
                     if (p.add) x += *reinterpret_cast<const f32x4*>(dst + i);
@@ -711,8 +774,8 @@ struct LmbWeight {
         at = At{ti * Loop::TI, tj * Loop::TJ};
     }
     __device__ __forceinline__ void place(Loop& loop) const {
-        loop.place_a((uint32_t)p.Dh * 2, p.Dh - 8 - at.i0);
-        loop.place_b((uint32_t)p.ldz * 2, p.ldz - 8 - at.j0);
+        loop.template place_columns<Loop::TI, Loop::IPA>(0, (uint32_t)p.Dh * 2, p.Dh - 8 - at.i0);
+        loop.template place_columns<Loop::TJ, Loop::IPB>(Loop::IPA, (uint32_t)p.ldz * 2, p.ldz - 8 - at.j0);
     }
     __device__ __forceinline__ void pair(Loop&, int q, typename Loop::Bases& b) const {
         const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
@@ -722,53 +785,63 @@ struct LmbWeight {
         b.b1 = b.b0 + (int64_t)64 * p.ldz;
     }
     __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
-        const int i0 = tile.i0, j0 = tile.j0;
-        const int n = loop.lane & 31, hi = loop.lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
+        const int lane = loop.lane_here(), n = lane & 31, hi = lane >> 5, wv = loop.w % WV, wh = loop.w / WV;
 #pragma unroll
         for (int c = 0; c < THW; ++c) {
-            const int v = p.v0 + j0 + (wh * THW + c) * 32 + n;
-            if (v >= p.V || j0 + (wh * THW + c) * 32 + n >= p.n) continue;
+            const int j = tile.j0 + (wh * THW + c) * 32 + n, v = p.v0 + j;
+            const bool live = j < p.n;                                  // (the same for lane and lane + 32)
             int scale = 0;
-            if (F16 && all > 0) {
+            if (F16 && all > 0 && live) {
                 const int e = p.sc.w_e[v];
                 scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
             }
 #pragma unroll
             for (int a = 0; a < TVW; ++a)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int i = i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;
-                    if (i >= p.Dh) continue;
-                    f32x4 x = {loop.acc[a][c][4 * g], loop.acc[a][c][4 * g + 1], loop.acc[a][c][4 * g + 2], loop.acc[a][c][4 * g + 3]};
-                    if constexpr (F16) {
+                for (int g = 0; g < 4; g += 2) {
+                    const int i = tile.i0 + (wv * TVW + a) * 32 + 8 * g + 4 * hi;      // and eight further
+                    float x[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = loop.acc[a][c][4 * g + e];
+                        if constexpr (F16) x[e] = ldexpf(x[e], scale);
                     }
                     if (p.dw_f32) {
                         float* dst = (float*)p.d_w + v * p.dw_stride + i;
-                        if (p.accumulate) x += *reinterpret_cast<const f32x4*>(dst);
-                        *reinterpret_cast<f32x4*>(dst) = x;
-                    } else {
-                        uint16_t* dst = (uint16_t*)p.d_w + v * p.dw_stride + i;
-                        if (p.accumulate) {
-                            float old[4];
-                            load_bf16<4>(dst, old);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] += old[e];
+                        for (int q = 0; q < 2; ++q) {
+                            if (!live || i + 8 * q >= p.Dh) continue;
+                            f32x4 y = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                            if (p.accumulate) y += *reinterpret_cast<const f32x4*>(dst + 8 * q);
+                            *reinterpret_cast<f32x4*>(dst + 8 * q) = y;
                         }
-                        *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                        continue;
                     }
+                    if (p.accumulate) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            if (!live || i + 8 * q >= p.Dh) continue;
+                            float old[4];
+                            load_bf16<4>((const uint16_t*)p.d_w + v * p.dw_stride + i + 8 * q, old);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[4 * q + e] += old[e];
+                        }
+                    }
+                    const uint32_t w[4] = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+                    const u32x4 out = lmb_eight(w);
+                    if (live && i + 4 * hi < p.Dh) *reinterpret_cast<u32x4*>((uint16_t*)p.d_w + v * p.dw_stride + i + 4 * hi) = out;
                 }
         }
     }
 };
 
 // Both in one launch: what a workgroup of the first has left over it spends on the second.
-template <bool F16, int BLOCK, int WV, int WH, int TVW, int THW>
-__global__ __launch_bounds__(64 * WV * WH, 1) void lmb_grad_kernel(LmbParams p) {
-    using Hidden = LmbHidden<F16, BLOCK, WV, WH, TVW, THW>;
-    using Weight = LmbWeight<F16, BLOCK, WV, WH, TVW, THW>;
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[Hidden::Loop::RING];
+template <bool F16, int BLOCK, typename H, typename W>
+__global__ __launch_bounds__(64 * H::WV * H::WH, 1) void lmb_grad_kernel(LmbParams p) {
+    static_assert(H::WV * H::WH == W::WV * W::WH, "one workgroup size");
+    using Hidden = LmbHidden<F16, BLOCK, H::WV, H::WH, H::TVW, H::THW>;
+    using Weight = LmbWeight<F16, BLOCK, W::WV, W::WH, W::TVW, W::THW>;
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[Hidden::Loop::RING > Weight::Loop::RING ? Hidden::Loop::RING : Weight::Loop::RING];
     if (blockIdx.x == 0 && threadIdx.x < 8) p.counters[threadIdx.x * 16] = 0;          // the next chunk's list of dz
     const int block = blockIdx.x, xcd = block & 7, wgs = gridDim.x >> 3;
     if (p.n2 > 0 && (p.queued || block < p.n2)) {
@@ -813,7 +886,8 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
     const int64_t row = p.row_idx ? p.row_idx[r] : r;
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < p.Dh; c += 1024 * gridDim.y) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
+#pragma unroll 4
+        for (int s = 0; s < p.splits * p.terms_h; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
         if (p.f16) {
             const int scale = p.sc.out[1] - 14 - p.sc.up[r];
 #pragma unroll
@@ -830,6 +904,13 @@ constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more row
 constexpr int LMB_FEW = 256;
 static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
 
+static int g_lmb_workgroups = 0;                      // dlm_set_option: workgroups of a launch that takes tiles from a list (0: as fit the chip)
+
+int lmb_set_workgroups(int v) {
+    if (v < 0 || v % 8) return fail(DLM_ERR_INVALID_ARG, "set_option: lmhead_bwd_workgroups must be a multiple of 8, or 0");
+    g_lmb_workgroups = v;
+    return DLM_OK;
+}
 int lmb_set_columns(int v) {
     if (v < 0 || v % 256) return fail(DLM_ERR_INVALID_ARG, "set_option: lmhead_bwd_columns must be a multiple of 256, or 0");
     g_lmb_columns = v;
@@ -838,6 +919,7 @@ int lmb_set_columns(int v) {
 
 // Workgroups that fit the chip, a multiple of 8
 static int device_wgs(int a_cu) {
+    if (g_lmb_workgroups > 0) return g_lmb_workgroups;
     static int cus[64];
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256 * a_cu;
@@ -848,8 +930,24 @@ static int device_wgs(int a_cu) {
     return cus[dev] * a_cu;
 }
 
+// A shape: its tiles, and the workgroups of it that a CU holds
+struct LmbTile {
+    int i, j, a_cu;
+};
+constexpr LmbTile LMB_TILES[] = {{256, 256, 1}, {256, 128, 1}, {256, 64, 1}, {128, 128, 2}, {64, 64, 4}};
+enum { LMB_256, LMB_256x128, LMB_256x64, LMB_128, LMB_64 };
+static int64_t lmb_tiles(int shape, int64_t i, int64_t j) {
+    return ((i + LMB_TILES[shape].i - 1) / LMB_TILES[shape].i) * ((j + LMB_TILES[shape].j - 1) / LMB_TILES[shape].j);
+}
+// The largest square tile of which there are enough for most CUs; fp32 gradients, whose sums take two more registers an entry, have none of 256.
+static int lmb_shape(int64_t i, int64_t j, bool wide) {
+    if (!wide && lmb_tiles(LMB_256, i, j) >= 160) return LMB_256;
+    return lmb_tiles(LMB_128, i, j) >= 160 ? LMB_128 : LMB_64;
+}
+
 struct LmbPlan {
-    int padded, terms_h, terms_w, terms, f16, tile, chunk, splits, ni, nj;
+    int padded, terms_h, terms_w, terms, f16, chunk, splits;
+    int dz, hidden, weight;        // shapes
     size_t rows_at, h_at, tail_at, dz_at, part_at, h16_at, w16_at, ints_at, counters_at, bytes;
 };
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -862,23 +960,28 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     p.terms_h = p.f16 ? 1 : wide_h ? 3 : 2;
     p.terms_w = p.f16 ? 1 : wide_w ? 3 : 2;
     p.terms = p.f16 ? 1 : wide ? 3 : 2;
-    p.tile = wide ? 128 : 256;
     const int64_t whole = ((int64_t)a->V + 255) & ~(int64_t)255;
     int64_t most = (int64_t)(LMB_DZ_BYTES / ((size_t)p.padded * 2 * p.terms)) & ~(int64_t)255;
     if (most < 256) most = 256;
     if (g_lmb_columns > 0 && most > g_lmb_columns) most = g_lmb_columns;
     p.chunk = (int)(whole < most ? whole : most);
-    p.ni = (a->Dh + p.tile - 1) / p.tile;
-    p.nj = (p.padded + p.tile - 1) / p.tile;
+    // few rows: tiles no higher than they are
+    const int64_t rows = (int64_t)p.padded * p.terms_h, columns = a->V < p.chunk ? a->V : p.chunk;
+    p.dz = lmb_shape(columns, p.padded, wide);
+    if (!wide && p.padded <= 128 && columns >= 160 * 256) p.dz = p.padded <= 64 ? LMB_256x64 : LMB_256x128;
+    p.weight = p.hidden = lmb_shape(a->Dh, columns, wide);
+    if (p.weight == LMB_256 && rows <= 128 && !p.f16) p.hidden = LMB_256x128;
     // Parts of d_hidden's sum.  In times of a pair of stages (1.8 us of a 256 x 256 tile): the launch takes what all its tiles take together, but no
     // less than d_hidden's rounds of tiles; a part costs its rows written and read again.
-    const int64_t tiles = (int64_t)p.ni * p.nj, pairs = (p.chunk + 63) / 64 * p.terms_h, wgs = p.tile == 128 ? 512 : 256;
-    const double rest = a->d_w ? (double)p.ni * ((p.chunk + p.tile - 1) / p.tile) * (p.padded / 64) * p.terms_w : 0.0;
-    const double part = (double)a->M * a->Dh * 8e-7 * (p.tile == 128 ? 4 : 1);
+    const LmbTile th = LMB_TILES[p.hidden], tw = LMB_TILES[p.weight];
+    const int64_t tiles = lmb_tiles(p.hidden, a->Dh, rows), pairs = (columns + 63) / 64, a_cu = th.a_cu, wgs = 256 * a_cu;
+    const double unit_h = th.i * th.j / 65536.0, unit_w = tw.i * tw.j / 65536.0;
+    const double rest = a->d_w ? lmb_tiles(p.weight, a->Dh, columns) * unit_w * (p.padded / 64) * p.terms_w : 0.0;
+    const double part = (double)a->M * p.terms_h * a->Dh * 8e-7;
     int best = 1;
     double least = 1e300;
     for (int s = 1; s <= 64 && s * 4 <= pairs; ++s) {
-        const double all = (tiles * pairs + rest) / wgs, rounds = (double)((tiles * s + wgs - 1) / wgs) * pairs / s, cost = (all > rounds ? all : rounds) + part * s;
+        const double all = (tiles * pairs * unit_h + rest) / 256, rounds = (double)((tiles * s + wgs - 1) / wgs) * pairs / s * unit_h * a_cu, cost = (all > rounds ? all : rounds) + part * s;
         if (cost < least) {
             least = cost;
             best = s;
@@ -896,7 +999,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     p.h_at = take((size_t)p.padded * a->Dh * 2);
     p.tail_at = take((size_t)64 * a->Dh * 2);
     p.dz_at = take((size_t)p.terms * p.padded * p.chunk * 2);
-    if (a->d_hidden) p.part_at = take((size_t)p.splits * a->M * a->Dh * 4);
+    if (a->d_hidden) p.part_at = take((size_t)p.splits * p.terms_h * a->M * a->Dh * 4);
     if (p.f16) {
         p.h16_at = take((size_t)p.padded * a->Dh * 2);
         p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
@@ -904,6 +1007,42 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     }
     p.bytes = at;
     return p;
+}
+
+static void launch_dz(const LmbPlan& plan, dim3 grid, hipStream_t st, const LmbParams& p) {
+#define LMB_DZ(S, TERMS, BLOCK) hipLaunchKernelGGL((lmb_dz_kernel<S, TERMS, BLOCK>), grid, dim3(256), 0, st, p)
+    if (plan.terms == 3) {
+        if (plan.dz == LMB_128) LMB_DZ(Lmb128, 3, 4);
+        else LMB_DZ(Lmb64, 3, 4);
+    } else if (plan.f16) {
+        if (plan.dz == LMB_256) LMB_DZ(Lmb256, 0, 0);
+        else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 0, 0);
+        else LMB_DZ(Lmb64, 0, 0);
+    } else {
+        if (plan.dz == LMB_256) LMB_DZ(Lmb256, 2, 0);
+        else if (plan.dz == LMB_256x128) LMB_DZ(Lmb256x128, 2, 0);
+        else if (plan.dz == LMB_256x64) LMB_DZ(Lmb256x64, 2, 0);
+        else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 2, 0);
+        else LMB_DZ(Lmb64, 2, 0);
+    }
+#undef LMB_DZ
+}
+static void launch_grad(const LmbPlan& plan, dim3 grid, hipStream_t st, const LmbParams& p) {
+#define LMB_GRAD(F16, BLOCK, H, W) hipLaunchKernelGGL((lmb_grad_kernel<F16, BLOCK, H, W>), grid, dim3(256), 0, st, p)
+    if (plan.terms == 3) {
+        if (plan.weight == LMB_128) LMB_GRAD(false, 4, Lmb128, Lmb128);
+        else LMB_GRAD(false, 4, Lmb64, Lmb64);
+    } else if (plan.f16) {
+        if (plan.weight == LMB_256) LMB_GRAD(true, 0, Lmb256, Lmb256);
+        else if (plan.weight == LMB_128) LMB_GRAD(true, 0, Lmb128, Lmb128);
+        else LMB_GRAD(true, 0, Lmb64, Lmb64);
+    } else {
+        if (plan.hidden == LMB_256) LMB_GRAD(false, 0, Lmb256, Lmb256);
+        else if (plan.hidden == LMB_256x128) LMB_GRAD(false, 0, Lmb256x128, Lmb256);
+        else if (plan.weight == LMB_128) LMB_GRAD(false, 0, Lmb128, Lmb128);
+        else LMB_GRAD(false, 0, Lmb64, Lmb64);
+    }
+#undef LMB_GRAD
 }
 
 static int validate_lmb(const dlm_lmhead_bwd_args* a, const char* who) {
@@ -996,6 +1135,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.sc.w16 = (uint16_t*)(ws + plan.w16_at);
         p.sc.tail16 = p.w_tail;
     }
+    p.last_e = (int)(((int64_t)a->V + 255) / 256 * 256) - 4;
     p.counters = (int*)(ws + plan.counters_at);
     p.d_hidden = a->d_hidden;
     p.dh_stride = a->d_hidden_stride_row;
@@ -1022,26 +1162,22 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.v0 = (int)v0;
         p.n = (int)(a->V - v0 < plan.chunk ? a->V - v0 : plan.chunk);
         p.add = v0 > 0;
-        const int64_t vt = (p.n + plan.tile - 1) / plan.tile, all = (p.n + 63) / 64;
-        p.splits = v0 > 0 && all * p.terms_h < 2 * plan.splits ? 1 : plan.splits;          // (parts that the last chunk has no work for stay as they are)
-        p.n2 = hidden ? (plan.ni * plan.nj * p.splits + 7) / 8 * 8 : 0;
-        const int64_t n1 = (vt * plan.nj + 7) / 8 * 8, n3 = a->d_w ? (plan.ni * vt + 7) / 8 * 8 : 0;
+        const int64_t pairs = (p.n + 63) / 64;
+        p.splits = v0 > 0 && pairs < 2 * plan.splits ? 1 : plan.splits;        // (parts that the last chunk has no work for stay as they are)
+        const auto up8 = [](int64_t n) { return (n + 7) / 8 * 8; };
+        const int64_t n1 = up8(lmb_tiles(plan.dz, p.n, plan.padded)), n3 = a->d_w ? up8(lmb_tiles(plan.weight, a->Dh, p.n)) : 0;
+        p.n2 = hidden ? (int)up8(lmb_tiles(plan.hidden, a->Dh, (int64_t)plan.padded * p.terms_h) * p.splits) : 0;
         // A list of tiles where they are more than the workgroups that fit the chip, and long enough to request the next one behind (see LmbLoop)
-        const int wgs = device_wgs(plan.tile == 128 ? 2 : 1);
         if (a->M > 0) {
+            const int wgs = device_wgs(LMB_TILES[plan.dz].a_cu);
             p.queued = n1 > wgs && a->Dh >= 128;
-            const dim3 grid((unsigned)(p.queued ? wgs : n1));
-            if (plan.terms == 3) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 2, 2, 3, 4>), grid, dim3(256), 0, st, p);
-            else if (plan.terms == 2) hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 2, 0>), grid, dim3(256), 0, st, p);
-            else hipLaunchKernelGGL((lmb_dz_kernel<2, 2, 4, 4, 0, 0>), grid, dim3(256), 0, st, p);
+            launch_dz(plan, dim3((unsigned)(p.queued ? wgs : n1)), st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
         }
         if (p.n2 + n3 == 0) continue;
-        p.queued = a->M > 0 && p.n2 + n3 > wgs && (!hidden || all * p.terms_h >= 2 * p.splits);
-        const dim3 grid((unsigned)(p.queued ? wgs : p.n2 + n3));
-        if (plan.terms == 3) hipLaunchKernelGGL((lmb_grad_kernel<false, 4, 2, 2, 2, 2>), grid, dim3(256), 0, st, p);
-        else if (plan.terms == 2) hipLaunchKernelGGL((lmb_grad_kernel<false, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((lmb_grad_kernel<true, 0, 2, 2, 4, 4>), grid, dim3(256), 0, st, p);
+        const int wgs = device_wgs(LMB_TILES[plan.weight].a_cu);
+        p.queued = a->M > 0 && p.n2 + n3 > wgs && (!hidden || pairs >= 2 * p.splits);
+        launch_grad(plan, dim3((unsigned)(p.queued ? wgs : p.n2 + n3)), st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_grad_kernel launch")) != DLM_OK) return rc;
     }
     if (!hidden) return DLM_OK;

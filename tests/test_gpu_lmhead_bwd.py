@@ -143,6 +143,39 @@ def test_gradient(M, Dh, V, types):
     near(d_w, dw, types[1] == F32)
 
 
+def check(c, types, live=None):
+    d_h, d_w = (torch.full((n, c.Dh), float("nan"), dtype=t, device=DEV) for n, t in ((c.M, types[0]), (c.V, types[1])))
+    c.call(d_h, d_w, live)
+    dh, bh, dw, bw = c.want(types[0] == F32, types[1] == F32, live)
+    within(d_h[:len(dh)], dh, bh)
+    within(d_w, dw, bw)
+    near(d_h[:len(dh)], dh, types[0] == F32)
+    near(d_w, dw, types[1] == F32)
+    assert d_h[len(dh):].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,Dh,V", [(50, 64, 41000), (100, 128, 41003), (200, 64, 41000), (300, 64, 40961), (300, 320, 12000), (20, 704, 12000)])
+def test_vocabularies_that_take_large_tiles(M, Dh, V, dtype):
+    check(Case(M, Dh, V, forbid=V - 1), (dtype, dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("live", [None, 60, 130])
+@pytest.mark.parametrize("M,Dh,V", [(16, 64, 1000), (70, 448, 1601), (200, 128, 3000), (330, 320, 2003), (300, 128, 13000), (140, 64, 41000)])
+def test_workgroups_that_take_one_tile_after_another(M, Dh, V, live, dtype):
+    """Eight or sixteen workgroups for all tiles, so that each takes many: in one chunk and in several."""
+    c = Case(M, Dh, V, forbid=3, gap=8 if V == 2003 else 0)
+    for workgroups, columns in ((8, 0), (16, 1024)):
+        dlm.set_option("lmhead_bwd_workgroups", workgroups)
+        dlm.set_option("lmhead_bwd_columns", columns)
+        try:
+            check(c, (dtype, dtype), live)
+        finally:
+            dlm.set_option("lmhead_bwd_workgroups", 0)
+            dlm.set_option("lmhead_bwd_columns", 0)
+
+
 @pytest.mark.parametrize("scatter", [False, True])
 @pytest.mark.parametrize("live", [None, 0, 1, 63, 64, 70, 1000, -5])
 def test_rows_by_index_and_a_count_on_the_device(scatter, live):
@@ -165,7 +198,10 @@ def test_one_gradient_alone_and_one_cotangent_alone():
     d_h, d_w = torch.zeros_like(both_h), torch.zeros_like(both_w)
     c.call(d_h, None)
     c.call(None, d_w)
-    assert torch.equal(d_h, both_h) and torch.equal(d_w, both_w)
+    dh, bh, dw, bw = c.want(False, True)
+    for a, b, want, bound in ((d_h, both_h, dh, bh), (d_w, both_w, dw, bw)):
+        within(a, want, bound)
+        within(b, want, bound)
     for lse, zt in ((True, False), (False, True)):
         kw = {} if lse else dict(d_lse=None)
         kw.update({} if zt else dict(d_ztarget=None, target=None))

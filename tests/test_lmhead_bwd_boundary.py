@@ -64,10 +64,10 @@ def test_workspace_sizes():
     for M in (1, 65, 512, 4096, 32768):
         kw = dict(M=M, V=126464, Dh=4096, w_stride_row=4096, hidden_stride_row=4096)
         both, rows, weights = (size(C.byref(_args(**kw, **m))) for m in ({}, dict(d_w=None), dict(d_hidden=None)))
-        assert weights < both == rows
-        most = (2 << 30) + 2 * (M + 63) * 4096 * 2 + 64 * M * 4096 * 4 + (8 << 20)
+        assert weights < both and weights < rows
+        most = (2 << 30) + 2 * (M + 63) * 4096 * 2 + 3 * 64 * M * 4096 * 4 + (8 << 20)
         assert both <= most + 126464 * 4096 * 2              # a copy of W
-        assert size(C.byref(_args(**kw, d_w_type=1))) <= most
+        assert size(C.byref(_args(**kw, d_w_type=1))) <= most and rows <= most + 126464 * 4096 * 2
 
 
 def test_binding_refuses_what_is_not_on_the_gpu():
