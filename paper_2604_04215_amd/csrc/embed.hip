@@ -18,10 +18,10 @@ struct EmbedParams {
     int64_t out_st;
 };
 
-// TPR threads a row
+// TPR threads a row, pieces of 16 bytes of what is written: the stores of a wavefront cover whole lines
 template <bool F32, int TPR>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
-    constexpr int ROWS = 256 / TPR;
+    constexpr int ROWS = 256 / TPR, E = Piece<F32>::E;
     const int l = threadIdx.x % TPR;
     const int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
     if (t >= p.T) return;
@@ -29,27 +29,41 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
     const bool known = (uint32_t)token < (uint32_t)p.V;
     const uint16_t* src = p.table + (int64_t)(known ? token : 0) * p.table_st;
 #pragma unroll 4
-    for (int c = 8 * l; c < p.Dh; c += 8 * TPR) {
-        float f[8];
-        Piece<false>::open(known ? *reinterpret_cast<const u32x4*>(src + c) : u32x4{0, 0, 0, 0}, f);
+    for (int c = E * l; c < p.Dh; c += E * TPR) {
+        float f[E];
+        load_bf16<E>(src + c, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = known ? f[e] * p.scale : 0.f;
-        if constexpr (F32) {
-            const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
-            Piece<true>::stream_out(p.out, t * p.out_st + c, Piece<true>::close(lo));
-            Piece<true>::stream_out(p.out, t * p.out_st + c + 4, Piece<true>::close(hi));
-        } else {
-            Piece<false>::stream_out(p.out, t * p.out_st + c, Piece<false>::close(f));
-        }
+        for (int e = 0; e < E; ++e) f[e] = known ? f[e] * p.scale : 0.f;
+        Piece<F32>::stream_out(p.out, t * p.out_st + c, Piece<F32>::close(f));
     }
 }
 
 // ---- gradient: sorting --------------------------------------------------------------------------------------
-// Runs of RUN tokens are sorted by themselves, a workgroup each, then up to MERGE runs at a time become one: an entry's place in the merged
+// Runs of 2^BITS tokens are sorted by themselves, a workgroup each, then up to MERGE runs at a time become one: an entry's place in the merged
 // run is its place in its own plus, for every other run, the number of entries there that go before it (a binary search each; equal
 // tokens stay in the order of their positions, since earlier runs hold earlier ones).
-constexpr int RUN = 2048, RUN_BITS = 11, MERGE = 32;
-constexpr int EMBED_MAX_V = (1 << (32 - RUN_BITS)) - 2;       // a token (or V: none) and a place in its run share 32 bits
+constexpr int MERGE = 32;
+constexpr int EMBED_MAX_V = (1 << 21) - 2;                    // a token (or V: none) and a place in its run share 32 bits: 21 and 11
+// 512 entries for a few tokens, which one wavefront sorts without a barrier; 8192, of which there are few to merge, where they leave the token
+// its bits (65536 tokens, us of the sort and the merge: runs of 2048 10 + 54, of 8192 32 + 19).
+inline int run_bits(int T, int V) { return T <= 512 ? 9 : T <= 2048 || V >= (1 << 19) - 1 ? 11 : 13; }
+
+// the value of lane ^ MASK, without a trip through LDS
+template <int MASK>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
+    if constexpr (MASK == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);
+    if constexpr (MASK == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);
+    if constexpr (MASK == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);     // 7 -, then 3 -
+    if constexpr (MASK == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);                                                    // rotated by 8 of 16
+    if constexpr (MASK == 16) {
+        const auto w = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return lane_id() & 16 ? w[0] : w[1];
+    }
+    if constexpr (MASK == 32) {
+        const auto w = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return lane_id() & 32 ? w[0] : w[1];
+    }
+}
 
 struct SortParams {
     int T, V;
@@ -62,13 +76,52 @@ struct SortParams {
     int pieces;
 };
 
-__global__ __launch_bounds__(256) void embed_sort_kernel(SortParams p) {
-    __shared__ uint32_t lds[RUN];
+// one step of the network: entries whose numbers differ in bit BIT put in order, up or down by bit SIZE; then the steps behind it
+template <int BITS, int SIZE, int BIT>
+__device__ __forceinline__ void embed_network(uint32_t (&k)[8], uint32_t* lds, int tid) {
+    constexpr int THREADS = 1 << (BITS - 3);
+    if constexpr (BIT < 3) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e >> BIT & 1) continue;
+            const int o = e | 1 << BIT;
+            const bool up = SIZE >= 3 ? SIZE == BITS || !(tid >> (SIZE >= 3 ? SIZE - 3 : 0) & 1) : !(e >> SIZE & 1);
+            const uint32_t lo = min(k[e], k[o]), hi = max(k[e], k[o]);
+            k[e] = up ? lo : hi;
+            k[o] = up ? hi : lo;
+        }
+    } else {
+        constexpr int MASK = 1 << (BIT - 3);
+        const bool up = SIZE == BITS || !(tid >> (SIZE - 3) & 1), lower = !(tid & MASK);
+        uint32_t other[8];
+        if constexpr (MASK < WAVE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) other[e] = from_lane_xor<MASK>(k[e]);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) lds[e * THREADS + tid] = k[e];
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) other[e] = lds[e * THREADS + (tid ^ MASK)];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = up == lower ? min(k[e], other[e]) : max(k[e], other[e]);
+    }
+    if constexpr (BIT > 0) embed_network<BITS, SIZE, BIT - 1>(k, lds, tid);
+    else if constexpr (SIZE < BITS) embed_network<BITS, SIZE + 1, SIZE>(k, lds, tid);
+}
+
+template <int BITS>
+__global__ __launch_bounds__(1 << (BITS - 3)) void embed_sort_kernel(SortParams p) {
+    constexpr int RUN = 1 << BITS, THREADS = RUN / 8;
+    __shared__ uint32_t lds[THREADS > WAVE ? RUN : 1];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= p.runs) {
         for (int64_t row = blockIdx.x - p.runs; row < p.rows; row += gridDim.x - p.runs) {
             const int n = (int)min((int64_t)p.pieces, p.total - row * p.pieces);
-            for (int i = tid; i < n; i += 256) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>((char*)p.table + row * p.pitch) + i);
+            #pragma unroll 4
+            for (int i = tid; i < n; i += THREADS) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>((char*)p.table + row * p.pitch) + i);
         }
         return;
     }
@@ -79,79 +132,48 @@ __global__ __launch_bounds__(256) void embed_sort_kernel(SortParams p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 8 * tid + e;
-        uint32_t token = 0xffffffffu >> RUN_BITS;
+        uint32_t token = 0xffffffffu >> BITS;
         if (i < n) {
             const int32_t x = p.tokens[t0 + i];
             token = (uint32_t)x < (uint32_t)p.V ? x : p.V;
         }
-        k[e] = token << RUN_BITS | i;
+        k[e] = token << BITS | i;
     }
     // Bitonic network over element numbers i = 8 tid + e: partners by the bits of i below 3 are in the thread's own registers, below 9 in the
     // wavefront, above in another one.
-#pragma unroll
-    for (int size = 1; size <= RUN_BITS; ++size) {
-#pragma unroll
-        for (int bit = size - 1; bit >= 0; --bit) {
-            if (bit < 3) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (e >> bit & 1) continue;
-                    const int o = e | 1 << bit;
-                    const bool up = size >= 3 ? !(tid >> (size - 3) & 1) : !(e >> size & 1);
-                    const uint32_t lo = min(k[e], k[o]), hi = max(k[e], k[o]);
-                    k[e] = up ? lo : hi;
-                    k[o] = up ? hi : lo;
-                }
-            } else {
-                const int mask = 1 << (bit - 3);
-                const bool up = size == RUN_BITS || !(tid >> (size - 3) & 1), lower = !(tid & mask);
-                uint32_t other[8];
-                if (mask < WAVE) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) other[e] = shfl_xor(k[e], mask);
-                } else {
-                    __syncthreads();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) lds[e * 256 + tid] = k[e];
-                    __syncthreads();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) other[e] = lds[e * 256 + (tid ^ mask)];
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) k[e] = up == lower ? min(k[e], other[e]) : max(k[e], other[e]);
-            }
-        }
-    }
+    embed_network<BITS, 1, 0>(k, lds, tid);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 8 * tid + e;
         if (i < n) {
-            p.token[t0 + i] = k[e] >> RUN_BITS;
+            p.token[t0 + i] = k[e] >> BITS;
             p.pos[t0 + i] = (int32_t)t0 + (k[e] & (RUN - 1));
         }
     }
 }
 
-// Runs of `len` entries, MERGE of them into one
+// Runs of `len` entries (a power of two), MERGE of them into one.  Eight runs are searched at a time: a search is a chain of trips to memory.  (Eight
+// probes a trip instead of one are slower, 78 us where 54: it is the loads themselves that take the time.)
 __global__ __launch_bounds__(256) void embed_merge_kernel(const int32_t* token, const int32_t* pos, int32_t* token_out, int32_t* pos_out, int T, int64_t len) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= T) return;
     const int x = token[i], at = pos[i];
     const int64_t run = i / len, group = run / MERGE * MERGE;
     int64_t to = group * len + (i - run * len);
-    for (int j = 0; j < MERGE; ++j) {
-        const int64_t r = group + j, r0 = r * len;
-        if (r0 >= T) break;
-        if (r == run) continue;
-        // entries of run r with a token below x, or, in an earlier run, at most x
-        const int y = x + (r < run ? 1 : 0);
-        int64_t lo = r0, hi = r0 + len < T ? r0 + len : T;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (token[mid] < y) lo = mid + 1;
-            else hi = mid;
+    for (int j0 = 0; j0 < MERGE && (group + j0) * len < T; j0 += 8) {
+        // entries of each run with a token below x, or, in an earlier run, at most x
+        int64_t lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lo[j] = 0;
+        for (int64_t step = len; step > 0; step >>= 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t r = group + j0 + j, last = r * len + lo[j] + step - 1;
+                if (lo[j] + step <= len && last < T && r != run && token[last] < x + (r < run ? 1 : 0)) lo[j] += step;
+            }
         }
-        to += lo - r0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) to += lo[j];
     }
     token_out[to] = x;
     pos_out[to] = at;
@@ -172,103 +194,131 @@ struct EmbedGradParams {
     float* part;                   // [groups][2][Dh]: the sum of a token that began in an earlier group; of one that goes on in the next
 };
 
-// the sum of a token's rows into the table
+// what a table holds of 4 entries
 template <bool F32>
-__device__ __forceinline__ void embed_store(const EmbedGradParams& p, int token, int c, const f32x4& a) {
+__device__ __forceinline__ f32x4 embed_held(const EmbedGradParams& p, int token, int c) {
     const int64_t at = (int64_t)token * p.table_st + c;
-    float f[4] = {a[0] * p.scale, a[1] * p.scale, a[2] * p.scale, a[3] * p.scale};
     if constexpr (F32) {
-        float* dst = (float*)p.table + at;
-        if (p.accumulate) {
-            const f32x4 old = *reinterpret_cast<const f32x4*>(dst);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] += old[e];
-        }
-        *reinterpret_cast<f32x4*>(dst) = f32x4{f[0], f[1], f[2], f[3]};
+        return *reinterpret_cast<const f32x4*>((const float*)p.table + at);
     } else {
-        uint16_t* dst = (uint16_t*)p.table + at;
-        if (p.accumulate) {
-            float old[4];
-            load_bf16<4>(dst, old);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] += old[e];
-        }
-        *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+        float old[4];
+        load_bf16<4>((const uint16_t*)p.table + at, old);
+        return f32x4{old[0], old[1], old[2], old[3]};
     }
+}
+// the sum of a token's rows into the table, on top of `old`
+template <bool F32>
+__device__ __forceinline__ void embed_store(const EmbedGradParams& p, int token, int c, const f32x4& a, const f32x4& old) {
+    const int64_t at = (int64_t)token * p.table_st + c;
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = a[e] * p.scale;
+    if (p.accumulate) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] += old[e];
+    }
+    if constexpr (F32) *reinterpret_cast<f32x4*>((float*)p.table + at) = f32x4{f[0], f[1], f[2], f[3]};
+    else *reinterpret_cast<u32x2*>((uint16_t*)p.table + at) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
 }
 
 // A wavefront adds the rows of one chunk, 64 pieces of each; at the end of a token it stores the sum.  The sums of a token that lies in several
 // chunks of the workgroup meet in LDS and are added in order by the wavefront that has its first row; those of one that lies in several
 // groups go to `part`.
-template <bool F32IN, bool F32>
+//
+// Rows come in batches, one ahead; with ACC what the table holds of each row's token comes with it, whether the token ends there or not (then it
+// is a line that is at hand already): asked for where a token ends, every such row would wait for all requests before it.
+template <bool F32IN, bool F32, bool ACC>
 __global__ __launch_bounds__(GROUP * WAVE) void embed_grad_kernel(EmbedGradParams p) {
     using P = Piece<F32IN>;
-    constexpr int E = P::E, Q = E / 4, AHEAD = 8;
+    constexpr int E = P::E, Q = E / 4, BATCH = ACC ? 4 : 8;
     __shared__ f32x4 lds[GROUP][2][Q][WAVE];       // [0]: of a token that began in an earlier chunk, [1]: of one that goes on in the next
+    __shared__ int ends[GROUP + 1][2];             // every chunk's first and last token; the one behind the group
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
     const int slices = gridDim.x / p.groups, group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
     const int c0 = (slice * WAVE + lane) * E, c = c0 < p.Dh ? c0 : 0;          // (lanes behind the row read its beginning, and store nothing)
     const bool live = c0 < p.Dh;
     const int64_t first = (int64_t)group * GROUP * p.chunk, i0 = first + (int64_t)wave * p.chunk;
     const int n = (int)max((int64_t)0, min((int64_t)p.chunk, p.T - i0));
-    const int32_t *token = p.token + i0, *pos = p.pos + i0;
-    const int x_first = n > 0 ? token[0] : p.V;
+    // the chunk's entries, one a lane
+    const int at = n > 0 ? min(lane, n - 1) : 0;
+    const int tokens = n > 0 ? p.token[i0 + at] : p.V, places = n > 0 ? p.pos[i0 + at] : 0;
+    const auto token_of = [&](int i) { return __builtin_amdgcn_readlane(tokens, i); };
+    const int x_first = token_of(0);
     int x_last = p.V;                              // the token of the chunk's end, where it began here and goes on
     if (x_first < p.V) {                           // (else the chunk holds no token: V sorts last)
-        const int before = i0 > 0 ? token[-1] : -1, behind = i0 + n < p.T ? token[n] : -1;
-        typename P::Raw ring[AHEAD];
+        const int before = i0 > 0 ? p.token[i0 - 1] : -1, behind = i0 + n < p.T ? p.token[i0 + n] : -1;
+        typename P::Raw rows[2][BATCH];
+        f32x4 old[2][ACC ? BATCH : 1][Q];
+        const auto request = [&](int k0, int b) {
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) ring[k] = P::stream(p.dy, (int64_t)pos[min(k, n - 1)] * p.dy_st + c);
-        float a[E];
+            for (int k = 0; k < BATCH; ++k) {
+                const int i = min(k0 + k, n - 1);
+                rows[b][k] = P::stream(p.dy, (int64_t)__builtin_amdgcn_readlane(places, i) * p.dy_st + c);
+                if constexpr (ACC) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) a[e] = 0.f;
+                    for (int q = 0; q < Q; ++q) old[b][k][q] = embed_held<F32>(p, token_of(i) < p.V ? token_of(i) : x_first, c + 4 * q);
+                }
+            }
+        };
+        f32x4 a[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) a[q] = f32x4{0.f, 0.f, 0.f, 0.f};
         bool began = x_first != before;            // the token at hand began in this chunk
-        for (int k0 = 0; k0 < n; k0 += AHEAD) {
+        const auto add = [&](int k0, int b) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
+            for (int k = 0; k < BATCH; ++k) {
                 const int i = k0 + k;
                 if (i >= n) break;
                 float f[E];
-                P::open(ring[k], f);
-                ring[k] = P::stream(p.dy, (int64_t)pos[min(i + AHEAD, n - 1)] * p.dy_st + c);
+                P::open(rows[b][k], f);
 #pragma unroll
-                for (int e = 0; e < E; ++e) a[e] += f[e];
-                const int x = token[i], next = i + 1 < n ? token[i + 1] : behind;
+                for (int e = 0; e < E; ++e) a[e / 4][e % 4] += f[e];
+                const int x = token_of(i), next = i + 1 < n ? token_of(i + 1) : behind;
                 if (x == next && i + 1 < n) continue;
                 const bool goes_on = x == next;    // into the next chunk
                 if (goes_on && began) x_last = x;
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
-                    const f32x4 sum = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                    if (!began || goes_on) lds[wave][began ? 1 : 0][q][lane] = sum;
-                    else if (x < p.V && live) embed_store<F32>(p, x, c + 4 * q, sum);
+                    if (!began || goes_on) lds[wave][began ? 1 : 0][q][lane] = a[q];
+                    else if (x < p.V && live) embed_store<F32>(p, x, c + 4 * q, a[q], old[b][ACC ? k : 0][q]);
+                    a[q] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
-#pragma unroll
-                for (int e = 0; e < E; ++e) a[e] = 0.f;
                 began = true;
             }
+        };
+        request(0, 0);
+        for (int k0 = 0; k0 < n; k0 += 2 * BATCH) {
+            if (k0 + BATCH < n) request(k0 + BATCH, 1);
+            add(k0, 0);
+            if (k0 + 2 * BATCH < n) request(k0 + 2 * BATCH, 0);
+            add(k0 + BATCH, 1);
         }
+    }
+    if (lane == 0) {
+        ends[wave][0] = x_first;
+        ends[wave][1] = n > 0 ? token_of(n - 1) : p.V;
+        if (wave == GROUP - 1) ends[GROUP][0] = first + (int64_t)GROUP * p.chunk < p.T ? p.token[first + (int64_t)GROUP * p.chunk] : p.V;
     }
     __syncthreads();
     // from this wavefront's chunk on: the token that began in it, and, the first wavefront, one that began in an earlier group
 #pragma unroll 1
     for (int which = wave == 0 ? 0 : 1; which < 2; ++which) {
-        const int x = which ? x_last : (group > 0 && x_first == p.token[first - 1] ? x_first : p.V);
+        const int x = which ? x_last : (group > 0 && x_first < p.V && x_first == p.token[first - 1] ? x_first : p.V);
         if (x >= p.V) continue;
         f32x4 sum[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) sum[q] = lds[wave][which][q][lane];
-        int64_t end = i0 + n;                      // behind the last entry added
-        for (int k = wave + 1; k < GROUP && end < p.T && p.token[end] == x && p.token[end - 1] == x; ++k) {
+        int k = wave;                              // the last chunk added
+        while (k + 1 < GROUP && ends[k][1] == x && ends[k + 1][0] == x) {
+            ++k;
 #pragma unroll
             for (int q = 0; q < Q; ++q) sum[q] += lds[k][0][q][lane];
-            end = min(end + p.chunk, (int64_t)p.T);
         }
-        const bool goes_on = end < p.T && p.token[end] == x && p.token[end - 1] == x;
+        const bool goes_on = k + 1 == GROUP && ends[k][1] == x && ends[GROUP][0] == x;
         if (!live) continue;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            if (which && !goes_on) embed_store<F32>(p, x, c + 4 * q, sum[q]);
+            if (which && !goes_on) embed_store<F32>(p, x, c + 4 * q, sum[q], ACC ? embed_held<F32>(p, x, c + 4 * q) : f32x4{0.f, 0.f, 0.f, 0.f});
             else *reinterpret_cast<f32x4*>(p.part + ((int64_t)group * 2 + which) * p.Dh + c + 4 * q) = sum[q];
         }
     }
@@ -295,7 +345,7 @@ __global__ __launch_bounds__(WAVE) void embed_join_kernel(EmbedGradParams p) {
     f32x4 a = *reinterpret_cast<const f32x4*>(p.part + ((int64_t)group * 2 + 1) * p.Dh + c);
 #pragma unroll 8
     for (int k = group + 1; k <= last; ++k) a += *reinterpret_cast<const f32x4*>(p.part + (int64_t)k * 2 * p.Dh + c);
-    embed_store<F32>(p, x, c, a);
+    embed_store<F32>(p, x, c, a, p.accumulate ? embed_held<F32>(p, x, c) : f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
@@ -323,17 +373,18 @@ static void launch_embed(const EmbedParams& all, hipStream_t st) {
 
 // How the gradient is cut up, and where its workspace holds what
 struct EmbedPlan {
-    int runs, levels, chunk, groups;
+    int bits, runs, levels, chunk, groups;
     size_t list_bytes, part_at, bytes;              // one list of T; the sums behind the lists
 };
-static EmbedPlan plan_embed(int T, int Dh) {
+static EmbedPlan plan_embed(int T, int V, int Dh) {
     EmbedPlan p = {};
-    p.runs = (int)(((int64_t)T + RUN - 1) / RUN);
+    p.bits = run_bits(T, V);
+    p.runs = (int)(((int64_t)T + (1 << p.bits) - 1) >> p.bits);
     for (int64_t n = p.runs; n > 1; n = (n + MERGE - 1) / MERGE) ++p.levels;
     // some 8192 wavefronts, of chunks that are neither so short that their borders cost more than their rows nor so long that a few run on alone
     const int64_t slices = (Dh + 511) / 512;
     int64_t chunk = T * slices / 8192;
-    chunk = chunk < 8 ? 8 : chunk > 128 ? 128 : chunk;
+    chunk = chunk < 8 ? 8 : chunk > WAVE ? WAVE : chunk;
     p.chunk = (int)chunk;
     p.groups = (int)((T + GROUP * chunk - 1) / (GROUP * chunk));
     p.list_bytes = ((size_t)T * 4 + 15) / 16 * 16;
@@ -364,7 +415,7 @@ extern "C" int dlm_embed(const dlm_embed_args* a, void* stream) {
 
 extern "C" size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args* a) {
     if (!a || a->struct_size != sizeof(dlm_embed_bwd_args) || a->T <= 0 || a->Dh <= 0) return 0;
-    return plan_embed(a->T, a->Dh).bytes;
+    return plan_embed(a->T, a->V, a->Dh).bytes;
 }
 
 extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
@@ -387,7 +438,7 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
         if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
     }
     hipStream_t st = (hipStream_t)stream;
-    const EmbedPlan plan = plan_embed(a->T, a->Dh);
+    const EmbedPlan plan = plan_embed(a->T, a->V, a->Dh);
     char* ws = (char*)a->workspace;
     int32_t* list[4];
     for (int i = 0; i < 4; ++i) list[i] = (int32_t*)(ws + i * plan.list_bytes);
@@ -399,13 +450,16 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
         s.pitch = gaps ? pitch : 4096 * 16;
         s.rows = (s.total + s.pieces - 1) / s.pieces;
     }
-    const int clear = (int)(s.rows < 2048 ? s.rows : 2048);
+    const int most = (2048 << 13) >> plan.bits;      // (as many threads whatever the workgroup's size)
+    const int clear = (int)(s.rows < most ? s.rows : most);
     if (plan.runs + clear == 0) return DLM_OK;
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(plan.runs + clear), dim3(256), 0, st, s);
+    if (plan.bits == 9) hipLaunchKernelGGL(embed_sort_kernel<9>, dim3(plan.runs + clear), dim3(64), 0, st, s);
+    else if (plan.bits == 11) hipLaunchKernelGGL(embed_sort_kernel<11>, dim3(plan.runs + clear), dim3(256), 0, st, s);
+    else hipLaunchKernelGGL(embed_sort_kernel<13>, dim3(plan.runs + clear), dim3(1024), 0, st, s);
     if ((rc = check_hip(hipGetLastError(), "embed_sort_kernel launch")) != DLM_OK) return rc;
     if (a->T == 0) return DLM_OK;
     int from = 0;
-    int64_t len = RUN;
+    int64_t len = 1 << plan.bits;
     for (int level = 0; level < plan.levels; ++level) {
         const int to = from ^ 2;
         hipLaunchKernelGGL(embed_merge_kernel, dim3((unsigned)(((int64_t)a->T + 255) / 256)), dim3(256), 0, st, list[from], list[from + 1], list[to], list[to + 1], a->T, len);
@@ -418,10 +472,16 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
     const bool in32 = a->d_out_type == DLM_ROW_F32, out32 = a->d_table_type == DLM_ROW_F32;
     const int per = in32 ? 256 : 512;
     const dim3 grid((unsigned)((int64_t)plan.groups * ((a->Dh + per - 1) / per))), threads(GROUP * WAVE);
-    if (in32 && out32) hipLaunchKernelGGL((embed_grad_kernel<true, true>), grid, threads, 0, st, p);
-    else if (in32) hipLaunchKernelGGL((embed_grad_kernel<true, false>), grid, threads, 0, st, p);
-    else if (out32) hipLaunchKernelGGL((embed_grad_kernel<false, true>), grid, threads, 0, st, p);
-    else hipLaunchKernelGGL((embed_grad_kernel<false, false>), grid, threads, 0, st, p);
+#define EMBED_GRAD(IN, OUT)                                                                                \
+    {                                                                                                    \
+        if (a->accumulate) hipLaunchKernelGGL((embed_grad_kernel<IN, OUT, true>), grid, threads, 0, st, p); \
+        else hipLaunchKernelGGL((embed_grad_kernel<IN, OUT, false>), grid, threads, 0, st, p);           \
+    }
+    if (in32 && out32) EMBED_GRAD(true, true)
+    else if (in32) EMBED_GRAD(true, false)
+    else if (out32) EMBED_GRAD(false, true)
+    else EMBED_GRAD(false, false)
+#undef EMBED_GRAD
     if ((rc = check_hip(hipGetLastError(), "embed_grad_kernel launch")) != DLM_OK) return rc;
     if (plan.groups < 2) return DLM_OK;
     const dim3 join(plan.groups - 1, (a->Dh + 255) / 256);

@@ -372,11 +372,12 @@ static void pick_norm(const NormParams& p, hipStream_t st) {
     else if (D <= 256) launch_norm<F32, 8, 32>(p, st);
     else if (D <= 512) launch_norm<F32, 8, 64>(p, st);
     else if (p.T > 2048) {
+        constexpr int N = F32 ? 16 : 32;            // (32 entries of fp32 a thread: 244 registers, 659 us where 16 take 250)
         if (D <= 1024) launch_norm<F32, 16, 64>(p, st);
-        else if (D <= 2048) launch_norm<F32, 32, 64>(p, st);
-        else if (D <= 4096) launch_norm<F32, 32, 128>(p, st);
-        else if (D <= 8192) launch_norm<F32, 32, 256>(p, st);
-        else launch_norm<F32, 32, 512>(p, st);
+        else if (D <= 2048) launch_norm<F32, N, 2048 / N>(p, st);
+        else if (D <= 4096) launch_norm<F32, N, 4096 / N>(p, st);
+        else if (D <= 8192) launch_norm<F32, N, 8192 / N>(p, st);
+        else launch_norm<F32, N, 16384 / N>(p, st);
     } else {
         if (D <= 1024) launch_norm<F32, 8, 128>(p, st);
         else if (D <= 2048) launch_norm<F32, 8, 256>(p, st);

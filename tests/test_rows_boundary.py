@@ -95,7 +95,7 @@ def test_workspace_sizes():
     assert L.dlm_embed_bwd_workspace_bytes(None) == 0 and L.dlm_row_norm_bwd_workspace_bytes(C.byref(_norm_bwd(struct_size=1))) == 0
     for T in (1, 333, 2048, 2049, 65536, 1 << 20, 1 << 28):
         n = L.dlm_embed_bwd_workspace_bytes(C.byref(_embed_bwd(T=T, Dh=4096)))
-        assert 8 * T <= n <= 32 * T + (1 << 29)
+        assert 8 * T <= n <= 16 * T + 64 + 2 * 4 * 4096 * (T // 128 + 1)
     assert L.dlm_row_norm_bwd_workspace_bytes(C.byref(_norm_bwd(T=1 << 30, D=16384))) <= 1 << 27
 
 
