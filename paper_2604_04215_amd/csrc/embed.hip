@@ -44,9 +44,13 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
 // tokens stay in the order of their positions, since earlier runs hold earlier ones).
 constexpr int MERGE = 32;
 constexpr int EMBED_MAX_V = (1 << 21) - 2;                    // a token (or V: none) and a place in its run share 32 bits: 21 and 11
-// 512 entries for a few tokens, which one wavefront sorts without a barrier; 8192, of which there are few to merge, where they leave the token
-// its bits (65536 tokens, us of the sort and the merge: runs of 2048 10 + 54, of 8192 32 + 19).
-inline int run_bits(int T, int V) { return T <= 512 ? 9 : T <= 2048 || V >= (1 << 19) - 1 ? 11 : 13; }
+// 512 entries for a few tokens, which one wavefront sorts without a barrier; 8192, of which there are few to merge, for many tokens, and where a
+// table is cleared meanwhile, if they leave the token its bits.  us of the sort and the merge in runs of 2048 / 8192: 3000 tokens 10 + 9 / 30,
+// 65536 tokens 10 + 54 / 31 + 19.
+inline int run_bits(int T, int V, bool clears) {
+    if (T <= 512) return 9;
+    return T <= 2048 || V >= (1 << 19) - 1 || (T <= 16384 && !clears) ? 11 : 13;
+}
 
 // the value of lane ^ MASK, without a trip through LDS
 template <int MASK>
@@ -376,9 +380,9 @@ struct EmbedPlan {
     int bits, runs, levels, chunk, groups;
     size_t list_bytes, part_at, bytes;              // one list of T; the sums behind the lists
 };
-static EmbedPlan plan_embed(int T, int V, int Dh) {
+static EmbedPlan plan_embed(int T, int V, int Dh, bool clears) {
     EmbedPlan p = {};
-    p.bits = run_bits(T, V);
+    p.bits = run_bits(T, V, clears);
     p.runs = (int)(((int64_t)T + (1 << p.bits) - 1) >> p.bits);
     for (int64_t n = p.runs; n > 1; n = (n + MERGE - 1) / MERGE) ++p.levels;
     // some 8192 wavefronts, of chunks that are neither so short that their borders cost more than their rows nor so long that a few run on alone
@@ -388,7 +392,7 @@ static EmbedPlan plan_embed(int T, int V, int Dh) {
     p.chunk = (int)chunk;
     p.groups = (int)((T + GROUP * chunk - 1) / (GROUP * chunk));
     p.list_bytes = ((size_t)T * 4 + 15) / 16 * 16;
-    p.part_at = p.list_bytes * (p.levels > 0 ? 4 : 2);
+    p.part_at = p.list_bytes * (T > 2048 ? 4 : 2);        // (a second pair of lists to merge into)
     p.bytes = p.part_at + (size_t)p.groups * 2 * Dh * sizeof(float);
     return p;
 }
@@ -415,7 +419,7 @@ extern "C" int dlm_embed(const dlm_embed_args* a, void* stream) {
 
 extern "C" size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args* a) {
     if (!a || a->struct_size != sizeof(dlm_embed_bwd_args) || a->T <= 0 || a->Dh <= 0) return 0;
-    return plan_embed(a->T, a->V, a->Dh).bytes;
+    return plan_embed(a->T, a->V, a->Dh, false).bytes;
 }
 
 extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
@@ -438,7 +442,7 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
         if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
     }
     hipStream_t st = (hipStream_t)stream;
-    const EmbedPlan plan = plan_embed(a->T, a->V, a->Dh);
+    const EmbedPlan plan = plan_embed(a->T, a->V, a->Dh, !a->accumulate);
     char* ws = (char*)a->workspace;
     int32_t* list[4];
     for (int i = 0; i < 4; ++i) list[i] = (int32_t*)(ws + i * plan.list_bytes);
