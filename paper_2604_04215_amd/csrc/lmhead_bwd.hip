@@ -900,8 +900,9 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 
 // ---- host ---------------------------------------------------------------------------------------------------
 constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more rows, fewer columns at a time
-// Up to so many rows two bf16 terms take less time than the pass over W that fp16 needs
-constexpr int LMB_FEW = 256;
+// Up to so many rows two bf16 terms take less time than the pass over W that fp16 needs.  Both gradients, two terms against fp16, V = 126464, Dh = 4096:
+// 128 rows 1000 against 1380 us, 160 1415 against 1380, 192 1392 against 1374, 256 1531 against 1410; V = 32000, Dh = 2048: 192 rows 216 against 208, 256 246 against 226.
+constexpr int LMB_FEW = 128;
 static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
 
 static int g_lmb_workgroups = 0;                      // dlm_set_option: workgroups of a launch that takes tiles from a list (0: as fit the chip)
@@ -968,7 +969,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     // few rows: tiles no higher than they are
     const int64_t rows = (int64_t)p.padded * p.terms_h, columns = a->V < p.chunk ? a->V : p.chunk;
     p.dz = lmb_shape(columns, p.padded, wide);
-    if (!wide && p.padded <= 128 && columns >= 160 * 256) p.dz = p.padded <= 64 ? LMB_256x64 : LMB_256x128;
+    if (p.dz == LMB_256 && p.padded <= 128) p.dz = p.padded <= 64 ? LMB_256x64 : LMB_256x128;
     p.weight = p.hidden = lmb_shape(a->Dh, columns, wide);
     if (p.weight == LMB_256 && rows <= 128 && !p.f16) p.hidden = LMB_256x128;
     // Parts of d_hidden's sum.  In times of a pair of stages (1.8 us of a 256 x 256 tile): the launch takes what all its tiles take together, but no
@@ -1019,8 +1020,7 @@ static void launch_dz(const LmbPlan& plan, dim3 grid, hipStream_t st, const LmbP
         else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 0, 0);
         else LMB_DZ(Lmb64, 0, 0);
     } else {
-        if (plan.dz == LMB_256) LMB_DZ(Lmb256, 2, 0);
-        else if (plan.dz == LMB_256x128) LMB_DZ(Lmb256x128, 2, 0);
+        if (plan.dz == LMB_256x128) LMB_DZ(Lmb256x128, 2, 0);
         else if (plan.dz == LMB_256x64) LMB_DZ(Lmb256x64, 2, 0);
         else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 2, 0);
         else LMB_DZ(Lmb64, 2, 0);

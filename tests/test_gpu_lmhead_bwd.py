@@ -3,7 +3,7 @@
 Bounds, u = 2^-24 (half a step of fp32), h = 2^-8 (half a step of bf16).  A sum of K products on the matrix pipes: a product passes at most 16 additions in
 its own instruction and K / 16 behind it; each may be off by 2 u (should it cut instead of round) of what is added up: s(K) = 2 u (16 + K / 16).
 Logits are off by e = inv_t s(Dh) sum|h w| and 4 u (|z| + |lse|), probabilities by p (exp(e) - 1 + 8 u).  dz is then rounded: to three terms of bf16 for fp32
-gradients, h^3 |dz|, to two up to 256 rows, h^2 |dz|, or to one fp16, 2^-11 |dz| or half its smallest step, 2^-25, of numbers up to 2^14: 2^-38 of the largest |dz| times
+gradients, h^3 |dz|, to two up to 128 rows, h^2 |dz|, or to one fp16, 2^-11 |dz| or half its smallest step, 2^-25, of numbers up to 2^14: 2^-38 of the largest |dz| times
 rows and columns of up to 2 in size.  A gradient is off by the sum of |its other operand| times that, by s(K) of what is added up (with up to 64 partial sums joined: 128 u more),
 and by its own rounding."""
 import numpy as np
@@ -101,7 +101,7 @@ class Case:
         def part(wide_):
             if wide_:
                 return off * (1 + H) + H ** 3 * size
-            if self.M <= 256 or wide_any:
+            if self.M <= 128 or wide_any:
                 return off * (1 + H) + H * H * size
             return off * (1 + H) + 2.0 ** -11 * size + 2.0 ** -36 * size.max(initial=0)
 
