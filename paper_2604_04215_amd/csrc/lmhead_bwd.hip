@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
                 for (int k = 0; k < 8; ++k) top = fmaxf(top, lmb_top8(kept[k]));
                 for (int c = 4096 + lane * 8; c < p.Dh; c += 512) top = fmaxf(top, lmb_top8(*reinterpret_cast<const u32x4*>(src + c)));
                 const int e = v < p.V ? lmb_exponent(top) : LMB_NONE;
-                if (v < p.V && lane == 0) p.sc.w_e[v] = e;
+                if (lane == 0) p.sc.w_e[v] = e;             // (of the rows behind the last too: their columns of dz are zero times a power of two)
                 most = max(most, e);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {

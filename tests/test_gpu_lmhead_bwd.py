@@ -331,6 +331,22 @@ def test_several_chunks_of_columns(columns):
     assert torch.equal(got[1], want[1])                 # each column is in one chunk
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,V", [(70, 333), (150, 333), (150, 1000), (300, 513)])
+def test_whatever_the_workspace_held(M, V, dtype):
+    c = Case(M, 128, V, forbid=2)
+    lse, target, d_zt, d_lse = c.arrays()
+    outs = []
+    for fill in (0, 0x3f, 0x7f, 0x80, 0xff):             # as numbers small, some 2^30, and negative; as floating point 0.7, large and NaN
+        d_h, d_w = (torch.full((n, 128), 7.0, dtype=dtype, device=DEV) for n in (M, V))
+        how = dict(target=target, d_ztarget=d_zt, d_lse=d_lse, d_hidden=d_h, d_w=d_w, forbid_token=2)
+        ws = torch.full((dlm.lmhead_bwd_workspace_bytes(c.hidden, c.w, lse, **how),), fill, dtype=U8, device=DEV)
+        dlm.lmhead_bwd(c.hidden, c.w, lse, workspace=ws, **how)
+        assert d_h.isfinite().all() and d_w.isfinite().all(), fill
+        outs.append((d_h, d_w))
+    assert all(torch.equal(a, b) for got in outs[1:] for a, b in zip(got, outs[0]))
+
+
 def test_the_same_every_time_on_another_stream_and_from_a_graph():
     c = Case(140, 256, 900, rows_total=200, scatter=True, forbid=899)
     lse, target, d_zt, d_lse = c.arrays()
