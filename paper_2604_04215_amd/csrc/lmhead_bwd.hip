@@ -192,7 +192,9 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     int up = 0;
     if (p.f16 && live) {
         const int e = p.sc.row_e[r], c = p.sc.row_c[r], most = lmb_most(p.sc.row_max, LMB_STATS);
-        up = e == LMB_NONE ? 0 : e + (c == LMB_NONE ? 0 : min(max(most - e - c, 0), 20));
+        // (a hidden row of zeros has any scale: the one that brings its gradient to the largest)
+        if (e == LMB_NONE) up = c == LMB_NONE ? 0 : (most == LMB_NONE ? 0 : most) - c;
+        else up = e + (c == LMB_NONE ? 0 : min(max(most - e - c, 0), 20));
     }
     for (int c = threadIdx.x * 8; c < p.Dh; c += 2048) {
         const uint16_t* src = p.hidden + row * p.h_stride + c;

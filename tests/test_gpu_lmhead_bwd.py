@@ -268,6 +268,30 @@ def test_rows_and_columns_of_very_different_size():
     within(d_w, dw, ((size + s(300) * np.abs(dz)).T @ np.abs(c.h) + np.abs(dz).T @ (2.0 ** -18 * top_h)[:, None]) * 1.01)
 
 
+@pytest.mark.parametrize("M,zeros,size", [(200, 200, 1.0), (300, 300, 2.0 ** 30), (200, 1, 2.0 ** -30), (260, 259, 2.0 ** 20)])
+def test_hidden_rows_of_zeros(M, zeros, size):
+    """Their gradient is not zero, and no other row's size is theirs."""
+    c = Case(M, 128, 333, forbid=7)
+    c.d_zt, c.d_lse = (np.nan_to_num(x) * np.float32(1000.0) for x in (c.d_zt, c.d_lse))
+    c.lse = np.nan_to_num(c.lse)
+    hidden = wide(c.hidden) * size
+    hidden[M - zeros:] = 0.0
+    w = wide(c.w) / max(size, 1.0)                       # logits of ordinary size
+    c.hidden, c.w = (torch.from_numpy(x.astype(np.float32)).to(BF16).to(DEV) for x in (hidden, w))
+    c.h = wide(c.hidden)
+    c.z = c.h @ wide(c.w).T
+    c.z[:, 7] = -np.inf
+    c.lse = np.log(np.exp(c.z).sum(1)).astype(np.float32)
+    d_h, d_w = (torch.full((n, 128), float("nan"), dtype=BF16, device=DEV) for n in (M, 333))
+    c.call(d_h, d_w)
+    dh, bh, dw, bw = c.want(False, False)
+    # dz of a row is 2^-11 off, or half the smallest step of what it is stored as: 2^-38 of the row's largest times W's sizes' spread, at most 2^10 here; the
+    # columns' largest entries differ by less
+    within(d_h, dh, bh + 2.0 ** -28 * np.abs(dh).max(1, keepdims=True))
+    within(d_w, dw, bw + 2.0 ** -28 * np.abs(dw).max())
+    near(d_h, dh, False)
+
+
 @pytest.mark.parametrize("M", [40, 300])
 def test_a_row_that_is_not_finite_spoils_no_other_row(M):
     c = Case(M, 128, 400)
