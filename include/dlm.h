@@ -698,7 +698,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  * gradients are wanted).  hidden and w have to be finite: other rows'
  * values are multiplied by dz that may be zero.
  * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 11 bits, as an fp16 scaled by row and column (rows whose |d_lse| + |d_ztarget| times
- * their largest entry is less than 2^-40 of the largest such product of the call lose bits), or, up to 128 rows, 16 bits.  Where a gradient is
+ * their largest entry is less than 2^-40 of the largest such product of the call lose bits; so do columns where a few rows of w are more than 2^20 larger than the rest), or, up to 128 rows, 16 bits.  Where a gradient is
  * fp32, it keeps 24, and all sums are added up in two floats: three to four times as long.
  * workspace: dlm_lmhead_bwd_workspace_bytes(args) bytes, 16-byte aligned; they depend on M, Dh, V, the types and which gradients are wanted.
  * Supported: Dh % 64 == 0, up to 65536; M up to 2^20; V up to 2^24; rows 16-byte aligned, strides multiples of 16 bytes, w_stride_row < 2^23.

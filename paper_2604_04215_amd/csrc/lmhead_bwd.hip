@@ -32,16 +32,18 @@ struct LmbRow {                    // what the logits' kernel knows of a row
 constexpr int LMB_NO_TARGET = -(1 << 28);
 
 // fp16 operands.  With e(x) the exponent of the largest entry of a row (its size lies in [2^e, 2^(e+1))):
-//   h16[m] = h[m] 2^(14 - up[m]),  up[m] = e(h[m]) + u;   w16[v] = w[v] 2^(14 - e(w[v]));   D[m][v] = dz[m][v] 2^(up[m] + e(w[v]) - K)
-//   d_hidden[m] = 2^(K - 14 - up[m]) sum_v D w16;   d_w[v] = 2^(K - 14 - e(w[v])) sum_m D h16
-// K = L + max_v e(w[v]) - 13 keeps D below 2^15, where L = max_m (e(h[m]) + c[m]) and 2^(c + 1) exceeds a row's |d_lse| + |d_ztarget|, inv_t included.
+//   h16[m] = h[m] 2^(14 - up[m]),  up[m] = e(h[m]) + u;   w16[v] = w[v] 2^(14 - f[v]);   D[m][v] = dz[m][v] 2^(up[m] + f[v] - K)
+//   d_hidden[m] = 2^(K - 14 - up[m]) sum_v D w16;   d_w[v] = 2^(K - 14 - f[v]) sum_m D h16
+// K = L + max_v f[v] - 13 keeps D below 2^15, where L = max_m (e(h[m]) + c[m]) and 2^(c + 1) exceeds a row's |d_lse| + |d_ztarget|, inv_t included.
 // u = min(L - e(h[m]) - c[m], 20) brings rows of small gradients up (h keeps its 8 bits in entries of 2^-11 of its largest and more): dz of 2^-8 of the largest
 // of its row keeps all 11 bits while the row's gradient is at most 2^40 below the largest.
+// f[v] = max(e(w[v]), F), F eight above the largest exponent of 256 rows spread over W: nearly always F for all, so that a small row of W does not make its
+// column of dz, of which d_w is summed, a small number too.  (What w16 loses there, 2^-31 of W's largest, counts for nothing in d_hidden.)
 struct LmbScale {
     int *row_e, *row_c, *up;       // [M rounded up to 64]
-    int* w_e;                      // [V rounded up to 256]
-    int *row_max, *w_max;          // by workgroup, by wavefront
-    int* out;                      // max_v e(w[v]), K
+    int* w_f;                      // f, [V rounded up to 256]
+    int *row_max, *w_some, *w_max; // by workgroup; exponents of some rows of W; by wavefront
+    int* out;                      // max_v f[v], K
     uint16_t *h16, *w16, *tail16;
 };
 constexpr int LMB_STATS = 256;     // workgroups that look for a largest exponent
@@ -65,7 +67,7 @@ struct LmbParams {
     uint16_t* w_tail;              // [64][Dh]: the last V % 64 rows of W, zeros behind them
     int f16;                       // dz is fp16 and scaled
     LmbScale sc;
-    int last_e;                    // the last four of w_e
+    int last_f;                    // the last four of w_f
     uint16_t* dz;                  // [terms][M rounded up to 64][ldz]
     int64_t dz_term;               // entries of a term
     int ldz;
@@ -110,7 +112,7 @@ __device__ __forceinline__ u32x4 lmb_half8(u32x4 v, bool any, int k) {
     return __builtin_bit_cast(u32x4, h);
 }
 
-// fp16 operands, first pass: exponents of the selected rows and of their gradients, a wavefront a row
+// fp16 operands, first pass: exponents of the selected rows and of their gradients, a wavefront a row; of a row of W a workgroup
 __global__ __launch_bounds__(256) void lmb_stat_kernel(LmbParams p) {
     __shared__ int meet[4];
     const int M = lmb_rows(p), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -128,6 +130,14 @@ __global__ __launch_bounds__(256) void lmb_stat_kernel(LmbParams p) {
             p.sc.row_c[r] = c;
         }
         if (e != LMB_NONE && c != LMB_NONE) most = max(most, e + c);
+    }
+    if (wave == 0) {
+        const uint16_t* w = p.w + (int64_t)blockIdx.x * p.V / LMB_STATS * p.w_stride;
+        float top = 0.f;
+#pragma unroll 8
+        for (int c = lane * 8; c < p.Dh; c += 512) top = fmaxf(top, lmb_top8(*reinterpret_cast<const u32x4*>(w + c)));
+        const int e = lmb_exponent(top);
+        if (lane == 0) p.sc.w_some[blockIdx.x] = e;
     }
     if (lane == 0) meet[wave] = most;
     __syncthreads();
@@ -152,6 +162,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
         if (p.f16) {
             // a wavefront a row, its first 4096 entries kept in registers
             int most = LMB_NONE;
+            const int some = lmb_most(p.sc.w_some, LMB_STATS), least = some == LMB_NONE ? LMB_NONE : some + 8;
             const int padded = (p.V + 63) & ~63, whole = p.V & ~63, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
             for (int v = (r - bound) * 4 + wave; v < padded; v += LMB_STATS * 8 * 4) {
                 uint16_t* dst = v < whole ? p.sc.w16 + (int64_t)v * p.Dh : p.sc.tail16 + (int64_t)(v - whole) * p.Dh;
@@ -166,16 +177,16 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) top = fmaxf(top, lmb_top8(kept[k]));
                 for (int c = 4096 + lane * 8; c < p.Dh; c += 512) top = fmaxf(top, lmb_top8(*reinterpret_cast<const u32x4*>(src + c)));
-                const int e = v < p.V ? lmb_exponent(top) : LMB_NONE;
-                if (lane == 0) p.sc.w_e[v] = e;             // (of the rows behind the last too: their columns of dz are zero times a power of two)
+                const int e = max(v < p.V ? lmb_exponent(top) : LMB_NONE, least);
+                if (lane == 0) p.sc.w_f[v] = e;             // (of the rows behind the last too: their columns of dz are zero times a power of two)
                 most = max(most, e);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int c = (k * WAVE + lane) * 8;
-                    if (c < p.Dh) __builtin_nontemporal_store(lmb_half8(kept[k], e != LMB_NONE, 14 - e), reinterpret_cast<u32x4*>(dst + c));
+                    if (c < p.Dh) __builtin_nontemporal_store(lmb_half8(kept[k], v < p.V && e != LMB_NONE, 14 - e), reinterpret_cast<u32x4*>(dst + c));
                 }
                 for (int c = 4096 + lane * 8; c < p.Dh; c += 512)
-                    *reinterpret_cast<u32x4*>(dst + c) = lmb_half8(*reinterpret_cast<const u32x4*>(src + c), e != LMB_NONE, 14 - e);
+                    *reinterpret_cast<u32x4*>(dst + c) = lmb_half8(*reinterpret_cast<const u32x4*>(src + c), v < p.V && e != LMB_NONE, 14 - e);
             }
             if (lane == 0) p.sc.w_max[(r - bound) * 4 + wave] = most;
             return;
@@ -595,7 +606,7 @@ struct LmbDz {
                     typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        const i32x4 we = *reinterpret_cast<const i32x4*>(p.sc.w_e + min(p.v0 + i + 8 * q, p.last_e));
+                        const i32x4 we = *reinterpret_cast<const i32x4*>(p.sc.w_f + min(p.v0 + i + 8 * q, p.last_f));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) f[4 * q + e] = ldexpf(1.f, we[e] == LMB_NONE ? 0 : we[e] - S);
                     }
@@ -794,7 +805,7 @@ struct LmbWeight {
             const bool live = j < p.n;                                  // (the same for lane and lane + 32)
             int scale = 0;
             if (F16 && all > 0 && live) {
-                const int e = p.sc.w_e[v];
+                const int e = p.sc.w_f[v];
                 scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
             }
 #pragma unroll
@@ -1006,7 +1017,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     if (p.f16) {
         p.h16_at = take((size_t)p.padded * a->Dh * 2);
         p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
-        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 33 + 2) * 4);
+        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 34 + 2) * 4);
     }
     p.bytes = at;
     return p;
@@ -1129,15 +1140,16 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.sc.row_e = ints;
         p.sc.row_c = ints + plan.padded;
         p.sc.up = ints + 2 * (int64_t)plan.padded;
-        p.sc.w_e = ints + 3 * (int64_t)plan.padded;
-        p.sc.row_max = p.sc.w_e + ((int64_t)a->V + 255) / 256 * 256;
-        p.sc.w_max = p.sc.row_max + LMB_STATS;
+        p.sc.w_f = ints + 3 * (int64_t)plan.padded;
+        p.sc.row_max = p.sc.w_f + ((int64_t)a->V + 255) / 256 * 256;
+        p.sc.w_some = p.sc.row_max + LMB_STATS;
+        p.sc.w_max = p.sc.w_some + LMB_STATS;
         p.sc.out = p.sc.w_max + LMB_STATS * 32;
         p.sc.h16 = (uint16_t*)(ws + plan.h16_at);
         p.sc.w16 = (uint16_t*)(ws + plan.w16_at);
         p.sc.tail16 = p.w_tail;
     }
-    p.last_e = (int)(((int64_t)a->V + 255) / 256 * 256) - 4;
+    p.last_f = (int)(((int64_t)a->V + 255) / 256 * 256) - 4;
     p.counters = (int*)(ws + plan.counters_at);
     p.d_hidden = a->d_hidden;
     p.dh_stride = a->d_hidden_stride_row;

@@ -292,6 +292,30 @@ def test_hidden_rows_of_zeros(M, zeros, size):
     near(d_h, dh, False)
 
 
+@pytest.mark.parametrize("M", [100, 200])
+@pytest.mark.parametrize("rows_of", ["half", "but one", "all"])
+def test_small_rows_of_w(M, rows_of):
+    """Their own gradient is not small: it is of dz and the hidden rows alone."""
+    c = Case(M, 128, 1000, forbid=999)
+    small = np.ones(1000)
+    small[::2 if rows_of == "half" else 1] = 2.0 ** -24
+    if rows_of == "but one":
+        small[500] = 1.0
+    c.w = torch.from_numpy((wide(c.w) * small[:, None]).astype(np.float32)).to(BF16).to(DEV)
+    c.z = c.h @ wide(c.w).T
+    c.z[:, 999] = -np.inf
+    c.lse = np.log(np.exp(c.z).sum(1)).astype(np.float32)
+    d_h, d_w = (torch.full((n, 128), float("nan"), dtype=BF16, device=DEV) for n in (M, 1000))
+    c.call(d_h, d_w)
+    dh, bh, dw, bw = c.want(False, False)
+    # dz is at most half the smallest step off, 2^-39 of the largest number, which is at most 2^9 times the largest product of a gradient and its row
+    within(d_w, dw, bw)
+    near(d_w, dw, False)
+    # a row of W loses half the smallest step of the 2^6 that the largest are brought to: 2^-31 of those
+    dz, _, _ = rows.lmhead_grad(c.h, wide(c.w), c.lse.astype(np.float64), c.d_lse.astype(np.float64), c.d_zt.astype(np.float64), c.target, 1.0, 999)
+    within(d_h, dh, bh + 2.0 ** -30 * np.abs(wide(c.w)).max() * np.abs(dz).sum(1, keepdims=True))
+
+
 @pytest.mark.parametrize("M", [40, 300])
 def test_a_row_that_is_not_finite_spoils_no_other_row(M):
     c = Case(M, 128, 400)
