@@ -691,8 +691,9 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *   lse        fp32, the forward call's; target, d_lse, d_ztarget are indexed like it (by r, or by row(r) with out_scatter).  d_lse or d_ztarget may be
  *              NULL: zero.  d_ztarget needs target; a target outside [0, V), or forbid_token, has no gradient.
  *              A row whose d_lse is zero may have any lse.
- *   d_hidden   optional, rows of d_hidden_type indexed like `hidden`: row(r) is written for every r, other rows are left as they are.  Rows named
- *              twice count twice for d_w; in d_hidden such a row holds the gradient of one of the two.
+ *   d_hidden   optional, rows of d_hidden_type indexed like `hidden`: row(r) is written for every r, other rows are left as they are.  Each entry of
+ *              row_idx counts by itself: a row that several name gets the sum of their gradients (in time that grows with M squared where row_idx
+ *              does not ascend).
  *   d_w        optional [V, Dh] of d_w_type; accumulate 0: written, else added to
  * The logits are not stored.  No atomics: deterministic (the order of sums depends on the sizes, the types and which
  * gradients are wanted).  hidden and w have to be finite: other rows'

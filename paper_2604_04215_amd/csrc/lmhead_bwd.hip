@@ -46,6 +46,7 @@ struct LmbScale {
     int* out;                      // max_v f[v], K
     uint16_t *h16, *w16, *tail16;
 };
+constexpr int LMB_ORDER = 64;      // wavefronts that look through row_idx
 constexpr int LMB_STATS = 256;     // workgroups that look for a largest exponent
 constexpr int LMB_NONE = -100000;  // exponent of a row of zeros
 
@@ -78,6 +79,7 @@ struct LmbParams {
     int n2;                        // workgroups of d_hidden (a multiple of 8), where each takes one tile; 0: it is not wanted
     int queued;                    // workgroups take one tile after the other
     int* counters;                 // of three lists of tiles: dz, d_hidden, d_w
+    int* order;                    // [LMB_ORDER] not 0: an entry of row_idx does not exceed the one before it
     void* d_hidden;
     int64_t dh_stride;
     int dh_f32;
@@ -158,6 +160,13 @@ __device__ __forceinline__ int lmb_most(const int* v, int n) {
 __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     const int M = lmb_rows(p), bound = (p.M + 63) & ~63, r = blockIdx.x;
     if (r == 0 && threadIdx.x < 24) p.counters[threadIdx.x * 16] = 0;
+    if (r < LMB_ORDER && p.row_idx && threadIdx.x < WAVE) {        // (there are 64 workgroups or more)
+        bool falls = false;
+#pragma unroll 4
+        for (int q = r * WAVE + threadIdx.x; q + 1 < M; q += LMB_ORDER * WAVE) falls |= p.row_idx[q + 1] <= p.row_idx[q];
+        const uint64_t any = __ballot(falls);
+        if (threadIdx.x == 0) p.order[r] = any != 0;
+    }
     if (r >= bound) {
         if (p.f16) {
             // a wavefront a row, its first 4096 entries kept in registers
@@ -892,13 +901,16 @@ __global__ __launch_bounds__(64 * H::WV * H::WH, 1) void lmb_grad_kernel(LmbPara
     } while (one_pair && list.index < list.len);
 }
 
-// The parts of d_hidden's sum, in order, into the rows that were selected
+// The parts of d_hidden's sum, in order, into the rows that were selected.  A row that is named several times gets all its entries' sums, in their order, from
+// the first of them; the others look for an earlier one and find it.  An ascending list has none, and needs no look: `order` says where it is not.
 __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
-    const int r = blockIdx.x;
-    if (r >= lmb_rows(p)) return;
-    const int64_t row = p.row_idx ? p.row_idx[r] : r;
-    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < p.Dh; c += 1024 * gridDim.y) {
+    __shared__ uint64_t same[4];
+    const int M = lmb_rows(p), r0 = blockIdx.x, wave = threadIdx.x >> 6;
+    if (r0 >= M) return;
+    const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const auto sum = [&](int r) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (c >= p.Dh) return x;
 #pragma unroll 4
         for (int s = 0; s < p.splits * p.terms_h; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
         if (p.f16) {
@@ -906,9 +918,28 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
         }
-        if (p.dh_f32) *reinterpret_cast<f32x4*>((float*)p.d_hidden + row * p.dh_stride + c) = x;
-        else *reinterpret_cast<u32x2*>((uint16_t*)p.d_hidden + row * p.dh_stride + c) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        return x;
+    };
+    f32x4 x = sum(r0);
+    const int row = p.row_idx ? p.row_idx[r0] : r0;
+    const bool twice = p.row_idx && __syncthreads_or(threadIdx.x < LMB_ORDER && p.order[threadIdx.x]);
+    for (int b = 0; twice && b < M; b += 256) {
+        const int r = b + threadIdx.x;
+        const uint64_t mine = __ballot(r < M && r != r0 && p.row_idx[r < M ? r : 0] == row);
+        __syncthreads();
+        if (lane_id() == 0) same[wave] = mine;
+        __syncthreads();
+        for (int k = 0; k < 4; ++k) {
+            for (uint64_t left = same[k]; left; left &= left - 1) {
+                const int other = b + 64 * k + __builtin_ctzll(left);
+                if (other < r0) return;
+                x += sum(other);
+            }
+        }
     }
+    if (c >= p.Dh) return;
+    if (p.dh_f32) *reinterpret_cast<f32x4*>((float*)p.d_hidden + row * p.dh_stride + c) = x;
+    else *reinterpret_cast<u32x2*>((uint16_t*)p.d_hidden + row * p.dh_stride + c) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
@@ -1008,7 +1039,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
         at += up256(bytes);
         return here;
     };
-    p.counters_at = take(3 * LMB_COUNTERS * sizeof(int));
+    p.counters_at = take((3 * LMB_COUNTERS + LMB_ORDER) * sizeof(int));
     p.rows_at = take((size_t)p.padded * sizeof(LmbRow));
     p.h_at = take((size_t)p.padded * a->Dh * 2);
     p.tail_at = take((size_t)64 * a->Dh * 2);
@@ -1151,6 +1182,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
     }
     p.last_f = (int)(((int64_t)a->V + 255) / 256 * 256) - 4;
     p.counters = (int*)(ws + plan.counters_at);
+    p.order = p.counters + 3 * LMB_COUNTERS;
     p.d_hidden = a->d_hidden;
     p.dh_stride = a->d_hidden_stride_row;
     p.dh_f32 = a->d_hidden_type == DLM_ROW_F32;

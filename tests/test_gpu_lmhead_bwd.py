@@ -191,6 +191,39 @@ def test_rows_by_index_and_a_count_on_the_device(scatter, live):
     assert (d_h[rest] == 7).all()
 
 
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("scatter", [False, True])
+@pytest.mark.parametrize("M,named,live", [(70, 5, None), (300, 70, 290), (700, 1, None), (1000, 900, None), (5000, 3000, 4700)])
+def test_rows_named_more_than_once_and_in_any_order(M, named, live, scatter, types):
+    c = Case(M, 64, 200, rows_total=M + 1, scatter=False, forbid=3)
+    c.scatter, c.n = scatter, named
+    c.hidden, c.idx = c.hidden[:named].contiguous(), c.rng.integers(0, named, M).astype(np.int32)
+    c.h = wide(c.hidden)[c.idx]
+    c.z = c.h @ wide(c.w).T
+    c.z[:, 3] = -np.inf
+    c.lse = np.log(np.exp(c.z).sum(1)).astype(np.float32)
+    if scatter:                                          # what belongs to a row is the same wherever it is named
+        last = np.zeros(named, dtype=int)
+        last[c.idx] = np.arange(M)
+        c.lse, c.target, c.d_zt, c.d_lse = (x[last[c.idx]] for x in (c.lse, c.target, c.d_zt, c.d_lse))
+    d_h, d_w = torch.full((named, 64), 7.0, dtype=types[0], device=DEV), torch.zeros((200, 64), dtype=types[1], device=DEV)
+    c.call(d_h, d_w, live)
+    again = torch.full_like(d_h, 7.0)
+    c.call(again, d_w, live)
+    assert torch.equal(d_h, again)
+    dh, bh, dw, bw = c.want(types[0] == F32, types[1] == F32, live)
+    want, bound, size = np.zeros((3, named, 64))
+    idx = c.idx[:len(dh)]
+    np.add.at(want, idx, dh)
+    np.add.at(size, idx, np.abs(dh))
+    np.add.at(bound, idx, bh)
+    there = np.unique(idx)
+    # up to M sums of a row are added one after the other: each addition half a step of what there is so far off
+    within(d_h[torch.from_numpy(there).to(DEV)], want[there], bound[there] + U * np.bincount(idx, minlength=named).max() * size[there])
+    within(d_w, dw, bw)
+    assert (np.delete(wide(d_h), there, 0) == 7).all()
+
+
 def test_one_gradient_alone_and_one_cotangent_alone():
     c = Case(70, 128, 300, forbid=3)
     both_h, both_w = torch.zeros((70, 128), dtype=BF16, device=DEV), torch.zeros((300, 128), dtype=F32, device=DEV)
