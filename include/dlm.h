@@ -599,7 +599,7 @@ int dlm_embed(const dlm_embed_args *args, void *stream);
  *               other rows are neither read nor written (micro-batches; a table that is the LM head's weight as well).
  * fp32 sums in an order that tokens and T decide, no atomics: deterministic.
  * workspace: dlm_embed_bwd_workspace_bytes(args) bytes (they depend on T and Dh), 16-byte aligned.
- * Supported: Dh % 8 == 0; V < 2^21 - 1; T <= 2^28.  d_out and d_table do not overlap. */
+ * Supported: Dh % 8 == 0, up to 65536; V < 2^21 - 1; T <= 2^28; T Dh <= 2^40.  d_out and d_table do not overlap. */
 typedef struct dlm_embed_bwd_args {
     uint32_t struct_size;
     int32_t T, V, Dh;
@@ -629,8 +629,8 @@ size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args *args);
  *   sum_out      optional [T, D], with residual only: s
  *   weight, bias optional bf16 [D]; NULL: 1, 0
  *   out          bf16 [T, D]
- * sum_out may be x or residual itself, out may be a bf16 x (same pointer and stride).  All in fp32; squares overflow for entries from 2^60 on (the
- * row then comes out as its bias).  eps >= 2^-126.
+ * sum_out may be x or residual itself, out may be a bf16 x (same pointer and stride).  All in fp32; sums of squares overflow for entries from 2^57 on
+ * (the row then comes out as its bias).  eps >= 2^-126.
  * Supported: D a multiple of 8, up to 16384. */
 typedef struct dlm_row_norm_args {
     uint32_t struct_size;
@@ -697,7 +697,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *   d_w        optional [V, Dh] of d_w_type; accumulate 0: written, else added to
  * The logits are not stored.  No atomics: deterministic (the order of sums depends on the sizes, the types and which
  * gradients are wanted).  hidden and w have to be finite: other rows'
- * values are multiplied by dz that may be zero.
+ * values are multiplied by dz that may be zero.  d_w overlaps neither w nor d_hidden; d_hidden may be hidden.
  * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 11 bits, as an fp16 scaled by row and column (rows whose |d_lse| + |d_ztarget| times
  * their largest entry is less than 2^-40 of the largest such product of the call lose bits; so do columns where a few rows of w are more than 2^20 larger than the rest), or, up to 128 rows, 16 bits.  Where a gradient is
  * fp32, it keeps 24, and all sums are added up in two floats: three to four times as long.

@@ -431,6 +431,8 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
     if ((rc = validate_embed(a->T, a->V, a->Dh, a->tokens, a->scale, who)) != DLM_OK) return rc;
     if (a->V > EMBED_MAX_V) return fail(DLM_ERR_UNSUPPORTED, "%s: V=%d (supported: up to %d)", who, a->V, EMBED_MAX_V);
     if (a->T > 1 << 28) return fail(DLM_ERR_UNSUPPORTED, "%s: T=%d (supported: up to 2^28)", who, a->T);
+    if (a->Dh > 1 << 16 || (int64_t)a->T * a->Dh > (int64_t)1 << 40) return fail(DLM_ERR_UNSUPPORTED, "%s: T=%d Dh=%d (supported: Dh up to 65536, T Dh up to 2^40)", who, a->T, a->Dh);
+    if (a->T > 0 && a->d_table && a->d_table == a->d_out) return fail(DLM_ERR_INVALID_ARG, "%s: d_table is d_out", who);
     if ((rc = validate_row_type(a->d_out_type, who, "d_out")) != DLM_OK) return rc;
     if ((rc = validate_row_type(a->d_table_type, who, "d_table")) != DLM_OK) return rc;
     if ((rc = validate_rows(a->d_out, a->d_out_stride, a->T, a->Dh, row_bytes(a->d_out_type), false, who, "d_out")) != DLM_OK) return rc;

@@ -1115,6 +1115,7 @@ static int validate_lmb(const dlm_lmhead_bwd_args* a, const char* who) {
     if (!a->lse) return fail(DLM_ERR_INVALID_ARG, "%s: null lse", who);
     if ((rc = validate_rows(a->hidden, a->hidden_stride_row, 2, a->Dh, 2, false, who, "hidden")) != DLM_OK) return rc;
     if ((rc = validate_rows(a->w, a->w_stride_row, a->V, a->Dh, 2, false, who, "w")) != DLM_OK) return rc;
+    if (a->d_w && (a->d_w == a->w || a->d_w == a->d_hidden)) return fail(DLM_ERR_INVALID_ARG, "%s: d_w is w or d_hidden", who);
     if (a->hidden_stride_row < a->Dh || (a->V > 1 && a->w_stride_row < a->Dh)) return fail(DLM_ERR_INVALID_ARG, "%s: row stride < Dh", who);
     if (a->V > 1 && a->w_stride_row >= 1 << 23) return fail(DLM_ERR_UNSUPPORTED, "%s: w_stride_row >= 2^23", who);
     return DLM_OK;

@@ -224,6 +224,18 @@ def test_rows_named_more_than_once_and_in_any_order(M, named, live, scatter, typ
     assert (np.delete(wide(d_h), there, 0) == 7).all()
 
 
+@pytest.mark.parametrize("M", [70, 300])
+def test_in_the_place_of_the_hidden_rows(M):
+    c = Case(M, 128, 300, rows_total=M + 30, forbid=3)
+    d_h, d_w = torch.zeros((M + 30, 128), dtype=BF16, device=DEV), torch.zeros((300, 128), dtype=BF16, device=DEV)
+    c.call(d_h, d_w)
+    before, there = c.hidden.clone(), torch.from_numpy(c.idx).long().to(DEV)
+    c.call(c.hidden, torch.zeros_like(d_w))
+    assert torch.equal(c.hidden[there], d_h[there])
+    before[there] = d_h[there]
+    assert torch.equal(c.hidden, before)
+
+
 def test_one_gradient_alone_and_one_cotangent_alone():
     c = Case(70, 128, 300, forbid=3)
     both_h, both_w = torch.zeros((70, 128), dtype=BF16, device=DEV), torch.zeros((300, 128), dtype=F32, device=DEV)

@@ -27,7 +27,7 @@ def test_struct_layout_matches_header(tmp_path):
 def _args(**kw):
     a = S.LmheadBwdArgs()
     f = dict(struct_size=C.sizeof(a), M=4, Dh=64, V=10, hidden=P, hidden_stride_row=64, w=P, w_stride_row=64, inv_temperature=1.0, forbid_token=-1, lse=P, target=P, d_lse=P,
-             d_ztarget=P, d_hidden=P, d_hidden_stride_row=64, d_w=P, d_w_stride_row=64, workspace=P, workspace_bytes=1 << 30)
+             d_ztarget=P, d_hidden=P, d_hidden_stride_row=64, d_w=3 * P, d_w_stride_row=64, workspace=P, workspace_bytes=1 << 30)
     for k, v in dict(f, **kw).items():
         setattr(a, k, v)
     return a
@@ -39,7 +39,7 @@ REFUSED = [(dict(struct_size=8), BAD), (dict(M=-1), BAD), (dict(Dh=0), BAD), (di
            (dict(d_lse=None, d_ztarget=None), BAD), (dict(target=None), BAD), (dict(lse=None), BAD), (dict(hidden=None), BAD), (dict(w=None), BAD),
            (dict(hidden=P + 8), UNSUPPORTED), (dict(w=P + 2), UNSUPPORTED), (dict(w_stride_row=32), BAD), (dict(hidden_stride_row=0), BAD), (dict(w_stride_row=68), UNSUPPORTED),
            (dict(w_stride_row=1 << 23), UNSUPPORTED), (dict(d_hidden_type=2), BAD), (dict(d_w_type=-1), BAD), (dict(d_hidden_stride_row=56), BAD), (dict(d_w_stride_row=0), BAD),
-           (dict(d_w=P + 8), UNSUPPORTED), (dict(d_w_type=1, d_w_stride_row=66), UNSUPPORTED), (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=100), WORKSPACE),
+           (dict(d_w=P + 8), UNSUPPORTED), (dict(d_w=P), BAD), (dict(d_w=3 * P, d_hidden=3 * P), BAD), (dict(d_w_type=1, d_w_stride_row=66), UNSUPPORTED), (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=100), WORKSPACE),
            (dict(workspace=P + 8), WORKSPACE)]
 
 

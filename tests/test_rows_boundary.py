@@ -37,7 +37,7 @@ def _embed(**kw):
 
 
 def _embed_bwd(**kw):
-    return _fill(S.EmbedBwdArgs, dict(T=4, V=10, Dh=64, tokens=P, d_out=P, d_out_stride=64, scale=1.0, d_table=P, d_table_stride=64, workspace=P,
+    return _fill(S.EmbedBwdArgs, dict(T=4, V=10, Dh=64, tokens=P, d_out=P, d_out_stride=64, scale=1.0, d_table=3 * P, d_table_stride=64, workspace=P,
                                       workspace_bytes=1 << 20), kw)
 
 
@@ -62,7 +62,8 @@ REFUSED = (
         (dict(out_type=2), BAD), (dict(table=None), BAD), (dict(out=None), BAD), (dict(table=P + 4), UNSUPPORTED), (dict(out_stride=56), BAD),
         (dict(out_stride=68), UNSUPPORTED), (dict(table_stride=-64), UNSUPPORTED)]]
     + [("dlm_embed_bwd", _embed_bwd, kw, code) for kw, code in TOKENS + [
-        (dict(d_out_type=3), BAD), (dict(d_table_type=-1), BAD), (dict(V=1 << 21), UNSUPPORTED), (dict(T=(1 << 28) + 1), UNSUPPORTED), (dict(d_out=None), BAD),
+        (dict(d_out_type=3), BAD), (dict(d_table_type=-1), BAD), (dict(V=1 << 21), UNSUPPORTED), (dict(T=(1 << 28) + 1), UNSUPPORTED), (dict(d_out=None), BAD), (dict(d_table=P), BAD),
+        (dict(Dh=65544, d_out_stride=65544, d_table_stride=65544), UNSUPPORTED), (dict(T=1 << 28, Dh=8192, d_out_stride=0, d_table_stride=8192), UNSUPPORTED),
         (dict(d_table=None), BAD), (dict(d_table_stride=32), BAD), (dict(d_out_stride=60), UNSUPPORTED), (dict(workspace=None), WORKSPACE),
         (dict(workspace_bytes=16), WORKSPACE), (dict(workspace=P + 4), WORKSPACE)]]
     + [("dlm_row_norm", _norm, kw, code) for kw, code in EPS + [
