@@ -44,12 +44,12 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
 // tokens stay in the order of their positions, since earlier runs hold earlier ones).
 constexpr int MERGE = 32;
 constexpr int EMBED_MAX_V = (1 << 21) - 2;                    // a token (or V: none) and a place in its run share 32 bits: 21 and 11
-// 512 entries for a few tokens, which one wavefront sorts without a barrier; 8192, of which there are few to merge, for many tokens, and where a
-// table is cleared meanwhile, if they leave the token its bits.  us of the sort and the merge in runs of 2048 / 8192: 3000 tokens 10 + 9 / 30,
-// 65536 tokens 10 + 54 / 31 + 19.
+// 512 entries for a few tokens, which one wavefront sorts without a barrier; 8192, of which there are fewer to merge, where a table is cleared meanwhile, if they
+// leave the token its bits.  Where none is, us of the whole call (Dh = 512) in runs of 2048 / 8192: 4096 tokens 33 / 39, 16384 38 / 60, 65536 92 / 101,
+// 131072 136 / 134, 300000 268 / 294.
 inline int run_bits(int T, int V, bool clears) {
     if (T <= 512) return 9;
-    return T <= 2048 || V >= (1 << 19) - 1 || (T <= 16384 && !clears) ? 11 : 13;
+    return T <= 2048 || V >= (1 << 19) - 1 || !clears ? 11 : 13;
 }
 
 // the value of lane ^ MASK, without a trip through LDS
@@ -156,28 +156,107 @@ __global__ __launch_bounds__(1 << (BITS - 3)) void embed_sort_kernel(SortParams 
     }
 }
 
-// Runs of `len` entries (a power of two), MERGE of them into one.  Eight runs are searched at a time: a search is a chain of trips to memory.  (Eight
-// probes a trip instead of one are slower, 78 us where 54: it is the loads themselves that take the time.)
+// Runs of `len` entries (a power of two, 256 or more), MERGE of them into one.  A workgroup has 256 neighbouring entries of one run, so few tokens of the others lie
+// between its first and its last: it looks for these two in every run, takes what stands between them into LDS and searches there.  65536 tokens in 32 runs:
+// 26 us, ten of them for the first searches, four for the copy, the rest in LDS; with searches in memory alone, chains of 11 trips, 54.
 __global__ __launch_bounds__(256) void embed_merge_kernel(const int32_t* token, const int32_t* pos, int32_t* token_out, int32_t* pos_out, int T, int64_t len) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    constexpr int ROOM = 16384, SAMPLES = 64, FEW = 32;
+    __shared__ int below[4][MERGE];                // entries of a run: below the first token, up to it, below the last, up to it
+    __shared__ int32_t between[ROOM];              // (first a sample of each run)
+    __shared__ int start[MERGE + 1];               // of each run's tokens in `between`
+    const int tid = threadIdx.x;
+    const int64_t b0 = (int64_t)blockIdx.x * 256, i = b0 + tid, run = b0 / len, group = run / MERGE * MERGE;
+    const auto count = [&](int j) { return (int)max((int64_t)0, min(len, T - (group + j) * len)); };
+    // the four searches of every run: among 64 entries of each, then, 32 lanes a search, among 32 at a time of what is left, a trip to memory each
+    int64_t seg = len / SAMPLES;
+#pragma unroll
+    for (int k = 0; k < MERGE * SAMPLES / 256; ++k) {
+        const int j = (k * 256 + tid) / SAMPLES;
+        const int64_t at = ((k * 256 + tid) % SAMPLES + 1) * seg - 1;
+        between[k * 256 + tid] = at < count(j) ? token[(group + j) * len + at] : 0x7fffffff;
+    }
+    const int first = token[b0], last = token[min(b0 + 255, (int64_t)T - 1)];
+    __syncthreads();
+    if (tid < 4 * MERGE) {
+        const int which = tid / MERGE, j = tid % MERGE, x = (which < 2 ? first : last) + (which & 1);
+        int lo = 0;
+#pragma unroll
+        for (int step = SAMPLES; step > 0; step >>= 1)
+            if (lo + step <= SAMPLES && between[j * SAMPLES + lo + step - 1] < x) lo += step;
+        below[which][j] = (int)min(lo * seg, (int64_t)count(j));
+    }
+    while (seg > 1) {
+        const int step = (int)max(seg / FEW, (int64_t)1), l = tid % FEW;
+        int32_t seen[4 * MERGE * FEW / 256];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4 * MERGE * FEW / 256; ++k) {
+            const int search = (k * 256 + tid) / FEW, j = search % MERGE;
+            const int64_t at = below[search / MERGE][j] + (int64_t)(l + 1) * step - 1;
+            seen[k] = (l + 1) * (int64_t)step <= seg && at < count(j) ? token[(group + j) * len + at] : 0x7fffffff;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4 * MERGE * FEW / 256; ++k) {
+            const int search = (k * 256 + tid) / FEW, which = search / MERGE;
+            const uint64_t under = __ballot(seen[k] < (which < 2 ? first : last) + (which & 1));
+            if (l == 0) below[which][search % MERGE] += __popc((uint32_t)(lane_id() < FEW ? under : under >> 32)) * step;
+        }
+        seg = step;
+    }
+    __syncthreads();
+    if (tid <= MERGE) {
+        int at = 0;
+#pragma unroll
+        for (int j = 0; j < MERGE; ++j) at += j < tid ? max(0, below[2][j] - below[1][j]) : 0;
+        start[tid] = at;
+    }
+    __syncthreads();
+    const bool here = start[MERGE] <= ROOM;        // (else every search is in memory: a token that this run lacks fills others)
+    if (here) {
+        for (int j = tid / WAVE; j < MERGE; j += 256 / WAVE) {
+#pragma unroll 4
+            for (int k = lane_id(); k < start[j + 1] - start[j]; k += WAVE) between[start[j] + k] = token[(group + j) * len + below[1][j] + k];
+        }
+        __syncthreads();
+    }
     if (i >= T) return;
     const int x = token[i], at = pos[i];
-    const int64_t run = i / len, group = run / MERGE * MERGE;
     int64_t to = group * len + (i - run * len);
     for (int j0 = 0; j0 < MERGE && (group + j0) * len < T; j0 += 8) {
         // entries of each run with a token below x, or, in an earlier run, at most x
-        int64_t lo[8];
+        int lo[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) lo[j] = 0;
-        for (int64_t step = len; step > 0; step >>= 1) {
+        for (int j = 0; j < 8; ++j) lo[j] = below[1][j0 + j];
+        if (x == first || x == last) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lo[j] = below[(x == first ? 0 : 2) + (group + j0 + j < run ? 1 : 0)][j0 + j];
+        } else if (here) {
+            int n[8], s0[8], most = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int64_t r = group + j0 + j, last = r * len + lo[j] + step - 1;
-                if (lo[j] + step <= len && last < T && r != run && token[last] < x + (r < run ? 1 : 0)) lo[j] += step;
+                s0[j] = start[j0 + j];
+                n[j] = start[j0 + j + 1] - s0[j];
+                s0[j] -= lo[j];                    // (lo[j] entries lie before those in LDS)
+                n[j] += lo[j];
+                most = max(most, n[j] - lo[j]);
+            }
+            for (int step = most > 0 ? 1 << (31 - __builtin_clz(most)) : 0; step > 0; step >>= 1) {
+                int seen[8];                       // (all eight asked for before the first is looked at)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) seen[j] = between[lo[j] + step <= n[j] ? s0[j] + lo[j] + step - 1 : 0];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) lo[j] += lo[j] + step <= n[j] && seen[j] < x + (group + j0 + j < run ? 1 : 0) ? step : 0;
+            }
+        } else {
+            for (int step = 1 << 28; step > 0; step >>= 1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (lo[j] + step <= below[2][j0 + j] && token[(group + j0 + j) * len + lo[j] + step - 1] < x + (group + j0 + j < run ? 1 : 0)) lo[j] += step;
             }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) to += lo[j];
+        for (int j = 0; j < 8; ++j) to += group + j0 + j == run ? 0 : lo[j];
     }
     token_out[to] = x;
     pos_out[to] = at;

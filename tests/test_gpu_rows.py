@@ -139,6 +139,25 @@ def test_embed_gradient_of_orders_that_cut_chunks_everywhere(kind):
     assert np.array_equal(wide(table), rows.embed_grad(tokens, wide(dy), T, 1.0)[0])
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["ascending", "descending", "mixed", "one run lacks what fills the others", "half of one", "none"])
+@pytest.mark.parametrize("T", [2305, 8193, 70000, 140001])
+def test_embed_gradient_merges_runs_of_any_order(T, kind, accumulate):
+    """Exact again, over one and two levels of merging; tokens that one stretch of the list lacks and the others are full of."""
+    V, Dh, rng = 70000, 8, np.random.default_rng(T)
+    at = np.arange(T)
+    few = np.where(at < 2048, at % 2 * 100, 50)
+    tokens = {"ascending": at * V // T, "descending": (T - 1 - at) * V // T, "mixed": rng.integers(-5, V + 5, T), "one run lacks what fills the others": few,
+              "half of one": np.where(rng.random(T) < 0.5, V - 1, rng.integers(0, 300, T)), "none": np.full(T, -1)}[kind].astype(np.int32)
+    dy = torch.from_numpy((at[:, None] * 7 + np.arange(Dh)) % 13 - 6).to(BF16).to(DEV)
+    table = torch.full((V, Dh), 3.0, dtype=F32, device=DEV)
+    grad_of(torch.from_numpy(tokens).to(DEV), dy, table, accumulate=accumulate)
+    want = np.zeros((V, Dh))
+    live = (tokens >= 0) & (tokens < V)
+    np.add.at(want, tokens[live], wide(dy)[live])
+    assert np.array_equal(wide(table), want + (3 if accumulate else 0))
+
+
 def test_embed_gradient_is_the_same_every_time_and_over_two_levels_of_merging():
     T, V = 140001, 90000                                        # 35 runs: more than are merged at once
     rng = np.random.default_rng(3)
