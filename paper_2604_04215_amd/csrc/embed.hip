@@ -4,6 +4,10 @@
 // so that the sum of a token's rows has one order and no atomics are needed), then every row is read once.  In a masked batch one token has half of
 // the rows, so the sorted list is cut into chunks of equal length whatever tokens they hold; the sums of a token that goes over the end
 // of a chunk are joined by a last launch.
+//
+// Measured: 65536 rows of 4096 into fp32 214 us, 5.5 TB/s of the 1.17 GB that it cannot do without (a copy: 6.2); 256 rows into bf16 3.9, of which the GPU works 2.7.
+// Gradient of 65536 rows of 4096, half of them of one token, added to an fp32 table of 126464: 256 us (sort 9, merge 26, sums 187, of 0.93 GB, join 7);
+// of 8192 rows of 3584 into a 16-bit table of 152064, which is cleared: 224 (sort beside 1.09 GB of zeros 190, sums 22, join 5); of 333 rows of 256: 14.7, three launches.
 #include "rows.hpp"
 
 namespace dlm {
@@ -18,7 +22,8 @@ struct EmbedParams {
     int64_t out_st;
 };
 
-// TPR threads a row, pieces of 16 bytes of what is written: the stores of a wavefront cover whole lines
+// TPR threads a row, pieces of 16 bytes of what is written: the stores of a wavefront cover whole lines.  (Eight entries
+// of fp32 a thread, two stores of 16 bytes that each fill half of every line: 412 us where this takes 214.)
 template <bool F32, int TPR>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p) {
     constexpr int ROWS = 256 / TPR, E = Piece<F32>::E;

@@ -6,6 +6,9 @@
 // The mean of a layer norm is taken twice: once over the entries, once over what is left when that mean is subtracted, whose sum would be
 // zero without rounding.  Rows of large mean and small deviation (or all equal) so lose nothing to the rounding of the mean, and the second sum
 // comes with the sum of squares: no further pass.
+//
+// Measured: 65536 rows of 3584 fp32, layer norm into bf16 258 us, 5.5 TB/s; the gradient of 65536 rows of 4096 bf16 with d_sum and the weight's 362, 5.9 TB/s (a copy
+// reaches 6.2); 256 rows of 4096 with a residual 4.1, of which the GPU works 3; the gradient of 333 rows of 896 8.4, two launches.
 #include "rows.hpp"
 
 namespace dlm {
@@ -159,7 +162,8 @@ struct NormGradParams {
 };
 
 // With n the normalised row, r its factor and g = dy w:  dx = r (g - [layer] mean(g) - n mean(g n)) + ds;  dw = sum of dy n;  db = sum of dy.
-// Every team takes one row after the other and keeps the sums of its columns in registers.
+// Every team takes one row after the other, the next one's pieces requested before this one's sums are formed, and keeps the sums of its columns in registers;
+// norm_sum_kernel adds the workgroups' (5.6 us for 1024 of 4096 columns).
 template <bool F32, int N, int TPR>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(NormGradParams p) {
     using P = Piece<F32>;
