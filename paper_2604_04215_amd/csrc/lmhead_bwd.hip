@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int c = (k * WAVE + lane) * 8;
-                    kept[k] = c < p.Dh ? *reinterpret_cast<const u32x4*>(src + c) : u32x4{0, 0, 0, 0};
+                    kept[k] = c < p.Dh ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + c)) : u32x4{0, 0, 0, 0};
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) top = fmaxf(top, lmb_top8(kept[k]));
