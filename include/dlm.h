@@ -688,7 +688,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *   dz_v = inv_temperature * (d_lse * p_v + d_ztarget * [v == target]);   d_hidden[row] = sum_v dz_v w[v];   d_w[v] = sum_rows dz_v hidden[row]
  * (a log-probability log p(target) = ztarget - lse with gradient g: d_ztarget = g, d_lse = -g).
  *   M, Dh, V, hidden, row_idx, m_dev, w, inv_temperature, forbid_token, out_scatter   as in the forward call
- *   lse        fp32, the forward call's; target, d_lse, d_ztarget are indexed like it (by r, or by row(r) with out_scatter).  d_lse or d_ztarget may be
+ *   lse        fp32, the forward call's (probabilities of at most 1 are relied upon); target, d_lse, d_ztarget are indexed like it (by r, or by row(r) with out_scatter).  d_lse or d_ztarget may be
  *              NULL: zero.  d_ztarget needs target; a target outside [0, V), or forbid_token, has no gradient.
  *              A row whose d_lse is zero may have any lse.
  *   d_hidden   optional, rows of d_hidden_type indexed like `hidden`: row(r) is written for every r, other rows are left as they are.  Each entry of

@@ -17,8 +17,8 @@
 //   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products added up in two floats (the logits too: an error of one is one of the
 //     probability).  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
 //
-// Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 11.2 ms, 1.2 PFLOP/s (W's copy 0.44, dz 3.74 at 1.19, the gradients 6.8 at 1.31); 512 rows, V = 126464,
-// Dh = 4096 1.95 ms (0.40, 0.50, 1.05); 64 rows 0.80, 4 rows 0.76, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
+// Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 11.2 ms, 1.2 PFLOP/s (W's copy 0.42, dz 3.74 at 1.19, the gradients 6.8 at 1.31); 512 rows, V = 126464,
+// Dh = 4096 1.95 ms (0.37, 0.50, 1.05); 64 rows 0.80, 4 rows 0.76, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
 #include "rows.hpp"
 
 namespace dlm {
@@ -184,6 +184,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int c = (k * WAVE + lane) * 8;
+                    // (past the caches, which cannot hold W: 410 -> 376 us of 126464 x 4096)
                     kept[k] = c < p.Dh ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + c)) : u32x4{0, 0, 0, 0};
                 }
 #pragma unroll
