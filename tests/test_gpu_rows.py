@@ -383,6 +383,22 @@ def test_on_another_stream_and_replayed_from_a_graph():
         assert all(torch.equal(eager[k], graphed[k]) for k in eager), k
 
 
+@pytest.mark.parametrize("T", [100, 1500, 3000, 70000])
+def test_whatever_the_workspaces_held(T):
+    rng = np.random.default_rng(T)
+    tokens, x, dy = torch.from_numpy(tokens_of(rng, T, 900)).to(DEV), rnd(rng, T, 72), rnd(rng, T, 72)
+    outs = []
+    for fill in (0, 0x3f, 0x80, 0xff):
+        ws = [torch.full((n,), fill, dtype=U8, device=DEV) for n in (dlm.embed_bwd_workspace_bytes(T, 900, 72), dlm.row_norm_bwd_workspace_bytes(T, 72))]
+        added, whole, d_x, d_w, d_b = torch.ones((900, 72), device=DEV), torch.ones((900, 72), device=DEV), torch.zeros_like(x), torch.zeros(72, device=DEV), torch.zeros(72, device=DEV)
+        dlm.embed_bwd(tokens, dy, added, accumulate=True, workspace=ws[0])
+        ws[0].fill_(fill)
+        dlm.embed_bwd(tokens, dy, whole, workspace=ws[0])
+        dlm.row_norm_bwd(dy, x, d_x, kind=dlm.NORM_LAYER, d_weight=d_w, d_bias=d_b, workspace=ws[1])
+        outs.append((added, whole, d_x, d_w, d_b))
+    assert all(torch.equal(a, b) for got in outs[1:] for a, b in zip(got, outs[0])) and all(t.isfinite().all() for t in outs[0])
+
+
 def test_binding_checks():
     x, t = torch.zeros((4, 64), dtype=BF16, device=DEV), torch.zeros(4, dtype=I32, device=DEV)
     with pytest.raises(ValueError, match="dtype"):
