@@ -695,12 +695,14 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *              row_idx counts by itself: a row that several name gets the sum of their gradients (in time that grows with M squared where row_idx
  *              does not ascend).
  *   d_w        optional [V, Dh] of d_w_type; accumulate 0: written, else added to
- * The logits are not stored.  No atomics: deterministic (the order of sums depends on the sizes, the types and which
+ * The logits are not stored.  No sum is formed by atomics: deterministic (the order of sums depends on the sizes, the types and which
  * gradients are wanted).  hidden and w have to be finite: other rows'
  * values are multiplied by dz that may be zero.  d_w overlaps neither w nor d_hidden; d_hidden may be hidden.
- * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 11 bits, as an fp16 scaled by row and column (rows whose |d_lse| + |d_ztarget| times
- * their largest entry is less than 2^-40 of the largest such product of the call lose bits; so do columns where a few rows of w are more than 2^20 larger than the rest), or, up to 128 rows, 16 bits.  Where a gradient is
- * fp32, it keeps 24, and all sums are added up in two floats: three to four times as long.
+ * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 128 rows, above that 11, as an fp16 with a scale of its own for each gradient:
+ *   for d_hidden an entry is besides up to 2^-38 of its row's (|d_lse| + |d_ztarget|) inv_temperature off (more where a few rows of w are over 2^8 larger than most: as
+ *   many times more as they are beyond that), for d_w up to 2^-22 of the largest |dz| of its column, both times the largest entry of their hidden rows.  So every row of
+ *   both gradients is right by its own size, of tokens that are unlikely in every row too.  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.
+ * Where a gradient is fp32, dz keeps 24 bits, and all sums are added up in two floats: three to four times as long.
  * workspace: dlm_lmhead_bwd_workspace_bytes(args) bytes, 16-byte aligned; they depend on M, Dh, V, the types and which gradients are wanted.
  * Supported: Dh % 64 == 0, up to 65536; M up to 2^20; V up to 2^24; rows 16-byte aligned, strides multiples of 16 bytes, w_stride_row < 2^23.
  * ------------------------------------------------------------------------- */

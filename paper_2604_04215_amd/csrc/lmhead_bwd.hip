@@ -12,7 +12,8 @@
 //
 // Rounding of dz.  One bf16 (8 bits) would make the error of a bf16 gradient 1.4 times that of rounding the gradient alone.  So:
 //   bf16 gradients, many rows: one fp16 term, 11 bits, at the same rate.  Its other operands are fp16 too, exact copies of hidden rows and of W
-//     but for powers of two (see LmbScale), which costs a pass over W: 3 % of the time of 4096 rows.
+//     but for powers of two (see LmbScale), which costs a pass over W: 3 % of the time of 4096 rows.  Each gradient has a dz of its own, scaled by the rows for
+//     d_hidden, by the columns for d_w: a token that is unlikely in every row has a small column of dz, of which all of its row of d_w is summed.
 //   bf16 gradients, few rows: two bf16 terms, 16 bits: twice the products where reading W takes longest, and no copy of it.
 //   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products added up in two floats (the logits too: an error of one is one of the
 //     probability).  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
@@ -34,21 +35,30 @@ struct LmbRow {                    // what the logits' kernel knows of a row
 };
 constexpr int LMB_NO_TARGET = -(1 << 28);
 
-// fp16 operands.  With e(x) the exponent of the largest entry of a row (its size lies in [2^e, 2^(e+1))):
-//   h16[m] = h[m] 2^(14 - up[m]),  up[m] = e(h[m]) + u;   w16[v] = w[v] 2^(14 - f[v]);   D[m][v] = dz[m][v] 2^(up[m] + f[v] - K)
-//   d_hidden[m] = 2^(K - 14 - up[m]) sum_v D w16;   d_w[v] = 2^(K - 14 - f[v]) sum_m D h16
-// K = L + max_v f[v] - 13 keeps D below 2^15, where L = max_m (e(h[m]) + c[m]) and 2^(c + 1) exceeds a row's |d_lse| + |d_ztarget|, inv_t included.
-// u = min(L - e(h[m]) - c[m], 20) brings rows of small gradients up (h keeps its 8 bits in entries of 2^-11 of its largest and more): dz of 2^-8 of the largest
-// of its row keeps all 11 bits while the row's gradient is at most 2^40 below the largest.
-// f[v] = max(e(w[v]), F), F eight above the largest exponent of 256 rows spread over W: nearly always F for all, so that a small row of W does not make its
-// column of dz, of which d_w is summed, a small number too.  (What w16 loses there, 2^-31 of W's largest, counts for nothing in d_hidden.)
+// fp16 operands.  With e(x) the exponent of the largest entry of a row (its size lies in [2^e, 2^(e+1))) and 2^(c + 1) above a row's |d_lse| + |d_ztarget|, inv_t
+// included, so that |dz| < 2^(c + 1):
+//   d_hidden[m] = 2^(S - 27 + c[m]) sum_v D w16[v],   D[m][v] = dz[m][v] 2^(13 - c[m] + f[v] - S),   w16[v] = w[v] 2^(14 - f[v]),   S = max_v f[v]
+//   d_w[v] = 2^(L - 27 - 16 k[v]) sum_m E h16[m],   E[m][v] = dz[m][v] 2^(13 + e(h[m]) - L + 16 k[v]),   h16[m] = h[m] 2^(14 - e(h[m])),   L = max_m (e(h[m]) + c[m])
+// D and E stay below 2^14 (2^15 where a probability is rounded above one).  f[v] = max(e(w[v]), F), F eight above the largest exponent of 256 rows spread over W:
+// nearly always F for all, so that small rows of W do not make their D small (what w16 loses there, 2^-31 of W's largest, counts for nothing in d_hidden).
+// k[v], 0 to 7, brings the largest |E| of a column to 2^-1 or more, so that E is 2^-24 of it off at most.  It is known when all rows of dz are: a wavefront scales its
+// panel of 32, 64 or 128 rows by the panel's own largest, and lmb_even_kernel brings the panels of a column, where they differ, to the smallest k among them (another
+// rounding of what falls below the normal numbers).  One dz for both, scaled by |d_lse| + |d_ztarget| alone, gave zeros for d_w of tokens whose probability is below 2^-39 in
+// every row, and few bits below 2^-28: all of a batch whose targets are 40 above the other logits.  What E takes: dz of 4096 rows, V = 152064, Dh = 3584 3960 -> 4290 us,
+// lmb_even_kernel 460 (it reads and writes nearly all of E, 5.5 TB/s, since the largest of 128 rows and that of 4096 are mostly over 2^8 apart); of 512 rows, V = 126464,
+// Dh = 4096 570 -> 615 and 53.
 struct LmbScale {
-    int *row_e, *row_c, *up;       // [M rounded up to 64]
+    int *row_e, *row_c;            // [M rounded up to 64]
+    int *hs, *ws;                  // 13 - c;  c + e(h) - L: the powers from dz to D (without f) and from there to E (without k); [M rounded up to 64]
     int* w_f;                      // f, [V rounded up to 256]
+    int* col;                      // k, [V rounded up to 256] (LMB_EMPTY: a column of zeros)
+    uint8_t* panel;                // k of a panel, [panels][ldz]
     int *row_max, *w_some, *w_max; // by workgroup; exponents of some rows of W; by wavefront
-    int* out;                      // max_v f[v], K
+    int* out;                      // S, L
     uint16_t *h16, *w16, *tail16;
+    uint16_t* e;                   // E, as dz
 };
+constexpr int LMB_EMPTY = 255;
 constexpr int LMB_ORDER = 64;      // wavefronts that look through row_idx
 constexpr int LMB_STATS = 256;     // workgroups that look for a largest exponent
 constexpr int LMB_NONE = -100000;  // exponent of a row of zeros
@@ -72,7 +82,7 @@ struct LmbParams {
     int f16;                       // dz is fp16 and scaled
     LmbScale sc;
     int last_f;                    // the last four of w_f
-    uint16_t* dz;                  // [terms][M rounded up to 64][ldz]
+    uint16_t* dz;                  // [terms][M rounded up to 64][ldz]; fp16: D
     int64_t dz_term;               // entries of a term
     int ldz;
     float* part;                   // [splits][terms][M][Dh]
@@ -163,6 +173,9 @@ __device__ __forceinline__ int lmb_most(const int* v, int n) {
 __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     const int M = lmb_rows(p), bound = (p.M + 63) & ~63, r = blockIdx.x;
     if (r == 0 && threadIdx.x < 24) p.counters[threadIdx.x * 16] = 0;
+    if (p.f16) {
+        for (int v = r * 256 + threadIdx.x; v < p.last_f + 4; v += gridDim.x * 256) p.sc.col[v] = LMB_EMPTY;
+    }
     if (r < LMB_ORDER && p.row_idx && threadIdx.x < WAVE) {        // (there are 64 workgroups or more)
         bool falls = false;
 #pragma unroll 4
@@ -213,17 +226,19 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
     if (r >= ((M + 63) & ~63)) return;
     const bool live = r < M;
     const int row = !live ? 0 : p.row_idx ? p.row_idx[r] : r;
-    int up = 0;
+    int hs = 0, ws = 0, e = 0;
     if (p.f16 && live) {
-        const int e = p.sc.row_e[r], c = p.sc.row_c[r], most = lmb_most(p.sc.row_max, LMB_STATS);
-        // (a hidden row of zeros has any scale: the one that brings its gradient to the largest)
-        if (e == LMB_NONE) up = c == LMB_NONE ? 0 : (most == LMB_NONE ? 0 : most) - c;
-        else up = e + (c == LMB_NONE ? 0 : min(max(most - e - c, 0), 20));
+        // (a row whose gradient is zero or not finite has any scale; of a hidden row of zeros nothing is to count for the columns' largest)
+        const int c = p.sc.row_c[r], most = lmb_most(p.sc.row_max, LMB_STATS);
+        e = p.sc.row_e[r];
+        if (c != LMB_NONE) hs = 13 - c;
+        if (e == LMB_NONE) ws = LMB_NONE;
+        else if (c != LMB_NONE) ws = c + e - most;
     }
     for (int c = threadIdx.x * 8; c < p.Dh; c += 2048) {
         const uint16_t* src = p.hidden + row * p.h_stride + c;
         *reinterpret_cast<u32x4*>(p.h + (int64_t)r * p.Dh + c) = live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0};
-        if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = lmb_half8(live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0}, live, 14 - up);
+        if (p.f16) *reinterpret_cast<u32x4*>(p.sc.h16 + (int64_t)r * p.Dh + c) = lmb_half8(live ? *reinterpret_cast<const u32x4*>(src) : u32x4{0, 0, 0, 0}, live && e != LMB_NONE, 14 - e);
     }
     if (threadIdx.x == 0) {
         LmbRow o = {INFINITY, 0.f, 0.f, LMB_NO_TARGET};
@@ -238,20 +253,23 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
             }
         }
         p.rows[r] = o;
-        if (p.f16) p.sc.up[r] = up;
+        if (p.f16) {
+            p.sc.hs[r] = hs;
+            p.sc.ws[r] = ws;
+        }
     }
 }
-// K, from what the workgroups found
+// S and L, from what the workgroups found
 __global__ __launch_bounds__(512) void lmb_scale_kernel(LmbParams p) {
     __shared__ int meet[8];
-    const int wave = threadIdx.x >> 6, L = lmb_most(p.sc.row_max, LMB_STATS), S0 = lmb_most(p.sc.w_max + wave * LMB_STATS * 4, LMB_STATS * 4);
+    const int wave = threadIdx.x >> 6, L = lmb_most(p.sc.row_max, LMB_STATS), S0 = p.d_hidden ? lmb_most(p.sc.w_max + wave * LMB_STATS * 4, LMB_STATS * 4) : LMB_NONE;
     if (lane_id() == 0) meet[wave] = S0;
     __syncthreads();
     if (threadIdx.x == 0) {
         int S = meet[0];
         for (int k = 1; k < 8; ++k) S = max(S, meet[k]);
         p.sc.out[0] = S == LMB_NONE ? 0 : S;
-        p.sc.out[1] = (L == LMB_NONE ? 0 : L) + (S == LMB_NONE ? 0 : S) - 13;
+        p.sc.out[1] = L == LMB_NONE ? 0 : L;
     }
 }
 
@@ -296,6 +314,40 @@ __device__ __forceinline__ void lmb_load_lds16(const void* base, uint32_t offset
 __device__ __forceinline__ u32x4 lmb_eight(const uint32_t (&w)[4]) {
     const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     return u32x4{x[0], y[0], x[1], y[1]};
+}
+
+// largest of 32 neighbouring lanes' numbers, for all of them
+__device__ __forceinline__ uint32_t lmb_most32(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true));       // lane ^ 1
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true));       // lane ^ 2
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true));      // 7 - lane of 8
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, true));      // 15 - lane of 16
+    const auto w = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max((uint32_t)w[0], (uint32_t)w[1]);
+}
+// Four neighbouring lanes' pieces x[0 .. 3] turned: lane b of the four gets piece b of each, lane u's in x[u].
+__device__ __forceinline__ void lmb_turn(u32x4 (&x)[4]) {
+    const int l = threadIdx.x;
+#pragma unroll
+    for (int bit = 1; bit < 4; bit *= 2) {
+        const bool up = l & bit;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t & bit) continue;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t a = x[t][k], b = x[t | bit][k], send = up ? a : b;
+                const uint32_t got = bit == 1 ? __builtin_amdgcn_mov_dpp(send, 0xB1, 0xf, 0xf, true) : __builtin_amdgcn_mov_dpp(send, 0x4E, 0xf, 0xf, true);
+                x[t][k] = up ? got : a;
+                x[t | bit][k] = up ? b : got;
+            }
+        }
+    }
+}
+// fp16 of two numbers, in a word
+__device__ __forceinline__ uint32_t lmb_halves(float a, float b) {
+    typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+    return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
 }
 
 template <int V, int H, int TV, int TH>
@@ -602,83 +654,173 @@ struct LmbDz {
         const int first = tile.i0 + wv * TVW * 32 + 4 * hi, v_first = p.v0 + first;                // the lane's first column
         const bool edge = p.v0 + tile.i0 + Loop::TI > p.V || (p.forbid >= p.v0 + tile.i0 && p.forbid < p.v0 + tile.i0 + Loop::TI);
         const float log2e = 1.4426950408889634f, k = p.inv_t * log2e;
-        const int S = TERMS == 0 ? p.sc.out[0] : 0, K = TERMS == 0 ? p.sc.out[1] : 0;
-        float off[THW], ra[THW], rc[THW];
-        int target[THW], m[THW];
+        float off[THW], ra[THW], rc[THW], ws[THW];
+        int target[THW];
+        const int m0 = tile.j0 + wh * THW * 32 + n;            // the lane's first row
 #pragma unroll
         for (int c = 0; c < THW; ++c) {
-            m[c] = tile.j0 + (wh * THW + c) * 32 + n;
-            const LmbRow row = p.rows[min(m[c], padded - 1)];
+            const int r = min(m0 + c * 32, padded - 1);
+            const LmbRow row = p.rows[r];
             off[c] = TERMS == 3 ? -row.lse : -row.lse * log2e;
-            const int up = TERMS == 0 ? p.sc.up[min(m[c], padded - 1)] - K + S : 0;
-            ra[c] = TERMS == 0 ? ldexpf(row.a, up) : row.a;
-            rc[c] = TERMS == 0 ? ldexpf(row.c, up) : row.c;
+            const int hs = TERMS == 0 ? p.sc.hs[r] : 0;
+            ra[c] = TERMS == 0 ? ldexpf(row.a, hs) : row.a;
+            rc[c] = TERMS == 0 ? ldexpf(row.c, hs) : row.c;
+            ws[c] = TERMS == 0 ? ldexpf(1.f, p.sc.ws[r]) : 1.f;
             target[c] = row.target - v_first;
         }
+        // eight columns of a row, i .. i + 3 and i + 8 .. i + 11
+        const auto eight = [&](int a, int g, int c, float (&d)[8]) {
+            const int i = first + a * 32 + 8 * g;
 #pragma unroll
-        for (int a = 0; a < TVW; ++a)
+            for (int q = 0; q < 2; ++q) {
 #pragma unroll
-            for (int g = 0; g < 4; g += 2) {
-                const int i = first + a * 32 + 8 * g;
-                float f[8];
-                if constexpr (TERMS == 0) {
-                    typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+                for (int e = 0; e < 4; ++e) {
+                    const float z = loop.acc[a][c][4 * (g + q) + e];
+                    // fp32 results: the difference first, a logit and lse are large where their difference is not
+                    float x;
+                    if constexpr (TERMS == 3) x = fast_exp2(fmaf(loop.low[a][c][4 * (g + q) + e], p.inv_t, fmaf(z, p.inv_t, off[c])) * log2e);
+                    else x = fast_exp2(fmaf(z, k, off[c]));
+                    d[4 * q + e] = ra[c] * x;
+                }
+                const uint32_t t = (uint32_t)(target[c] - a * 32 - 8 * (g + q));
+                if (t < 4) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const i32x4 we = *reinterpret_cast<const i32x4*>(p.sc.w_f + min(p.v0 + i + 8 * q, p.last_f));
+                    for (int e = 0; e < 4; ++e) d[4 * q + e] += t == e ? rc[c] : 0.f;
+                }
+            }
+            if (edge) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) f[4 * q + e] = ldexpf(1.f, we[e] == LMB_NONE ? 0 : we[e] - S);
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const int v = p.v0 + i + e / 4 * 8 + e % 4;
+                    if (v == p.forbid || v >= p.V) d[e] = 0.f;
+                }
+            }
+        };
+        if constexpr (TERMS == 0) {
+            // Two tiles of 32 columns at a time (one where there is one), for d_hidden and for d_w.  A row's 64 columns are a whole line: four lanes' pieces are turned, so that
+            // every store writes lines.  (Stores of 32 bytes of 32 rows: dz of 4096 rows, V = 50176, Dh = 3584 1600 us, lines 1430; with one dz for both gradients 1300.)
+            constexpr int NA = TVW < 2 ? 1 : 2;
+            // W's exponents of the columns ahead are asked for before the stores at hand: a load behind stores waits for them
+            typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+            i32x4 we[NA][4];
+            const auto exponents = [&](int a0) {
+#pragma unroll
+                for (int a = 0; a < NA; ++a)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) we[a][g] = *reinterpret_cast<const i32x4*>(p.sc.w_f + min(v_first + (a0 + a) * 32 + 8 * g, p.last_f));
+            };
+            const int S = p.d_hidden ? p.sc.out[0] : 0;
+            if (p.d_hidden) exponents(0);
+#pragma unroll
+            for (int a0 = 0; a0 < TVW; a0 += NA) {
+                u32x4 hold[2][THW][2 * NA];
+                uint32_t fs[NA][4];                    // four columns a register
+                if (p.d_hidden) {
+#pragma unroll
+                    for (int a = 0; a < NA; ++a)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            fs[a][g] = 0;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) fs[a][g] |= (uint32_t)(we[a][g][e] == LMB_NONE ? 0 : min(S - we[a][g][e], 127)) << 8 * e;
+                        }
                 }
 #pragma unroll
-                for (int c = 0; c < THW; ++c) {
-                    float d[8];
+                for (int t = 0; t < 2 * NA; ++t) {
+                    const int a = a0 + t / 2, g = t % 2 * 2;
+                    float d[THW][8];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
+                    for (int c = 0; c < THW; ++c) eight(a, g, c, d[c]);
+                    if (p.d_hidden) {
+                        float f[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float z = loop.acc[a][c][4 * (g + q) + e];
-                            // fp32 results: the difference first, a logit and lse are large where their difference is not
-                            float x;
-                            if constexpr (TERMS == 3) x = fast_exp2(fmaf(loop.low[a][c][4 * (g + q) + e], p.inv_t, fmaf(z, p.inv_t, off[c])) * log2e);
-                            else x = fast_exp2(fmaf(z, k, off[c]));
-                            d[4 * q + e] = ra[c] * x;
-                        }
-                        const uint32_t t = (uint32_t)(target[c] - a * 32 - 8 * (g + q));
-                        if (t < 4) {
+                        for (int e = 0; e < 8; ++e) f[e] = ldexpf(1.f, -(int)(fs[t / 2][g + e / 4] >> 8 * (e % 4) & 255));
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) d[4 * q + e] += t == e ? rc[c] : 0.f;
+                        for (int c = 0; c < THW; ++c) hold[0][c][t] = halves(d[c], f);
+                    }
+                    if (p.d_w) {
+                        float f[8];
+                        columns(tile, lane, first + a * 32 + 8 * g, d, ws, f);
+#pragma unroll
+                        for (int c = 0; c < THW; ++c) hold[1][c][t] = halves(d[c], f);
+                    }
+                }
+                if (p.d_hidden && a0 + NA < TVW) exponents(a0 + NA);
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {
+                    if (!(which ? p.d_w : p.d_hidden)) continue;
+                    uint16_t* dst = which ? p.sc.e : p.dz;
+#pragma unroll
+                    for (int c = 0; c < THW; ++c) {
+                        if constexpr (NA == 2) lmb_turn(hold[which][c]);
+#pragma unroll
+                        for (int u = 0; u < 2 * NA; ++u) {
+                            const int row = m0 + c * 32 + (NA == 2 ? u - (n & 3) : 0), col = first - 4 * hi + a0 * 32 + (NA == 2 ? 2 * (n & 3) + hi : 2 * u + hi) * 8;
+                            if (row < padded && col < p.ldz) *reinterpret_cast<u32x4*>(dst + (int64_t)row * p.ldz + col) = hold[which][c][u];
                         }
                     }
-                    if (edge) {
+                }
+            }
+        } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int v = p.v0 + i + e / 4 * 8 + e % 4;
-                            if (v == p.forbid || v >= p.V) d[e] = 0.f;
-                        }
-                    }
+            for (int a = 0; a < TVW; ++a)
 #pragma unroll
-                    for (int t = 0; t < (TERMS == 0 ? 1 : TERMS); ++t) {
-                        uint32_t w[4];
-                        if constexpr (TERMS == 0) {
-                            typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+                for (int g = 0; g < 4; g += 2) {
+                    const int at8 = first + a * 32 + 8 * g + 4 * hi;        // (lane and lane + 32 share 16 columns, lmb_eight gives each eight of them)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(d[2 * e] * f[2 * e]), (_Float16)(d[2 * e + 1] * f[2 * e + 1])});
-                        } else {
+                    for (int c = 0; c < THW; ++c) {
+                        float d[8];
+                        eight(a, g, c, d);
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t) {
                             // every term what the ones before it leave, which fp32 holds exactly
+                            uint32_t w[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 w[e] = pack_bf16x2(d[2 * e], d[2 * e + 1]);
                                 d[2 * e] -= __uint_as_float(w[e] << 16);
                                 d[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
                             }
+                            const u32x4 out = lmb_eight(w);
+                            if (m0 + c * 32 < padded && at8 < p.ldz) *reinterpret_cast<u32x4*>(p.dz + t * p.dz_term + (int64_t)(m0 + c * 32) * p.ldz + at8) = out;
                         }
-                        const u32x4 out = lmb_eight(w);
-                        const int at8 = i + 4 * hi;                     // (lane and lane + 32 share 16 columns, lmb_eight gives each eight of them)
-                        if (m[c] < padded && at8 < p.ldz) *reinterpret_cast<u32x4*>(p.dz + t * p.dz_term + (int64_t)m[c] * p.ldz + at8) = out;
                     }
                 }
+        }
+    }
+    // eight columns, scaled, in 16 bits
+    static __device__ __forceinline__ u32x4 halves(const float (&d)[8], const float (&f)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = lmb_halves(d[2 * e] * f[2 * e], d[2 * e + 1] * f[2 * e + 1]);
+        return lmb_eight(w);
+    }
+    // d_w's dz of eight columns, i .. i + 3 and i + 8 .. i + 11, of all the wavefront's rows: without the columns' scale in d, the scales in f
+    __device__ __forceinline__ void columns(const At& tile, int lane, int i, float (&d)[THW][8], const float (&ws)[THW], float (&f)[8]) const {
+        const int n = lane & 31, panel = tile.j0 / (32 * THW) + (int)(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) / WV;
+        uint32_t kept[2] = {0, 0};                         // the scales of four columns each
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float most = 0.f;
+#pragma unroll
+            for (int c = 0; c < THW; ++c) {
+                d[c][e] *= ws[c];
+                most = fmaxf(most, fabsf(d[c][e]));        // (NaN counts for nothing)
             }
+            const uint32_t top = lmb_most32(__float_as_uint(most));        // (of numbers that are not negative the bits have their order)
+            const int k = min(max(14 + 127 - (int)(top >> 23), 0) >> 4, 7);
+            f[e] = __uint_as_float(0x3f800000u + ((uint32_t)k << 27));     // 2^(16 k)
+            kept[e / 4] |= (uint32_t)(top > 0 ? k : LMB_EMPTY) << 8 * (e % 4);
+        }
+        if (panel * 32 * THW >= padded) return;
+        if (n == 0) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (i + 8 * q < p.ldz) *reinterpret_cast<uint32_t*>(p.sc.panel + (int64_t)panel * p.ldz + i + 8 * q) = kept[q];
+        }
+        const int mine = (n < 4 ? kept[0] : kept[1]) >> 8 * (n & 3) & 255;
+        // (the smallest of whole numbers: the same in any order.  Columns behind the vocabulary are empty.)
+        if (n < 8 && mine != LMB_EMPTY) __hip_atomic_fetch_min(p.sc.col + p.v0 + i + n / 4 * 8 + n % 4, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
 };
 template <typename S, int TERMS, int BLOCK>
@@ -695,6 +837,35 @@ __global__ __launch_bounds__(64 * S::WV * S::WH, 1) void lmb_dz_kernel(LmbParams
     }
     typename Job::Loop loop(ring);
     loop.run(job, list);
+}
+
+// E's panels of `rows` rows whose scale of a column is not the column's.  A lane has eight columns; most find nothing to do.
+__global__ __launch_bounds__(256) void lmb_even_kernel(LmbParams p, int rows) {
+    const int padded = (lmb_rows(p) + 63) & ~63, first = blockIdx.y * rows, c = (blockIdx.x * WAVE + lane_id()) * 8;
+    if (first >= padded || c >= p.n) return;
+    const uint8_t* k = p.sc.panel + (int64_t)blockIdx.y * p.ldz + c;
+    const int* col = p.sc.col + p.v0 + c;
+    int down[8], any = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        down[e] = k[e] == LMB_EMPTY ? 0 : 16 * (col[e] - k[e]);
+        any |= down[e];
+    }
+    if (any == 0) return;
+    // (`rows` and `padded` are multiples of 32: a wavefront's eight rows are there or not.  All eight are asked for before the first is stored.)
+    for (int r = first + (threadIdx.x / WAVE) * 8; r < min(first + rows, padded); r += 32) {
+        u32x4* at = reinterpret_cast<u32x4*>(p.sc.e + (int64_t)r * p.ldz + c);
+        u32x4 x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = at[(int64_t)q * p.ldz / 8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const f16x8 v = __builtin_bit_cast(f16x8, x[q]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[q][e] = lmb_halves(ldexpf((float)v[2 * e], down[2 * e]), ldexpf((float)v[2 * e + 1], down[2 * e + 1]));
+            at[(int64_t)q * p.ldz / 8] = x[q];
+        }
+    }
 }
 
 // ---- d_hidden's and d_w's products of a chunk ----------------------------------------------------------------
@@ -815,7 +986,7 @@ struct LmbWeight {
         const int term = (q >= all ? 1 : 0) + (q >= 2 * all ? 1 : 0), k = q - term * all;
         b.a0 = (const char*)((F16 ? p.sc.h16 : p.h) + (int64_t)64 * k * p.Dh + at.i0);
         b.a1 = b.a0 + (int64_t)64 * p.Dh;
-        b.b0 = (const char*)(p.dz + term * p.dz_term + (int64_t)64 * k * p.ldz + at.j0);
+        b.b0 = (const char*)((F16 ? p.sc.e : p.dz) + term * p.dz_term + (int64_t)64 * k * p.ldz + at.j0);
         b.b1 = b.b0 + (int64_t)64 * p.ldz;
     }
     __device__ __forceinline__ void store(const Loop& loop, const At& tile) const {
@@ -825,10 +996,7 @@ struct LmbWeight {
             const int j = tile.j0 + (wh * THW + c) * 32 + n, v = p.v0 + j;
             const bool live = j < p.n;                                  // (the same for lane and lane + 32)
             int scale = 0;
-            if (F16 && all > 0 && live) {
-                const int e = p.sc.w_f[v];
-                scale = p.sc.out[1] - 14 - (e == LMB_NONE ? p.sc.out[0] : e);
-            }
+            if (F16 && all > 0 && live) scale = p.sc.out[1] - 27 - 16 * (p.sc.col[v] & 7);
 #pragma unroll
             for (int a = 0; a < TVW; ++a)
 #pragma unroll
@@ -926,7 +1094,7 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 #pragma unroll 4
         for (int s = 0; s < p.splits * p.terms_h; ++s) x += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)s * p.M + r) * p.Dh + c);
         if (p.f16) {
-            const int scale = p.sc.out[1] - 14 - p.sc.up[r];
+            const int scale = p.sc.out[0] - 14 - p.sc.hs[r];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], scale);
         }
@@ -1005,7 +1173,7 @@ static int lmb_shape(int64_t i, int64_t j, bool wide) {
 struct LmbPlan {
     int padded, terms_h, terms_w, terms, f16, chunk, splits;
     int dz, hidden, weight;        // shapes
-    size_t rows_at, h_at, tail_at, dz_at, part_at, h16_at, w16_at, ints_at, counters_at, bytes;
+    size_t rows_at, h_at, tail_at, dz_at, e_at, panel_at, part_at, h16_at, w16_at, ints_at, counters_at, bytes;
 };
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -1018,7 +1186,8 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     p.terms_w = p.f16 ? 1 : wide_w ? 3 : 2;
     p.terms = p.f16 ? 1 : wide ? 3 : 2;
     const int64_t whole = ((int64_t)a->V + 255) & ~(int64_t)255;
-    int64_t most = (int64_t)(LMB_DZ_BYTES / ((size_t)p.padded * 2 * p.terms)) & ~(int64_t)255;
+    const int held = p.f16 && a->d_hidden && a->d_w ? 2 : p.terms;        // arrays of dz
+    int64_t most = (int64_t)(LMB_DZ_BYTES / ((size_t)p.padded * 2 * held)) & ~(int64_t)255;
     if (most < 256) most = 256;
     if (g_lmb_columns > 0 && most > g_lmb_columns) most = g_lmb_columns;
     p.chunk = (int)(whole < most ? whole : most);
@@ -1055,12 +1224,16 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     p.rows_at = take((size_t)p.padded * sizeof(LmbRow));
     p.h_at = take((size_t)p.padded * a->Dh * 2);
     p.tail_at = take((size_t)64 * a->Dh * 2);
-    p.dz_at = take((size_t)p.terms * p.padded * p.chunk * 2);
+    if (!p.f16 || a->d_hidden) p.dz_at = take((size_t)p.terms * p.padded * p.chunk * 2);
     if (a->d_hidden) p.part_at = take((size_t)p.splits * p.terms_h * a->M * a->Dh * 4);
     if (p.f16) {
         p.h16_at = take((size_t)p.padded * a->Dh * 2);
-        p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
-        p.ints_at = take(((size_t)3 * p.padded + whole + LMB_STATS * 34 + 2) * 4);
+        if (a->d_hidden) p.w16_at = take((size_t)(a->V & ~63) * a->Dh * 2);
+        if (a->d_w) {
+            p.e_at = take((size_t)p.padded * p.chunk * 2);
+            p.panel_at = take((size_t)(p.padded / 32) * p.chunk);
+        }
+        p.ints_at = take(((size_t)4 * p.padded + 2 * whole + LMB_STATS * 34 + 2) * 4);
     }
     p.bytes = at;
     return p;
@@ -1183,15 +1356,19 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         int* ints = (int*)(ws + plan.ints_at);
         p.sc.row_e = ints;
         p.sc.row_c = ints + plan.padded;
-        p.sc.up = ints + 2 * (int64_t)plan.padded;
-        p.sc.w_f = ints + 3 * (int64_t)plan.padded;
-        p.sc.row_max = p.sc.w_f + ((int64_t)a->V + 255) / 256 * 256;
+        p.sc.hs = ints + 2 * (int64_t)plan.padded;
+        p.sc.ws = ints + 3 * (int64_t)plan.padded;
+        p.sc.w_f = ints + 4 * (int64_t)plan.padded;
+        p.sc.col = p.sc.w_f + ((int64_t)a->V + 255) / 256 * 256;
+        p.sc.row_max = p.sc.col + ((int64_t)a->V + 255) / 256 * 256;
         p.sc.w_some = p.sc.row_max + LMB_STATS;
         p.sc.w_max = p.sc.w_some + LMB_STATS;
         p.sc.out = p.sc.w_max + LMB_STATS * 32;
         p.sc.h16 = (uint16_t*)(ws + plan.h16_at);
         p.sc.w16 = (uint16_t*)(ws + plan.w16_at);
         p.sc.tail16 = p.w_tail;
+        p.sc.e = (uint16_t*)(ws + plan.e_at);
+        p.sc.panel = (uint8_t*)(ws + plan.panel_at);
     }
     p.last_f = (int)(((int64_t)a->V + 255) / 256 * 256) - 4;
     p.counters = (int*)(ws + plan.counters_at);
@@ -1208,7 +1385,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
             hipLaunchKernelGGL(lmb_stat_kernel, dim3(LMB_STATS), dim3(256), 0, st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_stat_kernel launch")) != DLM_OK) return rc;
         }
-        const int more = plan.f16 ? LMB_STATS * 8 : a->V % 64 ? 64 : 0;
+        const int more = !plan.f16 ? (a->V % 64 ? 64 : 0) : a->d_hidden ? LMB_STATS * 8 : 0;        // (W's copy is d_hidden's)
         hipLaunchKernelGGL(lmb_gather_kernel, dim3(plan.padded + more), dim3(256), 0, st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_gather_kernel launch")) != DLM_OK) return rc;
         if (plan.f16) {
@@ -1232,6 +1409,11 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
             p.queued = n1 > wgs && a->Dh >= 128;
             launch_dz(plan, dim3((unsigned)(p.queued ? wgs : n1)), st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
+            const int panel = plan.dz == LMB_256 ? 128 : plan.dz == LMB_128 ? 64 : 32, panels = (plan.padded + panel - 1) / panel;
+            if (plan.f16 && a->d_w && panels > 1) {
+                hipLaunchKernelGGL(lmb_even_kernel, dim3((unsigned)((p.n + 511) / 512), panels), dim3(256), 0, st, p, panel);
+                if ((rc = check_hip(hipGetLastError(), "lmb_even_kernel launch")) != DLM_OK) return rc;
+            }
         }
         if (p.n2 + n3 == 0) continue;
         const int wgs = device_wgs(LMB_TILES[plan.weight].a_cu);
