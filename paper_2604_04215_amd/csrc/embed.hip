@@ -278,7 +278,8 @@ struct EmbedGradParams {
     void* table;
     int64_t table_st;
     int accumulate;
-    int chunk, groups;             // sorted entries a wavefront takes, workgroups of a slice of columns
+    int chunk, slices;             // sorted entries a wavefront takes, slices of columns
+    int group0;                    // the launch's first group
     float* part;                   // [groups][2][Dh]: the sum of a token that began in an earlier group; of one that goes on in the next
 };
 
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(GROUP * WAVE) void embed_grad_kernel(EmbedGradParam
     __shared__ f32x4 lds[GROUP][2][Q][WAVE];       // [0]: of a token that began in an earlier chunk, [1]: of one that goes on in the next
     __shared__ int ends[GROUP + 1][2];             // every chunk's first and last token; the one behind the group
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
-    const int slices = gridDim.x / p.groups, group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
+    const int nth = blockIdx.x / p.slices, slice = blockIdx.x - nth * p.slices, group = p.group0 + nth;
     const int c0 = (slice * WAVE + lane) * E, c = c0 < p.Dh ? c0 : 0;          // (lanes behind the row read its beginning, and store nothing)
     const bool live = c0 < p.Dh;
     const int64_t first = (int64_t)group * GROUP * p.chunk, i0 = first + (int64_t)wave * p.chunk;
@@ -557,22 +558,26 @@ extern "C" int dlm_embed_bwd(const dlm_embed_bwd_args* a, void* stream) {
         from = to;
         len *= MERGE;
     }
-    const EmbedGradParams p = {a->T, a->V, a->Dh, list[from], list[from + 1], a->d_out, a->d_out_stride, a->scale, a->d_table, a->d_table_stride,
-                               a->accumulate, plan.chunk, plan.groups, (float*)(ws + plan.part_at)};
     const bool in32 = a->d_out_type == DLM_ROW_F32, out32 = a->d_table_type == DLM_ROW_F32;
     const int per = in32 ? 256 : 512;
-    const dim3 grid((unsigned)((int64_t)plan.groups * ((a->Dh + per - 1) / per))), threads(GROUP * WAVE);
+    EmbedGradParams p = {a->T, a->V, a->Dh, list[from], list[from + 1], a->d_out, a->d_out_stride, a->scale, a->d_table, a->d_table_stride,
+                         a->accumulate, plan.chunk, (a->Dh + per - 1) / per, 0, (float*)(ws + plan.part_at)};
+    const dim3 threads(GROUP * WAVE);
+    const int most_groups = (1 << 21) / p.slices;    // of a launch: its threads stay below 2^32
 #define EMBED_GRAD(IN, OUT)                                                                                \
     {                                                                                                    \
         if (a->accumulate) hipLaunchKernelGGL((embed_grad_kernel<IN, OUT, true>), grid, threads, 0, st, p); \
         else hipLaunchKernelGGL((embed_grad_kernel<IN, OUT, false>), grid, threads, 0, st, p);           \
     }
-    if (in32 && out32) EMBED_GRAD(true, true)
-    else if (in32) EMBED_GRAD(true, false)
-    else if (out32) EMBED_GRAD(false, true)
-    else EMBED_GRAD(false, false)
+    for (; p.group0 < plan.groups; p.group0 += most_groups) {
+        const dim3 grid((unsigned)((plan.groups - p.group0 < most_groups ? plan.groups - p.group0 : most_groups) * p.slices));
+        if (in32 && out32) EMBED_GRAD(true, true)
+        else if (in32) EMBED_GRAD(true, false)
+        else if (out32) EMBED_GRAD(false, true)
+        else EMBED_GRAD(false, false)
+        if ((rc = check_hip(hipGetLastError(), "embed_grad_kernel launch")) != DLM_OK) return rc;
+    }
 #undef EMBED_GRAD
-    if ((rc = check_hip(hipGetLastError(), "embed_grad_kernel launch")) != DLM_OK) return rc;
     if (plan.groups < 2) return DLM_OK;
     const dim3 join(plan.groups - 1, (a->Dh + 255) / 256);
     if (out32) hipLaunchKernelGGL((embed_join_kernel<true>), join, dim3(WAVE), 0, st, p);
