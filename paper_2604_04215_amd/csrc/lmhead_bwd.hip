@@ -81,7 +81,7 @@ struct LmbParams {
     uint16_t* w_tail;              // [64][Dh]: the last V % 64 rows of W, zeros behind them
     int f16;                       // dz is fp16 and scaled
     LmbScale sc;
-    int last_f;                    // the last four of w_f
+    int last_f;                    // the last four of w_f and col
     uint16_t* dz;                  // [terms][M rounded up to 64][ldz]; fp16: D
     int64_t dz_term;               // entries of a term
     int ldz;
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256) void lmb_gather_kernel(LmbParams p) {
             int most = LMB_NONE;
             const int some = lmb_most(p.sc.w_some, LMB_STATS), least = some == LMB_NONE ? LMB_NONE : some + 8;
             const int padded = (p.V + 63) & ~63, whole = p.V & ~63, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            if (r == bound && padded + (int)threadIdx.x < p.last_f + 4) p.sc.w_f[padded + threadIdx.x] = least;      // (columns of the last tiles that no product takes)
             for (int v = (r - bound) * 4 + wave; v < padded; v += LMB_STATS * 8 * 4) {
                 uint16_t* dst = v < whole ? p.sc.w16 + (int64_t)v * p.Dh : p.sc.tail16 + (int64_t)(v - whole) * p.Dh;
                 const uint16_t* src = p.w + min(v, p.V - 1) * p.w_stride;
