@@ -737,7 +737,7 @@ size_t dlm_lmhead_bwd_workspace_bytes(const dlm_lmhead_bwd_args *args);
 
 /* dlm_set_option -- process-wide tuning / test knobs (not thread-safe against running calls).  These integers are the
  * ONLY mutable state the library keeps between calls (besides the per-device address of the built-in scratch of
- * dlm_lmhead_confidence_static); every default is the planner's choice, and every setting computes the same function.
+ * dlm_lmhead_confidence_static and each device's number of CUs, which is asked for once); every default is the planner's choice, and every setting computes the same function.
  *   "attn_variant"  0 = pick the attention kernel shape from the problem shape (default);
  *                   1 = 32-row workgroups whose wavefronts split the keys (needs g*Lq <= 32, otherwise falls back to 2),
  *                       sized for one workgroup per CU; 12 = the same sized for two (chosen for g*Lq <= 32, see 10);

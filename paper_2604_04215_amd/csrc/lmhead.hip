@@ -16,6 +16,7 @@
 //     a second kernel merges the V/TV partials per row in a fixed order
 //     (deterministic; ties resolve to the lowest vocabulary index).
 #include "common.hpp"
+#include "device.hpp"
 
 namespace dlm {
 
@@ -1599,17 +1600,6 @@ static int plan_capacity(int M) {
     for (int c : caps)
         if (M <= c) return c;
     return 0x7fffffff;
-}
-
-static int device_cus() {
-    static int cus[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-    if (cus[dev] == 0) {
-        int n = 0;
-        cus[dev] = (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0) ? n : 256;
-    }
-    return cus[dev];
 }
 
 // Workgroups of a launch that takes its tiles from a queue: one per CU, the same number on every XCD.

@@ -20,6 +20,7 @@
 //
 // Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 11.2 ms, 1.2 PFLOP/s (W's copy 0.42, dz 3.74 at 1.19, the gradients 6.8 at 1.31); 512 rows, V = 126464,
 // Dh = 4096 1.95 ms (0.37, 0.50, 1.05); 64 rows 0.80, 4 rows 0.76, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
+#include "device.hpp"
 #include "rows.hpp"
 
 namespace dlm {
@@ -1146,14 +1147,8 @@ int lmb_set_columns(int v) {
 // Workgroups that fit the chip, a multiple of 8
 static int device_wgs(int a_cu) {
     if (g_lmb_workgroups > 0) return g_lmb_workgroups;
-    static int cus[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256 * a_cu;
-    if (cus[dev] == 0) {
-        int n = 0;
-        cus[dev] = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n >= 8 ? n & ~7 : 256;
-    }
-    return cus[dev] * a_cu;
+    const int cus = device_cus();
+    return (cus >= 8 ? cus & ~7 : 8) * a_cu;
 }
 
 // A shape: its tiles, and the workgroups of it that a CU holds
