@@ -115,4 +115,23 @@ __device__ __forceinline__ int lane_id() { return threadIdx.x & (WAVE - 1); }
 template <typename T>
 __device__ __forceinline__ T shfl_xor(T v, int m) { return __shfl_xor(v, m, WAVE); }
 
+// sum over each group of LANES neighbouring lanes of a wavefront (a power of two); every lane of the group gets the same bits
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    static_assert(LANES == 4 || LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "a power of two, 4 .. 64");
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));                          // lane ^ 1
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));                          // lane ^ 2
+    if (LANES >= 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));         // 7 - lane of 8: the other four
+    if (LANES >= 16) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, true));        // 15 - lane of 16
+    if (LANES >= 32) {
+        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    }
+    if (LANES >= 64) {
+        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    }
+    return v;
+}
+
 }  // namespace dlm

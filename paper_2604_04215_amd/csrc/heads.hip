@@ -134,16 +134,6 @@ __device__ __forceinline__ u32x2 pack8_e4m3(const float (&f)[8], float inv_scale
     return v;
 }
 
-// sum over the D/16 lanes of a head; every lane gets the same bits
-template <int D>
-__device__ __forceinline__ float head_sum(float v) {
-    static_assert(D == 64 || D == 128, "4 or 8 lanes a head");
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));                    // lane ^ 1
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));                    // lane ^ 2
-    if (D == 128) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));     // 7 - lane of 8: the other four
-    return v;
-}
-
 // the 8 cosines and sines of a lane
 struct Angles {
     float c[8], s[8];
@@ -238,7 +228,7 @@ __global__ __launch_bounds__(256) void head_map_kernel(HeadParams p) {
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = fmaf(a[e], a[e], fmaf(b[e], b[e], sum));
-        const float r = __builtin_amdgcn_rsqf(head_sum<D>(sum) * (1.0f / D) + p.eps);
+        const float r = __builtin_amdgcn_rsqf(lanes_sum<D / 16>(sum) * (1.0f / D) + p.eps);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             a[e] *= r * wa[e];
@@ -339,7 +329,7 @@ __global__ __launch_bounds__(256) void head_map_grad_kernel(GradParams p) {
             unpack8(xb, nb);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fmaf(na[e], na[e], fmaf(nb[e], nb[e], sum));
-            const float r = __builtin_amdgcn_rsqf(head_sum<D>(sum) * (1.0f / D) + p.eps);
+            const float r = __builtin_amdgcn_rsqf(lanes_sum<D / 16>(sum) * (1.0f / D) + p.eps);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 a[e] *= r;
@@ -350,7 +340,7 @@ __global__ __launch_bounds__(256) void head_map_grad_kernel(GradParams p) {
                 b[e] *= wb[e];
                 dot = fmaf(a[e], na[e], fmaf(b[e], nb[e], dot));
             }
-            const float c = -(r * r) * (head_sum<D>(dot) * (1.0f / D));
+            const float c = -(r * r) * (lanes_sum<D / 16>(dot) * (1.0f / D));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 a[e] = fmaf(na[e], c, a[e]);
@@ -407,7 +397,7 @@ __global__ __launch_bounds__(1024) void head_grad_sum_kernel(GradSumParams p) {
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        v[e] = head_sum<128>(v[e]);                       // 8 lanes
+        v[e] = lanes_sum<128 / 16>(v[e]);                       // 8 lanes
         v[e] = over_heads<128>(v[e]);                     // and the eight eights
     }
     if (lane_id() == 0) s[threadIdx.x >> 6] = v;

@@ -279,12 +279,11 @@ __global__ __launch_bounds__(512) void lmb_scale_kernel(LmbParams p) {
 __device__ __forceinline__ void lmb_tile(int t, int ni, int nj, int gi, int gj, int& i, int& j) {
     const int band = t / (gi * nj), bi = min(gi, ni - band * gi);
     int r = t - band * gi * nj;
-    const int col = r / (bi * gj), bj = min(gj, nj - col * gj);
+    const int col = r / (bi * gj);
     r -= col * bi * gj;
     j = r / bi;
     i = band * gi + r - j * bi;
     j += col * gj;
-    (void)bj;
 }
 // Workgroups go round the 8 XCDs: each XCD has a stretch of the tile numbers.  With a counter a workgroup takes one tile after the other, in order;
 // `ahead` is the one behind the tile at hand, whose operands are requested before that one is done.

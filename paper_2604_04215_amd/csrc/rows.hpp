@@ -9,9 +9,6 @@ template <bool F32>
 struct Piece {
     static constexpr int E = F32 ? 4 : 8;
     using Raw = u32x4;
-    static __device__ __forceinline__ Raw load(const void* base, int64_t entry) {
-        return *reinterpret_cast<const u32x4*>((const char*)base + entry * (F32 ? 4 : 2));
-    }
     // past the caches: nothing reads it again soon
     static __device__ __forceinline__ Raw stream(const void* base, int64_t entry) {
         return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((const char*)base + entry * (F32 ? 4 : 2)));
@@ -51,25 +48,6 @@ __device__ __forceinline__ void load_bf16(const uint16_t* p, float (&f)[E]) {
             f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
         }
     }
-}
-
-// sum over each group of LANES neighbouring lanes of a wavefront (a power of two); every lane of the group gets the same bits
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-    static_assert(LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "a power of two, 8 .. 64");
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));                          // lane ^ 1
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));                          // lane ^ 2
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));                         // 7 - lane of 8
-    if (LANES >= 16) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, true));        // 15 - lane of 16
-    if (LANES >= 32) {
-        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
-    }
-    if (LANES >= 64) {
-        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
-    }
-    return v;
 }
 
 // Checks of rows [n, D] (host): `written`: they are outputs.  `bytes` an entry.
