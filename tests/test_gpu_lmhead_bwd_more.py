@@ -35,3 +35,128 @@ def test_what_is_put_into_the_workspace_does_not_depend_on_what_it_held(M, V, dt
         held.append(ws[2048:])                           # (behind the counters of the tile lists, which end as workgroups come)
     untouched = (held[0] == 0xaa) & (held[1] == 0x55)
     assert ((held[0] == held[1]) | untouched).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,Dh,V", [(300, 1024, 20000), (60, 512, 30000)])
+def test_two_calls_at_once(M, Dh, V, dtype):
+    """On two streams, neither of which waits for the other: each has its own workspace."""
+    h, w, lse, how = drawn(M, Dh, V, dtype)
+    size = dlm.lmhead_bwd_workspace_bytes(h, w, lse, **how)
+    runs = [dict(how, d_hidden=torch.zeros_like(how["d_hidden"]), d_w=torch.zeros_like(how["d_w"]), workspace=torch.empty(size, dtype=U8, device=DEV)) for _ in range(3)]
+    dlm.lmhead_bwd(h, w, lse, **runs[2])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for s, run in zip(streams, runs):
+            dlm.lmhead_bwd(h, w, lse, stream=s, **run)
+    torch.cuda.synchronize()
+    for run in runs[:2]:
+        assert torch.equal(run["d_hidden"], runs[2]["d_hidden"]) and torch.equal(run["d_w"], runs[2]["d_w"])
+
+
+# ---- fp32 gradients: sums in two floats, dz of 24 bits ---------------------------------------------------------
+# Inputs on which the arithmetic shows: a sum of numbers near one to which, in a later block of the sum, 2^20 and then -2^20 are added.  Added up in one float it
+# is rounded to a multiple of 2^-3 (up to 2^-4 off); with each block (128 products of a logit, 256 of a gradient) added to two floats, 2^20 - 2^20 is zero before it meets the rest.
+BIG = 2.0 ** 20
+U = 2.0 ** -24
+
+
+def one_float(products):
+    """The sum in one float, first to last."""
+    x = np.float32(0)
+    for p in products.astype(np.float32):
+        x = np.float32(x + p)
+    return float(x)
+
+
+def grads(h, w, lse, d_hidden=None, d_w=None, **how):
+    put = lambda x, t: torch.from_numpy(np.ascontiguousarray(x)).to(t).to(DEV)
+    h, w, lse = put(h, BF16), put(w, BF16), put(lse, F32)
+    how = {k: put(v, I32 if k == "target" else F32) for k, v in how.items()}
+    out = [torch.full(t.shape, float("nan"), dtype=F32, device=DEV) if on else None for t, on in ((h, d_hidden), (w, d_w))]
+    ws = torch.empty(dlm.lmhead_bwd_workspace_bytes(h, w, lse, d_hidden=out[0], d_w=out[1], **how), dtype=U8, device=DEV)
+    dlm.lmhead_bwd(h, w, lse, d_hidden=out[0], d_w=out[1], workspace=ws, **how)
+    return [None if t is None else wide(t) for t in out]
+
+
+def rounded(x):
+    return wide(torch.from_numpy(x).to(BF16))
+
+
+@pytest.mark.parametrize("M,V", [(3, 70), (200, 11000)])
+def test_logits_of_fp32_gradients_are_sums_in_two_floats(M, V):
+    """dz is all of d_w where the hidden row is one in a column of its own; a logit's sum of 128 products is off by at most s(128) of their sizes, 2^-24 2 (16 + 8)."""
+    rng = np.random.default_rng(M)
+    h, w = np.zeros((M, 256)), np.zeros((V, 256))
+    h[:, :128], w[:, :128] = rounded(rng.standard_normal((M, 128)) * 0.3), rounded(rng.standard_normal((V, 128)) * 0.3)
+    h[:, [128, 200]], w[:, 128], w[:, 200] = 2.0 ** 10, 2.0 ** 10, -2.0 ** 10
+    z, size = h[:, :128] @ w[:, :128].T, np.abs(h[:, :128]) @ np.abs(w[:, :128]).T
+    lse = np.float32(np.log(np.exp(z).sum(1)))
+    _, d_w = grads(h, w, lse, d_w=True, d_lse=np.eye(M)[0])
+    p = np.exp(z[0] - lse[0].astype(np.float64))
+    # 2^10 p: three terms of bf16 keep all of p, one product is exact
+    err = np.abs(d_w[:, 128] / 2.0 ** 10 / p - 1)
+    bound = np.expm1(48 * U * size[0] + 4 * U * (np.abs(z[0]) + abs(lse[0]))) + 16 * U
+    assert (err <= bound).all(), (err / bound).max()
+    # one float would be far off
+    plain = np.array([one_float(h[0] * w[v]) for v in range(20)])
+    assert (np.abs(plain - z[0][:20]) > 100 * bound[:20]).mean() > 0.5
+
+
+def test_large_logits_of_fp32_gradients_keep_what_a_float_cannot_hold():
+    """Logits of 4096 + delta, where a float has steps of 2^-11 and delta is less: the difference from lse is formed of both floats."""
+    V = 200
+    h, w = np.zeros((1, 256)), np.zeros((V, 256))
+    h[0, :64], w[:, :64], h[0, 128], w[:, 128] = 8.0, 8.0, 2.0 ** -6, np.arange(V) * 2.0 ** -13
+    delta = np.arange(V) * 2.0 ** -19
+    _, d_w = grads(h, w, np.float32([4097.0]), d_w=True, d_lse=np.ones(1))
+    want = np.exp(delta - 1)
+    # the exponent's product by log2(e), the exponential: a few roundings
+    assert (np.abs(d_w[:, 0] / 8 / want - 1) <= 16 * U).all(), np.abs(d_w[:, 0] / 8 / want - 1).max() / U
+    assert (np.float32(4096 + delta) == 4096).mean() > 0.5 and np.abs(np.exp(-delta) - 1).max() > 1000 * U
+
+
+@pytest.mark.parametrize("Dh", [128, 5120])
+def test_fp32_gradients_of_hidden_rows_are_sums_in_two_floats(Dh):
+    """Hidden rows of zeros: all probabilities of a row are exp(-lse)."""
+    rng = np.random.default_rng(Dh)
+    w = np.zeros((448, Dh))
+    w[:256] = rounded(rng.standard_normal((256, Dh)))
+    w[300], w[400] = BIG, -BIG
+    lse = np.float32(np.log(2.0) * np.array([0, 1, 3, 0.5, 2]))
+    d_h, _ = grads(np.zeros((5, Dh)), w, lse, d_hidden=True, d_lse=np.ones(5))
+    p, total, size = np.exp(-lse.astype(np.float64))[:, None], w[:256].sum(0), np.abs(w[:256]).sum(0)
+    # probabilities 8 u, blocks of 256 products s(256) = 2 u (16 + 16) of their sizes, three terms joined
+    bound = p * (np.abs(total) * 8 * U + 64 * U * size + 4 * U * np.abs(total))
+    assert (np.abs(d_h - p * total) <= bound).all(), (np.abs(d_h - p * total) / bound).max()
+    plain = np.array([one_float(w[:, i]) for i in range(20)])
+    assert (np.abs(plain - total[:20]) > 10 * bound[0, :20]).mean() > 0.5
+
+
+@pytest.mark.parametrize("Dh", [128, 5120])
+def test_fp32_gradients_of_w_are_sums_in_two_floats(Dh):
+    rng = np.random.default_rng(Dh + 1)
+    h, g = np.zeros((448, Dh)), np.zeros(448)
+    h[:256], g[:256] = rounded(rng.standard_normal((256, Dh))), np.float32(rng.standard_normal(256))
+    h[[300, 400]], g[300], g[400] = 2.0 ** 10, 2.0 ** 10, -2.0 ** 10
+    _, d_w = grads(h, np.zeros((448, Dh)), np.zeros(448), d_w=True, d_ztarget=g, target=np.full(448, 7))
+    total, size = g[:256] @ h[:256], np.abs(g[:256]) @ np.abs(h[:256])
+    # blocks of 256 products of three terms: s(256) of their sizes, and the result's own rounding
+    bound = 64 * U * size * 1.01 + U * np.abs(total)
+    assert (np.abs(d_w[7] - total) <= bound).all(), (np.abs(d_w[7] - total) / bound).max()
+    assert (np.delete(d_w, 7, 0) == 0).all()
+    plain = np.array([one_float(g * h[:, i]) for i in range(20)])
+    assert (np.abs(plain - total[:20]) > 10 * bound[:20]).mean() > 0.5
+
+
+@pytest.mark.parametrize("M,Dh,V", [(3, 64, 70), (300, 128, 500), (130, 5120, 400)])
+def test_fp32_gradients_keep_24_bits_of_dz(M, Dh, V):
+    """One target a row, entries of one: both gradients are dz itself, to the last bit."""
+    rng = np.random.default_rng(M)
+    g = np.float32(1 + rng.integers(0, 2 ** 23, M) * 2.0 ** -23) * np.float32(2.0) ** rng.integers(-20, 20, M).astype(np.float32)
+    d_h, d_w = grads(np.ones((M, Dh)), np.ones((V, Dh)), np.zeros(M), d_hidden=True, d_w=True, d_ztarget=g, target=np.arange(M))
+    assert np.array_equal(d_h, np.repeat(g[:, None].astype(np.float64), Dh, 1)) and np.array_equal(d_w[:M], d_h) and (d_w[M:] == 0).all()
+    sixteen = lambda x: rounded(x) + rounded(x - rounded(x))        # two terms
+    assert (sixteen(g.astype(np.float64)) != g).mean() > 0.9
