@@ -358,7 +358,7 @@ struct LmbShape {
 using Lmb256 = LmbShape<2, 2, 4, 4>;       // 256 x 256, one workgroup a CU
 using Lmb256x128 = LmbShape<4, 1, 2, 4>;   // one
 using Lmb256x64 = LmbShape<4, 1, 2, 2>;    // one
-using Lmb128 = LmbShape<2, 2, 2, 2>;       // 128 x 128, two
+using Lmb128 = LmbShape<2, 2, 2, 2>;       // 128 x 128, two, one with sums in two floats (371 registers)
 using Lmb64 = LmbShape<2, 2, 1, 1>;        // 64 x 64, four
 
 // The shape of a workgroup: WV x WH wavefronts of TVW x THW tiles of 32 x 32.
@@ -1143,19 +1143,19 @@ int lmb_set_columns(int v) {
     return DLM_OK;
 }
 
+// A shape: its tiles, and the workgroups of it that a CU holds, of the kernels for bf16 gradients and of those for fp32.  Planned for two of 128 x 128 a CU, fp32
+// gradients of 500 rows, V = 50000, Dh = 1536 take 1424 us, for one 1126; 64 rows of 32000 x 4096 498 and 421; 1000 rows 3525 either way.
+struct LmbTile {
+    int i, j, a_cu, a_cu_wide;
+};
+constexpr LmbTile LMB_TILES[] = {{256, 256, 1, 1}, {256, 128, 1, 1}, {256, 64, 1, 1}, {128, 128, 2, 1}, {64, 64, 4, 4}};
+enum { LMB_256, LMB_256x128, LMB_256x64, LMB_128, LMB_64 };
 // Workgroups that fit the chip, a multiple of 8
-static int device_wgs(int a_cu) {
+static int device_wgs(const LmbTile& tile, bool wide) {
     if (g_lmb_workgroups > 0) return g_lmb_workgroups;
     const int cus = device_cus();
-    return (cus >= 8 ? cus & ~7 : 8) * a_cu;
+    return (cus >= 8 ? cus & ~7 : 8) * (wide ? tile.a_cu_wide : tile.a_cu);
 }
-
-// A shape: its tiles, and the workgroups of it that a CU holds
-struct LmbTile {
-    int i, j, a_cu;
-};
-constexpr LmbTile LMB_TILES[] = {{256, 256, 1}, {256, 128, 1}, {256, 64, 1}, {128, 128, 2}, {64, 64, 4}};
-enum { LMB_256, LMB_256x128, LMB_256x64, LMB_128, LMB_64 };
 static int64_t lmb_tiles(int shape, int64_t i, int64_t j) {
     return ((i + LMB_TILES[shape].i - 1) / LMB_TILES[shape].i) * ((j + LMB_TILES[shape].j - 1) / LMB_TILES[shape].j);
 }
@@ -1195,7 +1195,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     // Parts of d_hidden's sum.  In times of a pair of stages (1.8 us of a 256 x 256 tile): the launch takes what all its tiles take together, but no
     // less than d_hidden's rounds of tiles; a part costs its rows written and read again.
     const LmbTile th = LMB_TILES[p.hidden], tw = LMB_TILES[p.weight];
-    const int64_t tiles = lmb_tiles(p.hidden, a->Dh, rows), pairs = (columns + 63) / 64, a_cu = th.a_cu, wgs = 256 * a_cu;
+    const int64_t tiles = lmb_tiles(p.hidden, a->Dh, rows), pairs = (columns + 63) / 64, a_cu = wide ? th.a_cu_wide : th.a_cu, wgs = 256 * a_cu;
     const double unit_h = th.i * th.j / 65536.0, unit_w = tw.i * tw.j / 65536.0;
     const double rest = a->d_w ? lmb_tiles(p.weight, a->Dh, columns) * unit_w * (p.padded / 64) * p.terms_w : 0.0;
     const double part = (double)a->M * p.terms_h * a->Dh * 8e-7;
@@ -1400,7 +1400,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
         p.n2 = hidden ? (int)up8(lmb_tiles(plan.hidden, a->Dh, (int64_t)plan.padded * p.terms_h) * p.splits) : 0;
         // A list of tiles where they are more than the workgroups that fit the chip, and long enough to request the next one behind (see LmbLoop)
         if (a->M > 0) {
-            const int wgs = device_wgs(LMB_TILES[plan.dz].a_cu);
+            const int wgs = device_wgs(LMB_TILES[plan.dz], plan.terms == 3);
             p.queued = n1 > wgs && a->Dh >= 128;
             launch_dz(plan, dim3((unsigned)(p.queued ? wgs : n1)), st, p);
             if ((rc = check_hip(hipGetLastError(), "lmb_dz_kernel launch")) != DLM_OK) return rc;
@@ -1411,7 +1411,7 @@ extern "C" int dlm_lmhead_bwd(const dlm_lmhead_bwd_args* a, void* stream) {
             }
         }
         if (p.n2 + n3 == 0) continue;
-        const int wgs = device_wgs(LMB_TILES[plan.weight].a_cu);
+        const int wgs = device_wgs(LMB_TILES[plan.weight], plan.terms == 3);
         p.queued = a->M > 0 && p.n2 + n3 > wgs && (!hidden || pairs >= 2 * p.splits);
         launch_grad(plan, dim3((unsigned)(p.queued ? wgs : p.n2 + n3)), st, p);
         if ((rc = check_hip(hipGetLastError(), "lmb_grad_kernel launch")) != DLM_OK) return rc;
