@@ -702,7 +702,8 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  *   for d_hidden an entry is besides up to 2^-38 of its row's (|d_lse| + |d_ztarget|) inv_temperature off (more where a few rows of w are over 2^8 larger than most: as
  *   many times more as they are beyond that), for d_w up to 2^-22 of the largest |dz| of its column, both times the largest entry of their hidden rows.  So every row of
  *   both gradients is right by its own size, of tokens that are unlikely in every row too.  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.
- * Where a gradient is fp32, dz keeps 24 bits, and all sums are added up in two floats: three to four times as long.
+ * Where a gradient is fp32, dz keeps 24 bits, and logits, d_w and each part of d_hidden are added up in two floats; the parts of d_hidden (up to 64 of the
+ *   vocabulary, times three terms, times the chunks that 2 GiB of dz make of it) are joined in fp32.
  * workspace: dlm_lmhead_bwd_workspace_bytes(args) bytes, 16-byte aligned; they depend on M, Dh, V, the types and which gradients are wanted.
  * Supported: Dh % 64 == 0, up to 65536; M up to 2^20; V up to 2^24; rows 16-byte aligned, strides multiples of 16 bytes, w_stride_row < 2^23.
  * ------------------------------------------------------------------------- */

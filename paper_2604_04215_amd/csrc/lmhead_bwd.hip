@@ -15,8 +15,8 @@
 //     but for powers of two (see LmbScale), which costs a pass over W: 3 % of the time of 4096 rows.  Each gradient has a dz of its own, scaled by the rows for
 //     d_hidden, by the columns for d_w: a token that is unlikely in every row has a small column of dz, of which all of its row of d_w is summed.
 //   bf16 gradients, few rows: two bf16 terms, 16 bits: twice the products where reading W takes longest, and no copy of it.
-//   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products added up in two floats (the logits too: an error of one is one of the
-//     probability).  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
+//   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products (of a logit 128: an error of one is one of the probability) added up in two floats; the
+//     parts of d_hidden's sum, and what its chunks of columns leave in them, are joined in one.  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
 //
 // Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 11.2 ms, 1.2 PFLOP/s (W's copy 0.42, dz 3.74 at 1.19, the gradients 6.8 at 1.31); 512 rows, V = 126464,
 // Dh = 4096 1.95 ms (0.37, 0.50, 1.05); 64 rows 0.80, 4 rows 0.76, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
