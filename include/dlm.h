@@ -701,7 +701,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 128 rows, above that 11, as an fp16 with a scale of its own for each gradient:
  *   for d_hidden an entry is besides up to 2^-38 of its row's (|d_lse| + |d_ztarget|) inv_temperature off (more where a few rows of w are over 2^8 larger than most: as
  *   many times more as they are beyond that), for d_w up to 2^-22 of the largest |dz| of its column, both times the largest entry of their hidden rows.  So every row of
- *   both gradients is right by its own size, of tokens that are unlikely in every row too.  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.
+ *   both gradients is right by its own size, of tokens that are unlikely in every row too (in d_w down to 2^-100 of the largest product of a hidden row and its gradient).  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.
  * Where a gradient is fp32, dz keeps 24 bits, and logits, d_w and each part of d_hidden are added up in two floats; the parts of d_hidden (up to 64 of the
  *   vocabulary, times three terms, times the chunks that 2 GiB of dz make of it) are joined in fp32.
  * workspace: dlm_lmhead_bwd_workspace_bytes(args) bytes, 16-byte aligned; they depend on M, Dh, V, the types and which gradients are wanted.

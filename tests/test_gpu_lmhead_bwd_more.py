@@ -56,6 +56,51 @@ def test_two_calls_at_once(M, Dh, V, dtype):
         assert torch.equal(run["d_hidden"], runs[2]["d_hidden"]) and torch.equal(run["d_w"], runs[2]["d_w"])
 
 
+@pytest.mark.parametrize("only", [None, "d_hidden", "d_w"])
+@pytest.mark.parametrize("columns", [0, 1024])
+def test_16_bit_gradients_of_many_rows_replayed_from_a_graph(columns, only):
+    """Other counts, probabilities and workspaces between the replays, with eager calls beside them: the columns' scales are found anew in every call."""
+    M, Dh, V = 700, 128, 2600
+    h, w, lse, how = drawn(M, Dh, V, BF16)
+    idx, count = torch.arange(M, dtype=I32, device=DEV).flip(0).contiguous(), torch.tensor([M], dtype=I32, device=DEV)
+    how = dict({k: how[k] for k in ("target", "d_ztarget", "d_lse")}, row_idx=idx, m_dev=count, out_scatter=True, forbid_token=7)
+    outs = [{k: t for k, t in (("d_hidden", torch.zeros_like(h)), ("d_w", torch.zeros_like(w))) if only in (None, k)} for _ in range(2)]
+    dlm.set_option("lmhead_bwd_columns", columns)
+    try:
+        ws = [torch.full((dlm.lmhead_bwd_workspace_bytes(h, w, lse, **how, **outs[0]),), 255, dtype=U8, device=DEV) for _ in range(2)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dlm.lmhead_bwd(h, w, lse, workspace=ws[1], **how, **outs[1])
+        given = lse.clone()
+        for live, up in ((700, 0.0), (700, 60.0), (129, 0.0), (0, 0.0), (1, 30.0), (512, 3.0), (700, 0.0)):
+            count.fill_(live)
+            lse.copy_(given + up * (torch.arange(M, device=DEV) % 3))        # probabilities of every size
+            for out, space in zip(outs, ws):
+                space.fill_(255)
+                for t in out.values():
+                    t.fill_(7.0)
+            graph.replay()
+            dlm.lmhead_bwd(h, w, lse, workspace=ws[0], **how, **outs[0])
+            torch.cuda.synchronize()
+            for k in outs[0]:
+                assert torch.equal(outs[0][k], outs[1][k]) and outs[0][k].isfinite().all(), (live, k)
+    finally:
+        dlm.set_option("lmhead_bwd_columns", 0)
+
+
+@pytest.mark.parametrize("M,V", [(200, 1), (200, 33), (129, 64), (1000, 257)])
+def test_16_bit_gradients_of_many_rows_added_up(M, V):
+    """accumulate: what is added is what is written without it, before its rounding: two roundings of bf16 (2^-8) instead of one."""
+    h, w, lse, how = drawn(M, 64, V, BF16)
+    base = torch.from_numpy(np.random.default_rng(V).standard_normal((V, 64))).to(BF16).to(DEV)
+    ws = torch.empty(dlm.lmhead_bwd_workspace_bytes(h, w, lse, **how), dtype=U8, device=DEV)
+    dlm.lmhead_bwd(h, w, lse, workspace=ws, **how)
+    alone, added = wide(how["d_w"]), base.clone()
+    dlm.lmhead_bwd(h, w, lse, workspace=ws, **dict(how, d_w=added), accumulate=True)
+    want = alone + wide(base)
+    assert (np.abs(wide(added) - want) <= 2.0 ** -8 * (np.abs(want) + np.abs(alone)) * 1.01 + 2.0 ** -24 * np.abs(wide(base))).all()
+
+
 # ---- fp32 gradients: sums in two floats, dz of 24 bits ---------------------------------------------------------
 # Inputs on which the arithmetic shows: a sum of numbers near one to which, in a later block of the sum, 2^20 and then -2^20 are added.  Added up in one float it
 # is rounded to a multiple of 2^-3 (up to 2^-4 off); with each block (128 products of a logit, 256 of a gradient) added to two floats, 2^20 - 2^20 is zero before it meets the rest.
