@@ -698,7 +698,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  * The logits are not stored.  No sum is formed by atomics: deterministic (the order of sums depends on the sizes, the types and which
  * gradients are wanted).  hidden and w have to be finite: other rows'
  * values are multiplied by dz that may be zero.  d_w overlaps neither w nor d_hidden; d_hidden may be hidden.
- * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 128 rows, above that 11, as an fp16 with a scale of its own for each gradient:
+ * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 256 rows and where M V Dh is at most 10^10, else 11, as an fp16 with a scale of its own for each gradient:
  *   for d_hidden an entry is besides up to 2^-38 of its row's (|d_lse| + |d_ztarget|) inv_temperature off (more where a few rows of w are over 2^8 larger than most: as
  *   many times more as they are beyond that), for d_w up to 2^-22 of the largest |dz| of its column, both times the largest entry of their hidden rows.  So every row of
  *   both gradients is right by its own size, of tokens that are unlikely in every row too (in d_w down to 2^-100 of the largest product of a hidden row and its gradient).  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.
@@ -786,6 +786,8 @@ size_t dlm_lmhead_bwd_workspace_bytes(const dlm_lmhead_bwd_args *args);
  *                   rows (of 8, 4, 8, 2 wavefronts; the workspace's size depends on it).
  *   "lmhead_bwd_columns" 0 = dlm_lmhead_bwd takes as many columns of the vocabulary at a time as fit 2 GiB of dz (default); n, a multiple of 256 =
  *                   at most n (the workspace's size depends on it).
+ *   "lmhead_bwd_few"  0 = dlm_lmhead_bwd chooses between two bf16 terms of dz and one fp16 by M, V and Dh (default); n = two terms up to n rows, one fp16 above
+ *                   (the workspace's size depends on it; so do the bits that dz keeps).
  *   "lmhead_bwd_workgroups" workgroups of the launches of dlm_lmhead_bwd that take their tiles from a list: 0 = as fit the device (default); n, a multiple of 8 =
  *                   n (tests: makes small calls take the list).
  * The knobs exist for tests and tuning sweeps. */

@@ -1235,6 +1235,7 @@ extern "C" int dlm_set_option(const char* name, int value) {
     if (!strcmp(name, "paged_shares")) return paged_set_shares(value);
     if (!strcmp(name, "paged_shape")) return paged_set_shape(value);
     if (!strcmp(name, "lmhead_bwd_columns")) return lmb_set_columns(value);
+    if (!strcmp(name, "lmhead_bwd_few")) return lmb_set_few(value);
     if (!strcmp(name, "lmhead_bwd_workgroups")) return lmb_set_workgroups(value);
     if (!strcmp(name, "attn_remap")) {
         if (value < 0 || value > 7) return fail(DLM_ERR_INVALID_ARG, "set_option: attn_remap must be 0..7");

@@ -30,6 +30,7 @@ int copy_set_unroll(int v);  // commit.hip
 int paged_set_shares(int v);  // paged_attn.hip
 int paged_set_shape(int v);  // paged_attn.hip
 int lmb_set_columns(int v);  // lmhead_bwd.hip
+int lmb_set_few(int v);      // lmhead_bwd.hip
 int lmb_set_workgroups(int v);  // lmhead_bwd.hip
 extern int g_attn_remap;     // attn.hip: bit 0 forward + dQ, bit 1 longest key range first, bit 2 dK / dV passes
 

@@ -1125,9 +1125,17 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 
 // ---- host ---------------------------------------------------------------------------------------------------
 constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more rows, fewer columns at a time
-// Up to so many rows two bf16 terms take less time than the pass over W that fp16 needs.  Both gradients, two terms against fp16, V = 126464, Dh = 4096:
-// 128 rows 1000 against 1380 us, 160 1415 against 1380, 192 1392 against 1374, 256 1531 against 1410; V = 32000, Dh = 2048: 192 rows 216 against 208, 256 246 against 226.
-constexpr int LMB_FEW = 128;
+// Two bf16 terms or one fp16: a product more for each gradient (2 M V Dh operations) against a pass over W and three launches of 20 us together.  Both gradients, us of two
+// terms / fp16: V = 126464, Dh = 4096 130 rows 1239 / 1335, 192 1305 / 1350, 256 1473 / 1414, 320 1952 / 1828, 512 2582 / 2057; 64000 x 2048 256 rows 420 / 444, 384 578 / 558;
+// 151000 x 896 256 rows 522 / 557, 384 715 / 707.  Small products do not pay for the launches at any number of rows: 8000 x 1024 512 rows 67 / 83, 700 99 / 102, 1000 115 / 111;
+// 40000 x 256 512 rows 122 / 170, 1000 236 / 252; 16000 x 1024 512 rows 112 / 124, 700 172 / 172.  Where they are alike two terms are: they keep 16 bits.
+constexpr int LMB_FEW = 256;
+constexpr double LMB_SMALL = 1e10;                    // M V Dh
+static int g_lmb_few = 0;                             // dlm_set_option: two terms up to so many rows and for none above (0: by the rule)
+static bool lmb_two_terms(int M, int V, int Dh) {
+    if (g_lmb_few > 0) return M <= g_lmb_few;
+    return M <= LMB_FEW || (double)M * V * Dh <= LMB_SMALL;
+}
 static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
 
 static int g_lmb_workgroups = 0;                      // dlm_set_option: workgroups of a launch that takes tiles from a list (0: as fit the chip)
@@ -1135,6 +1143,11 @@ static int g_lmb_workgroups = 0;                      // dlm_set_option: workgro
 int lmb_set_workgroups(int v) {
     if (v < 0 || v % 8) return fail(DLM_ERR_INVALID_ARG, "set_option: lmhead_bwd_workgroups must be a multiple of 8, or 0");
     g_lmb_workgroups = v;
+    return DLM_OK;
+}
+int lmb_set_few(int v) {
+    if (v < 0) return fail(DLM_ERR_INVALID_ARG, "set_option: lmhead_bwd_few must not be negative");
+    g_lmb_few = v;
     return DLM_OK;
 }
 int lmb_set_columns(int v) {
@@ -1176,7 +1189,7 @@ static LmbPlan plan_lmb(const dlm_lmhead_bwd_args* a) {
     LmbPlan p = {};
     p.padded = a->M > 0 ? (a->M + 63) & ~63 : 64;
     const bool wide_h = a->d_hidden && a->d_hidden_type == DLM_ROW_F32, wide_w = a->d_w && a->d_w_type == DLM_ROW_F32, wide = wide_h || wide_w;
-    p.f16 = !wide && a->M > LMB_FEW;
+    p.f16 = !wide && !lmb_two_terms(a->M, a->V, a->Dh);
     p.terms_h = p.f16 ? 1 : wide_h ? 3 : 2;
     p.terms_w = p.f16 ? 1 : wide_w ? 3 : 2;
     p.terms = p.f16 ? 1 : wide ? 3 : 2;
@@ -1244,7 +1257,8 @@ static void launch_dz(const LmbPlan& plan, dim3 grid, hipStream_t st, const LmbP
         else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 0, 0);
         else LMB_DZ(Lmb64, 0, 0);
     } else {
-        if (plan.dz == LMB_256x128) LMB_DZ(Lmb256x128, 2, 0);
+        if (plan.dz == LMB_256) LMB_DZ(Lmb256, 2, 0);
+        else if (plan.dz == LMB_256x128) LMB_DZ(Lmb256x128, 2, 0);
         else if (plan.dz == LMB_256x64) LMB_DZ(Lmb256x64, 2, 0);
         else if (plan.dz == LMB_128) LMB_DZ(Lmb128, 2, 0);
         else LMB_DZ(Lmb64, 2, 0);

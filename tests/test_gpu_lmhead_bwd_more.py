@@ -14,6 +14,14 @@ def wide(t):
     return t.detach().double().cpu().numpy()
 
 
+@pytest.fixture(autouse=True, params=[0, 128], ids=["by itself", "fp16 above 128 rows"])
+def few(request):
+    """The library's own choice, which for sizes like these is two bf16 terms, and one fp16."""
+    dlm.set_option("lmhead_bwd_few", request.param)
+    yield
+    dlm.set_option("lmhead_bwd_few", 0)
+
+
 def drawn(M, Dh, V, dtype, seed=0):
     """(hidden, w, lse, the other arguments) of a call"""
     rng = np.random.default_rng(seed + M + V)

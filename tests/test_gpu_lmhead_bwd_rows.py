@@ -5,7 +5,7 @@ t |dz| off, or, of numbers far below the largest of their kind:
   for d_hidden  2^-39 of the row's |d_lse| + |d_ztarget| (inv_t included) times the spread of W's rows, which is below 2^10 here: 2^-28;
   for d_w       2^-22 of the largest |dz| 2^e of the column, e the exponent of the largest entry of its hidden row; of which, with |h| < 2^(e + 1), the M rows
                 together make at most 2 M 2^-22 of that largest.  It is t of it, for which its own row already stands, up to M = 2^10.
-(Up to 128 rows two bf16 terms: h^2 |dz| and nothing beside it.)"""
+(Up to 128 rows two bf16 terms: h^2 |dz| and nothing beside it.  The library by itself takes them for sizes like these up to many more rows; here it is told not to.)"""
 import numpy as np
 import pytest
 import torch
@@ -17,6 +17,13 @@ from gpu_util import DEV, GuardedWorkspace
 pytestmark = pytest.mark.gpu
 U, H, T = 2.0 ** -24, 2.0 ** -8, 2.0 ** -11
 BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+@pytest.fixture(autouse=True)
+def few():
+    dlm.set_option("lmhead_bwd_few", 128)
+    yield
+    dlm.set_option("lmhead_bwd_few", 0)
 
 
 def wide(t):
