@@ -18,8 +18,8 @@
 //   fp32 gradients: three bf16 terms, 24 bits, and sums of 256 products (of a logit 128: an error of one is one of the probability) added up in two floats; the
 //     parts of d_hidden's sum, and what its chunks of columns leave in them, are joined in one.  Slower by design; 16 bits of dz and plain sums are 2e-6 off.
 //
-// Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 11.2 ms, 1.2 PFLOP/s (W's copy 0.42, dz 3.74 at 1.19, the gradients 6.8 at 1.31); 512 rows, V = 126464,
-// Dh = 4096 1.95 ms (0.37, 0.50, 1.05); 64 rows 0.80, 4 rows 0.76, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
+// Measured, both gradients in bf16: 4096 rows, V = 152064, Dh = 3584 12.1 ms, 1.1 PFLOP/s (W's copy 0.42, dz 4.29 at 1.04, its panels brought together 0.46, the gradients 6.92 at 1.29); 512 rows,
+// V = 126464, Dh = 4096 2.05 ms (0.37, 0.57, 0.05, 1.05); 256 rows 1.47, 64 0.73, 4 0.70, of 2.07 GB that it cannot do without.  A register-only loop of these products on such data reaches 1.81.
 #include "device.hpp"
 #include "rows.hpp"
 
