@@ -629,7 +629,7 @@ size_t dlm_embed_bwd_workspace_bytes(const dlm_embed_bwd_args *args);
  *   sum_out      optional [T, D], with residual only: s
  *   weight, bias optional bf16 [D]; NULL: 1, 0
  *   out          bf16 [T, D]
- * sum_out may be x or residual itself, out may be a bf16 x (same pointer and stride).  All in fp32; sums of squares overflow for entries from 2^57 on
+ * sum_out may be x or residual itself, out may be a bf16 x or residual (same pointer and stride), but not sum_out.  All in fp32; sums of squares overflow for entries from 2^57 on
  * (the row then comes out as its bias).  eps >= 2^-126.
  * Supported: D a multiple of 8, up to 16384. */
 typedef struct dlm_row_norm_args {

@@ -352,6 +352,13 @@ static int validate_norm(int T, int D, int kind, float eps, int type, const char
     return validate_row_type(type, who, "x");
 }
 
+// Rows written where an input of the same call lies have to be that input's own: an entry is read and written by one thread.
+static int validate_in_place(const void* out, int64_t stride, int bytes, const void* in, int64_t in_stride, int in_bytes, int T, const char* who, const char* names) {
+    if (!in || out != in) return DLM_OK;
+    if (bytes != in_bytes || (T > 1 && stride != in_stride)) return fail(DLM_ERR_INVALID_ARG, "%s: %s are one buffer of different types or strides", who, names);
+    return DLM_OK;
+}
+
 template <bool F32, int N, int TPR>
 static void launch_norm(const NormParams& all, hipStream_t st) {
     constexpr int TEAMS = TPR > 256 ? 1 : 256 / TPR, BYTES = F32 ? 4 : 2;
@@ -443,6 +450,13 @@ extern "C" int dlm_row_norm(const dlm_row_norm_args* a, void* stream) {
     if ((rc = validate_rows(a->out, a->out_stride, a->T, a->D, 2, true, who, "out")) != DLM_OK) return rc;
     if (!aligned16(a->weight) || !aligned16(a->bias)) return fail(DLM_ERR_UNSUPPORTED, "%s: weight / bias not 16-byte aligned", who);
     if (a->T == 0) return DLM_OK;
+    if (a->sum_out && a->sum_out == a->out) return fail(DLM_ERR_INVALID_ARG, "%s: sum_out is out", who);
+    if ((rc = validate_in_place(a->out, a->out_stride, 2, a->x, a->x_stride, bytes, a->T, who, "out and x")) != DLM_OK) return rc;
+    if ((rc = validate_in_place(a->out, a->out_stride, 2, a->residual, a->residual_stride, bytes, a->T, who, "out and residual")) != DLM_OK) return rc;
+    if (a->sum_out) {
+        if ((rc = validate_in_place(a->sum_out, a->sum_stride, bytes, a->x, a->x_stride, bytes, a->T, who, "sum_out and x")) != DLM_OK) return rc;
+        if ((rc = validate_in_place(a->sum_out, a->sum_stride, bytes, a->residual, a->residual_stride, bytes, a->T, who, "sum_out and residual")) != DLM_OK) return rc;
+    }
     NormParams p = {a->T, a->D, a->x, a->residual, a->x_stride, a->residual_stride, a->sum_out, a->sum_stride, (const uint16_t*)a->weight,
                     (const uint16_t*)a->bias, (uint16_t*)a->out, a->out_stride, a->eps, 1.0f / (float)a->D, a->kind == DLM_NORM_LAYER};
     if (a->x_type == DLM_ROW_F32) pick_norm<true>(p, (hipStream_t)stream);
@@ -475,6 +489,11 @@ extern "C" int dlm_row_norm_bwd(const dlm_row_norm_bwd_args* a, void* stream) {
     if (sums && need > 0) {
         if (!a->workspace || a->workspace_bytes < need) return fail(DLM_ERR_WORKSPACE, "%s: workspace of %zu bytes required", who, need);
         if (!aligned16(a->workspace)) return fail(DLM_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
+    }
+    if (a->T > 0) {
+        if ((rc = validate_in_place(a->d_x, a->d_x_stride, bytes, a->x, a->x_stride, bytes, a->T, who, "d_x and x")) != DLM_OK) return rc;
+        if ((rc = validate_in_place(a->d_x, a->d_x_stride, bytes, a->d_sum, a->d_sum_stride, bytes, a->T, who, "d_x and d_sum")) != DLM_OK) return rc;
+        if ((rc = validate_in_place(a->d_x, a->d_x_stride, bytes, a->d_out, a->d_out_stride, 2, a->T, who, "d_x and d_out")) != DLM_OK) return rc;
     }
     const int groups = grad_groups(a->T, a->D);
     float* part = sums ? (float*)a->workspace : nullptr;

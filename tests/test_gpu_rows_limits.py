@@ -80,3 +80,15 @@ def test_gradients_on_two_streams_at_once():
     torch.cuda.synchronize()
     for r in runs[:2]:
         assert all(torch.equal(r[k], runs[2][k]) for k in ("table", "d_x", "d_w", "d_b"))
+
+
+@pytest.mark.parametrize("T,D", [(5, 72), (33, 1032), (2100, 4096)])
+def test_norm_in_the_place_of_the_residual(T, D):
+    rng = np.random.default_rng(T)
+    x, residual = (torch.from_numpy(rng.standard_normal((T, D)).astype(np.float32)).to(torch.bfloat16).to(DEV) for _ in range(2))
+    total, out, total2 = (torch.zeros_like(x) for _ in range(3))
+    dlm.row_norm(x, out, residual=residual, sum_out=total, kind=dlm.NORM_LAYER)
+    dlm.row_norm(x, residual, residual=residual, sum_out=total2, kind=dlm.NORM_LAYER)
+    assert torch.equal(residual, out) and torch.equal(total2, total)
+    with pytest.raises(dlm.DlmError):
+        dlm.row_norm(x, x, residual=out, sum_out=x)
