@@ -698,7 +698,7 @@ size_t dlm_row_norm_bwd_workspace_bytes(const dlm_row_norm_bwd_args *args);
  * The logits are not stored; dz is, in 16 bits, up to 2 GiB of it at a time.  No sum is formed by atomics: deterministic (the order of sums depends on the sizes, the types and which
  * gradients are wanted).  hidden and w have to be finite: other rows'
  * values are multiplied by dz that may be zero.  d_w overlaps neither w nor d_hidden; d_hidden may be hidden.
- * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 256 rows and where M V Dh is at most 10^10, else 11, as an fp16 with a scale of its own for each gradient:
+ * Arithmetic: bf16 operands, fp32 sums.  For gradients of bf16 dz keeps 16 bits up to 256 rows, and up to 1024 where M^2 V Dh is at most 5 10^12, else 11, as an fp16 with a scale of its own for each gradient:
  *   for d_hidden an entry is besides up to 2^-38 of its row's (|d_lse| + |d_ztarget|) inv_temperature off (more where a few rows of w are over 2^8 larger than most: as
  *   many times more as they are beyond that), for d_w up to 2^-22 of the largest |dz| of its column, both times the largest entry of their hidden rows.  So every row of
  *   both gradients is right by its own size, of tokens that are unlikely in every row too (in d_w down to 2^-100 of the largest product of a hidden row and its gradient).  Entries of a hidden row below 2^-31 of its largest, of w below 2^-23, lose bits.

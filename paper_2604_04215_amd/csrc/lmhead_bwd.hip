@@ -699,7 +699,7 @@ struct LmbDz {
         };
         if constexpr (TERMS == 0) {
             // Two tiles of 32 columns at a time (one where there is one), for d_hidden and for d_w.  A row's 64 columns are a whole line: four lanes' pieces are turned, so that
-            // every store writes lines.  (Stores of 32 bytes of 32 rows: dz of 4096 rows, V = 50176, Dh = 3584 1600 us, lines 1430; with one dz for both gradients 1300.)
+            // every store writes lines; some twenty registers of the loop wait in scratch meanwhile.  (Stores of 32 bytes of 32 rows: dz of 4096 rows, V = 50176, Dh = 3584 1600 us, lines 1430; with one dz for both gradients 1300.)
             constexpr int NA = TVW < 2 ? 1 : 2;
             // W's exponents of the columns ahead are asked for before the stores at hand: a load behind stores waits for them
             typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
@@ -840,7 +840,7 @@ __global__ __launch_bounds__(64 * S::WV * S::WH, 1) void lmb_dz_kernel(LmbParams
     loop.run(job, list);
 }
 
-// E's panels of `rows` rows whose scale of a column is not the column's.  A lane has eight columns; most find nothing to do.
+// E's panels of `rows` rows whose scale of a column is not the column's.  A lane has eight columns.  (Nearly all of E of some thousand rows: bound by HBM.)
 __global__ __launch_bounds__(256) void lmb_even_kernel(LmbParams p, int rows) {
     const int padded = (lmb_rows(p) + 63) & ~63, first = blockIdx.y * rows, c = (blockIdx.x * WAVE + lane_id()) * 8;
     if (first >= padded || c >= p.n) return;
@@ -1125,16 +1125,17 @@ __global__ __launch_bounds__(256) void lmb_join_kernel(LmbParams p) {
 
 // ---- host ---------------------------------------------------------------------------------------------------
 constexpr size_t LMB_DZ_BYTES = (size_t)2 << 30;      // dz of a chunk: more rows, fewer columns at a time
-// Two bf16 terms or one fp16: a product more for each gradient (2 M V Dh operations) against a pass over W and three launches of 20 us together.  Both gradients, us of two
-// terms / fp16: V = 126464, Dh = 4096 130 rows 1239 / 1335, 192 1305 / 1350, 256 1473 / 1414, 320 1952 / 1828, 512 2582 / 2057; 64000 x 2048 256 rows 420 / 444, 384 578 / 558;
-// 151000 x 896 256 rows 522 / 557, 384 715 / 707.  Small products do not pay for the launches at any number of rows: 8000 x 1024 512 rows 67 / 83, 700 99 / 102, 1000 115 / 111;
-// 40000 x 256 512 rows 122 / 170, 1000 236 / 252; 16000 x 1024 512 rows 112 / 124, 700 172 / 172.  Where they are alike two terms are: they keep 16 bits.
-constexpr int LMB_FEW = 256;
-constexpr double LMB_SMALL = 1e10;                    // M V Dh
+// Two bf16 terms or one fp16: a product more for each gradient (2 M V Dh operations, in tiles that take M / 64 steps more one after the other) against a pass over W and three launches
+// of 20 us together.  Both gradients, us of two terms / fp16.  V = 126464, Dh = 4096 130 rows 1239 / 1335, 192 1305 / 1350, 256 1473 / 1414, 320 1952 / 1828, 512 2582 / 2057; 64000 x 2048 256
+// rows 420 / 444, 384 578 / 558; 151000 x 896 256 rows 522 / 557, 384 715 / 707.  Small products of up to a thousand rows do not pay for the launches: 8000 x 1024 512 rows 67 / 83, 700 99 / 102,
+// 1000 115 / 111; 40000 x 256 512 rows 122 / 170; 2000 x 4096 512 rows 85 / 92, 1000 136 / 128; 3500 x 4096 700 rows 198 / 141; 5000 x 256 1000 rows 52 / 66; 1352 x 896 900 rows 47 / 56,
+// 1656 94 / 82; 300 x 64 8192 rows 137 / 110.  Where they are alike two terms are: they keep 16 bits.
+constexpr int LMB_FEW = 256, LMB_SOME = 1024;
+constexpr double LMB_SMALL = 5e12;                    // M^2 V Dh
 static int g_lmb_few = 0;                             // dlm_set_option: two terms up to so many rows and for none above (0: by the rule)
 static bool lmb_two_terms(int M, int V, int Dh) {
     if (g_lmb_few > 0) return M <= g_lmb_few;
-    return M <= LMB_FEW || (double)M * V * Dh <= LMB_SMALL;
+    return M <= LMB_FEW || (M <= LMB_SOME && (double)M * M * V * Dh <= LMB_SMALL);
 }
 static int g_lmb_columns = 0;                         // dlm_set_option: most columns of a chunk (0: by the bytes)
 

@@ -5,7 +5,7 @@ t |dz| off, or, of numbers far below the largest of their kind:
   for d_hidden  2^-39 of the row's |d_lse| + |d_ztarget| (inv_t included) times the spread of W's rows, which is below 2^10 here: 2^-28;
   for d_w       2^-22 of the largest |dz| 2^e of the column, e the exponent of the largest entry of its hidden row; of which, with |h| < 2^(e + 1), the M rows
                 together make at most 2 M 2^-22 of that largest.  It is t of it, for which its own row already stands, up to M = 2^10.
-(Up to 128 rows two bf16 terms: h^2 |dz| and nothing beside it.  The library by itself takes them for sizes like these up to many more rows; here it is told not to.)"""
+(Up to 128 rows two bf16 terms: h^2 |dz| and nothing beside it.  The library by itself takes them for sizes like these up to 1024 rows; here it is told not to.)"""
 import numpy as np
 import pytest
 import torch
